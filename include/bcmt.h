@@ -194,9 +194,112 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
                                             const float* lse, const void* dO, void* dq, void* dk,
                                             void* dv, long ld_d, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of the language model around the mixer.
+ *
+ * Linear attention with a decay per head: BCMT's exponential memory (Sec. 3.5)
+ * taken per token instead of per block summary, as a token mixer of its own.
+ * Per sequence b and head h, with a = decay[h] and n = lengths[b] (T when
+ * lengths is NULL; values are clamped to [0, T]):
+ *     S_t = a S_{t-1} + k_t v_t^T,    o_t = scale * S_t^T q_t      for t < n,
+ * S_{-1} = state_in (zero when NULL), o_t = 0 for t >= n and state_out =
+ * S_{n-1} (state_in when n = 0).  Rows t >= n of q, k, v are never used,
+ * whatever they hold.  T = 1 is the step of incremental decoding.
+ *
+ *   q, k, v, o ... rows of token (b, t) start at x + (b*T + t)*ld elements, head
+ *            h at column h*dh (dh channels); each row stride ld >= H*dh is a
+ *            multiple of 8, so q, k, v may be slices of one projection's rows
+ *   decay    [H] fp32, each in [0, 1] (a^0 = 1 for a = 0 too); a constant: no
+ *            gradient is computed for it
+ *   lengths  [B] int32 device memory, or NULL
+ *   state    [B, H, dh, dh] fp32, row = channel of k, column = channel of v
+ *   Requirements: B, T, H >= 1; dh a multiple of 8, 8 <= dh <= 128; scale
+ *   finite and not 0; B*T <= 2^30; B*H*dh <= 2^26.  flags: BCMT_FLAG_CHECK only.
+ *   Arithmetic and states are fp32; with bf16 tensors the tensor-core form
+ *   rounds the decayed scores and the state to bf16 where they enter a product
+ *   with bf16 rows, while the running state itself keeps fp32. */
+typedef struct {
+  int B, T, H, dh;
+  int dtype;       /* bcmt_dtype of q, k, v, o and their gradients */
+  unsigned flags;
+  float scale;     /* usually 1 / sqrt(dh) */
+} bcmt_linattn_params;
+
+/* Bytes of workspace of one forward (backward = 0) or backward (1) call; free
+ * to reuse between calls.  Returns 0 for invalid parameters. */
+size_t bcmt_linattn_workspace_size(const bcmt_linattn_params* p, int backward);
+
+/* state_in and state_out may each be NULL, and may be the same buffer. */
+bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, long ld_q,
+                                 const void* k, long ld_k, const void* v, long ld_v,
+                                 const float* decay, const int* lengths, const float* state_in,
+                                 void* o, long ld_o, float* state_out, void* workspace,
+                                 void* stream);
+
+/* Gradients of sum(d_o * o) + sum(d_state_out * state_out) with respect to q, k,
+ * v and state_in, from the forward's inputs (nothing else is kept).
+ * d_state_out NULL: zero; d_state_in NULL: not computed (it must not be
+ * d_state_out's or state_in's buffer).  Rows t >= n of dq, dk, dv are zero. */
+bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o, long ld_do,
+                                  const void* q, long ld_q, const void* k, long ld_k,
+                                  const void* v, long ld_v, const float* decay,
+                                  const int* lengths, const float* state_in,
+                                  const float* d_state_out, void* dq, long ld_dq, void* dk,
+                                  long ld_dk, void* dv, long ld_dv, float* d_state_in,
+                                  void* workspace, void* stream);
+
+/* Scaled embedding lookup out[i] = scale * weight[ids[i]] and its gradient
+ * d_weight[v] = scale * (sum of d_out[i] over the i with ids[i] = v), the sum in
+ * fp32 in the order of i: the same bits at every run.  weight, d_weight [V, D];
+ * out, d_out [N, D]; ids [N] int32 (id_bytes 4) or int64 (8).  An id outside
+ * [0, V) gives a zero row and no gradient, and is reported as BCMT_ERR_ARG by
+ * the next bcmt_device_status (BCMT_FLAG_CHECK: by the call).  Every row of
+ * d_weight is written.  Requirements: N >= 0 (0: an empty batch), N <= 2^30,
+ * 1 <= V < 2^24, D a positive multiple of 8, scale finite.  flags:
+ * BCMT_FLAG_CHECK only. */
+typedef struct {
+  long long N;
+  int V, D;
+  int dtype;
+  int id_bytes;
+  unsigned flags;
+  float scale;
+} bcmt_embedding_params;
+
+/* Bytes of workspace of bcmt_embedding_backward; 0 for invalid parameters. */
+size_t bcmt_embedding_workspace_size(const bcmt_embedding_params* p);
+bcmt_status bcmt_embedding_forward(const bcmt_embedding_params* p, const void* ids,
+                                   const void* weight, void* out, void* stream);
+bcmt_status bcmt_embedding_backward(const bcmt_embedding_params* p, const void* ids,
+                                    const void* d_out, void* d_weight, void* workspace,
+                                    void* stream);
+
+/* Dropout of n elements: y_i = [residual_i +] keep_i * x_i / (1 - p), the mask
+ * recomputed from (seed, offset, i) wherever it is needed and never stored: the
+ * backward pass is the same call on dy (residual NULL) with the same seed and
+ * offset.  Element i takes 16-bit draw i % 8 of Philox4x32-10 with key `seed`
+ * and counter (i / 8, offset) -- word (i % 8) / 2, its low half first -- and is
+ * kept iff the draw is at least round(65536 p); a dropped element contributes
+ * exactly 0 even where x is infinite or NaN.  Use another offset for each place
+ * and step.  `step` (device memory, or NULL) is added to offset when the kernel
+ * runs, so a captured graph can draw a new mask at each replay.  y may be x or
+ * residual.  Requirements: n >= 0, 0 <= p <= 1.  flags: BCMT_FLAG_CHECK only. */
+typedef struct {
+  long long n;
+  int dtype;
+  unsigned flags;
+  double p;
+  unsigned long long seed, offset;
+  const unsigned long long* step;
+} bcmt_dropout_params;
+
+bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void* residual,
+                         void* y, void* stream);
+
 /* Reads and clears the device status word of the current device after
- * synchronising `stream`: BCMT_OK, or BCMT_ERR_TIMEOUT if any bounded
- * device-side wait has expired since the last read. */
+ * synchronising `stream`: BCMT_OK, BCMT_ERR_TIMEOUT if any bounded device-side
+ * wait has expired, or BCMT_ERR_ARG if an embedding id was outside its table,
+ * since the last read. */
 bcmt_status bcmt_device_status(void* stream);
 
 /* Message describing the last error of the calling thread ("" if none). */

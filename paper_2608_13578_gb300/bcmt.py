@@ -46,8 +46,29 @@ def make_params(B, T, D, H, L, dtype="bf16", input_is_x=True, flags=0) -> bcmt_p
     return bcmt_params(B, T, D, H, L, dt, 1 if input_is_x else 0, flags)
 
 
+class bcmt_linattn_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int),
+                ("dh", ctypes.c_int), ("dtype", ctypes.c_int), ("flags", ctypes.c_uint),
+                ("scale", ctypes.c_float)]
+
+
+class bcmt_embedding_params(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_longlong), ("V", ctypes.c_int), ("D", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("id_bytes", ctypes.c_int), ("flags", ctypes.c_uint),
+                ("scale", ctypes.c_float)]
+
+
+class bcmt_dropout_params(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_longlong), ("dtype", ctypes.c_int), ("flags", ctypes.c_uint),
+                ("p", ctypes.c_double), ("seed", ctypes.c_ulonglong),
+                ("offset", ctypes.c_ulonglong), ("step", ctypes.c_void_p)]
+
+
 _VP = ctypes.c_void_p
 _P = ctypes.POINTER(bcmt_params)
+_PL = ctypes.POINTER(bcmt_linattn_params)
+_PE = ctypes.POINTER(bcmt_embedding_params)
+_PD = ctypes.POINTER(bcmt_dropout_params)
 
 
 def _load():
@@ -81,6 +102,21 @@ def _load():
     lib.bcmt_attention_backward_noalloc.argtypes = [_P, _VP, _VP, _VP, ctypes.c_long, _VP, _VP,
                                                     _VP, _VP, _VP, _VP, ctypes.c_long, _VP]
     lib.bcmt_attention_backward_noalloc.restype = ctypes.c_int
+    _R = [_VP, ctypes.c_long]   # rows and their stride
+    lib.bcmt_linattn_workspace_size.argtypes = [_PL, ctypes.c_int]
+    lib.bcmt_linattn_workspace_size.restype = ctypes.c_size_t
+    lib.bcmt_linattn_forward.argtypes = [_PL] + _R * 3 + [_VP] * 3 + _R + [_VP] * 3
+    lib.bcmt_linattn_forward.restype = ctypes.c_int
+    lib.bcmt_linattn_backward.argtypes = [_PL] + _R * 4 + [_VP] * 4 + _R * 3 + [_VP] * 3
+    lib.bcmt_linattn_backward.restype = ctypes.c_int
+    lib.bcmt_embedding_workspace_size.argtypes = [_PE]
+    lib.bcmt_embedding_workspace_size.restype = ctypes.c_size_t
+    lib.bcmt_embedding_forward.argtypes = [_PE] + [_VP] * 4
+    lib.bcmt_embedding_forward.restype = ctypes.c_int
+    lib.bcmt_embedding_backward.argtypes = [_PE] + [_VP] * 5
+    lib.bcmt_embedding_backward.restype = ctypes.c_int
+    lib.bcmt_dropout.argtypes = [_PD] + [_VP] * 4
+    lib.bcmt_dropout.restype = ctypes.c_int
     lib.bcmt_test_set_tensor_cores.argtypes = [ctypes.c_int, ctypes.c_int]
     lib.bcmt_test_set_tensor_cores.restype = ctypes.c_int
     lib.bcmt_test_gemm.argtypes = [ctypes.c_int] * 6 + [_VP, ctypes.c_long, ctypes.c_long, _VP,
@@ -106,6 +142,9 @@ EXPORTED = ("bcmt_workspace_size", "bcmt_scratch_size", "bcmt_forward", "bcmt_ba
             "bcmt_device_status", "bcmt_last_error", "bcmt_profile_read", "bcmt_profile_reset",
             "bcmt_attention_backward_noalloc",
             "bcmt_decode_state_size", "bcmt_decode_reset", "bcmt_decode_step",
+            "bcmt_linattn_workspace_size", "bcmt_linattn_forward", "bcmt_linattn_backward",
+            "bcmt_embedding_workspace_size", "bcmt_embedding_forward", "bcmt_embedding_backward",
+            "bcmt_dropout",
             "bcmt_test_set_tensor_cores", "bcmt_test_gemm", "bcmt_test_gemm_group", "bcmt_test_attn",
             "bcmt_test_wait_expiry")
 
@@ -188,6 +227,46 @@ def bcmt_attention_backward_noalloc(p: bcmt_params, q, k, v, ld, o, lse, dO, dq,
     _check(LIB.bcmt_attention_backward_noalloc(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), ld,
                                                _ptr(o), _ptr(lse), _ptr(dO), _ptr(dq), _ptr(dk),
                                                _ptr(dv), ld_d, _stream(stream)))
+
+
+def bcmt_linattn_workspace_size(p: bcmt_linattn_params, backward: bool) -> int:
+    return LIB.bcmt_linattn_workspace_size(ctypes.byref(p), int(backward))
+
+
+def bcmt_linattn_forward(p: bcmt_linattn_params, q, ld_q, k, ld_k, v, ld_v, decay, lengths,
+                         state_in, o, ld_o, state_out, workspace, stream=None) -> None:
+    _check(LIB.bcmt_linattn_forward(ctypes.byref(p), _ptr(q), ld_q, _ptr(k), ld_k, _ptr(v), ld_v,
+                                    _ptr(decay), _ptr(lengths), _ptr(state_in), _ptr(o), ld_o,
+                                    _ptr(state_out), _ptr(workspace), _stream(stream)))
+
+
+def bcmt_linattn_backward(p: bcmt_linattn_params, d_o, ld_do, q, ld_q, k, ld_k, v, ld_v, decay,
+                          lengths, state_in, d_state_out, dq, ld_dq, dk, ld_dk, dv, ld_dv,
+                          d_state_in, workspace, stream=None) -> None:
+    _check(LIB.bcmt_linattn_backward(ctypes.byref(p), _ptr(d_o), ld_do, _ptr(q), ld_q, _ptr(k),
+                                     ld_k, _ptr(v), ld_v, _ptr(decay), _ptr(lengths),
+                                     _ptr(state_in), _ptr(d_state_out), _ptr(dq), ld_dq, _ptr(dk),
+                                     ld_dk, _ptr(dv), ld_dv, _ptr(d_state_in), _ptr(workspace),
+                                     _stream(stream)))
+
+
+def bcmt_embedding_workspace_size(p: bcmt_embedding_params) -> int:
+    return LIB.bcmt_embedding_workspace_size(ctypes.byref(p))
+
+
+def bcmt_embedding_forward(p: bcmt_embedding_params, ids, weight, out, stream=None) -> None:
+    _check(LIB.bcmt_embedding_forward(ctypes.byref(p), _ptr(ids), _ptr(weight), _ptr(out),
+                                      _stream(stream)))
+
+
+def bcmt_embedding_backward(p: bcmt_embedding_params, ids, d_out, d_weight, workspace,
+                            stream=None) -> None:
+    _check(LIB.bcmt_embedding_backward(ctypes.byref(p), _ptr(ids), _ptr(d_out), _ptr(d_weight),
+                                       _ptr(workspace), _stream(stream)))
+
+
+def bcmt_dropout(p: bcmt_dropout_params, x, residual, y, stream=None) -> None:
+    _check(LIB.bcmt_dropout(ctypes.byref(p), _ptr(x), _ptr(residual), _ptr(y), _stream(stream)))
 
 
 def bcmt_profile_reset() -> None:

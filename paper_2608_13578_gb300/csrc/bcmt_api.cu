@@ -1,6 +1,7 @@
 // C ABI of the BCMT token mixer: argument validation, workspace layout, and
 // the launch sequence of the forward (Sec. 3.2-3.8) and backward passes on the
 // caller's stream.  No device memory is allocated per call.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -16,6 +17,7 @@
 #include "../../include/bcmt_testing.h"
 #include "common.cuh"
 #include "internal.h"
+#include "linattn.h"
 #include "tc.cuh"
 
 namespace bcmt {
@@ -546,6 +548,88 @@ bcmt_status finish(const bcmt_params* p, cudaStream_t s) {
   return BCMT_OK;
 }
 
+// ------------------------------------------------ language-model operators
+bcmt_status check_flags(unsigned flags) {
+  if (flags & ~(unsigned)BCMT_FLAG_CHECK) return fail(BCMT_ERR_ARG, "unknown flag bits 0x%x", flags);
+  return BCMT_OK;
+}
+bcmt_status check_dtype(int dtype) {
+  if (dtype != BCMT_F32 && dtype != BCMT_BF16)
+    return fail(BCMT_ERR_ARG, "dtype must be BCMT_F32 or BCMT_BF16 (got %d)", dtype);
+  return BCMT_OK;
+}
+bcmt_status check_opt(const void* ptr, const char* name) {
+  return ptr ? check_ptr(ptr, name) : BCMT_OK;
+}
+
+bcmt_status check_linattn(const bcmt_linattn_params* p) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  if (p->B < 1 || p->T < 1 || p->H < 1)
+    return fail(BCMT_ERR_SHAPE, "B, T, H must be >= 1 (got %d %d %d)", p->B, p->T, p->H);
+  if (p->dh < 8 || p->dh % 8 != 0 || p->dh > 128)
+    return fail(BCMT_ERR_SHAPE, "head width dh = %d must be a multiple of 8 from 8 to 128", p->dh);
+  if ((long long)p->B * p->T > (1ll << 30))
+    return fail(BCMT_ERR_SHAPE, "B*T = %lld tokens is too large", (long long)p->B * p->T);
+  // the grids: (heads) x (segments, columns) CTAs along one axis
+  if ((long long)p->H > (1 << 20) || (long long)p->B * p->H * p->dh > (1ll << 26))
+    return fail(BCMT_ERR_SHAPE, "B*H*dh = %lld is too large", (long long)p->B * p->H * p->dh);
+  if (!isfinite(p->scale) || p->scale == 0.f)
+    return fail(BCMT_ERR_ARG, "scale must be finite and not 0");
+  return check_flags(p->flags);
+}
+bcmt_status check_rows(const bcmt_linattn_params* p, const void* ptr, long ld, const char* name) {
+  BCMT_TRY(check_ptr(ptr, name));
+  if (ld < (long)p->H * p->dh || ld % 8 != 0)
+    return fail(BCMT_ERR_ARG, "row stride %ld of %s must be a multiple of 8 and >= H*dh = %ld", ld,
+                name, (long)p->H * p->dh);
+  return BCMT_OK;
+}
+LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int* lengths,
+                     int npass, void* workspace, LinPlan* plan) {
+  LinArgs a{};
+  a.npass = npass;
+  a.B = p->B;
+  a.T = p->T;
+  a.H = p->H;
+  a.dh = p->dh;
+  a.decay = decay;
+  a.lengths = lengths;
+  *plan = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms());
+  a.nseg = plan->nseg;
+  a.seg_len = plan->seg_len;
+  const long long states = (long long)p->B * p->H * a.nseg * p->dh * p->dh;
+  for (int i = 0; i < npass; ++i) {
+    a.pass[i].s_in_mul = a.pass[i].s_out_mul = 1.f;
+    a.pass[i].out_mul = p->scale;
+    a.pass[i].seg = static_cast<float*>(workspace) + i * states;
+  }
+  return a;
+}
+
+bcmt_status check_embedding(const bcmt_embedding_params* p) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  if (p->N < 0 || p->N > (1ll << 30))
+    return fail(BCMT_ERR_SHAPE, "N = %lld must be in [0, 2^30]", p->N);
+  if (p->V < 1 || p->V >= (1 << 24)) return fail(BCMT_ERR_SHAPE, "V = %d must be in [1, 2^24)", p->V);
+  if (p->D < 8 || p->D % 8 != 0)
+    return fail(BCMT_ERR_SHAPE, "D = %d must be a positive multiple of 8", p->D);
+  if (p->id_bytes != 4 && p->id_bytes != 8)
+    return fail(BCMT_ERR_ARG, "id_bytes must be 4 or 8 (got %d)", p->id_bytes);
+  if (!isfinite(p->scale)) return fail(BCMT_ERR_ARG, "scale must be finite");
+  return check_flags(p->flags);
+}
+bcmt_status check_ids(const bcmt_embedding_params* p, const void* ids) {
+  if (!ids && p->N > 0) return fail(BCMT_ERR_ARG, "ids is NULL");
+  if (reinterpret_cast<uintptr_t>(ids) % p->id_bytes)
+    return fail(BCMT_ERR_ALIGN, "ids is not aligned to its %d-byte elements", p->id_bytes);
+  return BCMT_OK;
+}
+bcmt_status finish_flags(unsigned flags, cudaStream_t s) {
+  return (flags & BCMT_FLAG_CHECK) ? bcmt_device_status(s) : BCMT_OK;
+}
+
 // A wait that cannot end, bounded by `cap` SM clock cycles: one thread
 // initialises an mbarrier for one arrival and waits for its first phase, which
 // nothing completes.  The bounded wait expires, ORs kStatusTimeout into the
@@ -590,6 +674,7 @@ bcmt_status bcmt_device_status(void* stream) {
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e != cudaSuccess) return cuda_fail(e, "reading device status");
   if (v & kStatusTimeout) return fail(BCMT_ERR_TIMEOUT, "a bounded device-side wait expired");
+  if (v & kStatusBadIndex) return fail(BCMT_ERR_ARG, "an embedding id was outside its table");
   if (v) return fail(BCMT_ERR_CUDA, "device status 0x%x", v);
   return BCMT_OK;
 }
@@ -1163,6 +1248,168 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
   cudaError_t e = attn_bwd_simt_noalloc(lc, g.dtype, ab);
   if (e != cudaSuccess) return cuda_fail(e, "allocation-free attention backward");
   return finish(p, lc.stream);
+}
+
+// ------------------------------------------------ language-model operators
+size_t bcmt_linattn_workspace_size(const bcmt_linattn_params* p, int backward) {
+  if (check_linattn(p) != BCMT_OK) return 0;
+  const int npass = backward ? 3 : 1;
+  const LinPlan pl = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms());
+  const size_t states = pl.nseg > 1 ? (size_t)p->B * p->H * pl.nseg * p->dh * p->dh * 4 : 0;
+  return al256(std::max<size_t>(256, npass * states));
+}
+
+bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, long ld_q,
+                                 const void* k, long ld_k, const void* v, long ld_v,
+                                 const float* decay, const int* lengths, const float* state_in,
+                                 void* o, long ld_o, float* state_out, void* workspace,
+                                 void* stream) {
+  BCMT_TRY(check_linattn(p));
+  BCMT_TRY(check_rows(p, q, ld_q, "q"));
+  BCMT_TRY(check_rows(p, k, ld_k, "k"));
+  BCMT_TRY(check_rows(p, v, ld_v, "v"));
+  BCMT_TRY(check_rows(p, o, ld_o, "o"));
+  if (!decay) return fail(BCMT_ERR_ARG, "decay is NULL");
+  BCMT_TRY(check_opt(state_in, "state_in"));
+  BCMT_TRY(check_opt(state_out, "state_out"));
+  BCMT_TRY(check_ptr(workspace, "workspace"));
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  LinPlan pl;
+  LinArgs a = linattn_args(p, decay, lengths, 1, workspace, &pl);
+  LinPass& f = a.pass[0];
+  f.q = q;
+  f.ldq = ld_q;
+  f.k = k;
+  f.ldk = ld_k;
+  f.v = v;
+  f.ldv = ld_v;
+  f.o = o;
+  f.ldo = ld_o;
+  f.s_in = state_in;
+  f.s_out = state_out;
+  cudaError_t e = p->T == 1 ? linattn_step(lc, p->dtype, a) : linattn_simt(lc, p->dtype, a);
+  if (e != cudaSuccess) return cuda_fail(e, "linear attention forward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o, long ld_do,
+                                  const void* q, long ld_q, const void* k, long ld_k,
+                                  const void* v, long ld_v, const float* decay,
+                                  const int* lengths, const float* state_in,
+                                  const float* d_state_out, void* dq, long ld_dq, void* dk,
+                                  long ld_dk, void* dv, long ld_dv, float* d_state_in,
+                                  void* workspace, void* stream) {
+  BCMT_TRY(check_linattn(p));
+  BCMT_TRY(check_rows(p, d_o, ld_do, "d_o"));
+  BCMT_TRY(check_rows(p, q, ld_q, "q"));
+  BCMT_TRY(check_rows(p, k, ld_k, "k"));
+  BCMT_TRY(check_rows(p, v, ld_v, "v"));
+  BCMT_TRY(check_rows(p, dq, ld_dq, "dq"));
+  BCMT_TRY(check_rows(p, dk, ld_dk, "dk"));
+  BCMT_TRY(check_rows(p, dv, ld_dv, "dv"));
+  if (!decay) return fail(BCMT_ERR_ARG, "decay is NULL");
+  BCMT_TRY(check_opt(state_in, "state_in"));
+  BCMT_TRY(check_opt(d_state_out, "d_state_out"));
+  BCMT_TRY(check_opt(d_state_in, "d_state_in"));
+  if (d_state_in && (d_state_in == d_state_out || d_state_in == state_in))
+    return fail(BCMT_ERR_ARG, "d_state_in must have a buffer of its own");
+  BCMT_TRY(check_ptr(workspace, "workspace"));
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  LinPlan pl;
+  LinArgs a = linattn_args(p, decay, lengths, 3, workspace, &pl);
+  // dq = pass(do, v, k); dv = reverse pass(k, q, do); dk = reverse pass(v, do, q).
+  // The reverse states are kept without the scale (it multiplies the output),
+  // so the incoming gradient of the state is divided by it.
+  auto set = [&](LinPass& s, const void* x, long ldx, const void* y, long ldy, const void* z,
+                 long ldz, void* out, long ldout) {
+    s.q = x;
+    s.ldq = ldx;
+    s.k = y;
+    s.ldk = ldy;
+    s.v = z;
+    s.ldv = ldz;
+    s.o = out;
+    s.ldo = ldout;
+  };
+  set(a.pass[0], d_o, ld_do, v, ld_v, k, ld_k, dq, ld_dq);
+  set(a.pass[1], k, ld_k, q, ld_q, d_o, ld_do, dv, ld_dv);
+  set(a.pass[2], v, ld_v, d_o, ld_do, q, ld_q, dk, ld_dk);
+  a.pass[0].s_in = state_in;
+  a.pass[0].s_in_t = 1;
+  a.pass[2].s_in_t = 1;
+  for (int i = 1; i < 3; ++i) {
+    a.pass[i].rev = 1;
+    a.pass[i].s_in = d_state_out;
+    a.pass[i].s_in_mul = 1.f / p->scale;
+  }
+  a.pass[1].s_out = d_state_in;
+  a.pass[1].s_out_mul = p->scale;
+  cudaError_t e = linattn_simt(lc, p->dtype, a);
+  if (e != cudaSuccess) return cuda_fail(e, "linear attention backward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+size_t bcmt_embedding_workspace_size(const bcmt_embedding_params* p) {
+  if (check_embedding(p) != BCMT_OK) return 0;
+  return std::max<size_t>(256, embed_bwd_workspace(p->N, p->V, p->D));
+}
+
+bcmt_status bcmt_embedding_forward(const bcmt_embedding_params* p, const void* ids,
+                                   const void* weight, void* out, void* stream) {
+  BCMT_TRY(check_embedding(p));
+  BCMT_TRY(check_ids(p, ids));
+  BCMT_TRY(check_ptr(weight, "weight"));
+  if (p->N > 0) BCMT_TRY(check_ptr(out, "out"));
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  const EmbedArgs a{ids, p->id_bytes == 8, p->N, p->V, p->D, p->scale};
+  cudaError_t e = embed_fwd(lc, p->dtype, a, weight, out);
+  if (e != cudaSuccess) return cuda_fail(e, "embedding forward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_embedding_backward(const bcmt_embedding_params* p, const void* ids,
+                                    const void* d_out, void* d_weight, void* workspace,
+                                    void* stream) {
+  BCMT_TRY(check_embedding(p));
+  BCMT_TRY(check_ids(p, ids));
+  if (p->N > 0) BCMT_TRY(check_ptr(d_out, "d_out"));
+  BCMT_TRY(check_ptr(d_weight, "d_weight"));
+  BCMT_TRY(check_ptr(workspace, "workspace"));
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  const EmbedArgs a{ids, p->id_bytes == 8, p->N, p->V, p->D, p->scale};
+  cudaError_t e = embed_bwd(lc, p->dtype, a, d_out, d_weight, workspace);
+  if (e != cudaSuccess) return cuda_fail(e, "embedding backward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void* residual,
+                         void* y, void* stream) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  if (p->n < 0) return fail(BCMT_ERR_SHAPE, "n = %lld must be >= 0", p->n);
+  if (!(p->p >= 0.0 && p->p <= 1.0)) return fail(BCMT_ERR_ARG, "p = %g must be in [0, 1]", p->p);
+  BCMT_TRY(check_flags(p->flags));
+  if (p->n > 0) {
+    BCMT_TRY(check_ptr(x, "x"));
+    BCMT_TRY(check_opt(residual, "residual"));
+    BCMT_TRY(check_ptr(y, "y"));
+  }
+  if (reinterpret_cast<uintptr_t>(p->step) % 8)
+    return fail(BCMT_ERR_ALIGN, "step is not 8-byte aligned");
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  cudaError_t e = dropout(lc, p->dtype, x, residual, y, p->n, p->p, p->seed, p->offset, p->step);
+  if (e != cudaSuccess) return cuda_fail(e, "dropout");
+  return finish_flags(p->flags, lc.stream);
 }
 
 int bcmt_profile_read(const char** names, int* launches, double* ms, int cap) {

@@ -15,7 +15,7 @@ namespace bcmt {
 typedef __nv_bfloat16 bf16;
 
 // Bits OR-ed into the device status word.
-enum : unsigned { kStatusTimeout = 1u, kStatusBadLaunch = 2u };
+enum : unsigned { kStatusTimeout = 1u, kStatusBadLaunch = 2u, kStatusBadIndex = 4u };
 
 // Programmatic dependent launch.  Every kernel of the library is launched with
 // programmatic stream serialisation (launch_k below) and starts with

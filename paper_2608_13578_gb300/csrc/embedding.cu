@@ -1,0 +1,484 @@
+// Scaled embedding lookup out_i = s W[id_i], and its gradient by sorted tokens
+// dW[v] = s sum_{i: id_i = v} dy_i, summed in fp32 in position order (no
+// floating-point atomics: the result does not change from run to run) and
+// rounded once.
+#include <algorithm>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace bcmt {
+
+namespace {
+
+constexpr int kTile = 2048;      // ids sorted by one CTA of a radix pass
+constexpr int kSortThreads = 256;
+constexpr int kChunk = 32;       // sorted positions summed by one warp
+
+// The id at i, or -1 where it is outside [0, V).
+__device__ __forceinline__ int id_at(const void* ids, int is64, long long i, int V) {
+  const long long v = is64 ? static_cast<const long long*>(ids)[i] : static_cast<const int*>(ids)[i];
+  return v >= 0 && v < V ? (int)v : -1;
+}
+
+// 16 bytes of T as fp32 and back.
+template <class T>
+constexpr int vec_n() { return 16 / (int)sizeof(T); }
+template <class T>
+__device__ __forceinline__ void unpack16(const uint4& r, float* v) {
+  if constexpr (sizeof(T) == 2) {
+    unpack8(r, v);
+  } else {
+    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y);
+    v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+  }
+}
+template <class T>
+__device__ __forceinline__ void store16(T* p, const float* v) {
+  if constexpr (sizeof(T) == 2) store8(p, v);
+  else store4(p, v);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------- lookup
+// One thread per 16 bytes of output, four in flight.  Bandwidth-bound: the
+// output is written once and a row is read once from HBM (repeated tokens hit
+// L2).  An id outside [0, V) gives a zero row and sets kStatusBadIndex.
+template <class T>
+__global__ void __launch_bounds__(256)
+    embed_fwd_kernel(const void* __restrict__ ids, int is64, long long N, int V, int D,
+                     const T* __restrict__ W, float scale, T* __restrict__ out, unsigned* status) {
+  pdl_enter();
+  constexpr int VN = vec_n<T>();
+  const int rv = D / VN;
+  const long long total = N * rv, stride = (long long)gridDim.x * 256;
+  for (long long i0 = blockIdx.x * 256ll + threadIdx.x; i0 < total; i0 += 4 * stride) {
+    uint4 raw[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = i0 + u * stride;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (i < total) {
+        const long long r = i / rv;
+        const int c = (int)(i - r * rv);
+        const int id = id_at(ids, is64, r, V);
+        if (id >= 0) raw[u] = *reinterpret_cast<const uint4*>(W + (long long)id * D + c * VN);
+        else if (c == 0) atomicOr(status, kStatusBadIndex);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = i0 + u * stride;
+      if (i >= total) continue;
+      float v[VN];
+      unpack16<T>(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) v[e] *= scale;
+      store16<T>(out + i * VN, v);
+    }
+  }
+}
+
+// ------------------------------------------------------------------- gradient
+// A stable least-significant-digit radix sort of the ids (8 bits a pass, ids
+// outside [0, V) as key V, at the end), then a segmented sum over the sorted
+// positions.  The sort's launches occupy few SMs, so the CTAs beyond its tiles
+// clear the table's gradient meanwhile (rows that no token names stay zero).
+struct SortArgs {
+  const void* ids;
+  int is64;
+  int N, V, tiles;
+  int* key[2];
+  int* pos[2];
+  int* cnt[3];   // [tiles][256] per pass
+  int passes;
+  uint4* zero;   // the gradient, cleared by parts over the sort's launches
+  long long zero_n;
+  unsigned* status;
+};
+
+namespace {
+// CTAs from `first` on clear the part `part` of `parts`.
+__device__ __forceinline__ void clear_part(const SortArgs& a, int first, int part, int parts) {
+  const long long lo = a.zero_n * part / parts, hi = a.zero_n * (part + 1) / parts;
+  const uint4 z = make_uint4(0, 0, 0, 0);
+  for (long long i = lo + (long long)(blockIdx.x - first) * kSortThreads + threadIdx.x; i < hi;
+       i += (long long)(gridDim.x - first) * kSortThreads)
+    a.zero[i] = z;
+}
+}  // namespace
+
+// Keys and digit counts of the first pass.
+__global__ void __launch_bounds__(kSortThreads) embed_keys_kernel(const __grid_constant__ SortArgs a) {
+  __shared__ int hist[256];
+  pdl_enter();
+  if ((int)blockIdx.x >= a.tiles) {
+    clear_part(a, a.tiles, 0, a.passes + 1);
+    return;
+  }
+  const int tid = threadIdx.x;
+  hist[tid] = 0;
+  __syncthreads();
+  const int base = blockIdx.x * kTile;
+  for (int i = base + tid; i < min(a.N, base + kTile); i += kSortThreads) {
+    int id = id_at(a.ids, a.is64, i, a.V);
+    if (id < 0) {
+      id = a.V;
+      atomicOr(a.status, kStatusBadIndex);
+    }
+    a.key[0][i] = id;
+    atomicAdd(&hist[id & 255], 1);
+  }
+  __syncthreads();
+  a.cnt[0][blockIdx.x * 256 + tid] = hist[tid];
+  for (int p = 1; p < a.passes; ++p) a.cnt[p][blockIdx.x * 256 + tid] = 0;
+}
+
+// One stable pass: digit `p` of the keys.  Ranks: each warp takes 256
+// consecutive keys, 32 at a time, and ranks equal digits by lane order; the
+// warps' counts are then scanned in warp order and the tiles' in tile order.
+// The next pass's digit counts (integers: order does not matter) are taken on
+// the way, at the tiles where the keys land.
+__global__ void __launch_bounds__(kSortThreads)
+    embed_sort_kernel(const __grid_constant__ SortArgs a, int p) {
+  constexpr int NW = kSortThreads / 32, PER = kTile / kSortThreads;
+  __shared__ int wcnt[NW][256];
+  __shared__ int wsum[NW];
+  pdl_enter();
+  if ((int)blockIdx.x >= a.tiles) {
+    clear_part(a, a.tiles, p + 1, a.passes + 1);
+    return;
+  }
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int base = blockIdx.x * kTile;
+  const int* kin = a.key[p & 1];
+  const int* pin = a.pos[p & 1];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) wcnt[w][tid] = 0;
+  __syncthreads();
+  int key[PER], rank[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = base + warp * (PER * 32) + j * 32 + lane;
+    key[j] = i < a.N ? kin[i] : -1;
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int d = key[j] < 0 ? 256 : (key[j] >> (8 * p)) & 255;
+    const unsigned same = __match_any_sync(0xffffffffu, d);
+    const unsigned before = same & ((1u << lane) - 1u);
+    int start = 0;
+    if (d < 256) start = wcnt[warp][d];
+    __syncwarp();
+    if (d < 256 && before == 0) wcnt[warp][d] = start + __popc(same);
+    __syncwarp();
+    rank[j] = start + __popc(before);
+  }
+  // digit tid: keys before this tile's, over all digits and the earlier tiles
+  int total = 0, mine = 0;
+  for (int t = 0; t < a.tiles; ++t) {
+    const int c = a.cnt[p][t * 256 + tid];
+    total += c;
+    if (t < (int)blockIdx.x) mine += c;
+  }
+  int incl = total;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) wsum[warp] = incl;
+  __syncthreads();
+  int off = incl - total + mine;
+  for (int w = 0; w < warp; ++w) off += wsum[w];
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const int c = wcnt[w][tid];
+    wcnt[w][tid] = off;
+    off += c;
+  }
+  __syncthreads();
+  int* kout = a.key[(p + 1) & 1];
+  int* pout = a.pos[(p + 1) & 1];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    if (key[j] < 0) continue;
+    const int i = base + warp * (PER * 32) + j * 32 + lane;
+    const int dst = wcnt[warp][(key[j] >> (8 * p)) & 255] + rank[j];
+    kout[dst] = key[j];
+    pout[dst] = p == 0 ? i : pin[i];
+    if (p + 1 < a.passes)
+      atomicAdd(&a.cnt[p + 1][(dst / kTile) * 256 + ((key[j] >> (8 * (p + 1))) & 255)], 1);
+  }
+}
+
+// The segmented sum: a warp takes kChunk sorted positions and 32 vectors of
+// columns, adding the rows of equal keys in order.  A run inside the chunk is
+// finished here; what a run has in a chunk that it shares with a neighbour goes
+// to part[chunk][0] (the chunk's first run, when it began earlier) or
+// part[chunk][1] (its last run, when it goes on).
+struct SumArgs {
+  const int *key, *pos;
+  int N, V, D, chunks, cblocks;
+  float scale;
+  float* part;  // [chunks][2][D]
+};
+
+template <class T>
+__global__ void __launch_bounds__(256)
+    embed_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ dy,
+                     T* __restrict__ dw) {
+  constexpr int VN = vec_n<T>();
+  constexpr int U = 8;  // rows in flight
+  pdl_enter();
+  const int lane = threadIdx.x & 31;
+  const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (unit >= a.chunks * a.cblocks) return;
+  const int chunk = unit / a.cblocks, cb = unit - chunk * a.cblocks;
+  const int p0 = chunk * kChunk, cnt = min(kChunk, a.N - p0);
+  const int mykey = lane < cnt ? a.key[p0 + lane] : -1;
+  const int mypos = lane < cnt ? a.pos[p0 + lane] : 0;
+  const int prev = p0 > 0 ? a.key[p0 - 1] : -1;
+  const int next = p0 + cnt < a.N ? a.key[p0 + cnt] : -1;
+  const int col = (cb * 32 + lane) * VN;
+  const bool ok = col < a.D;
+  float acc[VN];
+#pragma unroll
+  for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+  bool from_prev = false;
+  for (int j0 = 0; j0 < cnt; j0 += U) {
+    uint4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = __shfl_sync(0xffffffffu, mypos, (j0 + u) & 31);
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (j0 + u < cnt && ok) raw[u] = *reinterpret_cast<const uint4*>(dy + (long long)row * a.D + col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u;
+      const int key = __shfl_sync(0xffffffffu, mykey, j & 31);
+      const int after = __shfl_sync(0xffffffffu, mykey, (j + 1) & 31);
+      if (j >= cnt) break;
+      if (key >= a.V) break;  // ids outside the table, sorted to the end
+      if (j == 0) from_prev = key == prev;
+      float v[VN];
+      unpack16<T>(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) acc[e] += v[e];
+      const bool last = j == cnt - 1;
+      if ((last ? next : after) == key && !last) continue;
+      const bool goes_on = last && next == key;
+      if (ok) {
+        if (from_prev || goes_on) {
+          float* d = a.part + ((long long)chunk * 2 + (from_prev ? 0 : 1)) * a.D + col;
+#pragma unroll
+          for (int e = 0; e < VN; e += 4) store4(d + e, acc + e);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
+          store16<T>(dw + (long long)key * a.D + col, acc);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+      from_prev = false;
+    }
+  }
+}
+
+// Joins the runs that cross chunks, in chunk order: the chunk in which such a
+// run begins owns it, and its warp adds part[chunk][1], part[chunk + 1][0], ...
+// A run of more than kLong chunks is cut among the CTA's warps and their sums
+// added in warp order.
+constexpr int kLong = 16;
+template <class T>
+__global__ void __launch_bounds__(256)
+    embed_join_kernel(const __grid_constant__ SumArgs a, T* __restrict__ dw) {
+  constexpr int VN = vec_n<T>();
+  __shared__ int run_len[8], run_key[8];
+  __shared__ float sums[8][32 * 8 + 4];
+  pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int chunk0 = blockIdx.x / a.cblocks * 8, cb = blockIdx.x % a.cblocks;
+  const int col = (cb * 32 + lane) * VN;
+  const bool ok = col < a.D;
+  auto add = [&](int lo, int hi, int chunk, float* acc) {  // parts lo .. hi-1 of the run
+    for (int m0 = lo; m0 < hi; m0 += 4) {
+      float v[4][VN];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int m = m0 + u;
+#pragma unroll
+        for (int e = 0; e < VN; ++e) v[u][e] = 0.f;
+        if (m < hi && ok) {
+          const float* s = a.part + ((long long)(chunk + m) * 2 + (m == 0 ? 1 : 0)) * a.D + col;
+#pragma unroll
+          for (int e = 0; e < VN; e += 4) load4(s + e, v[u] + e);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < VN; ++e) acc[e] += v[u][e];
+    }
+  };
+  auto finish = [&](int key, float* acc) {
+#pragma unroll
+    for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
+    store16<T>(dw + (long long)key * a.D + col, acc);
+  };
+  {
+    const int chunk = chunk0 + warp;
+    int len = 0, key = -1;
+    const int end = (chunk + 1) * kChunk;  // first position of the next chunk
+    if (chunk < a.chunks && end < a.N) {
+      key = a.key[end - 1];
+      const bool began_here = a.key[chunk * kChunk] != key || chunk == 0 ||
+                              a.key[chunk * kChunk - 1] != key;
+      if (key < a.V && a.key[end] == key && began_here) {
+        // the run's last position, by bisection: key[lo] == key, key[hi] != key or hi == N
+        int lo = end, hi = a.N;
+        while (hi - lo > 1) {
+          const int mid = lo + (hi - lo) / 2;
+          if (a.key[mid] == key) lo = mid;
+          else hi = mid;
+        }
+        len = lo / kChunk - chunk + 1;
+      }
+    }
+    if (lane == 0) {
+      run_len[warp] = len;
+      run_key[warp] = key;
+    }
+    if (len > 0 && len <= kLong) {
+      float acc[VN];
+#pragma unroll
+      for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+      add(0, len, chunk, acc);
+      if (ok) finish(key, acc);
+    }
+  }
+  __syncthreads();
+  for (int w = 0; w < 8; ++w) {
+    const int len = run_len[w];
+    if (len <= kLong) continue;
+    float acc[VN];
+#pragma unroll
+    for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+    const int per = (len + 7) / 8, lo = warp * per;
+    add(min(lo, len), min(lo + per, len), chunk0 + w, acc);
+#pragma unroll
+    for (int e = 0; e < VN; ++e) sums[warp][lane * VN + e] = acc[e];
+    __syncthreads();
+    if (warp == 0 && ok) {
+#pragma unroll
+      for (int e = 0; e < VN; ++e) acc[e] = sums[0][lane * VN + e];
+      for (int q = 1; q < 8; ++q)
+#pragma unroll
+        for (int e = 0; e < VN; ++e) acc[e] += sums[q][lane * VN + e];
+      finish(run_key[w], acc);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- host side
+namespace {
+struct BwdLayout {
+  size_t key[2], pos[2], cnt[3], part, bytes;
+  int tiles, passes, chunks;
+};
+BwdLayout bwd_layout(long long N, int V, int D) {
+  BwdLayout l{};
+  l.tiles = (int)((N + kTile - 1) / kTile);
+  l.chunks = (int)((N + kChunk - 1) / kChunk);
+  l.passes = V < (1 << 8) ? 1 : V < (1 << 16) ? 2 : 3;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = off;
+    off += (bytes + 255) & ~size_t(255);
+    return r;
+  };
+  for (int i = 0; i < 2; ++i) {
+    l.key[i] = take((size_t)N * 4);
+    l.pos[i] = take((size_t)N * 4);
+  }
+  for (int i = 0; i < l.passes; ++i) l.cnt[i] = take((size_t)l.tiles * 256 * 4);
+  l.part = take((size_t)l.chunks * 2 * D * 4);
+  l.bytes = off;
+  return l;
+}
+
+template <class T>
+cudaError_t fwd_typed(const Launch& lc, const EmbedArgs& a, const void* W, void* out) {
+  const long long vecs = a.N * (a.D / vec_n<T>());
+  const long long blocks = std::min<long long>((vecs + 1023) / 1024, 152ll * 64);
+  cudaError_t e = launch_k(embed_fwd_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, lc.stream,
+                           a.ids, a.is64, a.N, a.V, a.D, (const T*)W, a.scale, (T*)out, lc.status);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <class T>
+cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void* dw, void* ws) {
+  const BwdLayout l = bwd_layout(a.N, a.V, a.D);
+  char* w = static_cast<char*>(ws);
+  SortArgs s{};
+  s.ids = a.ids;
+  s.is64 = a.is64;
+  s.N = (int)a.N;
+  s.V = a.V;
+  s.tiles = l.tiles;
+  s.passes = a.N > 0 ? l.passes : 0;  // an empty batch only clears
+  for (int i = 0; i < 2; ++i) {
+    s.key[i] = reinterpret_cast<int*>(w + l.key[i]);
+    s.pos[i] = reinterpret_cast<int*>(w + l.pos[i]);
+  }
+  for (int i = 0; i < l.passes; ++i) s.cnt[i] = reinterpret_cast<int*>(w + l.cnt[i]);
+  s.zero = static_cast<uint4*>(dw);
+  s.zero_n = (long long)a.V * (a.D / vec_n<T>());
+  s.status = lc.status;
+  const unsigned clear = (unsigned)std::min<long long>((s.zero_n + 2047) / 2048, 152 * 8);
+  cudaError_t e = launch_k(embed_keys_kernel, dim3(l.tiles + clear), dim3(kSortThreads), 0,
+                           lc.stream, s);
+  if (e != cudaSuccess) return e;
+  if (a.N == 0) return cudaGetLastError();
+  for (int p = 0; p < l.passes; ++p) {
+    e = launch_k(embed_sort_kernel, dim3(l.tiles + clear), dim3(kSortThreads), 0, lc.stream, s, p);
+    if (e != cudaSuccess) return e;
+  }
+  SumArgs m{};
+  m.key = s.key[l.passes & 1];
+  m.pos = s.pos[l.passes & 1];
+  m.N = (int)a.N;
+  m.V = a.V;
+  m.D = a.D;
+  m.chunks = l.chunks;
+  m.cblocks = (a.D / vec_n<T>() + 31) / 32;
+  m.scale = a.scale;
+  m.part = reinterpret_cast<float*>(w + l.part);
+  const long long units = (long long)m.chunks * m.cblocks;
+  e = launch_k(embed_sum_kernel<T>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, lc.stream, m,
+               (const T*)dy, (T*)dw);
+  if (e != cudaSuccess) return e;
+  if (m.chunks > 1)
+    e = launch_k(embed_join_kernel<T>, dim3((unsigned)((m.chunks + 7) / 8 * m.cblocks)), dim3(256),
+                 0, lc.stream, m, (T*)dw);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+}  // namespace
+
+size_t embed_bwd_workspace(long long N, int V, int D) { return bwd_layout(N, V, D).bytes; }
+
+cudaError_t embed_fwd(const Launch& lc, int dtype, const EmbedArgs& a, const void* W, void* out) {
+  if (a.N == 0) return cudaSuccess;
+  return dtype == 0 ? fwd_typed<float>(lc, a, W, out) : fwd_typed<bf16>(lc, a, W, out);
+}
+
+cudaError_t embed_bwd(const Launch& lc, int dtype, const EmbedArgs& a, const void* dy, void* dw,
+                      void* ws) {
+  return dtype == 0 ? bwd_typed<float>(lc, a, dy, dw, ws) : bwd_typed<bf16>(lc, a, dy, dw, ws);
+}
+
+}  // namespace bcmt

@@ -266,4 +266,26 @@ struct DecodeArgs {
 cudaError_t decode_widen(const Launch& lc, int dtype, const void* x, float* out, long n);
 cudaError_t decode_step(const Launch& lc, int dtype, const DecodeArgs& a);
 
+// ------------------------------------------- embedding and dropout
+// Token ids (int32, or int64 when is64) of N tokens into a table [V, D].
+struct EmbedArgs {
+  const void* ids;
+  int is64;
+  long long N;
+  int V, D;
+  float scale;
+};
+// out[i] = scale * W[ids[i]]; an id outside [0, V) gives a zero row and sets
+// kStatusBadIndex.
+cudaError_t embed_fwd(const Launch& lc, int dtype, const EmbedArgs& a, const void* W, void* out);
+// dw[v] = scale * sum of dy[i] over the i with ids[i] = v, every row written;
+// ws: embed_bwd_workspace bytes.
+size_t embed_bwd_workspace(long long N, int V, int D);
+cudaError_t embed_bwd(const Launch& lc, int dtype, const EmbedArgs& a, const void* dy, void* dw,
+                      void* ws);
+// y = [res +] keep(seed, offset + *step, i) x / (1 - p)
+cudaError_t dropout(const Launch& lc, int dtype, const void* x, const void* res, void* y,
+                    long long n, double p, unsigned long long seed, unsigned long long offset,
+                    const unsigned long long* step);
+
 }  // namespace bcmt
