@@ -595,7 +595,8 @@ LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int
   a.dh = p->dh;
   a.decay = decay;
   a.lengths = lengths;
-  *plan = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms());
+  *plan = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(),
+                       g_use_tc_attn);
   a.nseg = plan->nseg;
   a.seg_len = plan->seg_len;
   const long long states = (long long)p->B * p->H * a.nseg * p->dh * p->dh;
@@ -1254,8 +1255,11 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
 size_t bcmt_linattn_workspace_size(const bcmt_linattn_params* p, int backward) {
   if (check_linattn(p) != BCMT_OK) return 0;
   const int npass = backward ? 3 : 1;
-  const LinPlan pl = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms());
-  const size_t states = pl.nseg > 1 ? (size_t)p->B * p->H * pl.nseg * p->dh * p->dh * 4 : 0;
+  int nseg = 1;  // whichever kernels run (bcmt_test_set_tensor_cores)
+  for (const bool tc : {false, true})
+    nseg = std::max(nseg, linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(), tc)
+                              .nseg);
+  const size_t states = nseg > 1 ? (size_t)p->B * p->H * nseg * p->dh * p->dh * 4 : 0;
   return al256(std::max<size_t>(256, npass * states));
 }
 
@@ -1289,7 +1293,9 @@ bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, lo
   f.ldo = ld_o;
   f.s_in = state_in;
   f.s_out = state_out;
-  cudaError_t e = p->T == 1 ? linattn_step(lc, p->dtype, a) : linattn_simt(lc, p->dtype, a);
+  cudaError_t e = p->T == 1 ? linattn_step(lc, p->dtype, a)
+                  : pl.tc   ? linattn_tc(lc, a)
+                            : linattn_simt(lc, p->dtype, a);
   if (e != cudaSuccess) return cuda_fail(e, "linear attention forward");
   return finish_flags(p->flags, lc.stream);
 }
@@ -1348,7 +1354,7 @@ bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o,
   }
   a.pass[1].s_out = d_state_in;
   a.pass[1].s_out_mul = p->scale;
-  cudaError_t e = linattn_simt(lc, p->dtype, a);
+  cudaError_t e = pl.tc ? linattn_tc(lc, a) : linattn_simt(lc, p->dtype, a);
   if (e != cudaSuccess) return cuda_fail(e, "linear attention backward");
   return finish_flags(p->flags, lc.stream);
 }

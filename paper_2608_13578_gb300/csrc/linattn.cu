@@ -389,13 +389,23 @@ cudaError_t simt_typed(const Launch& lc, const LinArgs& a) {
 }
 }  // namespace
 
-LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms) {
-  LinPlan pl{false, 1, T};
-  (void)dtype;
-  // enough CTAs for two on each SM, by cutting the tokens into segments of at
-  // least 64 (the walk is sequential: one segment's latency is the pass's)
-  const int slices = dh > 64 ? 2 : 1;
-  const long long ctas = (long long)B * H * slices * npass;
+LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms, bool allow_tc) {
+  const long long heads = (long long)B * H * npass;
+  LinPlan pl{allow_tc && dtype == 1 && T >= 32, 1, T};
+  if (pl.tc) {
+    // segments of whole chunks, enough for one CTA in every slot (two per SM up
+    // to width 64): the walk is sequential, and a slot left empty is lost
+    const long long slots = (long long)sms * (dh <= 64 ? 2 : 1);
+    const int chunks = (T + 127) / 128;
+    const long long n = std::max(1ll, std::min<long long>(slots / heads, chunks));
+    const int per = (int)((chunks + n - 1) / n);
+    pl.nseg = (chunks + per - 1) / per;
+    pl.seg_len = per * 128;
+    return pl;
+  }
+  // enough CTAs for two on each SM, by segments of at least 64 tokens (the walk
+  // is sequential: one segment's latency is the pass's)
+  const long long ctas = heads * (dh > 64 ? 2 : 1);
   const long long want = (2ll * sms + ctas - 1) / ctas;
   const long long most = std::max(1, T / 64);
   const long long n = std::max(1ll, std::min(want, most));

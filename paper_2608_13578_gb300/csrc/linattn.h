@@ -46,12 +46,14 @@ struct LinPlan {
   bool tc;
   int nseg, seg_len;
 };
-LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms);
+LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms, bool allow_tc);
 
 // The recurrence on CUDA cores in fp32, any dtype and head width.
 cudaError_t linattn_simt(const Launch& lc, int dtype, const LinArgs& a);
 // T = 1, forward: the state is read once and written once.
 cudaError_t linattn_step(const Launch& lc, int dtype, const LinArgs& a);
+// The chunked form on the tensor cores: bf16, segments of whole 128-token chunks.
+cudaError_t linattn_tc(const Launch& lc, const LinArgs& a);
 // Local segment states (in pass.seg) -> each segment's incoming state.
 cudaError_t linattn_combine(const Launch& lc, const LinArgs& a);
 

@@ -51,9 +51,19 @@ inline bool make_tmap(CUtensorMap* m, CUtensorMapDataType dt, const void* base, 
     bx[i] = box[i];
   }
   for (int i = 0; i < rank - 1; ++i) gs[i] = strides_bytes[i];
-  CUresult r = enc(m, dt, (cuuint32_t)rank, const_cast<void*>(base),
-                   gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  auto encode = [&]() {
+    return enc(m, dt, (cuuint32_t)rank, const_cast<void*>(base), gd, gs, bx, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  CUresult r = encode();
+  if (r == CUDA_ERROR_INVALID_CONTEXT) {
+    // a thread that has made no runtime call yet (autograd's workers) has no
+    // context current: cudaSetDevice binds its device's
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+    r = encode();
+  }
   return r == CUDA_SUCCESS;
 }
 

@@ -12,6 +12,7 @@ shapes, layouts) raise ``ValueError``; what the library refuses raises
 
 from __future__ import annotations
 
+import functools
 import math
 from typing import Optional, Tuple
 
@@ -20,22 +21,44 @@ import torch
 from . import bcmt as C
 
 _DTYPES = {torch.bfloat16: C.BCMT_BF16, torch.float32: C.BCMT_F32}
+_F32 = torch.float32
+
+# The calls below take a few microseconds of kernel time at small sizes, so
+# their own host time counts: checks format their message only when they fail,
+# parameters are built once per shape, and the stream is read as a raw handle.
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _need(ok: bool, msg: str):
-    if not ok:
-        raise ValueError(msg)
+def _device(t: torch.Tensor) -> torch.device:
+    dev = t.device
+    if dev.type != "cuda":
+        raise ValueError(f"tensors must be on a CUDA device, not {dev}")
+    return dev
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
-    _need(t.dtype in _DTYPES, f"{name} must be bfloat16 or float32, not {t.dtype}")
-    return _DTYPES[t.dtype]
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+    return dt
 
 
-def _on(device, **tensors):
-    _need(device.type == "cuda", f"tensors must be on a CUDA device, not {device}")
-    for name, t in tensors.items():
-        _need(t is None or t.device == device, f"{name} must be on {device}")
+def _check(t, name, shape, dtype, dev):
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+
+
+def _on_its_device(fn):
+    """Runs fn with its first tensor's device current (a switch only where it is not)."""
+    @functools.wraps(fn)
+    def call(*args, **kwargs):
+        first = args[0] if args else next(iter(kwargs.values()))
+        if first.is_cuda and first.get_device() != torch.cuda.current_device():
+            with torch.cuda.device(first.device):
+                return fn(*args, **kwargs)
+        return fn(*args, **kwargs)
+    return call
 
 
 def _dense(t):
@@ -47,7 +70,7 @@ def _dense(t):
 
 
 def _buffer(nbytes: int, device) -> torch.Tensor:
-    return torch.empty(max(256, nbytes), dtype=torch.uint8, device=device)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 # ------------------------------------------------------------ linear attention
@@ -55,37 +78,43 @@ def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
     """t [B, T, H, dh] as rows of one stride (a slice of a projection's output as
     it is, anything else copied), and that stride in elements."""
     B, T, H, dh = t.shape
-    ld = t.stride(1) if T > 1 else (t.stride(0) if B > 1 else H * dh)
-    ok = (t.stride(3) == 1 and (H == 1 or t.stride(2) == dh) and (B == 1 or t.stride(0) == T * ld)
-          and ld >= H * dh and ld % 8 == 0 and t.data_ptr() % 16 == 0)
-    return (t, ld) if ok else (_dense(t), H * dh)
+    sb, st, sh, sd = t.stride()
+    D = H * dh
+    ld = st if T > 1 else sb if B > 1 else D
+    if (sd == 1 and (H == 1 or sh == dh) and (B == 1 or sb == T * ld) and ld >= D and ld % 8 == 0
+            and t.data_ptr() % 16 == 0):
+        return t, ld
+    return _dense(t), D
 
 
-def _linattn_check(q, k, v, decay, lengths, state, T=None):
-    _need(q.dim() == 4, f"q must be [B, T, H, dh], not {tuple(q.shape)}")
-    B, T, H, dh = q.shape
-    _on(q.device, k=k, v=v, decay=decay, lengths=lengths, state=state)
+@functools.lru_cache(maxsize=4096)
+def _linattn_plan(B, T, H, dh, dt, scale, backward):
+    p = C.bcmt_linattn_params(B, T, H, dh, dt, 0, 1.0 / math.sqrt(dh) if scale is None else scale)
+    return p, max(256, C.bcmt_linattn_workspace_size(p, backward))
+
+
+def _linattn_check(q, k, v, decay, lengths, state):
+    dev = _device(q)
+    if q.dim() != 4:
+        raise ValueError(f"q must be [B, T, H, dh], not {tuple(q.shape)}")
     dt = _dtype(q, "q")
-    for name, t in (("k", k), ("v", v)):
-        _need(t.shape == q.shape and t.dtype == q.dtype,
-              f"{name} must have q's shape and type: {tuple(t.shape)} {t.dtype}")
-    _need(decay.shape == (H,) and decay.dtype == torch.float32,
-          f"decay must be float32 [{H}], not {decay.dtype} {tuple(decay.shape)}")
-    _need(not decay.requires_grad, "decay is a constant here: it gets no gradient")
+    shape = q.shape
+    _check(k, "k", shape, q.dtype, dev)
+    _check(v, "v", shape, q.dtype, dev)
+    B, T, H, dh = shape
+    _check(decay, "decay", (H,), _F32, dev)
+    if decay.requires_grad:
+        raise ValueError("decay is a constant here: it gets no gradient")
     if lengths is not None:
-        _need(lengths.shape == (B,) and lengths.dtype == torch.int32,
-              f"lengths must be int32 [{B}], not {lengths.dtype} {tuple(lengths.shape)}")
+        _check(lengths, "lengths", (B,), torch.int32, dev)
+        lengths = lengths.contiguous()
     if state is not None:
-        _need(state.shape == (B, H, dh, dh) and state.dtype == torch.float32,
-              f"state must be float32 {(B, H, dh, dh)}, not {state.dtype} {tuple(state.shape)}")
-    return dt
+        _check(state, "state", (B, H, dh, dh), _F32, dev)
+        state = _dense(state)
+    return dev, dt, decay.contiguous(), lengths, state
 
 
-def _linattn_params(q, scale, dt):
-    B, T, H, dh = q.shape
-    return C.bcmt_linattn_params(B, T, H, dh, dt, 0, 1.0 / math.sqrt(dh) if scale is None else scale)
-
-
+@_on_its_device
 def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, lengths=None,
                              state=None, state_out=None):
     """(o, state_out) of ``S_t = a S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t``.
@@ -95,50 +124,46 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
     T), state [B, H, dh, dh] fp32 (default zero).  scale defaults to
     1/sqrt(dh).  state_out: where the last state goes (default a new tensor; may
     be ``state``).  Tokens past a sequence's length give zero rows."""
-    dt = _linattn_check(q, k, v, decay, lengths, state)
-    if state_out is not None:
-        B, T, H, dh = q.shape
-        _need(state_out.shape == (B, H, dh, dh) and state_out.dtype == torch.float32
-              and state_out.is_contiguous() and state_out.device == q.device,
-              f"state_out must be dense float32 {(B, H, dh, dh)} on {q.device}")
-    with torch.cuda.device(q.device):
-        p = _linattn_params(q, scale, dt)
-        (q, lq), (k, lk), (v, lv) = _rows(q), _rows(k), _rows(v)
-        B, T, H, dh = q.shape
-        o = torch.empty(B, T, H, dh, dtype=q.dtype, device=q.device)
-        if state_out is None:
-            state_out = torch.empty(B, H, dh, dh, dtype=torch.float32, device=q.device)
-        ws = _buffer(C.bcmt_linattn_workspace_size(p, False), q.device)
-        C.bcmt_linattn_forward(p, q, lq, k, lk, v, lv, _dense(decay), _dense(lengths),
-                               _dense(state), o, H * dh, state_out, ws)
+    dev, dt, decay, lengths, state = _linattn_check(q, k, v, decay, lengths, state)
+    B, T, H, dh = q.shape
+    if state_out is None:
+        state_out = torch.empty((B, H, dh, dh), dtype=_F32, device=dev)
+    else:
+        _check(state_out, "state_out", (B, H, dh, dh), _F32, dev)
+        if not state_out.is_contiguous():
+            raise ValueError("state_out must be dense")
+    p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, False)
+    (q, lq), (k, lk), (v, lv) = _rows(q), _rows(k), _rows(v)
+    o = torch.empty((B, T, H, dh), dtype=q.dtype, device=dev)
+    ws = _buffer(nbytes, dev)
+    C.bcmt_linattn_forward(p, q, lq, k, lk, v, lv, decay, lengths, state, o, H * dh, state_out, ws,
+                           _raw_stream(dev.index))
     return o, state_out
 
 
+@_on_its_device
 def linear_attention_backward(do, q, k, v, decay, scale: Optional[float] = None, lengths=None,
                               state=None, dstate=None, need_dstate: Optional[bool] = None):
     """(dq, dk, dv, d_state) from the forward's inputs, do [B, T, H, dh] and the
     gradient dstate of the last state (default zero).  d_state, the gradient of
     the first state, is computed when a state was given (or by need_dstate),
     else None."""
-    dt = _linattn_check(q, k, v, decay, lengths, state)
-    _need(do.shape == q.shape and do.dtype == q.dtype and do.device == q.device,
-          f"do must have q's shape, type and device: {tuple(do.shape)} {do.dtype}")
-    if dstate is not None:
-        B, T, H, dh = q.shape
-        _need(dstate.shape == (B, H, dh, dh) and dstate.dtype == torch.float32
-              and dstate.device == q.device, f"dstate must be float32 {(B, H, dh, dh)}")
+    dev, dt, decay, lengths, state = _linattn_check(q, k, v, decay, lengths, state)
+    _check(do, "do", q.shape, q.dtype, dev)
+    B, T, H, dh = q.shape
+    D = H * dh
     if need_dstate is None:
         need_dstate = state is not None
-    with torch.cuda.device(q.device):
-        p = _linattn_params(q, scale, dt)
-        (do, ldo), (q, lq), (k, lk), (v, lv) = _rows(do), _rows(q), _rows(k), _rows(v)
-        B, T, H, dh = q.shape
-        dq, dk, dv = (torch.empty(B, T, H, dh, dtype=q.dtype, device=q.device) for _ in range(3))
-        ds = torch.empty(B, H, dh, dh, dtype=torch.float32, device=q.device) if need_dstate else None
-        ws = _buffer(C.bcmt_linattn_workspace_size(p, True), q.device)
-        C.bcmt_linattn_backward(p, do, ldo, q, lq, k, lk, v, lv, _dense(decay), _dense(lengths),
-                                _dense(state), _dense(dstate), dq, H * dh, dk, H * dh, dv, H * dh,
-                                ds, ws)
+    if dstate is not None:
+        _check(dstate, "dstate", (B, H, dh, dh), _F32, dev)
+        dstate = _dense(dstate)
+    p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, True)
+    (do, ldo), (q, lq), (k, lk), (v, lv) = _rows(do), _rows(q), _rows(k), _rows(v)
+    dq, dk, dv = (torch.empty((B, T, H, dh), dtype=q.dtype, device=dev) for _ in range(3))
+    ds = torch.empty((B, H, dh, dh), dtype=_F32, device=dev) if need_dstate else None
+    ws = _buffer(nbytes, dev)
+    C.bcmt_linattn_backward(p, do, ldo, q, lq, k, lk, v, lv, decay, lengths, state, dstate, dq, D,
+                            dk, D, dv, D, ds, ws, _raw_stream(dev.index))
     return dq, dk, dv, ds
 
 
@@ -147,10 +172,10 @@ def linear_attention_step(q, k, v, decay, state, scale: Optional[float] = None, 
     """One token of each sequence: q, k, v [B, 1, H, dh]; updates ``state`` (in
     place unless state_out is given) and returns o [B, 1, H, dh].  active [B]
     int32: sequences with 0 keep their state and get a zero row."""
-    _need(q.dim() == 4 and q.shape[1] == 1, f"q must be [B, 1, H, dh], not {tuple(q.shape)}")
-    if state_out is None:
-        state_out = state
-    return linear_attention_forward(q, k, v, decay, scale, active, state, state_out)[0]
+    if q.dim() != 4 or q.shape[1] != 1 or state is None:
+        raise ValueError(f"q must be [B, 1, H, dh], not {tuple(q.shape)}, and state a tensor")
+    return linear_attention_forward(q, k, v, decay, scale, active, state,
+                                    state if state_out is None else state_out)[0]
 
 
 class LinearAttention(torch.autograd.Function):
@@ -183,35 +208,48 @@ def linear_attention(q, k, v, decay, scale: Optional[float] = None, lengths=None
 
 
 # ------------------------------------------------------------------- embedding
-def _embedding_params(ids, V, D, dt, scale):
-    _need(ids.dtype in (torch.int32, torch.int64), f"ids must be int32 or int64, not {ids.dtype}")
-    return C.bcmt_embedding_params(ids.numel(), V, D, dt, ids.element_size(), 0, scale)
+@functools.lru_cache(maxsize=4096)
+def _embedding_plan(N, V, D, dt, id_bytes, scale):
+    p = C.bcmt_embedding_params(N, V, D, dt, id_bytes, 0, scale)
+    return p, max(256, C.bcmt_embedding_workspace_size(p))
 
 
+def _ids(ids, dev):
+    if ids.dtype != torch.int64 and ids.dtype != torch.int32:
+        raise ValueError(f"ids must be int32 or int64, not {ids.dtype}")
+    if ids.device != dev:
+        raise ValueError(f"ids must be on {dev}, not {ids.device}")
+    return ids.contiguous()
+
+
+@_on_its_device
 def embedding_forward(ids, weight, scale: float = 1.0):
     """``scale * weight[ids]``: ids of any shape (int32 or int64), weight [V, D].
     Ids outside the table give zero rows and are reported by
     ``bcmt.bcmt_device_status``."""
-    _need(weight.dim() == 2, f"weight must be [V, D], not {tuple(weight.shape)}")
-    _on(weight.device, ids=ids)
+    dev = _device(weight)
+    if weight.dim() != 2:
+        raise ValueError(f"weight must be [V, D], not {tuple(weight.shape)}")
+    ids = _ids(ids, dev)
     V, D = weight.shape
-    with torch.cuda.device(weight.device):
-        p = _embedding_params(ids, V, D, _dtype(weight, "weight"), scale)
-        out = torch.empty(*ids.shape, D, dtype=weight.dtype, device=weight.device)
-        C.bcmt_embedding_forward(p, ids.contiguous(), _dense(weight), out)
+    p, _ = _embedding_plan(ids.numel(), V, D, _dtype(weight, "weight"), ids.element_size(), scale)
+    out = torch.empty((*ids.shape, D), dtype=weight.dtype, device=dev)
+    C.bcmt_embedding_forward(p, ids, _dense(weight), out, _raw_stream(dev.index))
     return out
 
 
+@_on_its_device
 def embedding_backward(ids, dout, V: int, scale: float = 1.0):
     """Gradient [V, D] of the table from dout [*ids.shape, D]."""
-    _need(dout.shape[:-1] == ids.shape, f"dout must be [*ids.shape, D], not {tuple(dout.shape)}")
-    _on(dout.device, ids=ids)
+    dev = _device(dout)
+    if dout.shape[:-1] != ids.shape:
+        raise ValueError(f"dout must be [*ids.shape, D], not {tuple(dout.shape)}")
+    ids = _ids(ids, dev)
     D = dout.shape[-1]
-    with torch.cuda.device(dout.device):
-        p = _embedding_params(ids, V, D, _dtype(dout, "dout"), scale)
-        dw = torch.empty(V, D, dtype=dout.dtype, device=dout.device)
-        ws = _buffer(C.bcmt_embedding_workspace_size(p), dout.device)
-        C.bcmt_embedding_backward(p, ids.contiguous(), _dense(dout), dw, ws)
+    p, nbytes = _embedding_plan(ids.numel(), V, D, _dtype(dout, "dout"), ids.element_size(), scale)
+    dw = torch.empty((V, D), dtype=dout.dtype, device=dev)
+    ws = _buffer(nbytes, dev)
+    C.bcmt_embedding_backward(p, ids, _dense(dout), dw, ws, _raw_stream(dev.index))
     return dw
 
 
@@ -236,21 +274,22 @@ def embedding(ids, weight, scale: float = 1.0):
 
 
 # --------------------------------------------------------------------- dropout
+@_on_its_device
 def _dropout_call(x, p, seed, offset, residual, step):
-    _on(x.device, residual=residual, step=step)
+    dev = _device(x)
     dt = _dtype(x, "x")
     if residual is not None:
-        _need(residual.shape == x.shape and residual.dtype == x.dtype,
-              f"residual must have x's shape and type: {tuple(residual.shape)} {residual.dtype}")
+        _check(residual, "residual", x.shape, x.dtype, dev)
+        residual = _dense(residual)
     if step is not None:
-        _need(step.dtype == torch.int64 and step.numel() == 1, "step must be one int64")
+        if step.dtype != torch.int64 or step.numel() != 1 or step.device != dev:
+            raise ValueError(f"step must be one int64 on {dev}")
+        step = step.data_ptr()
+    x = _dense(x)
+    y = torch.empty(x.shape, dtype=x.dtype, device=dev)
     mask = (1 << 64) - 1
-    with torch.cuda.device(x.device):
-        x = _dense(x)
-        y = torch.empty_like(x)
-        prm = C.bcmt_dropout_params(x.numel(), dt, 0, p, seed & mask, offset & mask,
-                                    None if step is None else step.data_ptr())
-        C.bcmt_dropout(prm, x, _dense(residual), y)
+    prm = C.bcmt_dropout_params(x.numel(), dt, 0, p, seed & mask, offset & mask, step)
+    C.bcmt_dropout(prm, x, residual, y, _raw_stream(dev.index))
     return y
 
 
