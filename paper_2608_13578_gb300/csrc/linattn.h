@@ -38,6 +38,7 @@ struct LinArgs {
   const float* decay;     // [H]
   const int* lengths;     // [B] or null
   int nseg, seg_len;      // the tokens in nseg segments of seg_len
+  int joined;             // pass.seg holds the segments' incoming states, not their own
 };
 
 // How the passes are cut along the tokens (the same rule for the workspace
