@@ -44,16 +44,43 @@ namespace {
 
 constexpr int kRows = 128;  // tokens of a chunk
 
-// D[tmem] (+)= A[tmem] * B for one 16-deep K step: A bf16 pairs packed in 32-bit
-// columns, lane = row.
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
-                                            uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
+// Shared-memory matrix descriptors (128-byte swizzle, 8-row atoms of 1024 bytes)
+// as their two words: the upper one is the same for every operand here, the
+// lower one holds the address and the leading-dimension offset.  The issuing
+// threads work on lower words and 32-bit addresses, to stay within the few
+// registers they keep.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((lbo >> 4) << 16);
+}
+// D[tmem] (+)= A B over `steps` 16-deep K steps, whose operands advance by da
+// and db 16-byte units; the first step accumulates if acc0.
+template <int steps>
+__device__ __forceinline__ void issue(uint32_t d, uint32_t a, uint32_t da, uint32_t b, uint32_t db,
+                                      uint32_t idesc, uint32_t acc0) {
+#pragma unroll
+  for (int kk = 0; kk < steps; ++kk)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+        "r"(a + kk * da), "r"(b + kk * db), "r"(idesc), "r"(kk > 0 ? 1u : acc0), "r"(kDescHi)
+        : "memory");
+}
+// The same with A in TMEM: bf16 pairs packed in 32-bit columns, lane = row.
+template <int steps>
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t db,
+                                         uint32_t idesc) {
+#pragma unroll
+  for (int kk = 0; kk < steps; ++kk)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d),
+        "r"(a + kk * 8), "r"(b + kk * db), "r"(idesc), "r"(kk > 0 ? 1u : 0u), "r"(kDescHi)
+        : "memory");
 }
 // Whole warp: 16 columns of the warp's lane quarter (no wait).
 __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t* r) {
@@ -83,10 +110,11 @@ __device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b)
                "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
                : "memory");
 }
-// a^n.  Out of line, and the loops below mostly rolled: the roles run different
-// code at the same time, and unrolled copies of it (over 100 KB) made
-// instruction fetch the kernel's bound (13 us a chunk instead of under 3).
-__device__ __noinline__ float decay_pow(float a, int n) { return powf(a, (float)n); }
+// a^n from log2 a (a = 0: the logarithm is -inf).  The product's rounding shifts
+// the result by n |log2 a| 2^-24, below 2^-20 wherever a^n is above 2^-23.
+__device__ __forceinline__ float decay_pow(float lg, int n) {
+  return n == 0 ? 1.f : exp2f((float)n * lg);
+}
 
 // A warpgroup's share of the CTA's registers.
 template <int N>
@@ -132,6 +160,11 @@ __device__ __forceinline__ void key_terms(const uint4& k, uint32_t w, uint4& hi,
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
+// What a CTA's first threads work out for the others.
+struct Shared {
+  uint32_t tmem;
+  int b, h, seg, n, t_lo, t_hi, rev, have0;
+};
 template <int DP>
 struct TcGeo {
   static constexpr int kHalves = DP / 64;
@@ -143,33 +176,24 @@ struct TcGeo {
   static constexpr uint32_t kCols = DP == 64 ? 256 : 512;
   static constexpr uint32_t cO1 = DP == 64 ? 64 : 128, cO2 = cO1 + DP, cD = cO2 + DP;
   // at most 227 KB
-  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 96;
+  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 8 * 12 +
+                               (int)sizeof(Shared);
 };
 
 }  // namespace
 
-// `steps` K steps of a product whose operands advance by da and db 16-byte units
-// (a from shared memory), accumulating from the first step on if `acc0`.
-__device__ __forceinline__ void issue(uint32_t d, uint64_t a, uint32_t da, uint64_t b, uint32_t db,
-                                      uint32_t idesc, int steps, uint32_t acc0) {
-#pragma unroll 4
-  for (int kk = 0; kk < steps; ++kk, a += da, b += db)
-    tc::mma_bf16(d, a, b, idesc, kk > 0 ? 1u : acc0);
-}
-// The products of D: K'^T V into `acc`, K' in two terms over K and Q.
+// The products of D: K'^T V into `acc`, K' in two terms over K and Q of the stage
+// at shared address s.
 template <int DP>
-__device__ __forceinline__ void issue_state(uint32_t acc, const uint8_t* sQ, const uint8_t* sK,
-                                            const uint8_t* sV) {
+__device__ __forceinline__ void issue_state(uint32_t acc, uint32_t s) {
   using G = TcGeo<DP>;
   constexpr uint32_t id = tc::idesc_bf16(128, DP, 1, 1);
-  const uint64_t q = tc::sdesc(tc::smem_u32(sQ), G::kHalf, 1024);
-  const uint64_t k = tc::sdesc(tc::smem_u32(sK), G::kHalf, 1024);
-  const uint64_t v = tc::sdesc(tc::smem_u32(sV), G::kHalf, 1024);
+  const uint32_t q = desc_lo(s, G::kHalf), k = q + (G::kTile >> 4), v = k + (G::kTile >> 4);
   if (DP == 64) {  // rows 0..63 the second terms (over Q), rows 64..127 the first
-    issue(acc, q, 128, v, 128, id, kRows / 16, 0u);
+    issue<kRows / 16>(acc, q, 128, v, 128, id, 0u);
   } else {
-    issue(acc, k, 128, v, 128, id, kRows / 16, 0u);
-    issue(acc, q, 128, v, 128, id, kRows / 16, 1u);
+    issue<kRows / 16>(acc, k, 128, v, 128, id, 0u);
+    issue<kRows / 16>(acc, q, 128, v, 128, id, 1u);
   }
 }
 
@@ -183,392 +207,534 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int m, int t, int nt) 
   }
 }
 
+// A shared value, read where it is needed.
+template <class T>
+__device__ __forceinline__ T ld_once(const T* p) {
+  return *const_cast<const volatile T*>(p);
+}
+
 // The tokens of a segment that one CTA walks.
 struct Walk {
-  int n, seg_lo, seg_hi, t_lo, t_hi, nch;
+  int n, t_lo, t_hi, nch;
   bool rev;
   __device__ __forceinline__ Walk(const LinArgs& a, int b, int seg, bool r) : rev(r) {
     n = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-    seg_lo = seg * a.seg_len;
-    seg_hi = min(a.T, seg_lo + a.seg_len);
-    t_lo = min(seg_lo, n);
-    t_hi = min(seg_hi, n);
+    t_lo = min(seg * a.seg_len, n);
+    t_hi = min(min(a.T, seg * a.seg_len + a.seg_len), n);
+    nch = (t_hi - t_lo + kRows - 1) / kRows;
+  }
+  __device__ __forceinline__ explicit Walk(const Shared* s)
+      : n(ld_once(&s->n)), t_lo(ld_once(&s->t_lo)), t_hi(ld_once(&s->t_hi)),
+        rev(ld_once(&s->rev) != 0) {
     nch = (t_hi - t_lo + kRows - 1) / kRows;
   }
   __device__ __forceinline__ int start(int i) const { return t_lo + (rev ? nch - 1 - i : i) * kRows; }
   __device__ __forceinline__ int rows(int i) const { return min(kRows, t_hi - start(i)); }
+  // the chunk with fewer than kRows rows, or -1
+  __device__ __forceinline__ int ragged() const {
+    return (t_hi - t_lo) % kRows == 0 ? -1 : rev ? 0 : nch - 1;
+  }
   // 1 where the incoming state is not decayed by the chunk's first token in walk order
   __device__ __forceinline__ int fresh(int i) const { return rev && start(i) + rows(i) == n; }
 };
 
 // ------------------------------------------------------------------ the pass
-// Registers: the CTA's three warpgroups start with an equal share (80 a thread
-// where two CTAs share an SM, else 168); the state's rows need more, the single
-// issuing thread less (32 + 80 + 128 = 3 * 80, 88 + 168 + 240 <= 3 * 168).
+// Roles by warpgroup: one of rows (thread = row), NS of the state (thread = 64
+// columns of a row), one that issues.  At DP = 128 a CTA fills an SM's shared
+// memory, at DP = 64 two CTAs share it.
+// Registers: the warpgroups start with an equal share (80 a thread at DP = 64,
+// 128 at DP = 128) and trade; the sums stay within what the CTA started with.
 template <int DP>
-__global__ void __launch_bounds__(384, DP == 64 ? 2 : 1)
+struct Roles {
+  static constexpr int NS = DP == 64 ? 1 : 2;
+  static constexpr int kThreads = 128 * (NS + 2);
+  static constexpr int kRegIssue = DP == 64 ? 48 : 64, kRegRows = DP == 64 ? 80 : 128,
+                       kRegState = DP == 64 ? 112 : 152, kRegLaunch = DP == 64 ? 80 : 128;
+  static_assert(kRegIssue + kRegRows + NS * kRegState <= (NS + 2) * kRegLaunch, "registers");
+};
+
+// What the roles share: shared-memory layout, barriers, the walk.  Each role reads
+// it anew (nothing else is live across the split, so each keeps to the registers
+// that it has).
+template <int DP>
+struct View {
+  using G = TcGeo<DP>;
+  uint8_t* smem;
+  __device__ __forceinline__ View(uint8_t* raw) {
+    uint32_t s = (tc::smem_u32(raw) + 1023u) & ~1023u;
+    asm volatile("" : "+r"(s));  // a value of this role's own
+    smem = static_cast<uint8_t*>(__cvta_shared_to_generic(s));
+  }
+  __device__ __forceinline__ uint8_t* state() const { return smem + 2 * G::kStage; }
+  __device__ __forceinline__ float* pw() const {  // pw[d] = a^|d|, d = -127 .. 128
+    return reinterpret_cast<float*>(state() + G::kState) + 127;
+  }
+  __device__ __forceinline__ uint32_t* pt() const {  // a^0 .. a^127 in two bf16 terms
+    return reinterpret_cast<uint32_t*>(state() + G::kState + 4 * 256);
+  }
+  __device__ __forceinline__ uint64_t* bars() const {
+    return reinterpret_cast<uint64_t*>(state() + G::kState + 4 * 256 + 4 * 128);
+  }
+  __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 12); }
+};
+// Barriers: a stage's tiles have landed (2); product A done (2, its chunks
+// alternate), B, C, D done; P written and C, B read (rows); K' written, the
+// state's copy written and the rows past the end cleared (state).
+#define LINATTN_BARRIERS(v)                                                              \
+  uint64_t* bar = (v).bars();                                                            \
+  [[maybe_unused]] uint64_t *bar_full = bar, *bar_a = bar + 2, *bar_b = bar + 4,         \
+                            *bar_c = bar + 5, *bar_d = bar + 6, *bar_p = bar + 7,        \
+                            *bar_o = bar + 8, *bar_k = bar + 9, *bar_s = bar + 10,       \
+                            *bar_z = bar + 11;                                           \
+  bool ok = true; /* no wait of this thread has run out */                               \
+  auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); }
+
+// One thread: the products.
+template <int DP>
+__device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
+  using G = TcGeo<DP>;
+  const View<DP> vw(raw);
+  uint8_t* smem = vw.smem;
+  LINATTN_BARRIERS(vw);
+  const Walk w(vw.shared());
+  const uint32_t tmem = ld_once(&vw.shared()->tmem);
+  const bool have0 = ld_once(&vw.shared()->have0) != 0;
+  constexpr uint32_t idA = tc::idesc_bf16(128, 128, 0, 0);
+  constexpr uint32_t idO = tc::idesc_bf16(128, DP, 0, 1);
+  const uint32_t s0 = tc::smem_u32(smem);
+  const int nch = w.nch, ragged = w.ragged();  // the chunk with rows to clear, or -1
+  auto scores = [&](int i) {  // A of chunk i
+    wait(&bar_full[i & 1], i >> 1);
+    if (i == ragged) wait(bar_z, 0);
+    tc::fence_after_sync();
+    if (ok) {
+      const uint32_t dq = desc_lo(s0 + (i & 1) * G::kStage, 16), dk = dq + (G::kTile >> 4);
+#pragma unroll
+      for (int f = 0; f < G::kHalves; ++f)
+        issue<4>(tmem, dq + f * 1024, 2, dk + f * 1024, 2, idA, f > 0 ? 1u : 0u);
+    }
+    tc::mma_commit(&bar_a[i & 1]);
+  };
+  if (nch > 0) scores(0);
+#pragma unroll 1
+  for (int i = 0; i < nch; ++i) {
+    const uint32_t s = s0 + (i & 1) * G::kStage;
+    wait(bar_s, i);
+    if (i > 0) wait(bar_o, i - 1);
+    tc::fence_after_sync();
+    if (ok && (i > 0 || have0)) {
+      const uint32_t dq = desc_lo(s, 16), ds = desc_lo(s0 + 2 * G::kStage, DP * 128);
+#pragma unroll
+      for (int f = 0; f < G::kHalves; ++f)
+        issue<4>(tmem + G::cO2, dq + f * 1024, 2, ds + f * 512, 128, idO, f > 0 ? 1u : 0u);
+    }
+    tc::mma_commit(bar_b);
+    wait(bar_p, i);
+    tc::fence_after_sync();
+    if (ok)
+      issue_ts<kRows / 16>(tmem + G::cO1, tmem, desc_lo(s + 2 * G::kTile, G::kHalf), 128, idO);
+    tc::mma_commit(bar_c);
+    // the next chunk's scores replace P, and at DP = 64 also C: there D goes
+    // first.  So it does before a chunk whose last rows are to be cleared:
+    // the state's threads come to that only after this chunk's D.
+    const bool early = DP == 128 && i + 1 < nch && i + 1 != ragged;
+    if (early) {
+      wait(bar_c, i);
+      scores(i + 1);
+    }
+    wait(bar_k, i);
+    tc::fence_after_sync();
+    if (ok) issue_state<DP>(tmem + G::cD, s);
+    tc::mma_commit(bar_d);
+    if (!early && i + 1 < nch) {
+      wait(bar_c, i);
+      if (DP == 64) wait(bar_o, i);
+      scores(i + 1);
+    }
+  }
+  // no product is in flight when the CTA leaves, whatever ran out
+  if (nch > 0) tc::mbar_wait(bar_d, (nch - 1) & 1, status);
+}
+
+// One thread: the loads.
+template <int DP>
+__device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
+  using G = TcGeo<DP>;
+  const View<DP> vw(raw);
+  uint8_t* smem = vw.smem;
+  LINATTN_BARRIERS(vw);
+  const Walk w(vw.shared());
+  const int ps = blockIdx.y, h = ld_once(&vw.shared()->h);
+  const int tok0 = ld_once(&vw.shared()->b) * A.a.T;
+  int loaded = 0;
+  auto load = [&]() {  // the next chunk of the walk
+    const int i = loaded++;
+    uint8_t* s = smem + (i & 1) * G::kStage;
+    uint64_t* bf = &bar_full[i & 1];
+    const int row = tok0 + w.start(i);
+    tc::mbar_arrive_expect_tx(bf, 3 * G::kTile);
+#pragma unroll
+    for (int f = 0; f < G::kHalves; ++f) {
+      tc::tma_load_3d(s + f * G::kHalf, &A.map[A.mq[ps]], bf, f * 64, h, row);
+      tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mk[ps]], bf, f * 64, h, row);
+      tc::tma_load_3d(s + 2 * G::kTile + f * G::kHalf, &A.map[A.mv[ps]], bf, f * 64, h, row);
+    }
+  };
+  if (w.nch > 0) load();
+  if (w.nch > 1) load();
+  // every phase of bar_s is waited for in turn: a parity wait that skips one
+  // is satisfied by the phase before it
+  for (int i = 0; loaded < w.nch; ++i) {
+    wait(bar_s, i);
+    if (!ok) break;
+    // the state's threads have waited for D of chunk i - 1, issued after its C:
+    // nothing reads its stage any more
+    if (i > 0) load();
+  }
+  // the loads in flight land before the CTA leaves, however it went
+  for (int i = max(0, loaded - 2); i < loaded; ++i)
+    tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
+}
+
+// Four warps, thread = row of the chunk: P, and the output rows.
+template <int DP>
+__device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
+  using G = TcGeo<DP>;
+  const View<DP> vw(raw);
+  LINATTN_BARRIERS(vw);
+  const Walk w(vw.shared());
+  const float* pw = vw.pw();
+  const bool rev = w.rev, have0 = ld_once(&vw.shared()->have0) != 0;
+  const LinArgs& a = A.a;
+  const LinPass& p = a.pass[blockIdx.y];
+  const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5, r = tid, dh = a.dh;
+  const int h = ld_once(&vw.shared()->h);
+  const long long tok0 = (long long)ld_once(&vw.shared()->b) * a.T;
+  const uint32_t trow = ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16);
+  const bool wide = p.ldo % 16 == 0 && dh % 16 == 0 && (reinterpret_cast<uintptr_t>(p.o) & 31) == 0;
+  // P of the scores' block j (32 columns)
+  auto weigh = [&](int j, uint32_t* pk) {
+    if (rev ? j >= q : j <= q) {
+      uint32_t x[32];
+      tc::tmem_ld32_issue(trow + 32 * j, x);
+      const float* wt = pw + r - 32 * j;
+      tc::tmem_wait();
+#pragma unroll
+      for (int e = 0; e < 32; e += 2)
+        pk[e >> 1] = pack2(__uint_as_float(x[e]) * wt[-e], __uint_as_float(x[e + 1]) * wt[-e - 1]);
+      if (j == q) {  // the diagonal block: column l is seen up to (rev: from) row l
+        const uint32_t in = rev ? ~low_bits(lane) : low_bits(lane + 1);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (!((in >> (2 * e)) & 1u)) pk[e] &= 0xffff0000u;
+          if (!((in >> (2 * e + 1)) & 1u)) pk[e] &= 0x0000ffffu;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) pk[e] = 0u;
+    }
+  };
+  for (int i = 0; i < w.nch; ++i) {
+    const int t0 = w.start(i), m = w.rows(i);
+    wait(&bar_a[i & 1], i >> 1);
+    tc::fence_after_sync();
+    // block j of P covers half of the scores' block j / 2, which has been read
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+      uint32_t pk[16];
+      weigh(j, pk);
+      tmem_st16(trow + 16 * j, pk);
+    }
+    tmem_st_wait();
+    warp_arrive(bar_p, lane);
+
+    // ---- the chunk's output row
+    wait(bar_c, i);  // C was issued after B: both are done
+    tc::fence_after_sync();
+    const bool have = i > 0 || have0;
+    const float wq = r < m ? p.out_mul * pw[rev ? m - r - w.fresh(i) : r + 1] : 0.f;
+    const float2 mul2 = make_float2(p.out_mul, p.out_mul), wq2 = make_float2(wq, wq);
+    bf16* dst = (bf16*)p.o + (tok0 + t0 + r) * p.ldo + h * dh;
+#pragma unroll 1
+    for (int c0 = 0; c0 < DP; c0 += 16) {
+      uint32_t x1[16], x2[16];
+      tmem_ld16_issue(trow + G::cO1 + c0, x1);
+      if (have) tmem_ld16_issue(trow + G::cO2 + c0, x2);
+      tc::tmem_wait();
+      if (c0 + 16 == DP) warp_arrive(bar_o, lane);
+#pragma unroll
+      for (int c = 0; c < 16; c += 2) {
+        float2 y = __fmul2_rn(make_float2(__uint_as_float(x1[c]), __uint_as_float(x1[c + 1])), mul2);
+        if (have)
+          y = __ffma2_rn(make_float2(__uint_as_float(x2[c]), __uint_as_float(x2[c + 1])), wq2, y);
+        x1[c >> 1] = pack2(y.x, y.y);
+      }
+      if (r < m && ok) {
+#pragma unroll
+        for (int u = 0; u < 2; u += 2) {
+          const uint4 u0 = make_uint4(x1[4 * u], x1[4 * u + 1], x1[4 * u + 2], x1[4 * u + 3]);
+          const uint4 u1 = make_uint4(x1[4 * u + 4], x1[4 * u + 5], x1[4 * u + 6], x1[4 * u + 7]);
+          const int col = c0 + 8 * u;
+          if (wide) {
+            if (col < dh) store32(dst + col, u0, u1);
+          } else {
+            if (col < dh) *reinterpret_cast<uint4*>(dst + col) = u0;
+            if (col + 8 < dh) *reinterpret_cast<uint4*>(dst + col + 8) = u1;
+          }
+        }
+      }
+    }
+  }
+  // the rows past the sequence's end
+  const int seg_lo = ld_once(&vw.shared()->seg) * a.seg_len, seg_hi = min(a.T, seg_lo + a.seg_len);
+  const int r0 = max(seg_lo, w.n), rows = seg_hi - r0, dv = dh / 8;
+  for (int x = tid; x < rows * dv; x += 128) {
+    const int rr = x / dv, u = x - rr * dv;
+    *reinterpret_cast<uint4*>((bf16*)p.o + (tok0 + r0 + rr) * p.ldo + h * dh + u * 8) =
+        make_uint4(0, 0, 0, 0);
+  }
+}
+
+// 4 NS warps, thread = 64 columns of a row of the state; at DP = 64 the lower 64
+// threads keep the sums of the keys' second terms.
+template <int DP>
+__device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
+  using G = TcGeo<DP>;
+  constexpr int NS = Roles<DP>::NS;
+  const View<DP> vw(raw);
+  uint8_t *smem = vw.smem, *sS = vw.state();
+  LINATTN_BARRIERS(vw);
+  const Walk w(vw.shared());
+  const float* pw = vw.pw();
+  const uint32_t* pt = vw.pt();
+  const bool rev = w.rev, have0 = ld_once(&vw.shared()->have0) != 0;
+  const LinArgs& a = A.a;
+  const LinPass& p = a.pass[blockIdx.y];
+  const int dh = a.dh, seg = ld_once(&vw.shared()->seg);
+  const int bh = ld_once(&vw.shared()->b) * a.H + ld_once(&vw.shared()->h);
+  const long long st = (long long)dh * dh;
+  const float dec = pw[1], lg = log2f(dec);
+  const int tid = threadIdx.x, lane = tid & 31, r = tid & 127, q = r >> 5;
+  const int t = tid - 128, g = t >> 7, c64 = g * 64;
+  const bool lo_part = DP == 64 && r < 64;
+  const int srow = DP == 64 ? r & 63 : r;
+  float S[64];
+#pragma unroll
+  for (int c = 0; c < 64; ++c) S[c] = 0.f;
+  const bool mine = !lo_part && srow < dh;
+  const uint32_t tinc =
+      ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16) + G::cD + c64;
+  if (have0) {
+    // the incoming state, through the increment's TMEM columns: 16 columns of
+    // the row at a time
+    const float in_mul = w.n > 0 ? p.s_in_mul : 1.f;  // an empty sequence passes its state on
+#pragma unroll 1
+    for (int c0 = 0; c0 < 64; c0 += 16) {
+      const int col = c64 + c0;
+      float v[16];
+#pragma unroll
+      for (int c = 0; c < 16; ++c) v[c] = 0.f;
+      if (mine && a.nseg > 1 && a.joined) {
+        const float* src = p.seg + ((long long)bh * a.nseg + seg) * st + srow * dh + col;
+#pragma unroll
+        for (int c = 0; c < 16; c += 4)
+          if (col + c < dh) load4(src + c, v + c);
+      } else if (mine) {
+        if (p.s_in) {
+          const float* src = p.s_in + (long long)bh * st;
+          const long si = p.s_in_t ? 1 : dh, sj = p.s_in_t ? dh : 1;
+#pragma unroll
+          for (int c = 0; c < 16; ++c)
+            if (col + c < dh) v[c] = in_mul * src[srow * si + (col + c) * sj];
+        }
+        // the segments before this one, in walk order
+#pragma unroll 1
+        for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1) {
+          const int ms = min(max(w.n - s * a.seg_len, 0), a.seg_len);
+          if (ms == 0) continue;
+          const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
+          const float f = decay_pow(lg, ms - (fresh ? 1 : 0));
+          const float* src = p.seg + ((long long)bh * a.nseg + s) * st + srow * dh + col;
+#pragma unroll
+          for (int c = 0; c < 16; c += 4)
+            if (col + c < dh) {
+              float x[4];
+              load4(src + c, x);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[c + e] = fmaf(f, v[c + e], x[e]);
+            }
+        }
+      }
+      uint32_t u[16];
+#pragma unroll
+      for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(v[c]);
+      tmem_st16(tinc + c0, u);
+    }
+    tmem_st_wait();
+  }
+  float f = 0.f;
+  for (int i = 0;; ++i) {
+    // S <- f S + increment: the incoming state, then each chunk's
+    if (i > 0 || have0) {
+#pragma unroll
+      for (int c0 = 0; c0 < 64; c0 += 32) {
+        uint32_t d[32];
+        tc::tmem_ld32_issue(tinc + c0, d);
+        tc::tmem_wait();
+        const float2 f2 = make_float2(f, f);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const float2 y =
+              __ffma2_rn(f2, make_float2(S[c0 + c], S[c0 + c + 1]),
+                         make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])));
+          S[c0 + c] = y.x;
+          S[c0 + c + 1] = y.y;
+        }
+      }
+    }
+    if (i == w.nch) break;
+    if (!lo_part) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        *reinterpret_cast<uint4*>(sS + g * (DP * 128) + tc::sw128_offset(srow, u)) =
+            pack8(S + 8 * u);
+    }
+    tc::fence_proxy_async_smem();
+    warp_arrive(bar_s, lane);
+
+    uint8_t* sQ = smem + (i & 1) * G::kStage;
+    uint8_t* sK = sQ + G::kTile;
+    const int m = w.rows(i);
+    wait(&bar_full[i & 1], i >> 1);
+    if (m < kRows) {
+      // rows past the end may hold anything, and they meet zero weights only
+      clear_rows<DP>(sK, m, t, 128 * NS);
+      clear_rows<DP>(sK + G::kTile, m, t, 128 * NS);
+      tc::fence_proxy_async_smem();
+      warp_arrive(bar_z, lane);
+    }
+    wait(&bar_a[i & 1], i >> 1);  // the keys have been used
+    const uint32_t* wr = rev ? pt : pt + m - 1;
+    uint4 lo[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int idx = x * (128 * NS) + t, row = (idx >> 3) & 127;
+      const uint32_t off = (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7);
+      uint4 hi;
+      key_terms(*reinterpret_cast<const uint4*>(sK + off), row < m ? wr[rev ? row : -row] : 0u, hi,
+                lo[x]);
+      *reinterpret_cast<uint4*>(sK + off) = hi;
+    }
+    wait(bar_b, i);  // and so have the queries
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int idx = x * (128 * NS) + t, row = (idx >> 3) & 127;
+      *reinterpret_cast<uint4*>(sQ + (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7)) =
+          lo[x];
+    }
+    tc::fence_proxy_async_smem();
+    warp_arrive(bar_k, lane);
+    f = pw[m - w.fresh(i)];
+    wait(bar_d, i);
+    tc::fence_after_sync();
+  }
+  if (p.s_out && seg == (rev ? 0 : a.nseg - 1)) {  // uniform over the CTA
+    float* dst = p.s_out + (long long)bh * st + srow * dh + c64;
+    const float mul = w.n > 0 ? p.s_out_mul * (rev ? dec : 1.f) : 1.f;
+    if (DP == 64) {  // the two terms' sums, through the idle stages
+      float* x = reinterpret_cast<float*>(smem);
+      if (w.nch > 0) wait(bar_c, w.nch - 1);
+      if (lo_part) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[srow * 65 + c] = S[c];
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (!lo_part) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) S[c] += x[srow * 65 + c];
+      }
+    }
+    if (mine && ok) {
+#pragma unroll
+      for (int c = 0; c < 64; c += 4)
+        if (c64 + c < dh) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = S[c + e] * mul;
+          store4(dst + c, v);
+        }
+    }
+  }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     linattn_tc_kernel(const __grid_constant__ LinTcArgs A, unsigned* status) {
   using G = TcGeo<DP>;
+  using R = Roles<DP>;
+  constexpr int NS = R::NS;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = align1024(smem_raw);
-  uint8_t* sS = smem + 2 * G::kStage;
-  float* pw = reinterpret_cast<float*>(sS + G::kState) + 127;  // pw[d] = a^|d|, d = -127 .. 128
-  uint32_t* pt = reinterpret_cast<uint32_t*>(pw + 129);        // a^0 .. a^127 in two bf16 terms
-  uint64_t* bar = reinterpret_cast<uint64_t*>(pt + 128);
-  uint64_t* bar_full = bar;   // a stage's tiles have landed (2)
-  uint64_t* bar_a = bar + 2;  // products A .. D done
-  uint64_t* bar_b = bar + 3;
-  uint64_t* bar_c = bar + 4;
-  uint64_t* bar_d = bar + 5;
-  uint64_t* bar_p = bar + 6;  // P written (rows)
-  uint64_t* bar_o = bar + 7;  // C and B read (rows)
-  uint64_t* bar_k = bar + 8;  // K' written (state)
-  uint64_t* bar_s = bar + 9;  // the state's copy written (state)
-  uint64_t* bar_z = bar + 10;  // the rows past the end cleared (state; at most one chunk)
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 11);
-
-  const LinArgs& a = A.a;
-  const int ps = blockIdx.y;
-  const LinPass& p = a.pass[ps];
-  const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg;
-  const int b = bh / a.H, h = bh - b * a.H;
-  const bool rev = p.rev != 0;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3;
-  const int r = q * 32 + lane;
-
-  if (tid == 0) {
-    for (int i = 0; i < 6; ++i) tc::mbar_init(&bar[i], 1);
-    for (int i = 6; i < 11; ++i) tc::mbar_init(&bar[i], 4);
-    tc::fence_mbar_init();
-  }
-  if (warp == 8) {
-    if (lane < 3) tc::prefetch_tmap(&A.map[lane == 0 ? A.mq[ps] : lane == 1 ? A.mk[ps] : A.mv[ps]]);
-    tc::tmem_alloc(tslot, G::kCols);
-    tc::tmem_relinquish();
-  }
-  pdl_enter();
-  const Walk w(a, b, seg, rev);
-  const float dec = a.decay[h];
-  const int dh = a.dh;
-  const long long tok0 = (long long)b * a.T;
-  const long long st = (long long)dh * dh;
-  const bool have0 = p.s_in != nullptr || (a.nseg > 1 && seg != (rev ? a.nseg - 1 : 0));
-  if (tid < 129) {
-    const float x = decay_pow(dec, tid);
-    pw[tid] = x;
-    if (tid < 128) {
-      pw[-tid] = x;
-      pt[tid] = weight_terms(x);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  {
+    const View<DP> vw(smem_raw);
+    uint64_t* bar = vw.bars();
+    if (tid == 0) {
+      for (int i = 0; i < 7; ++i) tc::mbar_init(&bar[i], 1);
+      for (int i = 7; i < 9; ++i) tc::mbar_init(&bar[i], 4);
+      for (int i = 9; i < 12; ++i) tc::mbar_init(&bar[i], 4 * NS);
+      tc::fence_mbar_init();
+    }
+    const int ps = blockIdx.y;
+    if (warp == 4 + 4 * NS) {
+      if (lane < 3) tc::prefetch_tmap(&A.map[lane == 0 ? A.mq[ps] : lane == 1 ? A.mk[ps] : A.mv[ps]]);
+      tc::tmem_alloc(&vw.shared()->tmem, G::kCols);
+      tc::tmem_relinquish();
+    }
+    pdl_enter();
+    const LinArgs& a = A.a;
+    const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, b = bh / a.H, h = bh - b * a.H;
+    const bool rev = a.pass[ps].rev != 0;
+    if (tid == 32) {
+      Shared* sh = vw.shared();
+      sh->b = b;
+      sh->h = h;
+      sh->seg = seg;
+      sh->rev = rev;
+      sh->have0 = a.pass[ps].s_in != nullptr || (a.nseg > 1 && seg != (rev ? a.nseg - 1 : 0));
+      const Walk w(a, b, seg, rev);
+      sh->n = w.n;
+      sh->t_lo = w.t_lo;
+      sh->t_hi = w.t_hi;
+    }
+    if (tid >= 64 && tid < 193) {
+      const int d = tid - 64;
+      const float x = decay_pow(log2f(a.decay[h]), d);
+      vw.pw()[d] = d == 1 ? a.decay[h] : x;
+      if (d < 128) {
+        vw.pw()[-d] = x;
+        vw.pt()[d] = weight_terms(x);
+      }
     }
   }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmem = *tslot;
-  const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16);
-  bool ok = true;  // no wait of this thread has run out
-  auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); };
-
-  if (warp >= 8) {
-    reg_dec<DP == 64 ? 32 : 88>();
-    if (tid == 256) {
-      // ------------------------------------------------ loads and products
-      constexpr uint32_t idA = tc::idesc_bf16(128, 128, 0, 0);
-      constexpr uint32_t idO = tc::idesc_bf16(128, DP, 0, 1);
-      int loaded = 0;
-      auto load = [&]() {  // the next chunk of the walk
-        const int i = loaded++;
-        uint8_t* s = smem + (i & 1) * G::kStage;
-        uint64_t* bf = &bar_full[i & 1];
-        const int row = (int)(tok0 + w.start(i));
-        tc::mbar_arrive_expect_tx(bf, 3 * G::kTile);
-#pragma unroll
-        for (int f = 0; f < G::kHalves; ++f) {
-          tc::tma_load_3d(s + f * G::kHalf, &A.map[A.mq[ps]], bf, f * 64, h, row);
-          tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mk[ps]], bf, f * 64, h, row);
-          tc::tma_load_3d(s + 2 * G::kTile + f * G::kHalf, &A.map[A.mv[ps]], bf, f * 64, h, row);
-        }
-      };
-      if (w.nch > 0) load();
-      if (w.nch > 1) load();
-      for (int i = 0; i < w.nch; ++i) {
-        uint8_t* sQ = smem + (i & 1) * G::kStage;
-        uint8_t* sK = sQ + G::kTile;
-        uint8_t* sV = sK + G::kTile;
-        wait(&bar_full[i & 1], i >> 1);
-        if (w.rows(i) < kRows) wait(bar_z, 0);
-        if (i > 0) {  // P and, at DP = 64, P V share the scores' columns
-          wait(bar_c, i - 1);
-          wait(bar_o, i - 1);
-        }
-        tc::fence_after_sync();
-        const uint64_t dq = tc::sdesc(tc::smem_u32(sQ), 16, 1024);
-        if (ok) {
-          const uint64_t dk = tc::sdesc(tc::smem_u32(sK), 16, 1024);
-#pragma unroll
-          for (int f = 0; f < G::kHalves; ++f)
-            issue(tmem, dq + f * 1024, 2, dk + f * 1024, 2, idA, 4, f > 0 ? 1u : 0u);
-        }
-        tc::mma_commit(bar_a);
-        wait(bar_s, i);
-        // chunk i - 1 has had all its products: its stage takes chunk i + 1
-        if (ok && i > 0 && loaded < w.nch) load();
-        tc::fence_after_sync();
-        if (ok && (i > 0 || have0)) {
-          const uint64_t ds = tc::sdesc(tc::smem_u32(sS), DP * 128, 1024);
-#pragma unroll
-          for (int f = 0; f < G::kHalves; ++f)
-            issue(tmem + G::cO2, dq + f * 1024, 2, ds + f * 512, 128, idO, 4, f > 0 ? 1u : 0u);
-        }
-        tc::mma_commit(bar_b);
-        wait(bar_p, i);
-        tc::fence_after_sync();
-        if (ok) {
-          const uint64_t dv = tc::sdesc(tc::smem_u32(sV), G::kHalf, 1024);
-#pragma unroll 4
-          for (int kk = 0; kk < kRows / 16; ++kk)
-            mma_bf16_ts(tmem + G::cO1, tmem + kk * 8, dv + kk * 128, idO, kk > 0 ? 1u : 0u);
-        }
-        tc::mma_commit(bar_c);
-        wait(bar_k, i);
-        tc::fence_after_sync();
-        if (ok) issue_state<DP>(tmem + G::cD, sQ, sK, sV);
-        tc::mma_commit(bar_d);
-      }
-      if (!ok) {  // the loads in flight land before the CTA leaves
-        for (int i = max(0, loaded - 2); i < loaded; ++i)
-          tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
-      }
-    }
+  if (warp >= 4 + 4 * NS) {
+    reg_dec<R::kRegIssue>();
+    if (tid == 128 + 128 * NS) role_products<DP>(A, smem_raw, status);
+    if (tid == 160 + 128 * NS) role_loads<DP>(A, smem_raw, status);
     __syncwarp();
   } else if (warp < 4) {
-    // ------------------------------------------------------------- rows
-    const bool wide = p.ldo % 16 == 0 && dh % 16 == 0 && (reinterpret_cast<uintptr_t>(p.o) & 31) == 0;
-    for (int i = 0; i < w.nch; ++i) {
-      const int t0 = w.start(i), m = w.rows(i);
-      wait(bar_a, i);
-      tc::fence_after_sync();
-      // P, 32 columns at a time: block j of it covers half of the scores' block
-      // j / 2, which has been read by then
-#pragma unroll 1
-      for (int j = 0; j < 4; ++j) {
-        uint32_t pk[16];
-        if (rev ? j >= q : j <= q) {
-          uint32_t x[32];
-          tc::tmem_ld32_issue(trow + 32 * j, x);
-          const float* wt = pw + r - 32 * j;
-          tc::tmem_wait();
-#pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            pk[e >> 1] = pack2(__uint_as_float(x[e]) * wt[-e], __uint_as_float(x[e + 1]) * wt[-e - 1]);
-          if (j == q) {  // the diagonal block: column l is seen up to (rev: from) row l
-            const uint32_t in = rev ? ~low_bits(lane) : low_bits(lane + 1);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              if (!((in >> (2 * e)) & 1u)) pk[e] &= 0xffff0000u;
-              if (!((in >> (2 * e + 1)) & 1u)) pk[e] &= 0x0000ffffu;
-            }
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) pk[e] = 0u;
-        }
-        tmem_st16(trow + 16 * j, pk);
-      }
-      tmem_st_wait();
-      warp_arrive(bar_p, lane);
-
-      // ---- the chunk's output row
-      wait(bar_c, i);  // C was issued after B: both are done
-      tc::fence_after_sync();
-      const bool have = i > 0 || have0;
-      const float wq = r < m ? p.out_mul * pw[rev ? m - r - w.fresh(i) : r + 1] : 0.f;
-      bf16* dst = (bf16*)p.o + (tok0 + t0 + r) * p.ldo + h * dh;
-#pragma unroll 1
-      for (int c0 = 0; c0 < DP; c0 += 16) {
-        uint32_t x1[16], x2[16];
-        tmem_ld16_issue(trow + G::cO1 + c0, x1);
-        if (have) tmem_ld16_issue(trow + G::cO2 + c0, x2);
-        tc::tmem_wait();
-        if (c0 + 16 == DP) warp_arrive(bar_o, lane);
-        float o[16];
-        const float2 mul2 = make_float2(p.out_mul, p.out_mul), wq2 = make_float2(wq, wq);
-#pragma unroll
-        for (int c = 0; c < 16; c += 2) {
-          float2 y = __fmul2_rn(make_float2(__uint_as_float(x1[c]), __uint_as_float(x1[c + 1])), mul2);
-          if (have)
-            y = __ffma2_rn(make_float2(__uint_as_float(x2[c]), __uint_as_float(x2[c + 1])), wq2, y);
-          o[c] = y.x;
-          o[c + 1] = y.y;
-        }
-        if (r < m && ok) {
-          const uint4 u0 = pack8(o), u1 = pack8(o + 8);
-          if (wide) {
-            if (c0 < dh) store32(dst + c0, u0, u1);
-          } else {
-            if (c0 < dh) *reinterpret_cast<uint4*>(dst + c0) = u0;
-            if (c0 + 8 < dh) *reinterpret_cast<uint4*>(dst + c0 + 8) = u1;
-          }
-        }
-      }
-    }
-    // the rows past the sequence's end
-    const int r0 = max(w.seg_lo, w.n), rows = w.seg_hi - r0, dv = dh / 8;
-    for (int x = tid; x < rows * dv; x += 128) {
-      const int rr = x / dv, u = x - rr * dv;
-      *reinterpret_cast<uint4*>((bf16*)p.o + (tok0 + r0 + rr) * p.ldo + h * dh + u * 8) =
-          make_uint4(0, 0, 0, 0);
-    }
+    if constexpr (R::kRegRows > R::kRegLaunch) reg_inc<R::kRegRows>();
+    role_rows<DP>(A, smem_raw, status);
   } else {
-    // ------------------------------------------------------------ state
-    // thread: a row of the state; at DP = 64 the lower 64 threads keep the sums
-    // of the keys' second terms
-    reg_inc<DP == 64 ? 128 : 240>();
-    const int t = tid - 128;
-    const bool lo_part = DP == 64 && r < 64;
-    const int srow = DP == 64 ? r & 63 : r;
-    float S[DP];
-#pragma unroll
-    for (int c = 0; c < DP; ++c) S[c] = 0.f;
-    const bool mine = !lo_part && srow < dh;
-    if (have0) {
-      // the incoming state, through the increment's TMEM columns: 16 columns of
-      // the row at a time
-      const float in_mul = w.n > 0 ? p.s_in_mul : 1.f;  // an empty sequence passes its state on
-#pragma unroll 1
-      for (int c0 = 0; c0 < DP; c0 += 16) {
-        float v[16];
-#pragma unroll
-        for (int c = 0; c < 16; ++c) v[c] = 0.f;
-        if (mine && a.nseg > 1 && a.joined) {
-          const float* src = p.seg + ((long long)bh * a.nseg + seg) * st + srow * dh + c0;
-#pragma unroll
-          for (int c = 0; c < 16; c += 4)
-            if (c0 + c < dh) load4(src + c, v + c);
-        } else if (mine) {
-          if (p.s_in) {
-            const float* src = p.s_in + (long long)bh * st;
-            const long si = p.s_in_t ? 1 : dh, sj = p.s_in_t ? dh : 1;
-#pragma unroll
-            for (int c = 0; c < 16; ++c)
-              if (c0 + c < dh) v[c] = in_mul * src[srow * si + (c0 + c) * sj];
-          }
-          // the segments before this one, in walk order
-#pragma unroll 1
-          for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1) {
-            const int ms = min(max(w.n - s * a.seg_len, 0), a.seg_len);
-            if (ms == 0) continue;
-            const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
-            const float f = decay_pow(dec, ms - (fresh ? 1 : 0));
-            const float* src = p.seg + ((long long)bh * a.nseg + s) * st + srow * dh + c0;
-#pragma unroll
-            for (int c = 0; c < 16; c += 4)
-              if (c0 + c < dh) {
-                float x[4];
-                load4(src + c, x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[c + e] = fmaf(f, v[c + e], x[e]);
-              }
-          }
-        }
-        uint32_t u[16];
-#pragma unroll
-        for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(v[c]);
-        tmem_st16(trow + G::cD + c0, u);
-      }
-      tmem_st_wait();
-    }
-    float f = 0.f;
-    for (int i = 0;; ++i) {
-      // S <- f S + increment: the incoming state, then each chunk's
-      if (i > 0 || have0) {
-#pragma unroll
-        for (int c0 = 0; c0 < DP; c0 += 32) {
-          uint32_t d[32];
-          tc::tmem_ld32_issue(trow + G::cD + c0, d);
-          tc::tmem_wait();
-          const float2 f2 = make_float2(f, f);
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const float2 y =
-                __ffma2_rn(f2, make_float2(S[c0 + c], S[c0 + c + 1]),
-                           make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])));
-            S[c0 + c] = y.x;
-            S[c0 + c + 1] = y.y;
-          }
-        }
-      }
-      if (i == w.nch) break;
-      if (!lo_part) {
-#pragma unroll
-        for (int u = 0; u < DP / 8; ++u)
-          *reinterpret_cast<uint4*>(sS + (u >> 3) * (DP * 128) + tc::sw128_offset(srow, u & 7)) =
-              pack8(S + 8 * u);
-      }
-      tc::fence_proxy_async_smem();
-      warp_arrive(bar_s, lane);
-
-      uint8_t* sQ = smem + (i & 1) * G::kStage;
-      uint8_t* sK = sQ + G::kTile;
-      const int m = w.rows(i);
-      if (m < kRows) {
-        // rows past the end may hold anything, and they meet zero weights only
-        wait(&bar_full[i & 1], i >> 1);
-        clear_rows<DP>(sK, m, t, 128);
-        clear_rows<DP>(sK + G::kTile, m, t, 128);
-        tc::fence_proxy_async_smem();
-        warp_arrive(bar_z, lane);
-      }
-      wait(&bar_full[i & 1], i >> 1);
-      wait(bar_b, i);  // the keys and the queries have been used
-      const uint32_t* wr = rev ? pt : pt + m - 1;
-#pragma unroll 4
-      for (int x = 0; x < DP / 8; ++x) {
-        const int idx = x * 128 + t, row = (idx >> 3) & 127;
-        const uint32_t off = (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7);
-        uint4 hi, lo;
-        key_terms(*reinterpret_cast<const uint4*>(sK + off), row < m ? wr[rev ? row : -row] : 0u,
-                  hi, lo);
-        *reinterpret_cast<uint4*>(sK + off) = hi;
-        *reinterpret_cast<uint4*>(sQ + off) = lo;
-      }
-      tc::fence_proxy_async_smem();
-      warp_arrive(bar_k, lane);
-      f = pw[m - w.fresh(i)];
-      wait(bar_d, i);
-      tc::fence_after_sync();
-    }
-    if (p.s_out && seg == (rev ? 0 : a.nseg - 1)) {  // uniform over the CTA
-      float* dst = p.s_out + (long long)bh * st + srow * dh;
-      const float mul = w.n > 0 ? p.s_out_mul * (rev ? dec : 1.f) : 1.f;
-      if (DP == 64) {  // the two terms' sums, through the idle stages
-        float* x = reinterpret_cast<float*>(smem);
-        if (w.nch > 0) wait(bar_c, w.nch - 1);
-        if (lo_part) {
-#pragma unroll
-          for (int c = 0; c < DP; ++c) x[srow * 65 + c] = S[c];
-        }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (!lo_part) {
-#pragma unroll
-          for (int c = 0; c < DP; ++c) S[c] += x[srow * 65 + c];
-        }
-      }
-      if (mine && ok) {
-#pragma unroll
-        for (int c = 0; c < DP; c += 4)
-          if (c < dh) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = S[c + e] * mul;
-            store4(dst + c, v);
-          }
-      }
-    }
+    reg_inc<R::kRegState>();
+    role_state<DP>(A, smem_raw, status);
   }
   tc::fence_before_sync();
   __syncthreads();
-  if (warp == 8) tc::tmem_dealloc(tmem, G::kCols);
+  if (warp == 4 + 4 * NS) tc::tmem_dealloc(View<DP>(smem_raw).shared()->tmem, G::kCols);
 }
 
 // ---------------------------------------------------------- segment states
@@ -613,11 +779,11 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
   }
   pdl_enter();
   const Walk w(a, b, seg, rev);
-  const float dec = a.decay[h];
+  const float dec = a.decay[h], lg = log2f(dec);
   const int dh = a.dh;
   const long long tok0 = (long long)b * a.T;
   if (tid < 129) {
-    const float x = decay_pow(dec, tid);
+    const float x = decay_pow(lg, tid);
     pw[tid] = x;
     if (tid < 128) pt[tid] = weight_terms(x);
   }
@@ -647,19 +813,20 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
       if (w.nch > 0) load();
       if (w.nch > 1) load();
       for (int i = 0; i < w.nch; ++i) {
-        uint8_t* sQ = smem + (i & 1) * G::kStage;
         wait(bar_k, i);
         tc::fence_after_sync();
-        if (ok) issue_state<DP>(tmem + (i & 1) * DP, sQ, sQ + G::kTile, sQ + 2 * G::kTile);
+        if (ok) issue_state<DP>(tmem + (i & 1) * DP, tc::smem_u32(smem) + (i & 1) * G::kStage);
         tc::mma_commit(&bar_d[i & 1]);
         if (loaded < w.nch) {
           wait(&bar_d[i & 1], i >> 1);  // the stage is free again
           if (ok) load();
         }
       }
-      if (!ok) {
+      if (!ok) {  // the loads and products in flight end before the CTA leaves
         for (int i = max(0, loaded - 2); i < loaded; ++i)
           tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
+        for (int i = max(0, w.nch - 2); i < w.nch; ++i)
+          tc::mbar_wait(&bar_d[i & 1], (i >> 1) & 1, status);
       }
     }
     __syncwarp();
@@ -748,7 +915,8 @@ cudaError_t tc_launch(const Launch& lc, const LinTcArgs& A) {
     if (e != cudaSuccess) return e;
     if (A.a.joined && (e = linattn_combine(lc, A.a)) != cudaSuccess) return e;
   }
-  e = launch_k(linattn_tc_kernel<DP>, dim3(heads * A.a.nseg, A.a.npass), dim3(384), G::kSmem,
+  e = launch_k(linattn_tc_kernel<DP>, dim3(heads * A.a.nseg, A.a.npass),
+               dim3(Roles<DP>::kThreads), G::kSmem,
                lc.stream, A, lc.status);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -30,6 +30,15 @@ def F(cuda_ok):
     return lm_ops
 
 
+@pytest.fixture(autouse=True)
+def no_wait_ran_out(F):
+    """A bounded wait that expires leaves a result that may be wrong and a status."""
+    from paper_2608_13578_gb300 import bcmt as C
+    C.bcmt_device_status()
+    yield
+    C.bcmt_device_status()
+
+
 def np64(t):
     return None if t is None else t.detach().double().cpu().numpy()
 
@@ -108,6 +117,30 @@ def test_linear_attention_backward(F, B, T, H, dh, dtype, state):
         check_rel("d_state", got[3], ref[3], ts)
     else:
         assert got[3] is None
+
+
+# enough heads that one CTA walks several chunks of a head (no segments)
+WALKS = [(40, 4, 128, 300), (32, 10, 64, 385), (80, 1, 96, 512), (160, 2, 40, 260)]
+
+
+@pytest.mark.parametrize("B,H,dh,T", WALKS)
+@pytest.mark.parametrize("ragged", [False, True], ids=["full", "ragged"])
+def test_linear_attention_long_walks(F, B, H, dh, T, ragged):
+    lengths = [(37 * b + 101) % (T + 1) for b in range(B)] if ragged else None
+    d, r = make(B, T, H, dh, "bf16", 14, True, lengths)
+    o, S = F.linear_attention_forward(d["q"], d["k"], d["v"], d["decay"], None, d["n"], d["s0"])
+    got = F.linear_attention_backward(d["do"], d["q"], d["k"], d["v"], d["decay"], None, d["n"],
+                                      d["s0"], d["ds"])
+    some = [0, 1, B // 2, B - 1]
+    r = {k: v if k == "decay" or v is None else v[some] for k, v in r.items()}
+    ro, rS = R.linear_attention(r["q"], r["k"], r["v"], r["decay"], dh ** -0.5, r["n"], r["s0"])
+    ref = R.linear_attention_grads(r["do"], r["q"], r["k"], r["v"], r["decay"], dh ** -0.5, r["n"],
+                                   r["s0"], r["ds"])
+    to, ts = tolerances("bf16", T, dh)
+    for name, a, b, t in zip(("o", "state", "dq", "dk", "dv", "d_state"), (o, S, *got),
+                             (ro, rS, *ref), (to, ts, to, to, to, ts)):
+        check_rel(name, a[some], b, t)
+        assert torch.isfinite(a).all(), name
 
 
 LENGTHS = [(200, [0, 1, 200, 64]), (300, [300, 129, 128, 127]), (150, [0, 0, 0, 0]),
