@@ -92,7 +92,13 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t* r) {
         "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
 }
-// Whole warp: 16 columns of the warp's lane quarter, written.
+// Whole warp: 8 or 16 columns of the warp's lane quarter, written.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -176,7 +182,7 @@ struct TcGeo {
   static constexpr uint32_t kCols = DP == 64 ? 256 : 512;
   static constexpr uint32_t cO1 = DP == 64 ? 64 : 128, cO2 = cO1 + DP, cD = cO2 + DP;
   // at most 227 KB
-  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 8 * 12 +
+  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 4 * 32 + 8 * 12 +
                                (int)sizeof(Shared);
 };
 
@@ -239,18 +245,19 @@ struct Walk {
 };
 
 // ------------------------------------------------------------------ the pass
-// Roles by warpgroup: one of rows (thread = row), NS of the state (thread = 64
-// columns of a row), one that issues.  At DP = 128 a CTA fills an SM's shared
-// memory, at DP = 64 two CTAs share it.
-// Registers: the warpgroups start with an equal share (80 a thread at DP = 64,
-// 128 at DP = 128) and trade; the sums stay within what the CTA started with.
+// Roles by warpgroup: NW of rows, NW of the state (a thread has 64 columns of its
+// row in both), one that issues.  At DP = 128 a CTA fills an SM's shared memory
+// (NW = 2), at DP = 64 two CTAs share it (NW = 1).
+// Registers: the warpgroups start with an equal share (80 a thread at DP = 64, 96
+// at DP = 128) and trade; the sums stay within what the CTA started with.
 template <int DP>
 struct Roles {
-  static constexpr int NS = DP == 64 ? 1 : 2;
-  static constexpr int kThreads = 128 * (NS + 2);
-  static constexpr int kRegIssue = DP == 64 ? 48 : 64, kRegRows = DP == 64 ? 80 : 128,
-                       kRegState = DP == 64 ? 112 : 152, kRegLaunch = DP == 64 ? 80 : 128;
-  static_assert(kRegIssue + kRegRows + NS * kRegState <= (NS + 2) * kRegLaunch, "registers");
+  static constexpr int NW = DP == 64 ? 1 : 2;
+  static constexpr int kThreads = 128 * (2 * NW + 1);
+  static constexpr int kRegLaunch = DP == 64 ? 80 : 96;
+  static constexpr int kRegIssue = DP == 64 ? 48 : 64, kRegRows = DP == 64 ? 80 : 96,
+                       kRegState = 112;
+  static_assert(kRegIssue + NW * (kRegRows + kRegState) <= (2 * NW + 1) * kRegLaunch, "registers");
 };
 
 // What the roles share: shared-memory layout, barriers, the walk.  Each role reads
@@ -272,8 +279,11 @@ struct View {
   __device__ __forceinline__ uint32_t* pt() const {  // a^0 .. a^127 in two bf16 terms
     return reinterpret_cast<uint32_t*>(state() + G::kState + 4 * 256);
   }
+  __device__ __forceinline__ float* cw() const {  // a^(distance of column l from the far end)
+    return reinterpret_cast<float*>(state() + G::kState + 4 * 256 + 4 * 128);
+  }
   __device__ __forceinline__ uint64_t* bars() const {
-    return reinterpret_cast<uint64_t*>(state() + G::kState + 4 * 256 + 4 * 128);
+    return reinterpret_cast<uint64_t*>(state() + G::kState + 4 * 256 + 4 * 128 + 4 * 32);
   }
   __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 12); }
 };
@@ -334,19 +344,13 @@ __device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, 
     if (ok)
       issue_ts<kRows / 16>(tmem + G::cO1, tmem, desc_lo(s + 2 * G::kTile, G::kHalf), 128, idO);
     tc::mma_commit(bar_c);
-    // the next chunk's scores replace P, and at DP = 64 also C: there D goes
-    // first.  So it does before a chunk whose last rows are to be cleared:
-    // the state's threads come to that only after this chunk's D.
-    const bool early = DP == 128 && i + 1 < nch && i + 1 != ragged;
-    if (early) {
-      wait(bar_c, i);
-      scores(i + 1);
-    }
     wait(bar_k, i);
     tc::fence_after_sync();
     if (ok) issue_state<DP>(tmem + G::cD, s);
     tc::mma_commit(bar_d);
-    if (!early && i + 1 < nch) {
+    // the next chunk's scores replace P and, at DP = 64, C.  They come after D:
+    // ahead of it they would hold it up until the next chunk's tiles are there
+    if (i + 1 < nch) {
       wait(bar_c, i);
       if (DP == 64) wait(bar_o, i);
       scores(i + 1);
@@ -382,21 +386,20 @@ __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, uns
   };
   if (w.nch > 0) load();
   if (w.nch > 1) load();
-  // every phase of bar_s is waited for in turn: a parity wait that skips one
-  // is satisfied by the phase before it
+  // D of chunk i is its last product: its stage takes chunk i + 2.  (Every phase is
+  // waited for in turn: a parity wait that skips one is satisfied by the phase
+  // before it.)
   for (int i = 0; loaded < w.nch; ++i) {
-    wait(bar_s, i);
+    wait(bar_d, i);
     if (!ok) break;
-    // the state's threads have waited for D of chunk i - 1, issued after its C:
-    // nothing reads its stage any more
-    if (i > 0) load();
+    load();
   }
   // the loads in flight land before the CTA leaves, however it went
   for (int i = max(0, loaded - 2); i < loaded; ++i)
     tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
 }
 
-// Four warps, thread = row of the chunk: P, and the output rows.
+// 4 NW warps, thread = row of the chunk: P, and 64 columns of the output rows.
 template <int DP>
 __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
   using G = TcGeo<DP>;
@@ -407,44 +410,88 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
   const bool rev = w.rev, have0 = ld_once(&vw.shared()->have0) != 0;
   const LinArgs& a = A.a;
   const LinPass& p = a.pass[blockIdx.y];
-  const int tid = threadIdx.x, lane = tid & 31, q = tid >> 5, r = tid, dh = a.dh;
+  constexpr int NW = Roles<DP>::NW;
+  const int tid = threadIdx.x, lane = tid & 31, g = tid >> 7, r = tid & 127, q = r >> 5, dh = a.dh;
+  const float* cw = vw.cw();
   const int h = ld_once(&vw.shared()->h);
   const long long tok0 = (long long)ld_once(&vw.shared()->b) * a.T;
   const uint32_t trow = ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16);
   const bool wide = p.ldo % 16 == 0 && dh % 16 == 0 && (reinterpret_cast<uintptr_t>(p.o) & 31) == 0;
-  // P of the scores' block j (32 columns)
-  auto weigh = [&](int j, uint32_t* pk) {
-    if (rev ? j >= q : j <= q) {
-      uint32_t x[32];
-      tc::tmem_ld32_issue(trow + 32 * j, x);
-      const float* wt = pw + r - 32 * j;
-      tc::tmem_wait();
+  // P of the scores' columns 16 hh .. 16 hh + 15
+  auto weigh = [&](int hh, const uint32_t* x, uint32_t* pk) {
+    const int j = hh >> 1, l0 = (hh & 1) * 16;
+    if (j == q) {  // the diagonal block: column l is seen up to (rev: from) row l
+      const float* wt = pw + lane - l0;
+      const uint32_t in = (rev ? ~low_bits(lane) : low_bits(lane + 1)) >> l0;
 #pragma unroll
-      for (int e = 0; e < 32; e += 2)
-        pk[e >> 1] = pack2(__uint_as_float(x[e]) * wt[-e], __uint_as_float(x[e + 1]) * wt[-e - 1]);
-      if (j == q) {  // the diagonal block: column l is seen up to (rev: from) row l
-        const uint32_t in = rev ? ~low_bits(lane) : low_bits(lane + 1);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (!((in >> (2 * e)) & 1u)) pk[e] &= 0xffff0000u;
-          if (!((in >> (2 * e + 1)) & 1u)) pk[e] &= 0x0000ffffu;
-        }
+      for (int e = 0; e < 16; e += 2) {
+        const float v0 = __uint_as_float(x[e]) * wt[-e];
+        const float v1 = __uint_as_float(x[e + 1]) * wt[-e - 1];
+        pk[e >> 1] = pack2((in >> e) & 1u ? v0 : 0.f, (in >> (e + 1)) & 1u ? v1 : 0.f);
       }
-    } else {
+    } else {  // a^(distance) as the row's distance from the block times the column's in it
+      const float base = rev ? pw[32 * (j - q) - lane] : pw[32 * (q - j) + lane - 31];
+      const float2 base2 = make_float2(base, base);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) pk[e] = 0u;
+      for (int e = 0; e < 16; e += 4) {
+        const float4 c4 = *reinterpret_cast<const float4*>(cw + l0 + e);
+        const float2 v0 =
+            __fmul2_rn(__fmul2_rn(make_float2(c4.x, c4.y), base2),
+                       make_float2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])));
+        const float2 v1 =
+            __fmul2_rn(__fmul2_rn(make_float2(c4.z, c4.w), base2),
+                       make_float2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])));
+        pk[e >> 1] = pack2(v0.x, v0.y);
+        pk[(e >> 1) + 1] = pack2(v1.x, v1.y);
+      }
     }
   };
+  // the halves hh of blocks that the row sees
+  const int h0 = rev ? 2 * q : 0, h1 = rev ? 8 : 2 * q + 2;
   for (int i = 0; i < w.nch; ++i) {
     const int t0 = w.start(i), m = w.rows(i);
     wait(&bar_a[i & 1], i >> 1);
     tc::fence_after_sync();
-    // block j of P covers half of the scores' block j / 2, which has been read
+    if (NW == 1) {
+      // half hh of P covers columns of the scores' half hh / 2, read by then; the
+      // next half's scores are on their way under this one's arithmetic
+      uint32_t x[2][16];
+      tmem_ld16_issue(trow + 16 * h0, x[0]);
 #pragma unroll 1
-    for (int j = 0; j < 4; ++j) {
-      uint32_t pk[16];
-      weigh(j, pk);
-      tmem_st16(trow + 16 * j, pk);
+      for (int hh = h0; hh < h1; hh += 2) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          uint32_t pk[8];
+          tc::tmem_wait();
+          if (hh + y + 1 < h1) tmem_ld16_issue(trow + 16 * (hh + y + 1), x[1 - y]);
+          weigh(hh + y, x[y], pk);
+          tmem_st8(trow + 8 * (hh + y), pk);
+        }
+      }
+    } else {
+      // the quarter's two warps take every other half
+      uint32_t pk[4][8];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int hh = h0 + g + 2 * y;
+        if (hh >= h1) break;
+        uint32_t x[16];
+        tmem_ld16_issue(trow + 16 * hh, x);
+        tc::tmem_wait();
+        weigh(hh, x, pk[y]);
+      }
+      // both have read their scores: P may replace them
+      tc::fence_before_sync();
+      asm volatile("bar.sync %0, 64;" ::"r"(q + 1) : "memory");
+      tc::fence_after_sync();
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        if (h0 + g + 2 * y < h1) tmem_st8(trow + 8 * (h0 + g + 2 * y), pk[y]);
+    }
+    {
+      const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll 1
+      for (int hh = (rev ? 0 : h1) + g; hh < (rev ? h0 : 8); hh += NW) tmem_st8(trow + 8 * hh, zero);
     }
     tmem_st_wait();
     warp_arrive(bar_p, lane);
@@ -457,12 +504,12 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
     const float2 mul2 = make_float2(p.out_mul, p.out_mul), wq2 = make_float2(wq, wq);
     bf16* dst = (bf16*)p.o + (tok0 + t0 + r) * p.ldo + h * dh;
 #pragma unroll 1
-    for (int c0 = 0; c0 < DP; c0 += 16) {
+    for (int c0 = g * 64; c0 < g * 64 + 64; c0 += 16) {
       uint32_t x1[16], x2[16];
       tmem_ld16_issue(trow + G::cO1 + c0, x1);
       if (have) tmem_ld16_issue(trow + G::cO2 + c0, x2);
       tc::tmem_wait();
-      if (c0 + 16 == DP) warp_arrive(bar_o, lane);
+      if ((c0 & 48) == 48) warp_arrive(bar_o, lane);
 #pragma unroll
       for (int c = 0; c < 16; c += 2) {
         float2 y = __fmul2_rn(make_float2(__uint_as_float(x1[c]), __uint_as_float(x1[c + 1])), mul2);
@@ -471,17 +518,13 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
         x1[c >> 1] = pack2(y.x, y.y);
       }
       if (r < m && ok) {
-#pragma unroll
-        for (int u = 0; u < 2; u += 2) {
-          const uint4 u0 = make_uint4(x1[4 * u], x1[4 * u + 1], x1[4 * u + 2], x1[4 * u + 3]);
-          const uint4 u1 = make_uint4(x1[4 * u + 4], x1[4 * u + 5], x1[4 * u + 6], x1[4 * u + 7]);
-          const int col = c0 + 8 * u;
-          if (wide) {
-            if (col < dh) store32(dst + col, u0, u1);
-          } else {
-            if (col < dh) *reinterpret_cast<uint4*>(dst + col) = u0;
-            if (col + 8 < dh) *reinterpret_cast<uint4*>(dst + col + 8) = u1;
-          }
+        const uint4 u0 = make_uint4(x1[0], x1[1], x1[2], x1[3]);
+        const uint4 u1 = make_uint4(x1[4], x1[5], x1[6], x1[7]);
+        if (wide) {
+          if (c0 < dh) store32(dst + c0, u0, u1);
+        } else {
+          if (c0 < dh) *reinterpret_cast<uint4*>(dst + c0) = u0;
+          if (c0 + 8 < dh) *reinterpret_cast<uint4*>(dst + c0 + 8) = u1;
         }
       }
     }
@@ -489,19 +532,19 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
   // the rows past the sequence's end
   const int seg_lo = ld_once(&vw.shared()->seg) * a.seg_len, seg_hi = min(a.T, seg_lo + a.seg_len);
   const int r0 = max(seg_lo, w.n), rows = seg_hi - r0, dv = dh / 8;
-  for (int x = tid; x < rows * dv; x += 128) {
+  for (int x = tid; x < rows * dv; x += 128 * NW) {
     const int rr = x / dv, u = x - rr * dv;
     *reinterpret_cast<uint4*>((bf16*)p.o + (tok0 + r0 + rr) * p.ldo + h * dh + u * 8) =
         make_uint4(0, 0, 0, 0);
   }
 }
 
-// 4 NS warps, thread = 64 columns of a row of the state; at DP = 64 the lower 64
+// 4 NW warps, thread = 64 columns of a row of the state; at DP = 64 the lower 64
 // threads keep the sums of the keys' second terms.
 template <int DP>
 __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
   using G = TcGeo<DP>;
-  constexpr int NS = Roles<DP>::NS;
+  constexpr int NW = Roles<DP>::NW;
   const View<DP> vw(raw);
   uint8_t *smem = vw.smem, *sS = vw.state();
   LINATTN_BARRIERS(vw);
@@ -516,7 +559,7 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
   const long long st = (long long)dh * dh;
   const float dec = pw[1], lg = log2f(dec);
   const int tid = threadIdx.x, lane = tid & 31, r = tid & 127, q = r >> 5;
-  const int t = tid - 128, g = t >> 7, c64 = g * 64;
+  const int t = tid - 128 * NW, g = t >> 7, c64 = g * 64;
   const bool lo_part = DP == 64 && r < 64;
   const int srow = DP == 64 ? r & 63 : r;
   float S[64];
@@ -609,8 +652,8 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
     wait(&bar_full[i & 1], i >> 1);
     if (m < kRows) {
       // rows past the end may hold anything, and they meet zero weights only
-      clear_rows<DP>(sK, m, t, 128 * NS);
-      clear_rows<DP>(sK + G::kTile, m, t, 128 * NS);
+      clear_rows<DP>(sK, m, t, 128 * NW);
+      clear_rows<DP>(sK + G::kTile, m, t, 128 * NW);
       tc::fence_proxy_async_smem();
       warp_arrive(bar_z, lane);
     }
@@ -619,7 +662,7 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
     uint4 lo[8];
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
-      const int idx = x * (128 * NS) + t, row = (idx >> 3) & 127;
+      const int idx = x * (128 * NW) + t, row = (idx >> 3) & 127;
       const uint32_t off = (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7);
       uint4 hi;
       key_terms(*reinterpret_cast<const uint4*>(sK + off), row < m ? wr[rev ? row : -row] : 0u, hi,
@@ -629,7 +672,7 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
     wait(bar_b, i);  // and so have the queries
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
-      const int idx = x * (128 * NS) + t, row = (idx >> 3) & 127;
+      const int idx = x * (128 * NW) + t, row = (idx >> 3) & 127;
       *reinterpret_cast<uint4*>(sQ + (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7)) =
           lo[x];
     }
@@ -673,7 +716,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     linattn_tc_kernel(const __grid_constant__ LinTcArgs A, unsigned* status) {
   using G = TcGeo<DP>;
   using R = Roles<DP>;
-  constexpr int NS = R::NS;
+  constexpr int NW = R::NW;
   extern __shared__ uint8_t smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   {
@@ -681,12 +724,11 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     uint64_t* bar = vw.bars();
     if (tid == 0) {
       for (int i = 0; i < 7; ++i) tc::mbar_init(&bar[i], 1);
-      for (int i = 7; i < 9; ++i) tc::mbar_init(&bar[i], 4);
-      for (int i = 9; i < 12; ++i) tc::mbar_init(&bar[i], 4 * NS);
+      for (int i = 7; i < 12; ++i) tc::mbar_init(&bar[i], 4 * NW);
       tc::fence_mbar_init();
     }
     const int ps = blockIdx.y;
-    if (warp == 4 + 4 * NS) {
+    if (warp == 8 * NW) {
       if (lane < 3) tc::prefetch_tmap(&A.map[lane == 0 ? A.mq[ps] : lane == 1 ? A.mk[ps] : A.mv[ps]]);
       tc::tmem_alloc(&vw.shared()->tmem, G::kCols);
       tc::tmem_relinquish();
@@ -714,19 +756,20 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
       if (d < 128) {
         vw.pw()[-d] = x;
         vw.pt()[d] = weight_terms(x);
+        if (d < 32) vw.cw()[rev ? d : 31 - d] = d == 1 ? a.decay[h] : x;
       }
     }
   }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  if (warp >= 4 + 4 * NS) {
+  if (warp >= 8 * NW) {
     reg_dec<R::kRegIssue>();
-    if (tid == 128 + 128 * NS) role_products<DP>(A, smem_raw, status);
-    if (tid == 160 + 128 * NS) role_loads<DP>(A, smem_raw, status);
+    if (tid == 256 * NW) role_products<DP>(A, smem_raw, status);
+    if (tid == 256 * NW + 32) role_loads<DP>(A, smem_raw, status);
     __syncwarp();
-  } else if (warp < 4) {
-    if constexpr (R::kRegRows > R::kRegLaunch) reg_inc<R::kRegRows>();
+  } else if (warp < 4 * NW) {
+    reg_dec<R::kRegRows>();
     role_rows<DP>(A, smem_raw, status);
   } else {
     reg_inc<R::kRegState>();
@@ -734,7 +777,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
   }
   tc::fence_before_sync();
   __syncthreads();
-  if (warp == 4 + 4 * NS) tc::tmem_dealloc(View<DP>(smem_raw).shared()->tmem, G::kCols);
+  if (warp == 8 * NW) tc::tmem_dealloc(View<DP>(smem_raw).shared()->tmem, G::kCols);
 }
 
 // ---------------------------------------------------------- segment states
