@@ -92,19 +92,11 @@ __device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t* r) {
         "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
 }
-// Whole warp: 8 or 16 columns of the warp's lane quarter, written.
+// Whole warp: 8 columns of the warp's lane quarter, written.
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() {
@@ -182,7 +174,7 @@ struct TcGeo {
   static constexpr uint32_t kCols = DP == 64 ? 256 : 512;
   static constexpr uint32_t cO1 = DP == 64 ? 64 : 128, cO2 = cO1 + DP, cD = cO2 + DP;
   // at most 227 KB
-  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 4 * 32 + 8 * 12 +
+  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 4 * 32 + 8 * 13 +
                                (int)sizeof(Shared);
 };
 
@@ -285,17 +277,20 @@ struct View {
   __device__ __forceinline__ uint64_t* bars() const {
     return reinterpret_cast<uint64_t*>(state() + G::kState + 4 * 256 + 4 * 128 + 4 * 32);
   }
-  __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 12); }
+  __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 13); }
 };
-// Barriers: a stage's tiles have landed (2); product A done (2, its chunks
-// alternate), B, C, D done; P written and C, B read (rows); K' written, the
-// state's copy written and the rows past the end cleared (state).
+// Barriers: a stage's tiles have landed, products A and D done (two of each, for
+// alternate chunks); B, C done; P written and C, B read (rows); K' written, the
+// state's copy written and the rows past the end cleared (state).  A wait names
+// a phase by its parity alone, so nobody may be able to complete two phases of a
+// barrier before one of its waiters has looked at the first: where one role
+// could run that far ahead of another, there are two barriers.
 #define LINATTN_BARRIERS(v)                                                              \
   uint64_t* bar = (v).bars();                                                            \
-  [[maybe_unused]] uint64_t *bar_full = bar, *bar_a = bar + 2, *bar_b = bar + 4,         \
-                            *bar_c = bar + 5, *bar_d = bar + 6, *bar_p = bar + 7,        \
-                            *bar_o = bar + 8, *bar_k = bar + 9, *bar_s = bar + 10,       \
-                            *bar_z = bar + 11;                                           \
+  [[maybe_unused]] uint64_t *bar_full = bar, *bar_a = bar + 2, *bar_d = bar + 4,         \
+                            *bar_b = bar + 6, *bar_c = bar + 7, *bar_p = bar + 8,        \
+                            *bar_o = bar + 9, *bar_k = bar + 10, *bar_s = bar + 11,      \
+                            *bar_z = bar + 12;                                           \
   bool ok = true; /* no wait of this thread has run out */                               \
   auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); }
 
@@ -347,7 +342,7 @@ __device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, 
     wait(bar_k, i);
     tc::fence_after_sync();
     if (ok) issue_state<DP>(tmem + G::cD, s);
-    tc::mma_commit(bar_d);
+    tc::mma_commit(&bar_d[i & 1]);
     // the next chunk's scores replace P and, at DP = 64, C.  They come after D:
     // ahead of it they would hold it up until the next chunk's tiles are there
     if (i + 1 < nch) {
@@ -357,7 +352,7 @@ __device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, 
     }
   }
   // no product is in flight when the CTA leaves, whatever ran out
-  if (nch > 0) tc::mbar_wait(bar_d, (nch - 1) & 1, status);
+  if (nch > 0) tc::mbar_wait(&bar_d[(nch - 1) & 1], ((nch - 1) >> 1) & 1, status);
 }
 
 // One thread: the loads.
@@ -386,11 +381,9 @@ __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, uns
   };
   if (w.nch > 0) load();
   if (w.nch > 1) load();
-  // D of chunk i is its last product: its stage takes chunk i + 2.  (Every phase is
-  // waited for in turn: a parity wait that skips one is satisfied by the phase
-  // before it.)
+  // D of chunk i is its last product: its stage takes chunk i + 2
   for (int i = 0; loaded < w.nch; ++i) {
-    wait(bar_d, i);
+    wait(&bar_d[i & 1], i >> 1);
     if (!ok) break;
     load();
   }
@@ -568,58 +561,47 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
   const bool mine = !lo_part && srow < dh;
   const uint32_t tinc =
       ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16) + G::cD + c64;
-  if (have0) {
-    // the incoming state, through the increment's TMEM columns: 16 columns of
-    // the row at a time
-    const float in_mul = w.n > 0 ? p.s_in_mul : 1.f;  // an empty sequence passes its state on
-#pragma unroll 1
-    for (int c0 = 0; c0 < 64; c0 += 16) {
-      const int col = c64 + c0;
-      float v[16];
+  if (mine) {
+    const bool joined = a.nseg > 1 && a.joined;
+    const float* src = joined   ? p.seg + ((long long)bh * a.nseg + seg) * st
+                       : p.s_in ? p.s_in + (long long)bh * st
+                                : nullptr;
+    if (src && (joined || !p.s_in_t)) {
 #pragma unroll
-      for (int c = 0; c < 16; ++c) v[c] = 0.f;
-      if (mine && a.nseg > 1 && a.joined) {
-        const float* src = p.seg + ((long long)bh * a.nseg + seg) * st + srow * dh + col;
+      for (int c = 0; c < 64; c += 4)
+        if (c64 + c < dh) load4(src + srow * dh + c64 + c, S + c);
+    } else if (src) {
 #pragma unroll
-        for (int c = 0; c < 16; c += 4)
-          if (col + c < dh) load4(src + c, v + c);
-      } else if (mine) {
-        if (p.s_in) {
-          const float* src = p.s_in + (long long)bh * st;
-          const long si = p.s_in_t ? 1 : dh, sj = p.s_in_t ? dh : 1;
-#pragma unroll
-          for (int c = 0; c < 16; ++c)
-            if (col + c < dh) v[c] = in_mul * src[srow * si + (col + c) * sj];
-        }
-        // the segments before this one, in walk order
-#pragma unroll 1
-        for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1) {
-          const int ms = min(max(w.n - s * a.seg_len, 0), a.seg_len);
-          if (ms == 0) continue;
-          const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
-          const float f = decay_pow(lg, ms - (fresh ? 1 : 0));
-          const float* src = p.seg + ((long long)bh * a.nseg + s) * st + srow * dh + col;
-#pragma unroll
-          for (int c = 0; c < 16; c += 4)
-            if (col + c < dh) {
-              float x[4];
-              load4(src + c, x);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[c + e] = fmaf(f, v[c + e], x[e]);
-            }
-        }
-      }
-      uint32_t u[16];
-#pragma unroll
-      for (int c = 0; c < 16; ++c) u[c] = __float_as_uint(v[c]);
-      tmem_st16(tinc + c0, u);
+      for (int c = 0; c < 64; ++c)
+        if (c64 + c < dh) S[c] = src[(c64 + c) * dh + srow];
     }
-    tmem_st_wait();
+    if (!joined) {
+      if (p.s_in_mul != 1.f && w.n > 0) {  // an empty sequence passes its state on as it is
+#pragma unroll
+        for (int c = 0; c < 64; ++c) S[c] *= p.s_in_mul;
+      }
+      // the segments before this one, in walk order
+#pragma unroll 1
+      for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1) {
+        const int ms = min(max(w.n - s * a.seg_len, 0), a.seg_len);
+        if (ms == 0) continue;
+        const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
+        const float f = decay_pow(lg, ms - (fresh ? 1 : 0));
+        const float* x = p.seg + ((long long)bh * a.nseg + s) * st + srow * dh + c64;
+#pragma unroll
+        for (int c = 0; c < 64; c += 4)
+          if (c64 + c < dh) {
+            float v[4];
+            load4(x + c, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[c + e] = fmaf(f, S[c + e], v[e]);
+          }
+      }
+    }
   }
   float f = 0.f;
   for (int i = 0;; ++i) {
-    // S <- f S + increment: the incoming state, then each chunk's
-    if (i > 0 || have0) {
+    if (i > 0) {  // S <- f S + the last chunk's increment
 #pragma unroll
       for (int c0 = 0; c0 < 64; c0 += 32) {
         uint32_t d[32];
@@ -679,7 +661,7 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
     tc::fence_proxy_async_smem();
     warp_arrive(bar_k, lane);
     f = pw[m - w.fresh(i)];
-    wait(bar_d, i);
+    wait(&bar_d[i & 1], i >> 1);
     tc::fence_after_sync();
   }
   if (p.s_out && seg == (rev ? 0 : a.nseg - 1)) {  // uniform over the CTA
@@ -723,8 +705,8 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     const View<DP> vw(smem_raw);
     uint64_t* bar = vw.bars();
     if (tid == 0) {
-      for (int i = 0; i < 7; ++i) tc::mbar_init(&bar[i], 1);
-      for (int i = 7; i < 12; ++i) tc::mbar_init(&bar[i], 4 * NW);
+      for (int i = 0; i < 8; ++i) tc::mbar_init(&bar[i], 1);
+      for (int i = 8; i < 13; ++i) tc::mbar_init(&bar[i], 4 * NW);
       tc::fence_mbar_init();
     }
     const int ps = blockIdx.y;
@@ -797,8 +779,8 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
   uint64_t* bar = reinterpret_cast<uint64_t*>(pt + 128);
   uint64_t* bar_full = bar;   // (2)
   uint64_t* bar_d = bar + 2;  // (2)
-  uint64_t* bar_k = bar + 4;
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 5);
+  uint64_t* bar_k = bar + 4;  // (2): K' of the next chunk may be written before D is issued
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 6);
 
   const LinArgs& a = A.a;
   const int ps = blockIdx.y;
@@ -812,7 +794,8 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
   const int r = q * 32 + lane;
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) tc::mbar_init(&bar[i], 1);
-    tc::mbar_init(bar_k, 8);
+    tc::mbar_init(&bar_k[0], 8);
+    tc::mbar_init(&bar_k[1], 8);
     tc::fence_mbar_init();
   }
   if (warp == 8) {
@@ -856,7 +839,7 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
       if (w.nch > 0) load();
       if (w.nch > 1) load();
       for (int i = 0; i < w.nch; ++i) {
-        wait(bar_k, i);
+        wait(&bar_k[i & 1], i >> 1);
         tc::fence_after_sync();
         if (ok) issue_state<DP>(tmem + (i & 1) * DP, tc::smem_u32(smem) + (i & 1) * G::kStage);
         tc::mma_commit(&bar_d[i & 1]);
@@ -913,7 +896,7 @@ __global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
         *reinterpret_cast<uint4*>(sQ + off) = lo;
       }
       tc::fence_proxy_async_smem();
-      warp_arrive(bar_k, lane);
+      warp_arrive(&bar_k[i & 1], lane);
       if (i > 0) add(i - 1);
     }
     if (w.nch > 0) add(w.nch - 1);
