@@ -7,13 +7,21 @@ residual blocks (mixer, then a GELU MLP), a final LayerNorm, an untied LM head
 and next-token cross-entropy, trained with AdamW.  The paper does not print its
 block wiring; these are the standard choices, named as readings in the design
 notes.  Only the mixer is this library: ``BCMTMixer`` calls the C ABI's forward
-and backward kernels.  Embeddings, LayerNorm, MLP, LM head, loss and optimizer
-are PyTorch's own CUDA kernels.
+and backward kernels.  Embeddings (but see ``embed_scale``), LayerNorm, MLP, LM head,
+loss and optimizer are PyTorch's own CUDA kernels.
 
 ``mixer="dense"`` swaps in ordinary dense causal attention of the same shape
 (x W_qkv -> PyTorch SDPA with a causal mask -> W_O), the baseline the paper
 compares against; ``honly=True`` is the HOnly ablation of Sec. 4.5 (no block
-summaries and no memory: Y = H).
+summaries and no memory: Y = H).  ``mixer="linear"`` is linear attention with a
+decay per head (BCMT's exponential memory taken per token), by the library's
+operators; its state makes the model a recurrent one, so ``generate`` reads a
+batch of prompts in one pass and then decodes token by token at a cost that does
+not grow with the length.
+
+``embed_scale`` and ``dropout`` put the library's scaled embedding (with its
+gradient by sorted tokens) and its counter-based dropout in place of PyTorch's
+embedding and of no dropout; both are off by default.
 """
 
 from __future__ import annotations
@@ -25,6 +33,7 @@ import torch
 import torch.nn as nn
 import torch.nn.functional as F
 
+from . import lm_ops
 from .layer import BCMTMixer
 
 
@@ -37,14 +46,18 @@ class GPTConfig:
     mlp: int = 2048
     L: int = 64
     T: int = 1024
-    mixer: str = "bcmt"          # "bcmt" or "dense"
+    mixer: str = "bcmt"          # "bcmt", "dense" or "linear"
     honly: bool = False
     decay: float = 0.8           # broadcast per-channel decay (Sec. 3.5)
     learn_decay: bool = False    # learned per-channel decay (Sec. 5, future work)
+    embed_scale: float = 0.0     # > 0: the library's embedding, rows times this
+    dropout: float = 0.0         # > 0: after the embedding and on both branches of a block
+    dropout_seed: int = 0
 
 
 class Mixer(nn.Module):
-    """The token mixer of one block: BCMT (Sec. 3.3-3.8) or dense causal attention."""
+    """The token mixer of one block: BCMT (Sec. 3.3-3.8), dense causal attention
+    or linear attention with a decay per head."""
 
     def __init__(self, c: GPTConfig):
         super().__init__()
@@ -62,12 +75,20 @@ class Mixer(nn.Module):
                 self.decay = nn.Parameter(decay)
             else:
                 self.register_buffer("decay", decay)
+        elif c.mixer == "linear":
+            # memories of about 32 to 512 tokens, in powers of two over the heads
+            e = torch.linspace(5.0, 9.0, c.H) if c.H > 1 else torch.tensor([6.0])
+            self.register_buffer("decay", 1.0 - torch.exp2(-e))
         elif c.mixer != "dense":
             raise ValueError(f"unknown mixer {c.mixer!r}")
 
     def _apply(self, fn, *args, **kwargs):
-        # the decay stays fp32 whatever dtype the rest of the model takes
+        # the decay stays fp32 whatever dtype the rest of the model takes (near 1
+        # it would not survive bf16 and back)
+        kept = self.decay.detach() if self.c.mixer == "linear" else None
         out = super()._apply(fn, *args, **kwargs)
+        if kept is not None and self.decay.dtype != torch.float32:
+            self.decay = kept.to(self.decay.device)
         if self.c.mixer == "bcmt" and self.decay.dtype != torch.float32:
             self.decay.data = self.decay.data.float()
         return out
@@ -77,24 +98,48 @@ class Mixer(nn.Module):
         if c.mixer == "bcmt":
             return BCMTMixer.apply(x, self.w_qkv, self.w_o, self.w_p, self.w_m, self.w_g,
                                    self.decay, c.L, c.H, c.honly)
+        if c.mixer == "linear":
+            return self.recurrent(x)[0]
         B, T, D = x.shape
         q, k, v = (x @ self.w_qkv).view(B, T, 3, c.H, D // c.H).permute(2, 0, 3, 1, 4)
         o = F.scaled_dot_product_attention(q, k, v, is_causal=True)
         return o.transpose(1, 2).reshape(B, T, D) @ self.w_o
 
 
+    def recurrent(self, x, state=None, lengths=None):
+        """Linear attention from a state [B, H, dh, dh] (None: from nothing):
+        (output rows, last state).  lengths [B] int32: tokens per sequence."""
+        B, T, D = x.shape
+        q, k, v = (x @ self.w_qkv).view(B, T, 3, self.c.H, D // self.c.H).unbind(2)
+        o, state = lm_ops.linear_attention(q, k, v, self.decay, lengths=lengths, state=state)
+        return o.reshape(B, T, D) @ self.w_o, state
+
+
 class Block(nn.Module):
     def __init__(self, c: GPTConfig):
         super().__init__()
+        self.c = c
         self.ln1 = nn.LayerNorm(c.D)
         self.mix = Mixer(c)
         self.ln2 = nn.LayerNorm(c.D)
         self.fc1 = nn.Linear(c.D, c.mlp)
         self.fc2 = nn.Linear(c.mlp, c.D)
 
-    def forward(self, x):
+    def forward(self, x, drop=None):
+        """drop(branch, residual, site): the branch with dropout, plus the residual."""
+        if drop is not None:
+            x = drop(self.mix(self.ln1(x)), x, 0)
+            return drop(self.mlp(x), x, 1)
         x = x + self.mix(self.ln1(x))
-        return x + self.fc2(F.gelu(self.fc1(self.ln2(x))))
+        return x + self.mlp(x)
+
+    def mlp(self, x):
+        return self.fc2(F.gelu(self.fc1(self.ln2(x))))
+
+    def recurrent(self, x, state, lengths=None):
+        m, state = self.mix.recurrent(self.ln1(x), state, lengths)
+        x = x + m
+        return x + self.mlp(x), state
 
 
 class GPT(nn.Module):
@@ -106,12 +151,45 @@ class GPT(nn.Module):
         self.blocks = nn.ModuleList(Block(c) for _ in range(c.layers))
         self.ln_f = nn.LayerNorm(c.D)
         self.head = nn.Linear(c.D, c.vocab, bias=False)
+        # training steps done: part of the dropout's counter, on the device so that
+        # a captured step draws new masks at each replay
+        self.register_buffer("drop_step", torch.zeros(1, dtype=torch.int64), persistent=False)
+
+    def embed(self, ids):
+        if self.c.embed_scale > 0:
+            return lm_ops.embedding(ids, self.tok.weight, self.c.embed_scale)
+        return self.tok(ids)
+
+    def _drop(self, x, residual, site: int):
+        # places are 2^40 steps apart in the counter's upper half
+        return lm_ops.dropout(x, self.c.dropout, self.c.dropout_seed, site << 40,
+                              residual=residual, step=self.drop_step)
 
     def forward(self, ids):
-        x = self.tok(ids) + self.pos[: ids.shape[1]]
-        for blk in self.blocks:
-            x = blk(x)
+        x = self.embed(ids) + self.pos[: ids.shape[1]]
+        if self.training and self.c.dropout > 0:
+            x = self._drop(x, None, 0)
+            for i, blk in enumerate(self.blocks):
+                x = blk(x, lambda y, res, s, i=i: self._drop(y, res, 1 + 2 * i + s))
+        else:
+            for blk in self.blocks:
+                x = blk(x)
         return self.head(self.ln_f(x))
+
+    def recurrent(self, ids, pos, states=None, lengths=None):
+        """The model as a recurrence (``mixer="linear"``): tokens ids [B, n] at
+        positions pos[b] .. pos[b] + n - 1 on top of the states of an earlier call
+        (None: from nothing); lengths [B] int32: valid tokens of each row of ids.
+        Returns (logits [B, n, vocab], states)."""
+        if self.c.mixer != "linear":
+            raise ValueError(f"mixer {self.c.mixer!r} has no recurrent form")
+        at = pos[:, None] + torch.arange(ids.shape[1], device=ids.device)
+        x = self.embed(ids) + self.pos[at.clamp(max=self.c.T - 1)]
+        out = []
+        for i, blk in enumerate(self.blocks):
+            x, s = blk.recurrent(x, None if states is None else states[i], lengths)
+            out.append(s)
+        return self.head(self.ln_f(x)), out
 
 
 def build(c: GPTConfig, device="cuda", dtype=torch.bfloat16, seed: int = 0) -> GPT:
@@ -131,6 +209,8 @@ def train_step(model: GPT, opt, ids, targets):
     loss.backward()
     opt.step()
     opt.zero_grad(set_to_none=True)
+    if model.c.dropout > 0:
+        model.drop_step += 1
     if model.c.mixer == "bcmt" and model.c.learn_decay:
         with torch.no_grad():
             for blk in model.blocks:
@@ -138,12 +218,38 @@ def train_step(model: GPT, opt, ids, targets):
     return loss
 
 
+@torch.no_grad()
+def generate(model: GPT, ids, new_tokens: int, lengths=None):
+    """Greedy continuation of the prompts ids [B, n] (``mixer="linear"``): the
+    prompts in one pass, then one token of every sequence per step.  lengths [B]
+    int32: the prompts' own lengths (default n, each at least 1); positions past
+    the model's T share its last position embedding.  Returns
+    [B, new_tokens]."""
+    B, n = ids.shape
+    was_training = model.training
+    model.eval()
+    try:
+        pos = torch.zeros(B, dtype=torch.int64, device=ids.device)
+        logits, states = model.recurrent(ids, pos, None, lengths)
+        last = torch.full_like(pos, n) if lengths is None else lengths.long()
+        tok = logits[torch.arange(B, device=ids.device), last - 1].argmax(-1, keepdim=True)
+        out = [tok]
+        for i in range(new_tokens - 1):
+            logits, states = model.recurrent(tok, last + i, states)
+            tok = logits[:, 0].argmax(-1, keepdim=True)
+            out.append(tok)
+        return torch.cat(out, dim=1)
+    finally:
+        model.train(was_training)
+
+
 def flops_per_token(c: GPTConfig) -> float:
     """Algorithmic forward+backward flops per token (3x the forward): the
-    mixer's 10 D^2 + 2 D (L+1) + 2 D^2 / L (dense: L -> T; HOnly: no W_m, W_g),
-    the MLP's 4 D m and the LM head's 2 D V."""
+    mixer's 10 D^2 + 2 D (L+1) + 2 D^2 / L (dense: L -> T; HOnly: no W_m, W_g;
+    linear: 8 D^2 + 4 D dh for the state's update and its use), the MLP's 4 D m
+    and the LM head's 2 D V."""
     D, L = c.D, (c.T if c.mixer == "dense" else c.L)
-    mix = 8 * D * D + 2 * D * (L + 1)
+    mix = 8 * D * D + (4 * D * (D // c.H) if c.mixer == "linear" else 2 * D * (L + 1))
     if c.mixer == "bcmt" and not c.honly:
         mix += 2 * D * D + 2 * D * D / c.L
     return 3.0 * (c.layers * (mix + 4 * D * c.mlp) + 2 * D * c.vocab)

@@ -26,7 +26,8 @@ _F32 = torch.float32
 # The calls below take a few microseconds of kernel time at small sizes, so
 # their own host time counts: checks format their message only when they fail,
 # parameters are built once per shape, and the stream is read as a raw handle.
-_raw_stream = torch._C._cuda_getCurrentRawStream
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) \
+    or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _device(t: torch.Tensor) -> torch.device:
