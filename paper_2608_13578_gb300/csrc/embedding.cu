@@ -99,13 +99,17 @@ struct SortArgs {
 };
 
 namespace {
-// CTAs from `first` on clear the part `part` of `parts`.
+// CTAs from `first` on clear the part `part` of `parts`, eight stores a thread.
 __device__ __forceinline__ void clear_part(const SortArgs& a, int first, int part, int parts) {
   const long long lo = a.zero_n * part / parts, hi = a.zero_n * (part + 1) / parts;
   const uint4 z = make_uint4(0, 0, 0, 0);
-  for (long long i = lo + (long long)(blockIdx.x - first) * kSortThreads + threadIdx.x; i < hi;
-       i += (long long)(gridDim.x - first) * kSortThreads)
-    a.zero[i] = z;
+  const long long step = 8ll * kSortThreads;
+  for (long long i0 = lo + (blockIdx.x - first) * step + threadIdx.x; i0 < hi;
+       i0 += (gridDim.x - first) * step) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u * kSortThreads < hi) a.zero[i0 + u * kSortThreads] = z;
+  }
 }
 }  // namespace
 
@@ -121,19 +125,42 @@ __global__ void __launch_bounds__(kSortThreads) embed_keys_kernel(const __grid_c
   hist[tid] = 0;
   __syncthreads();
   const int base = blockIdx.x * kTile;
-  for (int i = base + tid; i < min(a.N, base + kTile); i += kSortThreads) {
-    int id = id_at(a.ids, a.is64, i, a.V);
-    if (id < 0) {
-      id = a.V;
+  constexpr int PER = kTile / kSortThreads;
+  int id[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = base + j * kSortThreads + tid;
+    id[j] = i < a.N ? id_at(a.ids, a.is64, i, a.V) : 0;
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = base + j * kSortThreads + tid;
+    if (i >= a.N) continue;
+    if (id[j] < 0) {
+      id[j] = a.V;
       atomicOr(a.status, kStatusBadIndex);
     }
-    a.key[0][i] = id;
-    atomicAdd(&hist[id & 255], 1);
+    a.key[0][i] = id[j];
+    atomicAdd(&hist[id[j] & 255], 1);
   }
   __syncthreads();
   a.cnt[0][blockIdx.x * 256 + tid] = hist[tid];
   for (int p = 1; p < a.passes; ++p) a.cnt[p][blockIdx.x * 256 + tid] = 0;
 }
+
+namespace {
+// The lanes of `among` whose 8-bit digit is this lane's, by a ballot per bit (a
+// match instruction takes a step per distinct value, hundreds of cycles here).
+__device__ __forceinline__ unsigned equal_lanes(int d, unsigned among) {
+  unsigned m = among;
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const unsigned v = __ballot_sync(0xffffffffu, (d >> b) & 1);
+    m &= ((d >> b) & 1) ? v : ~v;
+  }
+  return m;
+}
+}  // namespace
 
 // One stable pass: digit `p` of the keys.  Ranks: each warp takes 256
 // consecutive keys, 32 at a time, and ranks equal digits by lane order; the
@@ -157,30 +184,36 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
   for (int w = 0; w < NW; ++w) wcnt[w][tid] = 0;
   __syncthreads();
-  int key[PER], rank[PER];
+  int key[PER], pos[PER], rank[PER];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = base + warp * (PER * 32) + j * 32 + lane;
     key[j] = i < a.N ? kin[i] : -1;
+    pos[j] = p == 0 || i >= a.N ? i : pin[i];
   }
+  unsigned same[PER];  // the warp's lanes with an equal digit
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    const int d = key[j] < 0 ? 256 : (key[j] >> (8 * p)) & 255;
-    const unsigned same = __match_any_sync(0xffffffffu, d);
-    const unsigned before = same & ((1u << lane) - 1u);
-    int start = 0;
-    if (d < 256) start = wcnt[warp][d];
+    const int d = (key[j] >> (8 * p)) & 255;
+    same[j] = equal_lanes(d, __ballot_sync(0xffffffffu, key[j] >= 0));
+    const unsigned before = same[j] & ((1u << lane) - 1u);
+    const int start = wcnt[warp][d];
     __syncwarp();
-    if (d < 256 && before == 0) wcnt[warp][d] = start + __popc(same);
+    if (key[j] >= 0 && before == 0) wcnt[warp][d] = start + __popc(same[j]);
     __syncwarp();
     rank[j] = start + __popc(before);
   }
   // digit tid: keys before this tile's, over all digits and the earlier tiles
   int total = 0, mine = 0;
-  for (int t = 0; t < a.tiles; ++t) {
-    const int c = a.cnt[p][t * 256 + tid];
-    total += c;
-    if (t < (int)blockIdx.x) mine += c;
+  for (int t0 = 0; t0 < a.tiles; t0 += 16) {  // sixteen loads in flight
+    int c[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) c[u] = t0 + u < a.tiles ? a.cnt[p][(t0 + u) * 256 + tid] : 0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      total += c[u];
+      if (t0 + u < (int)blockIdx.x) mine += c[u];
+    }
   }
   int incl = total;
 #pragma unroll
@@ -204,12 +237,25 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     if (key[j] < 0) continue;
-    const int i = base + warp * (PER * 32) + j * 32 + lane;
     const int dst = wcnt[warp][(key[j] >> (8 * p)) & 255] + rank[j];
     kout[dst] = key[j];
-    pout[dst] = p == 0 ? i : pin[i];
-    if (p + 1 < a.passes)
-      atomicAdd(&a.cnt[p + 1][(dst / kTile) * 256 + ((key[j] >> (8 * (p + 1))) & 255)], 1);
+    pout[dst] = pos[j];
+    rank[j] = dst / kTile;
+  }
+  if (p + 1 < a.passes) {
+    // one addition for the warp's keys with equal digits that land in one tile: a
+    // frequent token's keys would all add to one counter
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int d = (key[j] >> (8 * (p + 1))) & 255;
+      const unsigned eq = equal_lanes(d, same[j]);
+      const int first = __ffs(eq) - 1;
+      const int t = __shfl_sync(0xffffffffu, rank[j], first < 0 ? 0 : first);
+      const bool lead = key[j] >= 0 && lane == first;
+      const unsigned near = eq & __ballot_sync(0xffffffffu, key[j] >= 0 && rank[j] == t);
+      if (lead) atomicAdd(&a.cnt[p + 1][t * 256 + d], __popc(near));
+      else if (key[j] >= 0 && rank[j] != t) atomicAdd(&a.cnt[p + 1][rank[j] * 256 + d], 1);
+    }
   }
 }
 
@@ -225,15 +271,20 @@ struct SumArgs {
   float* part;  // [chunks][2][D]
 };
 
+// All of a warp's rows are brought to shared memory at once (32 asynchronous
+// copies of 512 bytes, 16 KB a warp, 192 KB in flight on an SM), and the loop that
+// adds them is rolled: with the rows in registers its unrolled copies of the
+// stores made instruction fetch the bound.
+constexpr int kSumWarps = 4;
 template <class T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(32 * kSumWarps)
     embed_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ dy,
                      T* __restrict__ dw) {
   constexpr int VN = vec_n<T>();
-  constexpr int U = 8;  // rows in flight
+  extern __shared__ uint4 sum_rows[];  // [warp][position][lane]
   pdl_enter();
-  const int lane = threadIdx.x & 31;
-  const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int unit = blockIdx.x * kSumWarps + warp;
   if (unit >= a.chunks * a.cblocks) return;
   const int chunk = unit / a.cblocks, cb = unit - chunk * a.cblocks;
   const int p0 = chunk * kChunk, cnt = min(kChunk, a.N - p0);
@@ -243,48 +294,54 @@ __global__ void __launch_bounds__(256)
   const int next = p0 + cnt < a.N ? a.key[p0 + cnt] : -1;
   const int col = (cb * 32 + lane) * VN;
   const bool ok = col < a.D;
+  uint4* mine = sum_rows + (warp * kChunk) * 32 + lane;  // each lane reads what it copied
+  // keys past V are ids outside the table, sorted to the end
+  const int used = __popc(__ballot_sync(0xffffffffu, lane < cnt && mykey < a.V));
+  if (used == 0) return;
+  const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
+#pragma unroll 8
+  for (int j = 0; j < kChunk; ++j) {
+    const long long row = __shfl_sync(0xffffffffu, mypos, j);
+    if (j < used && ok)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + j * 512),
+                   "l"(dy + row * a.D + col)
+                   : "memory");
+  }
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  // where a run of equal keys ends in the chunk (the last position always does)
+  const int nxt = __shfl_down_sync(0xffffffffu, mykey, 1);
+  const unsigned ends = __ballot_sync(0xffffffffu, lane == cnt - 1 || nxt != mykey);
+  bool from_prev = __shfl_sync(0xffffffffu, mykey, 0) == prev;
   float acc[VN];
 #pragma unroll
   for (int e = 0; e < VN; ++e) acc[e] = 0.f;
-  bool from_prev = false;
-  for (int j0 = 0; j0 < cnt; j0 += U) {
-    uint4 raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int row = __shfl_sync(0xffffffffu, mypos, (j0 + u) & 31);
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (j0 + u < cnt && ok) raw[u] = *reinterpret_cast<const uint4*>(dy + (long long)row * a.D + col);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + u;
-      const int key = __shfl_sync(0xffffffffu, mykey, j & 31);
-      const int after = __shfl_sync(0xffffffffu, mykey, (j + 1) & 31);
-      if (j >= cnt) break;
-      if (key >= a.V) break;  // ids outside the table, sorted to the end
-      if (j == 0) from_prev = key == prev;
+  int j = 0;
+  while (j < used) {
+    const int end = j + __ffs(ends >> j);  // one past the run's last position
+#pragma unroll 4
+    for (int i = j; i < end; ++i) {
       float v[VN];
-      unpack16<T>(raw[u], v);
+      unpack16<T>(mine[i * 32], v);
 #pragma unroll
       for (int e = 0; e < VN; ++e) acc[e] += v[e];
-      const bool last = j == cnt - 1;
-      if ((last ? next : after) == key && !last) continue;
-      const bool goes_on = last && next == key;
-      if (ok) {
-        if (from_prev || goes_on) {
-          float* d = a.part + ((long long)chunk * 2 + (from_prev ? 0 : 1)) * a.D + col;
-#pragma unroll
-          for (int e = 0; e < VN; e += 4) store4(d + e, acc + e);
-        } else {
-#pragma unroll
-          for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
-          store16<T>(dw + (long long)key * a.D + col, acc);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < VN; ++e) acc[e] = 0.f;
-      from_prev = false;
     }
+    const int key = __shfl_sync(0xffffffffu, mykey, j);
+    const bool goes_on = end == cnt && next == key;
+    if (ok) {
+      if (from_prev || goes_on) {
+        float* d = a.part + ((long long)chunk * 2 + (from_prev ? 0 : 1)) * a.D + col;
+#pragma unroll
+        for (int e = 0; e < VN; e += 4) store4(d + e, acc + e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
+        store16<T>(dw + (long long)key * a.D + col, acc);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+    from_prev = false;
+    j = end;
   }
 }
 
@@ -338,14 +395,20 @@ __global__ void __launch_bounds__(256)
       const bool began_here = a.key[chunk * kChunk] != key || chunk == 0 ||
                               a.key[chunk * kChunk - 1] != key;
       if (key < a.V && a.key[end] == key && began_here) {
-        // the run's last position, by bisection: key[lo] == key, key[hi] != key or hi == N
-        int lo = end, hi = a.N;
-        while (hi - lo > 1) {
-          const int mid = lo + (hi - lo) / 2;
-          if (a.key[mid] == key) lo = mid;
-          else hi = mid;
+        // the chunk in which the run ends: mostly the next one; else doubled steps
+        // and a bisection over the chunks' first keys (c_lo's is key, c_hi's is not)
+        int c_lo = chunk + 1, c_hi = chunk + 2;
+        while (c_hi < a.chunks && a.key[c_hi * kChunk] == key) {
+          c_lo = c_hi;
+          c_hi += c_hi - chunk;
         }
-        len = lo / kChunk - chunk + 1;
+        c_hi = min(c_hi, a.chunks);
+        while (c_hi - c_lo > 1) {
+          const int mid = c_lo + (c_hi - c_lo) / 2;
+          if (a.key[mid * kChunk] == key) c_lo = mid;
+          else c_hi = mid;
+        }
+        len = c_lo - chunk + 1;
       }
     }
     if (lane == 0) {
@@ -439,7 +502,7 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   s.zero = static_cast<uint4*>(dw);
   s.zero_n = (long long)a.V * (a.D / vec_n<T>());
   s.status = lc.status;
-  const unsigned clear = (unsigned)std::min<long long>((s.zero_n + 2047) / 2048, 152 * 8);
+  const unsigned clear = (unsigned)std::min<long long>((s.zero_n + 2047) / 2048, 152 * 4);
   cudaError_t e = launch_k(embed_keys_kernel, dim3(l.tiles + clear), dim3(kSortThreads), 0,
                            lc.stream, s);
   if (e != cudaSuccess) return e;
@@ -459,8 +522,11 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   m.scale = a.scale;
   m.part = reinterpret_cast<float*>(w + l.part);
   const long long units = (long long)m.chunks * m.cblocks;
-  e = launch_k(embed_sum_kernel<T>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, lc.stream, m,
-               (const T*)dy, (T*)dw);
+  constexpr int smem = kSumWarps * kChunk * 512;
+  static std::atomic<unsigned long long> opted{0};
+  if ((e = smem_opt_in(embed_sum_kernel<T>, smem, &opted)) != cudaSuccess) return e;
+  e = launch_k(embed_sum_kernel<T>, dim3((unsigned)((units + kSumWarps - 1) / kSumWarps)),
+               dim3(32 * kSumWarps), smem, lc.stream, m, (const T*)dy, (T*)dw);
   if (e != cudaSuccess) return e;
   if (m.chunks > 1)
     e = launch_k(embed_join_kernel<T>, dim3((unsigned)((m.chunks + 7) / 8 * m.cblocks)), dim3(256),
