@@ -11,8 +11,11 @@ namespace bcmt {
 
 namespace {
 
-constexpr int kTile = 2048;      // ids sorted by one CTA of a radix pass
 constexpr int kSortThreads = 256;
+// ids sorted by one CTA of a radix pass: a CTA's scattered stores take a cycle
+// each, so small batches are cut finer; every CTA reads every tile's counts, so
+// large ones are not
+inline int sort_tile(long long N) { return N <= (1 << 17) ? 1024 : 4096; }
 constexpr int kChunk = 32;       // sorted positions summed by one warp
 
 // The id at i, or -1 where it is outside [0, V).
@@ -89,8 +92,8 @@ struct SortArgs {
   const void* ids;
   int is64;
   int N, V, tiles;
-  int* key[2];
-  int* pos[2];
+  int* key;      // [N] the ids
+  int2* pair[2]; // [N] (key, position), sorted by the digits so far
   int* cnt[3];   // [tiles][256] per pass
   int passes;
   uint4* zero;   // the gradient, cleared by parts over the sort's launches
@@ -114,7 +117,9 @@ __device__ __forceinline__ void clear_part(const SortArgs& a, int first, int par
 }  // namespace
 
 // Keys and digit counts of the first pass.
+template <int PER>
 __global__ void __launch_bounds__(kSortThreads) embed_keys_kernel(const __grid_constant__ SortArgs a) {
+  constexpr int kTile = PER * kSortThreads;
   __shared__ int hist[256];
   pdl_enter();
   if ((int)blockIdx.x >= a.tiles) {
@@ -125,7 +130,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_keys_kernel(const __grid_c
   hist[tid] = 0;
   __syncthreads();
   const int base = blockIdx.x * kTile;
-  constexpr int PER = kTile / kSortThreads;
   int id[PER];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
@@ -140,7 +144,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_keys_kernel(const __grid_c
       id[j] = a.V;
       atomicOr(a.status, kStatusBadIndex);
     }
-    a.key[0][i] = id[j];
+    a.key[i] = id[j];
     atomicAdd(&hist[id[j] & 255], 1);
   }
   __syncthreads();
@@ -167,9 +171,10 @@ __device__ __forceinline__ unsigned equal_lanes(int d, unsigned among) {
 // warps' counts are then scanned in warp order and the tiles' in tile order.
 // The next pass's digit counts (integers: order does not matter) are taken on
 // the way, at the tiles where the keys land.
+template <int PER>
 __global__ void __launch_bounds__(kSortThreads)
     embed_sort_kernel(const __grid_constant__ SortArgs a, int p) {
-  constexpr int NW = kSortThreads / 32, PER = kTile / kSortThreads;
+  constexpr int NW = kSortThreads / 32, kTile = PER * kSortThreads;
   __shared__ int wcnt[NW][256];
   __shared__ int wsum[NW];
   pdl_enter();
@@ -179,8 +184,7 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int base = blockIdx.x * kTile;
-  const int* kin = a.key[p & 1];
-  const int* pin = a.pos[p & 1];
+  const int2* in = a.pair[(p + 1) & 1];
 #pragma unroll
   for (int w = 0; w < NW; ++w) wcnt[w][tid] = 0;
   __syncthreads();
@@ -188,8 +192,9 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = base + warp * (PER * 32) + j * 32 + lane;
-    key[j] = i < a.N ? kin[i] : -1;
-    pos[j] = p == 0 || i >= a.N ? i : pin[i];
+    const int2 x = i >= a.N ? make_int2(-1, 0) : p == 0 ? make_int2(a.key[i], i) : in[i];
+    key[j] = x.x;
+    pos[j] = x.y;
   }
   unsigned same[PER];  // the warp's lanes with an equal digit
 #pragma unroll
@@ -205,12 +210,12 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   // digit tid: keys before this tile's, over all digits and the earlier tiles
   int total = 0, mine = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 16) {  // sixteen loads in flight
-    int c[16];
+  for (int t0 = 0; t0 < a.tiles; t0 += 32) {  // 32 loads in flight
+    int c[32];
 #pragma unroll
-    for (int u = 0; u < 16; ++u) c[u] = t0 + u < a.tiles ? a.cnt[p][(t0 + u) * 256 + tid] : 0;
+    for (int u = 0; u < 32; ++u) c[u] = t0 + u < a.tiles ? a.cnt[p][(t0 + u) * 256 + tid] : 0;
 #pragma unroll
-    for (int u = 0; u < 16; ++u) {
+    for (int u = 0; u < 32; ++u) {
       total += c[u];
       if (t0 + u < (int)blockIdx.x) mine += c[u];
     }
@@ -232,14 +237,12 @@ __global__ void __launch_bounds__(kSortThreads)
     off += c;
   }
   __syncthreads();
-  int* kout = a.key[(p + 1) & 1];
-  int* pout = a.pos[(p + 1) & 1];
+  int2* out = a.pair[p & 1];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     if (key[j] < 0) continue;
     const int dst = wcnt[warp][(key[j] >> (8 * p)) & 255] + rank[j];
-    kout[dst] = key[j];
-    pout[dst] = pos[j];
+    out[dst] = make_int2(key[j], pos[j]);
     rank[j] = dst / kTile;
   }
   if (p + 1 < a.passes) {
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(kSortThreads)
 // to part[chunk][0] (the chunk's first run, when it began earlier) or
 // part[chunk][1] (its last run, when it goes on).
 struct SumArgs {
-  const int *key, *pos;
+  const int2* pair;  // (key, position), sorted
   int N, V, D, chunks, cblocks;
   float scale;
   float* part;  // [chunks][2][D]
@@ -288,10 +291,10 @@ __global__ void __launch_bounds__(32 * kSumWarps)
   if (unit >= a.chunks * a.cblocks) return;
   const int chunk = unit / a.cblocks, cb = unit - chunk * a.cblocks;
   const int p0 = chunk * kChunk, cnt = min(kChunk, a.N - p0);
-  const int mykey = lane < cnt ? a.key[p0 + lane] : -1;
-  const int mypos = lane < cnt ? a.pos[p0 + lane] : 0;
-  const int prev = p0 > 0 ? a.key[p0 - 1] : -1;
-  const int next = p0 + cnt < a.N ? a.key[p0 + cnt] : -1;
+  const int2 my = lane < cnt ? a.pair[p0 + lane] : make_int2(-1, 0);
+  const int mykey = my.x, mypos = my.y;
+  const int prev = p0 > 0 ? a.pair[p0 - 1].x : -1;
+  const int next = p0 + cnt < a.N ? a.pair[p0 + cnt].x : -1;
   const int col = (cb * 32 + lane) * VN;
   const bool ok = col < a.D;
   uint4* mine = sum_rows + (warp * kChunk) * 32 + lane;  // each lane reads what it copied
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(256)
   const int col = (cb * 32 + lane) * VN;
   const bool ok = col < a.D;
   auto add = [&](int lo, int hi, int chunk, float* acc) {  // parts lo .. hi-1 of the run
-    for (int m0 = lo; m0 < hi; m0 += 4) {
+    for (int m0 = lo; m0 < hi; m0 += 4) {  // four loads in flight
       float v[4][VN];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -391,24 +394,24 @@ __global__ void __launch_bounds__(256)
     int len = 0, key = -1;
     const int end = (chunk + 1) * kChunk;  // first position of the next chunk
     if (chunk < a.chunks && end < a.N) {
-      key = a.key[end - 1];
-      const bool began_here = a.key[chunk * kChunk] != key || chunk == 0 ||
-                              a.key[chunk * kChunk - 1] != key;
-      if (key < a.V && a.key[end] == key && began_here) {
-        // the chunk in which the run ends: mostly the next one; else doubled steps
-        // and a bisection over the chunks' first keys (c_lo's is key, c_hi's is not)
-        int c_lo = chunk + 1, c_hi = chunk + 2;
-        while (c_hi < a.chunks && a.key[c_hi * kChunk] == key) {
-          c_lo = c_hi;
-          c_hi += c_hi - chunk;
+      key = a.pair[end - 1].x;
+      const int first = a.pair[chunk * kChunk].x, after = a.pair[end].x;
+      const int before = chunk > 0 ? a.pair[chunk * kChunk - 1].x : -1;
+      if (key < a.V && after == key && (first != key || before != key)) {
+        // the last chunk that begins with key: 32 probes at a time, at strides of
+        // 1, 32, 1024, ... chunks until one misses, then back down
+        int lo = chunk + 1, stride = 1, hits = 32;
+        auto probe = [&]() {
+          const long long c = lo + (lane + 1ll) * stride;
+          hits = __popc(__ballot_sync(0xffffffffu, c < a.chunks && a.pair[c * kChunk].x == key));
+          lo += hits * stride;
+        };
+        for (probe(); hits == 32; probe()) stride *= 32;
+        while (stride > 1) {
+          stride /= 32;
+          probe();
         }
-        c_hi = min(c_hi, a.chunks);
-        while (c_hi - c_lo > 1) {
-          const int mid = c_lo + (c_hi - c_lo) / 2;
-          if (a.key[mid * kChunk] == key) c_lo = mid;
-          else c_hi = mid;
-        }
-        len = c_lo - chunk + 1;
+        len = lo - chunk + 1;
       }
     }
     if (lane == 0) {
@@ -450,12 +453,12 @@ __global__ void __launch_bounds__(256)
 // ---------------------------------------------------------------- host side
 namespace {
 struct BwdLayout {
-  size_t key[2], pos[2], cnt[3], part, bytes;
+  size_t key, pair[2], cnt[3], part, bytes;
   int tiles, passes, chunks;
 };
 BwdLayout bwd_layout(long long N, int V, int D) {
   BwdLayout l{};
-  l.tiles = (int)((N + kTile - 1) / kTile);
+  l.tiles = (int)((N + sort_tile(N) - 1) / sort_tile(N));
   l.chunks = (int)((N + kChunk - 1) / kChunk);
   l.passes = V < (1 << 8) ? 1 : V < (1 << 16) ? 2 : 3;
   size_t off = 0;
@@ -464,10 +467,8 @@ BwdLayout bwd_layout(long long N, int V, int D) {
     off += (bytes + 255) & ~size_t(255);
     return r;
   };
-  for (int i = 0; i < 2; ++i) {
-    l.key[i] = take((size_t)N * 4);
-    l.pos[i] = take((size_t)N * 4);
-  }
+  l.key = take((size_t)N * 4);
+  for (int i = 0; i < 2; ++i) l.pair[i] = take((size_t)N * 8);
   for (int i = 0; i < l.passes; ++i) l.cnt[i] = take((size_t)l.tiles * 256 * 4);
   l.part = take((size_t)l.chunks * 2 * D * 4);
   l.bytes = off;
@@ -494,26 +495,26 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   s.V = a.V;
   s.tiles = l.tiles;
   s.passes = a.N > 0 ? l.passes : 0;  // an empty batch only clears
-  for (int i = 0; i < 2; ++i) {
-    s.key[i] = reinterpret_cast<int*>(w + l.key[i]);
-    s.pos[i] = reinterpret_cast<int*>(w + l.pos[i]);
-  }
+  s.key = reinterpret_cast<int*>(w + l.key);
+  for (int i = 0; i < 2; ++i) s.pair[i] = reinterpret_cast<int2*>(w + l.pair[i]);
   for (int i = 0; i < l.passes; ++i) s.cnt[i] = reinterpret_cast<int*>(w + l.cnt[i]);
   s.zero = static_cast<uint4*>(dw);
   s.zero_n = (long long)a.V * (a.D / vec_n<T>());
   s.status = lc.status;
   const unsigned clear = (unsigned)std::min<long long>((s.zero_n + 2047) / 2048, 152 * 4);
-  cudaError_t e = launch_k(embed_keys_kernel, dim3(l.tiles + clear), dim3(kSortThreads), 0,
-                           lc.stream, s);
+  const dim3 grid(l.tiles + clear);
+  const bool fine = sort_tile(a.N) == 1024;
+  cudaError_t e = fine ? launch_k(embed_keys_kernel<4>, grid, dim3(kSortThreads), 0, lc.stream, s)
+                       : launch_k(embed_keys_kernel<16>, grid, dim3(kSortThreads), 0, lc.stream, s);
   if (e != cudaSuccess) return e;
   if (a.N == 0) return cudaGetLastError();
   for (int p = 0; p < l.passes; ++p) {
-    e = launch_k(embed_sort_kernel, dim3(l.tiles + clear), dim3(kSortThreads), 0, lc.stream, s, p);
+    e = fine ? launch_k(embed_sort_kernel<4>, grid, dim3(kSortThreads), 0, lc.stream, s, p)
+             : launch_k(embed_sort_kernel<16>, grid, dim3(kSortThreads), 0, lc.stream, s, p);
     if (e != cudaSuccess) return e;
   }
   SumArgs m{};
-  m.key = s.key[l.passes & 1];
-  m.pos = s.pos[l.passes & 1];
+  m.pair = s.pair[(l.passes - 1) & 1];
   m.N = (int)a.N;
   m.V = a.V;
   m.D = a.D;

@@ -335,7 +335,8 @@ def ids_like(kind, N, V, g):
     (33, 256, 72, "zipf", torch.int64), (2048, 257, 264, "zipf", torch.int64),
     (2049, 40000, 64, "uniform", torch.int32), (5000, 70000, 16, "uniform", torch.int64),
     (9000, 300, 768, "zipf", torch.int64), (20000, 512, 128, "same", torch.int64),
-    (4097, 65536, 8, "zipf", torch.int64), (0, 100, 16, "uniform", torch.int64),
+    (4097, 65536, 8, "zipf", torch.int64), (150001, 3000, 16, "zipf", torch.int32),
+    (140000, 20, 8, "same", torch.int64), (0, 100, 16, "uniform", torch.int64),
 ])
 def test_embedding_and_its_gradient(F, N, V, D, kind, ints, dtype):
     g = torch.Generator().manual_seed(N + V)
