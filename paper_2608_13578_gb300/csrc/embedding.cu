@@ -274,77 +274,69 @@ struct SumArgs {
   float* part;  // [chunks][2][D]
 };
 
-// All of a warp's rows are brought to shared memory at once (32 asynchronous
-// copies of 512 bytes, 16 KB a warp, 192 KB in flight on an SM), and the loop that
-// adds them is rolled: with the rows in registers its unrolled copies of the
-// stores made instruction fetch the bound.
-constexpr int kSumWarps = 4;
+// Four rows in flight a warp and 48 registers a thread, so that 40 warps share an
+// SM (80 KB in flight): the additions of a warp are a chain, which only other warps
+// can fill (eight rows and half the warps: 4 us slower at 65536 x 768; rows
+// streamed through shared memory by 12 warps: 8 us slower).
 template <class T>
-__global__ void __launch_bounds__(32 * kSumWarps)
+__global__ void __launch_bounds__(256, 5)
     embed_sum_kernel(const __grid_constant__ SumArgs a, const T* __restrict__ dy,
                      T* __restrict__ dw) {
   constexpr int VN = vec_n<T>();
-  extern __shared__ uint4 sum_rows[];  // [warp][position][lane]
+  constexpr int U = 4;  // rows in flight
   pdl_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int unit = blockIdx.x * kSumWarps + warp;
+  const int lane = threadIdx.x & 31;
+  const int unit = blockIdx.x * 8 + (threadIdx.x >> 5);
   if (unit >= a.chunks * a.cblocks) return;
-  const int chunk = unit / a.cblocks, cb = unit - chunk * a.cblocks;
+  const int chunk = unit / a.cblocks, col = ((unit - chunk * a.cblocks) * 32 + lane) * VN;
   const int p0 = chunk * kChunk, cnt = min(kChunk, a.N - p0);
   const int2 my = lane < cnt ? a.pair[p0 + lane] : make_int2(-1, 0);
-  const int mykey = my.x, mypos = my.y;
   const int prev = p0 > 0 ? a.pair[p0 - 1].x : -1;
   const int next = p0 + cnt < a.N ? a.pair[p0 + cnt].x : -1;
-  const int col = (cb * 32 + lane) * VN;
   const bool ok = col < a.D;
-  uint4* mine = sum_rows + (warp * kChunk) * 32 + lane;  // each lane reads what it copied
   // keys past V are ids outside the table, sorted to the end
-  const int used = __popc(__ballot_sync(0xffffffffu, lane < cnt && mykey < a.V));
-  if (used == 0) return;
-  const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
-#pragma unroll 8
-  for (int j = 0; j < kChunk; ++j) {
-    const long long row = __shfl_sync(0xffffffffu, mypos, j);
-    if (j < used && ok)
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + j * 512),
-                   "l"(dy + row * a.D + col)
-                   : "memory");
-  }
-  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+  const int used = __popc(__ballot_sync(0xffffffffu, lane < cnt && my.x < a.V));
   // where a run of equal keys ends in the chunk (the last position always does)
-  const int nxt = __shfl_down_sync(0xffffffffu, mykey, 1);
-  const unsigned ends = __ballot_sync(0xffffffffu, lane == cnt - 1 || nxt != mykey);
-  bool from_prev = __shfl_sync(0xffffffffu, mykey, 0) == prev;
+  const int nxt = __shfl_down_sync(0xffffffffu, my.x, 1);
+  const unsigned ends = __ballot_sync(0xffffffffu, lane == cnt - 1 || nxt != my.x);
+  bool from_prev = __shfl_sync(0xffffffffu, my.x, 0) == prev;
   float acc[VN];
 #pragma unroll
   for (int e = 0; e < VN; ++e) acc[e] = 0.f;
-  int j = 0;
-  while (j < used) {
-    const int end = j + __ffs(ends >> j);  // one past the run's last position
-#pragma unroll 4
-    for (int i = j; i < end; ++i) {
+#pragma unroll 1
+  for (int j0 = 0; j0 < used; j0 += U) {
+    uint4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long long row = __shfl_sync(0xffffffffu, my.y, j0 + u);
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (j0 + u < used && ok) raw[u] = *reinterpret_cast<const uint4*>(dy + row * a.D + col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u;
       float v[VN];
-      unpack16<T>(mine[i * 32], v);
+      unpack16<T>(raw[u], v);
 #pragma unroll
       for (int e = 0; e < VN; ++e) acc[e] += v[e];
-    }
-    const int key = __shfl_sync(0xffffffffu, mykey, j);
-    const bool goes_on = end == cnt && next == key;
-    if (ok) {
-      if (from_prev || goes_on) {
-        float* d = a.part + ((long long)chunk * 2 + (from_prev ? 0 : 1)) * a.D + col;
+      if (j >= used || !((ends >> j) & 1u)) continue;
+      const int key = __shfl_sync(0xffffffffu, my.x, j);
+      const bool goes_on = j == cnt - 1 && next == key;
+      if (ok) {
+        if (from_prev || goes_on) {
+          float* d = a.part + ((long long)chunk * 2 + (from_prev ? 0 : 1)) * a.D + col;
 #pragma unroll
-        for (int e = 0; e < VN; e += 4) store4(d + e, acc + e);
-      } else {
+          for (int e = 0; e < VN; e += 4) store4(d + e, acc + e);
+        } else {
 #pragma unroll
-        for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
-        store16<T>(dw + (long long)key * a.D + col, acc);
+          for (int e = 0; e < VN; ++e) acc[e] *= a.scale;
+          store16<T>(dw + (long long)key * a.D + col, acc);
+        }
       }
-    }
 #pragma unroll
-    for (int e = 0; e < VN; ++e) acc[e] = 0.f;
-    from_prev = false;
-    j = end;
+      for (int e = 0; e < VN; ++e) acc[e] = 0.f;
+      from_prev = false;
+    }
   }
 }
 
@@ -523,11 +515,8 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   m.scale = a.scale;
   m.part = reinterpret_cast<float*>(w + l.part);
   const long long units = (long long)m.chunks * m.cblocks;
-  constexpr int smem = kSumWarps * kChunk * 512;
-  static std::atomic<unsigned long long> opted{0};
-  if ((e = smem_opt_in(embed_sum_kernel<T>, smem, &opted)) != cudaSuccess) return e;
-  e = launch_k(embed_sum_kernel<T>, dim3((unsigned)((units + kSumWarps - 1) / kSumWarps)),
-               dim3(32 * kSumWarps), smem, lc.stream, m, (const T*)dy, (T*)dw);
+  e = launch_k(embed_sum_kernel<T>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, lc.stream, m,
+               (const T*)dy, (T*)dw);
   if (e != cudaSuccess) return e;
   if (m.chunks > 1)
     e = launch_k(embed_join_kernel<T>, dim3((unsigned)((m.chunks + 7) / 8 * m.cblocks)), dim3(256),
