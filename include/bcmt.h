@@ -226,7 +226,8 @@ typedef struct {
 } bcmt_linattn_params;
 
 /* Bytes of workspace of one forward (backward = 0) or backward (1) call; free
- * to reuse between calls.  Returns 0 for invalid parameters. */
+ * to reuse between calls.  256 means that the call uses none, and then NULL may
+ * be passed.  Returns 0 for invalid parameters. */
 size_t bcmt_linattn_workspace_size(const bcmt_linattn_params* p, int backward);
 
 /* state_in and state_out may each be NULL, and may be the same buffer. */

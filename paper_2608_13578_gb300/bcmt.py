@@ -166,9 +166,13 @@ def _stream(s) -> Optional[int]:
     return s.cuda_stream
 
 
-def _check(code: int):
+def check(code: int):
+    """Raises BCMTError for the status of a call made through LIB."""
     if code != BCMT_OK:
         raise BCMTError(code, bcmt_last_error())
+
+
+_check = check
 
 
 def bcmt_last_error() -> str:

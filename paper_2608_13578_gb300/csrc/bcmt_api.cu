@@ -585,6 +585,21 @@ bcmt_status check_rows(const bcmt_linattn_params* p, const void* ptr, long ld, c
                 name, (long)p->H * p->dh);
   return BCMT_OK;
 }
+// Bytes of one call's workspace: 256 where no segment states are needed.
+size_t linattn_workspace(const bcmt_linattn_params* p, int backward) {
+  const int npass = backward ? 3 : 1;
+  int nseg = 1;  // whichever kernels run (bcmt_test_set_tensor_cores)
+  for (const bool tc : {false, true})
+    nseg = std::max(nseg, linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(), tc)
+                              .nseg);
+  const size_t states = nseg > 1 ? (size_t)p->B * p->H * nseg * p->dh * p->dh * 4 : 0;
+  return al256(std::max<size_t>(256, npass * states));
+}
+// A call that needs no segment states takes a NULL workspace.
+bcmt_status check_linattn_workspace(const bcmt_linattn_params* p, int backward, const void* ws) {
+  if (!ws && linattn_workspace(p, backward) <= 256) return BCMT_OK;
+  return check_ptr(ws, "workspace");
+}
 LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int* lengths,
                      int npass, void* workspace, LinPlan* plan) {
   LinArgs a{};
@@ -1254,13 +1269,7 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
 // ------------------------------------------------ language-model operators
 size_t bcmt_linattn_workspace_size(const bcmt_linattn_params* p, int backward) {
   if (check_linattn(p) != BCMT_OK) return 0;
-  const int npass = backward ? 3 : 1;
-  int nseg = 1;  // whichever kernels run (bcmt_test_set_tensor_cores)
-  for (const bool tc : {false, true})
-    nseg = std::max(nseg, linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(), tc)
-                              .nseg);
-  const size_t states = nseg > 1 ? (size_t)p->B * p->H * nseg * p->dh * p->dh * 4 : 0;
-  return al256(std::max<size_t>(256, npass * states));
+  return linattn_workspace(p, backward);
 }
 
 bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, long ld_q,
@@ -1276,7 +1285,7 @@ bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, lo
   if (!decay) return fail(BCMT_ERR_ARG, "decay is NULL");
   BCMT_TRY(check_opt(state_in, "state_in"));
   BCMT_TRY(check_opt(state_out, "state_out"));
-  BCMT_TRY(check_ptr(workspace, "workspace"));
+  BCMT_TRY(check_linattn_workspace(p, 0, workspace));
   unsigned* sp = status_ptr();
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};
@@ -1321,7 +1330,7 @@ bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o,
   BCMT_TRY(check_opt(d_state_in, "d_state_in"));
   if (d_state_in && (d_state_in == d_state_out || d_state_in == state_in))
     return fail(BCMT_ERR_ARG, "d_state_in must have a buffer of its own");
-  BCMT_TRY(check_ptr(workspace, "workspace"));
+  BCMT_TRY(check_linattn_workspace(p, 1, workspace));
   unsigned* sp = status_ptr();
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};

@@ -12,6 +12,7 @@ shapes, layouts) raise ``ValueError``; what the library refuses raises
 
 from __future__ import annotations
 
+import ctypes
 import functools
 import math
 from typing import Optional, Tuple
@@ -75,33 +76,43 @@ def _buffer(nbytes: int, device) -> torch.Tensor:
 
 
 # ------------------------------------------------------------ linear attention
-def _rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
-    """t [B, T, H, dh] as rows of one stride (a slice of a projection's output as
-    it is, anything else copied), and that stride in elements."""
-    B, T, H, dh = t.shape
-    sb, st, sh, sd = t.stride()
-    D = H * dh
-    ld = st if T > 1 else sb if B > 1 else D
-    if (sd == 1 and (H == 1 or sh == dh) and (B == 1 or sb == T * ld) and ld >= D and ld % 8 == 0
-            and t.data_ptr() % 16 == 0):
-        return t, ld
-    return _dense(t), D
+def _is_rows(stride, shape) -> bool:
+    B, T, H, dh = shape
+    sb, st, sh, sd = stride
+    ld = st if T > 1 else sb if B > 1 else H * dh
+    return (sd == 1 and (H == 1 or sh == dh) and (B == 1 or sb == T * ld) and ld >= H * dh
+            and ld % 8 == 0)
+
+
+def _rows(t: torch.Tensor, shape) -> Tuple[torch.Tensor, int, int]:
+    """t [B, T, H, dh] as rows of one stride: (tensor, address, stride in elements).
+    A slice of a projection's output is taken as it is, anything else copied."""
+    stride = t.stride()
+    ptr = t.data_ptr()
+    if ptr % 16 or not _is_rows(stride, shape):
+        t = _dense(t)
+        return t, t.data_ptr(), shape[2] * shape[3]
+    return t, ptr, stride[1] if shape[1] > 1 else stride[0] if shape[0] > 1 else shape[2] * shape[3]
 
 
 @functools.lru_cache(maxsize=4096)
 def _linattn_plan(B, T, H, dh, dt, scale, backward):
+    """(parameters by reference, bytes of workspace; 0 where the call needs none)."""
     p = C.bcmt_linattn_params(B, T, H, dh, dt, 0, 1.0 / math.sqrt(dh) if scale is None else scale)
-    return p, max(256, C.bcmt_linattn_workspace_size(p, backward))
+    n = C.bcmt_linattn_workspace_size(p, backward)
+    return ctypes.byref(p), n if n > 256 else 0
 
 
 def _linattn_check(q, k, v, decay, lengths, state):
     dev = _device(q)
-    if q.dim() != 4:
-        raise ValueError(f"q must be [B, T, H, dh], not {tuple(q.shape)}")
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4:
+        raise ValueError(f"q must be [B, T, H, dh], not {tuple(shape)}")
     dt = _dtype(q, "q")
-    shape = q.shape
-    _check(k, "k", shape, q.dtype, dev)
-    _check(v, "v", shape, q.dtype, dev)
+    if k.shape != shape or k.dtype != dtype or k.device != dev:
+        _check(k, "k", shape, dtype, dev)
+    if v.shape != shape or v.dtype != dtype or v.device != dev:
+        _check(v, "v", shape, dtype, dev)
     B, T, H, dh = shape
     _check(decay, "decay", (H,), _F32, dev)
     if decay.requires_grad:
@@ -115,6 +126,10 @@ def _linattn_check(q, k, v, decay, lengths, state):
     return dev, dt, decay.contiguous(), lengths, state
 
 
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
 @_on_its_device
 def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, lengths=None,
                              state=None, state_out=None):
@@ -126,19 +141,21 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
     1/sqrt(dh).  state_out: where the last state goes (default a new tensor; may
     be ``state``).  Tokens past a sequence's length give zero rows."""
     dev, dt, decay, lengths, state = _linattn_check(q, k, v, decay, lengths, state)
-    B, T, H, dh = q.shape
+    shape = q.shape
+    B, T, H, dh = shape
     if state_out is None:
         state_out = torch.empty((B, H, dh, dh), dtype=_F32, device=dev)
-    else:
+    elif state_out is not state:
         _check(state_out, "state_out", (B, H, dh, dh), _F32, dev)
         if not state_out.is_contiguous():
             raise ValueError("state_out must be dense")
     p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, False)
-    (q, lq), (k, lk), (v, lv) = _rows(q), _rows(k), _rows(v)
-    o = torch.empty((B, T, H, dh), dtype=q.dtype, device=dev)
-    ws = _buffer(nbytes, dev)
-    C.bcmt_linattn_forward(p, q, lq, k, lk, v, lv, decay, lengths, state, o, H * dh, state_out, ws,
-                           _raw_stream(dev.index))
+    (q, pq, lq), (k, pk, lk), (v, pv, lv) = _rows(q, shape), _rows(k, shape), _rows(v, shape)
+    o = torch.empty(shape, dtype=q.dtype, device=dev)
+    ws = _buffer(nbytes, dev) if nbytes else None
+    C.check(C.LIB.bcmt_linattn_forward(
+        p, pq, lq, pk, lk, pv, lv, decay.data_ptr(), _address(lengths), _address(state),
+        o.data_ptr(), H * dh, state_out.data_ptr(), _address(ws), _raw_stream(dev.index)))
     return o, state_out
 
 
@@ -150,8 +167,9 @@ def linear_attention_backward(do, q, k, v, decay, scale: Optional[float] = None,
     the first state, is computed when a state was given (or by need_dstate),
     else None."""
     dev, dt, decay, lengths, state = _linattn_check(q, k, v, decay, lengths, state)
-    _check(do, "do", q.shape, q.dtype, dev)
-    B, T, H, dh = q.shape
+    shape = q.shape
+    _check(do, "do", shape, q.dtype, dev)
+    B, T, H, dh = shape
     D = H * dh
     if need_dstate is None:
         need_dstate = state is not None
@@ -159,12 +177,15 @@ def linear_attention_backward(do, q, k, v, decay, scale: Optional[float] = None,
         _check(dstate, "dstate", (B, H, dh, dh), _F32, dev)
         dstate = _dense(dstate)
     p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, True)
-    (do, ldo), (q, lq), (k, lk), (v, lv) = _rows(do), _rows(q), _rows(k), _rows(v)
-    dq, dk, dv = (torch.empty((B, T, H, dh), dtype=q.dtype, device=dev) for _ in range(3))
+    (do, pd, ldo), (q, pq, lq) = _rows(do, shape), _rows(q, shape)
+    (k, pk, lk), (v, pv, lv) = _rows(k, shape), _rows(v, shape)
+    dq, dk, dv = (torch.empty(shape, dtype=q.dtype, device=dev) for _ in range(3))
     ds = torch.empty((B, H, dh, dh), dtype=_F32, device=dev) if need_dstate else None
-    ws = _buffer(nbytes, dev)
-    C.bcmt_linattn_backward(p, do, ldo, q, lq, k, lk, v, lv, decay, lengths, state, dstate, dq, D,
-                            dk, D, dv, D, ds, ws, _raw_stream(dev.index))
+    ws = _buffer(nbytes, dev) if nbytes else None
+    C.check(C.LIB.bcmt_linattn_backward(
+        p, pd, ldo, pq, lq, pk, lk, pv, lv, decay.data_ptr(), _address(lengths), _address(state),
+        _address(dstate), dq.data_ptr(), D, dk.data_ptr(), D, dv.data_ptr(), D, _address(ds),
+        _address(ws), _raw_stream(dev.index)))
     return dq, dk, dv, ds
 
 
@@ -212,7 +233,7 @@ def linear_attention(q, k, v, decay, scale: Optional[float] = None, lengths=None
 @functools.lru_cache(maxsize=4096)
 def _embedding_plan(N, V, D, dt, id_bytes, scale):
     p = C.bcmt_embedding_params(N, V, D, dt, id_bytes, 0, scale)
-    return p, max(256, C.bcmt_embedding_workspace_size(p))
+    return ctypes.byref(p), max(256, C.bcmt_embedding_workspace_size(p))
 
 
 def _ids(ids, dev):
@@ -235,7 +256,9 @@ def embedding_forward(ids, weight, scale: float = 1.0):
     V, D = weight.shape
     p, _ = _embedding_plan(ids.numel(), V, D, _dtype(weight, "weight"), ids.element_size(), scale)
     out = torch.empty((*ids.shape, D), dtype=weight.dtype, device=dev)
-    C.bcmt_embedding_forward(p, ids, _dense(weight), out, _raw_stream(dev.index))
+    weight = _dense(weight)
+    C.check(C.LIB.bcmt_embedding_forward(p, ids.data_ptr(), weight.data_ptr(), out.data_ptr(),
+                                         _raw_stream(dev.index)))
     return out
 
 
@@ -250,7 +273,9 @@ def embedding_backward(ids, dout, V: int, scale: float = 1.0):
     p, nbytes = _embedding_plan(ids.numel(), V, D, _dtype(dout, "dout"), ids.element_size(), scale)
     dw = torch.empty((V, D), dtype=dout.dtype, device=dev)
     ws = _buffer(nbytes, dev)
-    C.bcmt_embedding_backward(p, ids, _dense(dout), dw, ws, _raw_stream(dev.index))
+    dout = _dense(dout)
+    C.check(C.LIB.bcmt_embedding_backward(p, ids.data_ptr(), dout.data_ptr(), dw.data_ptr(),
+                                          ws.data_ptr(), _raw_stream(dev.index)))
     return dw
 
 
@@ -290,7 +315,8 @@ def _dropout_call(x, p, seed, offset, residual, step):
     y = torch.empty(x.shape, dtype=x.dtype, device=dev)
     mask = (1 << 64) - 1
     prm = C.bcmt_dropout_params(x.numel(), dt, 0, p, seed & mask, offset & mask, step)
-    C.bcmt_dropout(prm, x, residual, y, _raw_stream(dev.index))
+    C.check(C.LIB.bcmt_dropout(ctypes.byref(prm), x.data_ptr(), _address(residual), y.data_ptr(),
+                               _raw_stream(dev.index)))
     return y
 
 

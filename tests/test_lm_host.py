@@ -73,6 +73,18 @@ def test_linattn_refuses_bad_params(C, field, value, code):
     assert e.value.code == getattr(C, code), C.bcmt_last_error()
 
 
+def test_linattn_workspace_is_needed_for_long_sequences_only(C):
+    short = C.bcmt_linattn_params(2, 5, 2, 16, C.BCMT_BF16, 0, 0.25)
+    assert C.bcmt_linattn_workspace_size(short, False) == 256
+    for dt in (C.BCMT_BF16, C.BCMT_F32):
+        long = C.bcmt_linattn_params(1, 5000, 2, 16, dt, 0, 0.25)
+        assert C.bcmt_linattn_workspace_size(long, False) > 256
+        for ws, code in ((None, C.BCMT_ERR_ARG), (A + 8, C.BCMT_ERR_ALIGN)):
+            with pytest.raises(C.BCMTError) as e:
+                C.bcmt_linattn_forward(long, A, 32, A, 32, A, 32, A, None, None, A, 32, A, ws, 0)
+            assert e.value.code == code
+
+
 def test_linattn_refuses_bad_pointers_and_strides(C):
     p = C.bcmt_linattn_params(2, 5, 2, 16, C.BCMT_BF16, 0, 0.25)
 
@@ -88,7 +100,6 @@ def test_linattn_refuses_bad_pointers_and_strides(C):
     assert forward(q=None) == C.BCMT_ERR_ARG
     assert forward(o=None) == C.BCMT_ERR_ARG
     assert forward(decay=None) == C.BCMT_ERR_ARG
-    assert forward(ws=None) == C.BCMT_ERR_ARG
     assert forward(k=A + 8) == C.BCMT_ERR_ALIGN
     assert forward(s0=A + 4) == C.BCMT_ERR_ALIGN
     assert forward(lv=24) == C.BCMT_ERR_ARG      # shorter than a row
