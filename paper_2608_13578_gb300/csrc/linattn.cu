@@ -276,19 +276,20 @@ __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_const
       x[c] = mul * (p.s_in_t ? src[(long long)(j + c) * dh + i] : src[e0 + c]);
   }
   float* w = p.seg + (long long)bh * a.nseg * st + e0;
+  const bool out = a.all && p.s_out;
   for (int s0 = 0; s0 < a.nseg; s0 += 4) {
     float loc[4][4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int s = p.rev ? a.nseg - 1 - (s0 + u) : s0 + u;
-      if (s0 + u < a.nseg - 1) load4(w + (long long)s * st, loc[u]);
+      if (s0 + u < a.nseg - (out ? 0 : 1)) load4(w + (long long)s * st, loc[u]);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (s0 + u >= a.nseg) break;
       const int s = p.rev ? a.nseg - 1 - (s0 + u) : s0 + u;
       store4(w + (long long)s * st, x);
-      if (s0 + u == a.nseg - 1) break;
+      if (s0 + u == a.nseg - 1 && !out) break;
       const int lo = s * a.seg_len;
       const int m = min(max(n - lo, 0), a.seg_len);  // valid tokens of the segment
       if (m == 0) continue;
@@ -297,6 +298,12 @@ __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_const
 #pragma unroll
       for (int c = 0; c < 4; ++c) x[c] = fmaf(f, x[c], loc[u][c]);
     }
+  }
+  if (out) {
+    const float mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x[c] *= mul;
+    store4(p.s_out + (long long)bh * st + e0, x);
   }
 }
 

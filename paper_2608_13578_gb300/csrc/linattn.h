@@ -39,6 +39,7 @@ struct LinArgs {
   const int* lengths;     // [B] or null
   int nseg, seg_len;      // the tokens in nseg segments of seg_len
   int joined;             // pass.seg holds the segments' incoming states, not their own
+  int all;                // the join of the segments gives the outgoing state too
 };
 
 // How the passes are cut along the tokens (the same rule for the workspace
@@ -55,7 +56,8 @@ cudaError_t linattn_simt(const Launch& lc, int dtype, const LinArgs& a);
 cudaError_t linattn_step(const Launch& lc, int dtype, const LinArgs& a);
 // The chunked form on the tensor cores: bf16, segments of whole 128-token chunks.
 cudaError_t linattn_tc(const Launch& lc, const LinArgs& a);
-// Local segment states (in pass.seg) -> each segment's incoming state.
+// Local segment states (in pass.seg) -> each segment's incoming state, and with
+// a.all the outgoing state.
 cudaError_t linattn_combine(const Launch& lc, const LinArgs& a);
 
 }  // namespace bcmt

@@ -38,6 +38,7 @@ struct LinTcArgs {
   CUtensorMap map[4];
   LinArgs a;
   int mq[3], mk[3], mv[3];  // the pass's maps
+  int out;                  // the pass with an outgoing state, or -1
 };
 
 namespace {
@@ -156,6 +157,29 @@ __device__ __forceinline__ void key_terms(const uint4& k, uint32_t w, uint4& hi,
   }
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// The same in three bf16 terms (hi, mid, lo: 24 bits), by fp32 arithmetic.  mid is
+// multiplied by `half`.
+__device__ __forceinline__ void key_terms3(const uint4& k, float w, float half, uint4& hi,
+                                           uint4& mid, uint4& lo) {
+  float v[8], t[8];
+  unpack8(k, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= w;
+  hi = pack8(v);
+  unpack8(hi, t);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] -= t[e];
+  mid = pack8(v);
+  unpack8(mid, t);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    v[e] -= t[e];
+    t[e] *= half;
+  }
+  mid = pack8(t);
+  lo = pack8(v);
 }
 
 // What a CTA's first threads work out for the others.
@@ -339,20 +363,19 @@ __device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, 
     if (ok)
       issue_ts<kRows / 16>(tmem + G::cO1, tmem, desc_lo(s + 2 * G::kTile, G::kHalf), 128, idO);
     tc::mma_commit(bar_c);
+    if (i + 1 == nch) break;  // nobody reads the state after the last chunk
     wait(bar_k, i);
     tc::fence_after_sync();
     if (ok) issue_state<DP>(tmem + G::cD, s);
     tc::mma_commit(&bar_d[i & 1]);
     // the next chunk's scores replace P and, at DP = 64, C.  They come after D:
     // ahead of it they would hold it up until the next chunk's tiles are there
-    if (i + 1 < nch) {
-      wait(bar_c, i);
-      if (DP == 64) wait(bar_o, i);
-      scores(i + 1);
-    }
+    wait(bar_c, i);
+    if (DP == 64) wait(bar_o, i);
+    scores(i + 1);
   }
   // no product is in flight when the CTA leaves, whatever ran out
-  if (nch > 0) tc::mbar_wait(&bar_d[(nch - 1) & 1], ((nch - 1) >> 1) & 1, status);
+  if (nch > 0) tc::mbar_wait(bar_c, (nch - 1) & 1, status);
 }
 
 // One thread: the loads.
@@ -599,6 +622,22 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       }
     }
   }
+  if (mine && p.s_out && a.nseg > 1 && !a.joined && seg == (rev ? 0 : a.nseg - 1)) {
+    // the outgoing state: this segment's own contribution on top
+    const float out_mul = w.n > 0 ? p.s_out_mul * (rev ? dec : 1.f) : 1.f;
+    const float f = decay_pow(lg, w.t_hi - w.t_lo - (w.nch > 0 ? w.fresh(0) : 0));
+    const float* x = p.seg + ((long long)bh * a.nseg + seg) * st + srow * dh + c64;
+    float* dst = p.s_out + (long long)bh * st + srow * dh + c64;
+#pragma unroll
+    for (int c = 0; c < 64; c += 4)
+      if (c64 + c < dh) {
+        float v[4];
+        load4(x + c, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = out_mul * fmaf(f, S[c + e], v[e]);
+        store4(dst + c, v);
+      }
+  }
   float f = 0.f;
   for (int i = 0;; ++i) {
     if (i > 0) {  // S <- f S + the last chunk's increment
@@ -619,11 +658,27 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       }
     }
     if (i == w.nch) break;
+    uint8_t* copy = sS + g * (DP * 128);
+    if (DP == 64 && i > 0) {  // the second terms' sums join, by way of the copy's place
+      if (lo_part) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          *reinterpret_cast<uint4*>(copy + tc::sw128_offset(srow, u)) = pack8(S + 8 * u);
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
     if (!lo_part) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        *reinterpret_cast<uint4*>(sS + g * (DP * 128) + tc::sw128_offset(srow, u)) =
-            pack8(S + 8 * u);
+      for (int u = 0; u < 8; ++u) {
+        uint4* to = reinterpret_cast<uint4*>(copy + tc::sw128_offset(srow, u));
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        if (DP == 64 && i > 0) unpack8(*to, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += S[8 * u + e];
+        *to = pack8(v);
+      }
     }
     tc::fence_proxy_async_smem();
     warp_arrive(bar_s, lane);
@@ -639,6 +694,7 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       tc::fence_proxy_async_smem();
       warp_arrive(bar_z, lane);
     }
+    if (i + 1 == w.nch) break;
     wait(&bar_a[i & 1], i >> 1);  // the keys have been used
     const uint32_t* wr = rev ? pt : pt + m - 1;
     uint4 lo[8];
@@ -664,33 +720,215 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
     wait(&bar_d[i & 1], i >> 1);
     tc::fence_after_sync();
   }
-  if (p.s_out && seg == (rev ? 0 : a.nseg - 1)) {  // uniform over the CTA
-    float* dst = p.s_out + (long long)bh * st + srow * dh + c64;
-    const float mul = w.n > 0 ? p.s_out_mul * (rev ? dec : 1.f) : 1.f;
-    if (DP == 64) {  // the two terms' sums, through the idle stages
-      float* x = reinterpret_cast<float*>(smem);
-      if (w.nch > 0) wait(bar_c, w.nch - 1);
-      if (lo_part) {
+}
+
+// ------------------------------------------------------------------ states
+// A state to fp32 accuracy: what a segment adds (from zero, before the segments'
+// join) or, with one segment, the outgoing state.  Product D alone, with K' in
+// three bf16 terms (24 bits of each decayed key): the walk above needs its state
+// for bf16 outputs only and has two.  The second and third terms have a tile each,
+// K and V two stages; the halves of a chunk's tokens are products of their own,
+// so that one half's terms are written under the other's product, and the
+// increments alternate between two accumulators.
+// DP = 64: the terms are the 64-row halves of two products, [mid | hi] and
+// [lo | mid] with half of the second term in mid; DP = 128: three products.
+// The first 4 DP threads hold the state (32 columns of a row each), the warp after
+// them issues.
+template <int DP>
+__device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, int seg,
+                                          uint8_t* smem_raw, unsigned* status) {
+  using G = TcGeo<DP>;
+  constexpr int HC = 32, NT = 4 * DP, kIssue = NT / 32;
+  uint8_t* smem = align1024(smem_raw);
+  uint8_t *sLo = smem, *sMid = smem + G::kTile, *stages = smem + 2 * G::kTile;
+  float* pw = reinterpret_cast<float*>(smem + 6 * G::kTile);  // a^0 .. a^128
+  uint64_t* bar = reinterpret_cast<uint64_t*>(pw + 130);
+  uint64_t* bar_full = bar;   // K and V have landed (2)
+  uint64_t* bar_d = bar + 2;  // D of a half done (2)
+  uint64_t* bar_k = bar + 4;  // K' of a half written (2)
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 6);
+
+  const LinArgs& a = A.a;
+  const LinPass& p = a.pass[ps];
+  const bool rev = p.rev != 0;
+  const int b = bh / a.H, h = bh - b * a.H;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, g = warp >> 2;
+  const int r = q * 32 + lane;
+  if (tid == 0) {
+    for (int i = 0; i < 4; ++i) tc::mbar_init(&bar[i], 1);
+    for (int i = 4; i < 6; ++i) tc::mbar_init(&bar[i], NT / 32);
+    tc::fence_mbar_init();
+  }
+  if (warp == kIssue) {
+    if (lane < 2) tc::prefetch_tmap(&A.map[lane == 0 ? A.mk[ps] : A.mv[ps]]);
+    tc::tmem_alloc(tslot, 2 * DP);
+    tc::tmem_relinquish();
+  }
+  pdl_enter();
+  const Walk w(a, b, seg, rev);
+  const int dh = a.dh;
+  if (tid < 129) pw[tid] = tid == 1 ? a.decay[h] : decay_pow(log2f(a.decay[h]), tid);
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  bool ok = true;
+  auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); };
+
+  if (warp >= kIssue) {
+    if (tid == NT) {
+      const uint32_t tmem = ld_once(tslot);
+      int loaded = 0;
+      const int tok0 = b * a.T;
+      auto load = [&]() {
+        const int i = loaded++;
+        uint8_t* s = stages + (i & 1) * 2 * G::kTile;
+        uint64_t* bf = &bar_full[i & 1];
+        const int row = tok0 + w.start(i);
+        tc::mbar_arrive_expect_tx(bf, 2 * G::kTile);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[srow * 65 + c] = S[c];
+        for (int f = 0; f < G::kHalves; ++f) {
+          tc::tma_load_3d(s + f * G::kHalf, &A.map[A.mk[ps]], bf, f * 64, h, row);
+          tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mv[ps]], bf, f * 64, h, row);
+        }
+      };
+      if (w.nch > 0) load();
+      if (w.nch > 1) load();
+      constexpr uint32_t id = tc::idesc_bf16(128, DP, 1, 1);
+#pragma unroll 1
+      for (int i = 0; i < w.nch; ++i) {
+        const uint32_t lo = tc::smem_u32(sLo), mid = tc::smem_u32(sMid),
+                       k = tc::smem_u32(stages) + (i & 1) * 2 * G::kTile, v = k + G::kTile,
+                       acc = tmem + (i & 1) * DP;
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+          wait(&bar_k[x], i);
+          tc::fence_after_sync();
+          const uint32_t o = x * 4 * 128, dv = desc_lo(v, G::kHalf) + o;
+          if (ok && DP == 64) {
+            issue<4>(acc, desc_lo(mid, k - mid) + o, 128, dv, 128, id, x);
+            issue<4>(acc, desc_lo(lo, mid - lo) + o, 128, dv, 128, id, 1u);
+          } else if (ok) {
+            issue<4>(acc, desc_lo(k, G::kHalf) + o, 128, dv, 128, id, x);
+            issue<4>(acc, desc_lo(mid, G::kHalf) + o, 128, dv, 128, id, 1u);
+            issue<4>(acc, desc_lo(lo, G::kHalf) + o, 128, dv, 128, id, 1u);
+          }
+          tc::mma_commit(&bar_d[x]);
+        }
+        if (loaded < w.nch || i + 1 == w.nch) wait(&bar_d[1], i);  // the stage is free again
+        if (ok && loaded < w.nch) load();
       }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (!lo_part) {
-#pragma unroll
-        for (int c = 0; c < 64; ++c) S[c] += x[srow * 65 + c];
+      if (!ok) {  // the loads in flight land before the CTA leaves
+        for (int i = max(0, loaded - 2); i < loaded; ++i)
+          tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
       }
     }
+    __syncwarp();
+  } else {
+    const uint32_t trow = ld_once(tslot) + ((uint32_t)(q * 32) << 16) + g * HC;
+    const bool lo_part = DP == 64 && r < 64;
+    const int srow = DP == 64 ? r & 63 : r;
+    const bool mine = !lo_part && srow < dh;
+    const bool whole = a.nseg == 1;  // the outgoing state
+    float S[HC];
+#pragma unroll
+    for (int c = 0; c < HC; ++c) S[c] = 0.f;
+    if (whole && mine && p.s_in) {
+      const float* src = p.s_in + (long long)bh * dh * dh;
+      const float mul = w.n > 0 ? p.s_in_mul : 1.f;
+#pragma unroll
+      for (int c = 0; c < HC; ++c) {
+        const int col = g * HC + c;
+        if (col < dh) S[c] = mul * (p.s_in_t ? src[col * dh + srow] : src[srow * dh + col]);
+      }
+    }
+    auto add = [&](int i) {  // chunk i's increment
+      wait(&bar_d[1], i);
+      tc::fence_after_sync();
+      const float f = pw[w.rows(i) - (whole ? w.fresh(i) : 0)];
+      float d[HC];
+      tc::tmem_ld32(trow + (i & 1) * DP, d);
+#pragma unroll
+      for (int c = 0; c < HC; ++c) S[c] = fmaf(f, S[c], d[c]);
+    };
+#pragma unroll 1
+    for (int i = 0; i < w.nch; ++i) {
+      uint8_t* sK = stages + (i & 1) * 2 * G::kTile;
+      const int m = w.rows(i);
+      wait(&bar_full[i & 1], i >> 1);
+      if (m < kRows) {  // rows past the end may hold anything, and they meet zero weights only
+        clear_rows<DP>(sK, m, tid, NT);
+        clear_rows<DP>(sK + G::kTile, m, tid, NT);
+        asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory");
+      }
+#pragma unroll 1
+      for (int x = 0; x < 2; ++x) {
+        // the last chunk's product has used this half's second and third terms
+        if (i > 0 && x == 0) wait(&bar_d[0], i - 1);
+        if (i > 0 && x == 1) add(i - 1);
+        uint4 k[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int idx = u * NT + tid, row = x * 64 + ((idx >> 3) & 63);
+          k[u] = *reinterpret_cast<const uint4*>(sK + (idx >> 9) * G::kHalf +
+                                                 tc::sw128_offset(row, idx & 7));
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int idx = u * NT + tid, row = x * 64 + ((idx >> 3) & 63);
+          const uint32_t off = (idx >> 9) * G::kHalf + tc::sw128_offset(row, idx & 7);
+          uint4 hi, mid, lo;
+          key_terms3(k[u], row < m ? pw[rev ? row : m - 1 - row] : 0.f, DP == 64 ? 0.5f : 1.f, hi,
+                     mid, lo);
+          *reinterpret_cast<uint4*>(sK + off) = hi;
+          *reinterpret_cast<uint4*>(sMid + off) = mid;
+          *reinterpret_cast<uint4*>(sLo + off) = lo;
+        }
+        tc::fence_proxy_async_smem();
+        warp_arrive(&bar_k[x], lane);
+      }
+    }
+    if (w.nch > 0) add(w.nch - 1);
+    if (DP == 64) {  // the halves' sums, through the idle tiles
+      float* x = reinterpret_cast<float*>(smem);
+      if (lo_part) {
+#pragma unroll
+        for (int c = 0; c < HC; ++c) x[srow * 65 + g * HC + c] = S[c];
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory");
+      if (!lo_part) {
+#pragma unroll
+        for (int c = 0; c < HC; ++c) S[c] += x[srow * 65 + g * HC + c];
+      }
+    }
+    float* dst = whole ? p.s_out + (long long)bh * dh * dh + srow * dh
+                       : p.seg + ((long long)bh * a.nseg + seg) * dh * dh + srow * dh;
+    const float mul = whole && w.n > 0 ? p.s_out_mul * (rev ? pw[1] : 1.f) : 1.f;
     if (mine && ok) {
 #pragma unroll
-      for (int c = 0; c < 64; c += 4)
-        if (c64 + c < dh) {
+      for (int c = 0; c < HC; c += 4)
+        if (g * HC + c < dh) {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = S[c + e] * mul;
-          store4(dst + c, v);
+          store4(dst + g * HC + c, v);
         }
     }
   }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == kIssue) tc::tmem_dealloc(ld_once(tslot), 2 * DP);
+}
+
+// The segments' states (the last one's own contribution is needed for the outgoing
+// state only), or the outgoing state after a walk that reads the same buffer.
+template <int DP>
+__global__ void __launch_bounds__(4 * DP + 32, DP == 64 ? 2 : 1)
+    linattn_state_kernel(const __grid_constant__ LinTcArgs A, unsigned* status) {
+  extern __shared__ uint8_t smem_raw[];
+  const int ps = blockIdx.y, nseg = A.a.nseg;
+  const int bh = blockIdx.x / nseg, seg = blockIdx.x - bh * nseg;
+  if (!A.a.pass[ps].s_out && seg == (A.a.pass[ps].rev ? 0 : nseg - 1)) return;
+  state_cta<DP>(A, ps, bh, seg, smem_raw, status);
 }
 
 template <int DP>
@@ -700,6 +938,10 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
   using R = Roles<DP>;
   constexpr int NW = R::NW;
   extern __shared__ uint8_t smem_raw[];
+  if (blockIdx.y == A.a.npass) {  // the outgoing state, beside the walks
+    state_cta<DP>(A, A.out, blockIdx.x, 0, smem_raw, status);
+    return;
+  }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   {
     const View<DP> vw(smem_raw);
@@ -762,168 +1004,6 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
   if (warp == 8 * NW) tc::tmem_dealloc(View<DP>(smem_raw).shared()->tmem, G::kCols);
 }
 
-// ---------------------------------------------------------- segment states
-// The state that a segment adds (from zero, before the segments' join): product
-// D alone, its increments double-buffered in TMEM, so that the next chunk's K'
-// is written under this one's product.  Reads K and V once: bandwidth-bound.
-template <int DP>
-__global__ void __launch_bounds__(288, DP == 64 ? 2 : 1)
-    linattn_state_kernel(const __grid_constant__ LinTcArgs A, unsigned* status) {
-  using G = TcGeo<DP>;
-  constexpr int HC = DP / 2;  // columns of a state row that a thread holds
-  constexpr uint32_t kCols = 2 * DP;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = align1024(smem_raw);
-  float* pw = reinterpret_cast<float*>(smem + 2 * G::kStage + G::kState);  // a^0 .. a^128
-  uint32_t* pt = reinterpret_cast<uint32_t*>(pw + 130);                    // in two bf16 terms
-  uint64_t* bar = reinterpret_cast<uint64_t*>(pt + 128);
-  uint64_t* bar_full = bar;   // (2)
-  uint64_t* bar_d = bar + 2;  // (2)
-  uint64_t* bar_k = bar + 4;  // (2): K' of the next chunk may be written before D is issued
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 6);
-
-  const LinArgs& a = A.a;
-  const int ps = blockIdx.y;
-  const LinPass& p = a.pass[ps];
-  const bool rev = p.rev != 0;
-  // nobody needs the last segment's own contribution
-  const int per = a.nseg - 1;
-  const int bh = blockIdx.x / per, seg = blockIdx.x - bh * per + (rev ? 1 : 0);
-  const int b = bh / a.H, h = bh - b * a.H;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, g = (warp >> 2) & 1;
-  const int r = q * 32 + lane;
-  if (tid == 0) {
-    for (int i = 0; i < 4; ++i) tc::mbar_init(&bar[i], 1);
-    tc::mbar_init(&bar_k[0], 8);
-    tc::mbar_init(&bar_k[1], 8);
-    tc::fence_mbar_init();
-  }
-  if (warp == 8) {
-    if (lane < 2) tc::prefetch_tmap(&A.map[lane == 0 ? A.mk[ps] : A.mv[ps]]);
-    tc::tmem_alloc(tslot, kCols);
-    tc::tmem_relinquish();
-  }
-  pdl_enter();
-  const Walk w(a, b, seg, rev);
-  const float dec = a.decay[h], lg = log2f(dec);
-  const int dh = a.dh;
-  const long long tok0 = (long long)b * a.T;
-  if (tid < 129) {
-    const float x = decay_pow(lg, tid);
-    pw[tid] = x;
-    if (tid < 128) pt[tid] = weight_terms(x);
-  }
-  tc::fence_before_sync();
-  __syncthreads();
-  tc::fence_after_sync();
-  const uint32_t tmem = *tslot;
-  const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16);
-  bool ok = true;
-  auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); };
-
-  if (warp == 8) {
-    if (lane == 0) {
-      int loaded = 0;
-      auto load = [&]() {
-        const int i = loaded++;
-        uint8_t* s = smem + (i & 1) * G::kStage;
-        uint64_t* bf = &bar_full[i & 1];
-        const int row = (int)(tok0 + w.start(i));
-        tc::mbar_arrive_expect_tx(bf, 2 * G::kTile);
-#pragma unroll
-        for (int f = 0; f < G::kHalves; ++f) {
-          tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mk[ps]], bf, f * 64, h, row);
-          tc::tma_load_3d(s + 2 * G::kTile + f * G::kHalf, &A.map[A.mv[ps]], bf, f * 64, h, row);
-        }
-      };
-      if (w.nch > 0) load();
-      if (w.nch > 1) load();
-      for (int i = 0; i < w.nch; ++i) {
-        wait(&bar_k[i & 1], i >> 1);
-        tc::fence_after_sync();
-        if (ok) issue_state<DP>(tmem + (i & 1) * DP, tc::smem_u32(smem) + (i & 1) * G::kStage);
-        tc::mma_commit(&bar_d[i & 1]);
-        if (loaded < w.nch) {
-          wait(&bar_d[i & 1], i >> 1);  // the stage is free again
-          if (ok) load();
-        }
-      }
-      if (!ok) {  // the loads and products in flight end before the CTA leaves
-        for (int i = max(0, loaded - 2); i < loaded; ++i)
-          tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
-        for (int i = max(0, w.nch - 2); i < w.nch; ++i)
-          tc::mbar_wait(&bar_d[i & 1], (i >> 1) & 1, status);
-      }
-    }
-    __syncwarp();
-  } else {
-    const bool lo_part = DP == 64 && r < 64;
-    const int srow = DP == 64 ? r & 63 : r;
-    float S[HC];
-#pragma unroll
-    for (int c = 0; c < HC; ++c) S[c] = 0.f;
-    auto add = [&](int i) {  // chunk i's increment
-      wait(&bar_d[i & 1], i >> 1);
-      tc::fence_after_sync();
-      const float f = pw[w.rows(i)];
-#pragma unroll
-      for (int c0 = 0; c0 < HC; c0 += 32) {
-        float d[32];
-        tc::tmem_ld32(trow + (i & 1) * DP + g * HC + c0, d);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) S[c0 + c] = fmaf(f, S[c0 + c], d[c]);
-      }
-    };
-    for (int i = 0; i < w.nch; ++i) {
-      uint8_t* sQ = smem + (i & 1) * G::kStage;
-      uint8_t* sK = sQ + G::kTile;
-      const int m = w.rows(i);
-      wait(&bar_full[i & 1], i >> 1);
-      if (m < kRows) {  // rows past the end may hold anything, and they meet zero weights only
-        clear_rows<DP>(sK, m, tid, 256);
-        clear_rows<DP>(sK + G::kTile, m, tid, 256);
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-      }
-      const uint32_t* wr = rev ? pt : pt + m - 1;
-#pragma unroll 4
-      for (int x = 0; x < DP / 16; ++x) {
-        const int idx = x * 256 + tid, row = (idx >> 3) & 127;
-        const uint32_t off = (idx >> 10) * G::kHalf + tc::sw128_offset(row, idx & 7);
-        uint4 hi, lo;
-        key_terms(*reinterpret_cast<const uint4*>(sK + off), row < m ? wr[rev ? row : -row] : 0u,
-                  hi, lo);
-        *reinterpret_cast<uint4*>(sK + off) = hi;
-        *reinterpret_cast<uint4*>(sQ + off) = lo;
-      }
-      tc::fence_proxy_async_smem();
-      warp_arrive(&bar_k[i & 1], lane);
-      if (i > 0) add(i - 1);
-    }
-    if (w.nch > 0) add(w.nch - 1);
-    float* dst = p.seg + ((long long)bh * a.nseg + seg) * dh * dh + srow * dh;
-    if (DP == 64) {  // the two terms' sums, through the idle stages
-      float* x = reinterpret_cast<float*>(smem);
-      if (lo_part) {
-#pragma unroll
-        for (int c = 0; c < HC; ++c) x[srow * 65 + g * HC + c] = S[c];
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (!lo_part) {
-#pragma unroll
-        for (int c = 0; c < HC; ++c) S[c] += x[srow * 65 + g * HC + c];
-      }
-    }
-    if (!lo_part && srow < dh && ok) {
-#pragma unroll
-      for (int c = 0; c < HC; c += 4)
-        if (g * HC + c < dh) store4(dst + g * HC + c, S + c);
-    }
-  }
-  tc::fence_before_sync();
-  __syncthreads();
-  if (warp == 8) tc::tmem_dealloc(tmem, kCols);
-}
-
 // ---------------------------------------------------------------- host side
 namespace {
 
@@ -934,17 +1014,27 @@ cudaError_t tc_launch(const Launch& lc, const LinTcArgs& A) {
   cudaError_t e = smem_opt_in(linattn_tc_kernel<DP>, G::kSmem, &opted);
   if (e != cudaSuccess) return e;
   const unsigned heads = (unsigned)A.a.B * A.a.H;
+  if ((e = smem_opt_in(linattn_state_kernel<DP>, G::kSmem, &opted_state)) != cudaSuccess) return e;
+  auto states = [&](int passes) {
+    return launch_k(linattn_state_kernel<DP>, dim3(heads * A.a.nseg, passes), dim3(4 * DP + 32), G::kSmem,
+                    lc.stream, A, lc.status);
+  };
   if (A.a.nseg > 1) {
-    if ((e = smem_opt_in(linattn_state_kernel<DP>, G::kSmem, &opted_state)) != cudaSuccess) return e;
-    e = launch_k(linattn_state_kernel<DP>, dim3(heads * (A.a.nseg - 1), A.a.npass), dim3(288),
-                 G::kSmem, lc.stream, A, lc.status);
-    if (e != cudaSuccess) return e;
+    if ((e = states(A.a.npass)) != cudaSuccess) return e;
     if (A.a.joined && (e = linattn_combine(lc, A.a)) != cudaSuccess) return e;
   }
-  e = launch_k(linattn_tc_kernel<DP>, dim3(heads * A.a.nseg, A.a.npass),
-               dim3(Roles<DP>::kThreads), G::kSmem,
-               lc.stream, A, lc.status);
-  return e != cudaSuccess ? e : cudaGetLastError();
+  // One segment: the outgoing state is a product of its own, by CTAs beside the
+  // walks, or after them where it overwrites the state that they read
+  const bool whole = A.out >= 0 && A.a.nseg == 1;
+  bool after = false;
+  for (int i = 0; whole && i < A.a.npass; ++i)
+    after = after || A.a.pass[i].s_in == A.a.pass[A.out].s_out;
+  e = launch_k(linattn_tc_kernel<DP>,
+               dim3(heads * A.a.nseg, A.a.npass + (whole && !after ? 1 : 0)),
+               dim3(Roles<DP>::kThreads), G::kSmem, lc.stream, A, lc.status);
+  if (e != cudaSuccess) return e;
+  if (after && (e = states(A.out + 1)) != cudaSuccess) return e;
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -954,6 +1044,10 @@ cudaError_t linattn_tc(const Launch& lc, const LinArgs& a) {
   A.a = a;
   // few segments: each CTA joins the states before its own; a state updated in
   // place is read before any CTA writes it only if a kernel of its own joins
+  A.a.all = 1;
+  A.out = -1;
+  for (int i = 0; i < a.npass; ++i)
+    if (a.pass[i].s_out) A.out = i;
   A.a.joined = a.nseg > 8 || (a.pass[0].s_in && a.pass[0].s_in == a.pass[0].s_out);
   int nmaps = 0;
   const void* base[4];
