@@ -266,17 +266,19 @@ __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_const
   const int n = valid_tokens(a, b);
   const float dec = a.decay[h];
   const float full = powf(dec, (float)a.seg_len);
+  // the state's row and column: row-major, or groups of 4 columns (a.grouped)
+  const int hi = a.grouped ? e0 / 4 / dh : e0 / dh, rest = a.grouped ? e0 / 4 - hi * dh : e0 - hi * dh;
+  const int i = a.grouped ? rest : hi, j = a.grouped ? hi * 4 : rest;
   float x[4] = {0.f, 0.f, 0.f, 0.f};
   if (p.s_in) {
     const float* src = p.s_in + (long long)bh * st;
-    const int i = e0 / dh, j = e0 - i * dh;
     const float mul = n > 0 ? p.s_in_mul : 1.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      x[c] = mul * (p.s_in_t ? src[(long long)(j + c) * dh + i] : src[e0 + c]);
+      x[c] = mul * (p.s_in_t ? src[(long long)(j + c) * dh + i] : src[i * dh + j + c]);
   }
   float* w = p.seg + (long long)bh * a.nseg * st + e0;
-  const bool out = a.all && p.s_out;
+  const bool out = a.grouped && p.s_out;
   for (int s0 = 0; s0 < a.nseg; s0 += 4) {
     float loc[4][4];
 #pragma unroll
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_const
     const float mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) x[c] *= mul;
-    store4(p.s_out + (long long)bh * st + e0, x);
+    store4(p.s_out + (long long)bh * st + i * dh + j, x);
   }
 }
 

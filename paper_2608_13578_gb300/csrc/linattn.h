@@ -39,7 +39,9 @@ struct LinArgs {
   const int* lengths;     // [B] or null
   int nseg, seg_len;      // the tokens in nseg segments of seg_len
   int joined;             // pass.seg holds the segments' incoming states, not their own
-  int all;                // the join of the segments gives the outgoing state too
+  // the tensor-core form's segment states: groups of 4 columns of all rows together,
+  // and the join gives the outgoing state too
+  int grouped;
 };
 
 // How the passes are cut along the tokens (the same rule for the workspace
@@ -57,7 +59,7 @@ cudaError_t linattn_step(const Launch& lc, int dtype, const LinArgs& a);
 // The chunked form on the tensor cores: bf16, segments of whole 128-token chunks.
 cudaError_t linattn_tc(const Launch& lc, const LinArgs& a);
 // Local segment states (in pass.seg) -> each segment's incoming state, and with
-// a.all the outgoing state.
+// a.grouped the outgoing state.
 cudaError_t linattn_combine(const Launch& lc, const LinArgs& a);
 
 }  // namespace bcmt

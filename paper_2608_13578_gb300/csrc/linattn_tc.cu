@@ -415,6 +415,45 @@ __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, uns
     tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
 }
 
+// The outgoing state of head bh from the segments' own (threads t of nt).
+__device__ __forceinline__ void join_out(const LinArgs& a, const LinPass& p, int bh, int n,
+                                         float lg, float dec, int t, int nt) {
+  const int dh = a.dh, st = dh * dh;
+  const float out_mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
+  for (int e = t; e < st / 8; e += nt) {  // 8 columns of a row
+    const int col = e / dh * 8, row = e - col / 8 * dh, at = col * dh + row * 4;
+    float x[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c] = 0.f;
+    if (p.s_in) {
+      const float mul = n > 0 ? p.s_in_mul : 1.f;
+      load4(p.s_in + (long long)bh * st + row * dh + col, x);
+      load4(p.s_in + (long long)bh * st + row * dh + col + 4, x + 4);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[c] *= mul;
+    }
+#pragma unroll 2
+    for (int i = 0; i < a.nseg; ++i) {
+      const int s = p.rev ? a.nseg - 1 - i : i;
+      const int m = min(max(n - s * a.seg_len, 0), a.seg_len);
+      const bool fresh = p.rev && n <= s * a.seg_len + a.seg_len;  // holds the last valid token
+      const float* src = p.seg + ((long long)bh * a.nseg + s) * st + at;
+      float v[8];
+      load4(src, v);
+      load4(src + dh * 4, v + 4);
+      if (m == 0) continue;
+      const float f = decay_pow(lg, m - (fresh ? 1 : 0));
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[c] = fmaf(f, x[c], v[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c] *= out_mul;
+    float* dst = p.s_out + (long long)bh * st + row * dh + col;
+    store4(dst, x);
+    store4(dst + 4, x + 4);
+  }
+}
+
 // 4 NW warps, thread = row of the chunk: P, and 64 columns of the output rows.
 template <int DP>
 __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
@@ -462,6 +501,11 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
       }
     }
   };
+  if (a.nseg > 1 && !a.joined && p.s_out) {  // while the last segment's first tiles are on their way
+    const Shared* sh = vw.shared();
+    if (ld_once(&sh->seg) == (rev ? 0 : a.nseg - 1))
+      join_out(a, p, ld_once(&sh->b) * a.H + h, w.n, log2f(a.decay[h]), a.decay[h], tid, 128 * NW);
+  }
   // the halves hh of blocks that the row sees
   const int h0 = rev ? 2 * q : 0, h1 = rev ? 8 : 2 * q + 2;
   for (int i = 0; i < w.nch; ++i) {
@@ -586,13 +630,15 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16) + G::cD + c64;
   if (mine) {
     const bool joined = a.nseg > 1 && a.joined;
-    const float* src = joined   ? p.seg + ((long long)bh * a.nseg + seg) * st
+    const float* src = joined   ? p.seg + ((long long)bh * a.nseg + seg) * st + srow * 4
                        : p.s_in ? p.s_in + (long long)bh * st
                                 : nullptr;
     if (src && (joined || !p.s_in_t)) {
+      src += joined ? c64 * dh : srow * dh + c64;
+      const int step = joined ? dh : 1;
 #pragma unroll
       for (int c = 0; c < 64; c += 4)
-        if (c64 + c < dh) load4(src + srow * dh + c64 + c, S + c);
+        if (c64 + c < dh) load4(src + c * step, S + c);
     } else if (src) {
 #pragma unroll
       for (int c = 0; c < 64; ++c)
@@ -610,33 +656,17 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
         if (ms == 0) continue;
         const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
         const float f = decay_pow(lg, ms - (fresh ? 1 : 0));
-        const float* x = p.seg + ((long long)bh * a.nseg + s) * st + srow * dh + c64;
+        const float* x = p.seg + ((long long)bh * a.nseg + s) * st + c64 * dh + srow * 4;
 #pragma unroll
         for (int c = 0; c < 64; c += 4)
           if (c64 + c < dh) {
             float v[4];
-            load4(x + c, v);
+            load4(x + c * dh, v);
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[c + e] = fmaf(f, S[c + e], v[e]);
           }
       }
     }
-  }
-  if (mine && p.s_out && a.nseg > 1 && !a.joined && seg == (rev ? 0 : a.nseg - 1)) {
-    // the outgoing state: this segment's own contribution on top
-    const float out_mul = w.n > 0 ? p.s_out_mul * (rev ? dec : 1.f) : 1.f;
-    const float f = decay_pow(lg, w.t_hi - w.t_lo - (w.nch > 0 ? w.fresh(0) : 0));
-    const float* x = p.seg + ((long long)bh * a.nseg + seg) * st + srow * dh + c64;
-    float* dst = p.s_out + (long long)bh * st + srow * dh + c64;
-#pragma unroll
-    for (int c = 0; c < 64; c += 4)
-      if (c64 + c < dh) {
-        float v[4];
-        load4(x + c, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = out_mul * fmaf(f, S[c + e], v[e]);
-        store4(dst + c, v);
-      }
   }
   float f = 0.f;
   for (int i = 0;; ++i) {
@@ -723,15 +753,17 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
 }
 
 // ------------------------------------------------------------------ states
-// A state to fp32 accuracy: what a segment adds (from zero, before the segments'
-// join) or, with one segment, the outgoing state.  Product D alone, with K' in
-// three bf16 terms (24 bits of each decayed key): the walk above needs its state
-// for bf16 outputs only and has two.  The second and third terms have a tile each,
-// K and V two stages; the halves of a chunk's tokens are products of their own,
-// so that one half's terms are written under the other's product, and the
-// increments alternate between two accumulators.
-// DP = 64: the terms are the 64-row halves of two products, [mid | hi] and
-// [lo | mid] with half of the second term in mid; DP = 128: three products.
+// The state that a segment adds (from zero, before the segments' join) or, with
+// one segment, the outgoing state: product D alone.  A state that the call returns
+// is made to fp32 accuracy, with K' in three bf16 terms (24 bits of each decayed
+// key); one that is only a bf16 operand of the outputs has two, as in the walk.
+// The second and third terms have a tile each, K and V two stages; the halves of
+// a chunk's tokens are products of their own, so that one half's terms are written
+// under the other's product, and the increments alternate between two accumulators.
+// DP = 64: the terms are the 64-row halves of products, [mid | hi] and [lo | mid]
+// with half of the second term in mid; DP = 128: a product for each term.
+// A segment's state is stored with the 4-column groups of all rows together (the
+// threads of a warp hold a row each).
 // The first 4 DP threads hold the state (32 columns of a row each), the warp after
 // them issues.
 template <int DP>
@@ -751,6 +783,7 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
   const LinArgs& a = A.a;
   const LinPass& p = a.pass[ps];
   const bool rev = p.rev != 0;
+  const bool three = p.s_out != nullptr;
   const int b = bh / a.H, h = bh - b * a.H;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, g = warp >> 2;
   const int r = q * 32 + lane;
@@ -806,11 +839,11 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
           const uint32_t o = x * 4 * 128, dv = desc_lo(v, G::kHalf) + o;
           if (ok && DP == 64) {
             issue<4>(acc, desc_lo(mid, k - mid) + o, 128, dv, 128, id, x);
-            issue<4>(acc, desc_lo(lo, mid - lo) + o, 128, dv, 128, id, 1u);
+            if (three) issue<4>(acc, desc_lo(lo, mid - lo) + o, 128, dv, 128, id, 1u);
           } else if (ok) {
             issue<4>(acc, desc_lo(k, G::kHalf) + o, 128, dv, 128, id, x);
             issue<4>(acc, desc_lo(mid, G::kHalf) + o, 128, dv, 128, id, 1u);
-            issue<4>(acc, desc_lo(lo, G::kHalf) + o, 128, dv, 128, id, 1u);
+            if (three) issue<4>(acc, desc_lo(lo, G::kHalf) + o, 128, dv, 128, id, 1u);
           }
           tc::mma_commit(&bar_d[x]);
         }
@@ -832,14 +865,14 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
     float S[HC];
 #pragma unroll
     for (int c = 0; c < HC; ++c) S[c] = 0.f;
-    if (whole && mine && p.s_in) {
+    if (whole && mine && p.s_in) {  // (not transposed: no pass has s_in_t and s_out)
       const float* src = p.s_in + (long long)bh * dh * dh;
       const float mul = w.n > 0 ? p.s_in_mul : 1.f;
 #pragma unroll
-      for (int c = 0; c < HC; ++c) {
-        const int col = g * HC + c;
-        if (col < dh) S[c] = mul * (p.s_in_t ? src[col * dh + srow] : src[srow * dh + col]);
-      }
+      for (int c = 0; c < HC; c += 4)
+        if (g * HC + c < dh) load4(src + srow * dh + g * HC + c, S + c);
+#pragma unroll
+      for (int c = 0; c < HC; ++c) S[c] *= mul;
     }
     auto add = [&](int i) {  // chunk i's increment
       wait(&bar_d[1], i);
@@ -876,12 +909,16 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
         for (int u = 0; u < 2; ++u) {
           const int idx = u * NT + tid, row = x * 64 + ((idx >> 3) & 63);
           const uint32_t off = (idx >> 9) * G::kHalf + tc::sw128_offset(row, idx & 7);
+          const float wt = row < m ? pw[rev ? row : m - 1 - row] : 0.f;
           uint4 hi, mid, lo;
-          key_terms3(k[u], row < m ? pw[rev ? row : m - 1 - row] : 0.f, DP == 64 ? 0.5f : 1.f, hi,
-                     mid, lo);
+          if (three) {
+            key_terms3(k[u], wt, DP == 64 ? 0.5f : 1.f, hi, mid, lo);
+            *reinterpret_cast<uint4*>(sLo + off) = lo;
+          } else {
+            key_terms(k[u], weight_terms(wt), hi, mid);
+          }
           *reinterpret_cast<uint4*>(sK + off) = hi;
           *reinterpret_cast<uint4*>(sMid + off) = mid;
-          *reinterpret_cast<uint4*>(sLo + off) = lo;
         }
         tc::fence_proxy_async_smem();
         warp_arrive(&bar_k[x], lane);
@@ -901,7 +938,8 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
       }
     }
     float* dst = whole ? p.s_out + (long long)bh * dh * dh + srow * dh
-                       : p.seg + ((long long)bh * a.nseg + seg) * dh * dh + srow * dh;
+                       : p.seg + ((long long)bh * a.nseg + seg) * dh * dh + srow * 4;
+    const int step = whole ? 1 : dh;
     const float mul = whole && w.n > 0 ? p.s_out_mul * (rev ? pw[1] : 1.f) : 1.f;
     if (mine && ok) {
 #pragma unroll
@@ -910,7 +948,7 @@ __device__ __forceinline__ void state_cta(const LinTcArgs& A, int ps, int bh, in
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = S[c + e] * mul;
-          store4(dst + g * HC + c, v);
+          store4(dst + (g * HC + c) * step, v);
         }
     }
   }
@@ -1044,7 +1082,7 @@ cudaError_t linattn_tc(const Launch& lc, const LinArgs& a) {
   A.a = a;
   // few segments: each CTA joins the states before its own; a state updated in
   // place is read before any CTA writes it only if a kernel of its own joins
-  A.a.all = 1;
+  A.a.grouped = 1;
   A.out = -1;
   for (int i = 0; i < a.npass; ++i)
     if (a.pass[i].s_out) A.out = i;
