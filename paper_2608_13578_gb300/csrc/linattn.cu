@@ -56,8 +56,10 @@ __device__ __forceinline__ void load_run(const float* p, float* v) {
 // channels; the next stage's rows are loaded into registers under this one's
 // arithmetic.  Per token and lane: DK/8 * 4 * (multiply, two fused
 // multiply-adds), and the sum over the 8 row groups as a reduce-scatter of the
-// four columns (4 shuffles).  Arithmetic-bound: 3 instructions per state
-// element and token.
+// four columns (4 shuffles).  Rows are taken in pairs by the packed fp32
+// instructions: 1.5 instructions per state element and token.  Bound by those and
+// the latency of the sums: 4 x 4096 tokens of 8 heads of width 64 take 154 us (183
+// without pairs), 2 x 2048 of width 128 take 142 us (167).
 // `local`: states only, from zero, into pass.seg (the first launch of a
 // segmented walk).
 template <class T, int DK, int NW>
@@ -91,11 +93,11 @@ __global__ void __launch_bounds__(NW * 32)
   const T* gv = (const T*)p.v + tok0 * p.ldv + h * dh + c0;
   const long long st = (long long)dh * dh;
 
-  float S[R][4];
+  float2 S[R / 2][4];  // pairs of rows, for the packed fp32 arithmetic
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R / 2; ++r)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) S[r][c] = 0.f;
+    for (int c = 0; c < 4; ++c) S[r][c] = make_float2(0.f, 0.f);
   auto row_of = [&](int r) { return (r / V) * 8 * V + g * V + (r % V); };
   const bool col_ok = c0 + col < dh;  // dh is a multiple of 8: the quad is whole or absent
   if (!local && col_ok) {
@@ -115,7 +117,8 @@ __global__ void __launch_bounds__(NW * 32)
         const int row = row_of(r);
         if (row >= dh) continue;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) S[r][c] = mul * src[row * si + (c0 + col + c) * sj];
+        for (int c = 0; c < 4; ++c)
+          (r & 1 ? S[r / 2][c].y : S[r / 2][c].x) = mul * src[row * si + (c0 + col + c) * sj];
       }
     }
   }
@@ -180,9 +183,11 @@ __global__ void __launch_bounds__(NW * 32)
     if (s0 + TS < cnt_all) load(s0 + TS);
     if (!local && s0 > 0) flush(buf ^ 1, s0 - TS);
     const int cnt = min(TS, cnt_all - s0);
+#pragma unroll(DK <= 32 ? 2 : 1)  // two tokens' sums overlap: 29.5 -> 22.7 us at 2 x 999, width 32
     for (int i = 0; i < cnt; ++i) {
       // the incoming state of a reverse walk is not decayed by its first token
       const float f = (p.rev && token(s0 + i) == n - 1) ? 1.f : dec;
+      const float2 f2 = make_float2(f, f);
       float vv[4];
       load4(&sv[buf][i][col], vv);
       float kk[R], qq[R];
@@ -190,21 +195,29 @@ __global__ void __launch_bounds__(NW * 32)
       for (int r = 0; r < R; r += V) load_run<V>(&sk[buf][i][row_of(r)], kk + r);
       if (local) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R / 2; ++r)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) S[r][c] = fmaf(kk[r], vv[c], f * S[r][c]);
+          for (int c = 0; c < 4; ++c)
+            S[r][c] = __ffma2_rn(make_float2(kk[2 * r], kk[2 * r + 1]), make_float2(vv[c], vv[c]),
+                                 __fmul2_rn(f2, S[r][c]));
         continue;
       }
 #pragma unroll
       for (int r = 0; r < R; r += V) load_run<V>(&sq[buf][i][row_of(r)], qq + r);
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      float2 acc2[4];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int r = 0; r < R / 2; ++r) {
+        const float2 q2 = make_float2(qq[2 * r], qq[2 * r + 1]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          S[r][c] = fmaf(kk[r], vv[c], f * S[r][c]);
-          acc[c] = fmaf(qq[r], S[r][c], acc[c]);
+          S[r][c] = __ffma2_rn(make_float2(kk[2 * r], kk[2 * r + 1]), make_float2(vv[c], vv[c]),
+                               __fmul2_rn(f2, S[r][c]));
+          acc2[c] = r == 0 ? __fmul2_rn(q2, S[r][c]) : __ffma2_rn(q2, S[r][c], acc2[c]);
         }
+      }
+      float acc[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] = acc2[c].x + acc2[c].y;
       // reduce-scatter over the 8 row groups: lane bits 0 and 1 pick the column
       const bool hi0 = g & 1, hi1 = g & 2;
       const float s0a = hi0 ? acc[0] : acc[2], s1a = hi0 ? acc[1] : acc[3];
@@ -245,7 +258,7 @@ __global__ void __launch_bounds__(NW * 32)
       if (row >= dh) continue;
       float v[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = S[r][c] * mul;
+      for (int c = 0; c < 4; ++c) v[c] = (r & 1 ? S[r / 2][c].y : S[r / 2][c].x) * mul;
       store4(dst + (long long)row * dh + c0 + col, v);
     }
   }
@@ -255,7 +268,7 @@ __global__ void __launch_bounds__(NW * 32)
 // Walks the segments of one head in the pass's order, one thread per four
 // state elements: on entry seg[s] is segment s's own contribution (from a zero
 // state), on return the state coming into segment s.  In place; latency-bound
-// (a load, a multiply-add and a store per segment, loads ahead by four).
+// (a load, a multiply-add and a store per segment, 16 loads in flight).
 __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_constant__ LinArgs a) {
   pdl_enter();
   const LinPass& p = a.pass[blockIdx.y];
@@ -279,15 +292,16 @@ __global__ void __launch_bounds__(256) linattn_combine_kernel(const __grid_const
   }
   float* w = p.seg + (long long)bh * a.nseg * st + e0;
   const bool out = a.grouped && p.s_out;
-  for (int s0 = 0; s0 < a.nseg; s0 += 4) {
-    float loc[4][4];
+  constexpr int kBatch = 16;  // loads in flight: each is a memory latency
+  for (int s0 = 0; s0 < a.nseg; s0 += kBatch) {
+    float loc[kBatch][4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kBatch; ++u) {
       const int s = p.rev ? a.nseg - 1 - (s0 + u) : s0 + u;
       if (s0 + u < a.nseg - (out ? 0 : 1)) load4(w + (long long)s * st, loc[u]);
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < kBatch; ++u) {
       if (s0 + u >= a.nseg) break;
       const int s = p.rev ? a.nseg - 1 - (s0 + u) : s0 + u;
       store4(w + (long long)s * st, x);
@@ -412,11 +426,13 @@ LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms,
     pl.seg_len = per * 128;
     return pl;
   }
-  // enough CTAs for two on each SM, by segments of at least 64 tokens (the walk
-  // is sequential: one segment's latency is the pass's)
+  // enough CTAs for eight on each SM, by segments of at least 24 tokens: the walk
+  // is sequential, and one segment's latency is the pass's.  Two CTAs an SM and 64
+  // tokens took 277 us for 183 at 4 x 4096 of width 64, 39 for 31 at 1 x 200 of 4
+  // heads of width 128; segments of 32 and of 24 tokens differ by 2 to 4 us in small calls
   const long long ctas = heads * (dh > 64 ? 2 : 1);
-  const long long want = (2ll * sms + ctas - 1) / ctas;
-  const long long most = std::max(1, T / 64);
+  const long long want = (8ll * sms + ctas - 1) / ctas;
+  const long long most = std::max(1, T / 24);
   const long long n = std::max(1ll, std::min(want, most));
   if (n > 1) {
     pl.seg_len = (int)((T + n - 1) / n);
