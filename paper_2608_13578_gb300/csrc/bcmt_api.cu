@@ -590,8 +590,10 @@ size_t linattn_workspace(const bcmt_linattn_params* p, int backward) {
   const int npass = backward ? 3 : 1;
   int nseg = 1;  // whichever kernels run (bcmt_test_set_tensor_cores)
   for (const bool tc : {false, true})
-    nseg = std::max(nseg, linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(), tc)
-                              .nseg);
+    for (const bool ragged : {false, true})
+      nseg = std::max(nseg, linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(), tc,
+                                         ragged)
+                                .nseg);
   const size_t states = nseg > 1 ? (size_t)p->B * p->H * nseg * p->dh * p->dh * 4 : 0;
   return al256(std::max<size_t>(256, npass * states));
 }
@@ -611,7 +613,7 @@ LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int
   a.decay = decay;
   a.lengths = lengths;
   *plan = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(),
-                       g_use_tc_attn);
+                       g_use_tc_attn, lengths != nullptr);
   a.nseg = plan->nseg;
   a.seg_len = plan->seg_len;
   const long long states = (long long)p->B * p->H * a.nseg * p->dh * p->dh;

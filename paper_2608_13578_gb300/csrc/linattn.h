@@ -50,7 +50,8 @@ struct LinPlan {
   bool tc;
   int nseg, seg_len;
 };
-LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms, bool allow_tc);
+LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms, bool allow_tc,
+                     bool ragged);
 
 // The recurrence on CUDA cores in fp32, any dtype and head width.
 cudaError_t linattn_simt(const Launch& lc, int dtype, const LinArgs& a);

@@ -29,6 +29,7 @@ _F32 = torch.float32
 # parameters are built once per shape, and the stream is read as a raw handle.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) \
     or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _device(t: torch.Tensor) -> torch.device:
@@ -56,7 +57,7 @@ def _on_its_device(fn):
     @functools.wraps(fn)
     def call(*args, **kwargs):
         first = args[0] if args else next(iter(kwargs.values()))
-        if first.is_cuda and first.get_device() != torch.cuda.current_device():
+        if first.is_cuda and first.get_device() != _current_device():
             with torch.cuda.device(first.device):
                 return fn(*args, **kwargs)
         return fn(*args, **kwargs)
