@@ -217,7 +217,8 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
  *   finite and not 0; B*T <= 2^30; B*H*dh <= 2^26.  flags: BCMT_FLAG_CHECK only.
  *   Arithmetic and states are fp32; with bf16 tensors the tensor-core form
  *   rounds the decayed scores and the state to bf16 where they enter a product
- *   with bf16 rows, while the running state itself keeps fp32. */
+ *   with bf16 rows.  The running state is an fp32 sum whose decayed keys carry 16
+ *   bits, in the states that a call returns 24. */
 typedef struct {
   int B, T, H, dh;
   int dtype;       /* bcmt_dtype of q, k, v, o and their gradients */
