@@ -210,7 +210,7 @@ struct TcGeo {
   static constexpr uint32_t kCols = DP == 64 ? 256 : 512;
   static constexpr uint32_t cO1 = DP == 64 ? 64 : 128, cO2 = cO1 + DP, cD = cO2 + DP;
   // at most 227 KB
-  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 4 * 32 + 8 * 13 +
+  static constexpr int kSmem = 1024 + 2 * kStage + kState + 4 * 256 + 4 * 128 + 4 * 32 + 8 * 14 +
                                (int)sizeof(Shared);
 };
 
@@ -313,11 +313,12 @@ struct View {
   __device__ __forceinline__ uint64_t* bars() const {
     return reinterpret_cast<uint64_t*>(state() + G::kState + 4 * 256 + 4 * 128 + 4 * 32);
   }
-  __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 13); }
+  __device__ __forceinline__ Shared* shared() const { return reinterpret_cast<Shared*>(bars() + 14); }
 };
 // Barriers: a stage's tiles have landed, products A and D done (two of each, for
 // alternate chunks); B, C done; P written and C, B read (rows); K' written, the
-// state's copy written and the rows past the end cleared (state).  A wait names
+// state's copy written, the rows past the end cleared and the joined state read
+// from stage 1 (state).  A wait names
 // a phase by its parity alone, so nobody may be able to complete two phases of a
 // barrier before one of its waiters has looked at the first: where one role
 // could run that far ahead of another, there are two barriers.
@@ -326,7 +327,7 @@ struct View {
   [[maybe_unused]] uint64_t *bar_full = bar, *bar_a = bar + 2, *bar_d = bar + 4,         \
                             *bar_b = bar + 6, *bar_c = bar + 7, *bar_p = bar + 8,        \
                             *bar_o = bar + 9, *bar_k = bar + 10, *bar_s = bar + 11,      \
-                            *bar_z = bar + 12;                                           \
+                            *bar_z = bar + 12, *bar_j = bar + 13;                        \
   bool ok = true; /* no wait of this thread has run out */                               \
   auto wait = [&](uint64_t* x, int parity) { ok = ok && tc::mbar_wait(x, parity & 1, status); }
 
@@ -390,34 +391,42 @@ __device__ __forceinline__ void role_products(const LinTcArgs& A, uint8_t* raw, 
   if (nch > 0) tc::mbar_wait(bar_c, (nch - 1) & 1, status);
 }
 
-// One thread: the loads.
+// Loads chunk i of a walk of head h (the sequence's first token row: tok0).
+template <int DP>
+__device__ __forceinline__ void load_chunk(const LinTcArgs& A, const View<DP>& vw, const Walk& w,
+                                           int ps, int h, int tok0, int i) {
+  using G = TcGeo<DP>;
+  uint8_t* s = vw.smem + (i & 1) * G::kStage;
+  uint64_t* full = vw.bars() + (i & 1);
+  const int row = tok0 + w.start(i);
+  tc::mbar_arrive_expect_tx(full, 3 * G::kTile);
+#pragma unroll
+  for (int f = 0; f < G::kHalves; ++f) {
+    tc::tma_load_3d(s + f * G::kHalf, &A.map[A.mq[ps]], full, f * 64, h, row);
+    tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mk[ps]], full, f * 64, h, row);
+    tc::tma_load_3d(s + 2 * G::kTile + f * G::kHalf, &A.map[A.mv[ps]], full, f * 64, h, row);
+  }
+}
+
+// One thread: the loads (the first chunk's is on its way).
 template <int DP>
 __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
-  using G = TcGeo<DP>;
   const View<DP> vw(raw);
-  uint8_t* smem = vw.smem;
   LINATTN_BARRIERS(vw);
   const Walk w(vw.shared());
   const int ps = blockIdx.y, h = ld_once(&vw.shared()->h);
   const int tok0 = ld_once(&vw.shared()->b) * A.a.T;
-  int loaded = 0;
+  int loaded = min(w.nch, 1);
   auto load = [&]() {  // the next chunk of the walk
-    const int i = loaded++;
-    uint8_t* s = smem + (i & 1) * G::kStage;
-    uint64_t* bf = &bar_full[i & 1];
-    const int row = tok0 + w.start(i);
-    tc::mbar_arrive_expect_tx(bf, 3 * G::kTile);
-#pragma unroll
-    for (int f = 0; f < G::kHalves; ++f) {
-      tc::tma_load_3d(s + f * G::kHalf, &A.map[A.mq[ps]], bf, f * 64, h, row);
-      tc::tma_load_3d(s + G::kTile + f * G::kHalf, &A.map[A.mk[ps]], bf, f * 64, h, row);
-      tc::tma_load_3d(s + 2 * G::kTile + f * G::kHalf, &A.map[A.mv[ps]], bf, f * 64, h, row);
-    }
+    load_chunk<DP>(A, vw, w, ps, h, tok0, loaded);
+    ++loaded;
   };
-  if (w.nch > 0) load();
-  if (w.nch > 1) load();
+  if (w.nch > 1) {
+    if (A.a.nseg > 1 && !A.a.joined) wait(bar_j, 0);  // the joined state is there until then
+    if (ok) load();
+  }
   // D of chunk i is its last product: its stage takes chunk i + 2
-  for (int i = 0; loaded < w.nch; ++i) {
+  for (int i = 0; ok && loaded < w.nch; ++i) {
     wait(&bar_d[i & 1], i >> 1);
     if (!ok) break;
     load();
@@ -427,25 +436,30 @@ __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, uns
     tc::mbar_wait(&bar_full[i & 1], (i >> 1) & 1, status);
 }
 
-// The outgoing state of head bh from the segments' own (threads t of nt), in fp32.
-__device__ __forceinline__ void join_out(const LinArgs& a, const LinPass& p, int bh, int n,
-                                         float lg, float dec, int t, int nt) {
+// The state coming into segment seg of head bh, from the states of the segments
+// before it, to shared memory (in their layout), and after the last segment the
+// outgoing state (threads t of nt).  All threads of the CTA share it, 8 columns of
+// a row at a time, so that a state takes one latency of L2.
+__device__ __forceinline__ void join_states(const LinArgs& a, const LinPass& p, int bh, int seg,
+                                            int n, float* to, int t, int nt) {
   const int dh = a.dh, st = dh * dh;
-  const float out_mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
-  for (int e = t; e < st / 8; e += nt) {  // 8 columns of a row
+  const float dec = a.decay[bh % a.H], lg = log2f(dec);
+  const bool last = p.s_out && seg == (p.rev ? 0 : a.nseg - 1);
+  const int before = p.rev ? a.nseg - 1 - seg : seg;
+  for (int e = t; e < st / 8; e += nt) {
     const int col = e / dh * 8, row = e - col / 8 * dh, at = col * dh + row * 4;
     float x[8];
 #pragma unroll
     for (int c = 0; c < 8; ++c) x[c] = 0.f;
     if (p.s_in) {
-      const float mul = n > 0 ? p.s_in_mul : 1.f;
-      load4(p.s_in + (long long)bh * st + row * dh + col, x);
-      load4(p.s_in + (long long)bh * st + row * dh + col + 4, x + 4);
+      const float* src = p.s_in + (long long)bh * st;
+      const float mul = n > 0 ? p.s_in_mul : 1.f;  // an empty sequence passes its state on
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[c] *= mul;
+      for (int c = 0; c < 8; ++c)
+        x[c] = mul * (p.s_in_t ? src[(col + c) * dh + row] : src[row * dh + col + c]);
     }
-#pragma unroll 2
-    for (int i = 0; i < a.nseg; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < before + (last ? 1 : 0); ++i) {  // in walk order
       const int s = p.rev ? a.nseg - 1 - i : i;
       const int m = min(max(n - s * a.seg_len, 0), a.seg_len);
       const bool fresh = p.rev && n <= s * a.seg_len + a.seg_len;  // holds the last valid token
@@ -453,20 +467,29 @@ __device__ __forceinline__ void join_out(const LinArgs& a, const LinPass& p, int
       float v[8];
       load4(src, v);
       load4(src + dh * 4, v + 4);
+      if (i == before) {
+        store4(to + at, x);
+        store4(to + at + dh * 4, x + 4);
+      }
       if (m == 0) continue;
       const float f = decay_pow(lg, m - (fresh ? 1 : 0));
 #pragma unroll
       for (int c = 0; c < 8; ++c) x[c] = fmaf(f, x[c], v[c]);
     }
+    if (last) {
+      const float mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) x[c] *= out_mul;
-    float* dst = p.s_out + (long long)bh * st + row * dh + col;
-    store4(dst, x);
-    store4(dst + 4, x + 4);
+      for (int c = 0; c < 8; ++c) x[c] *= mul;
+      float* dst = p.s_out + (long long)bh * st + row * dh + col;
+      store4(dst, x);
+      store4(dst + 4, x + 4);
+    } else {
+      store4(to + at, x);
+      store4(to + at + dh * 4, x + 4);
+    }
   }
 }
 
-// 4 NW warps, thread = row of the chunk: P, and 64 columns of the output rows.
 template <int DP>
 __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
   using G = TcGeo<DP>;
@@ -513,11 +536,6 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
       }
     }
   };
-  if (a.nseg > 1 && !a.joined && p.s_out) {  // while the last segment's first tiles are on their way
-    const Shared* sh = vw.shared();
-    if (ld_once(&sh->seg) == (rev ? 0 : a.nseg - 1))
-      join_out(a, p, ld_once(&sh->b) * a.H + h, w.n, log2f(a.decay[h]), a.decay[h], tid, 128 * NW);
-  }
   // the halves hh of blocks that the row sees
   const int h0 = rev ? 2 * q : 0, h1 = rev ? 8 : 2 * q + 2;
   for (int i = 0; i < w.nch; ++i) {
@@ -623,13 +641,12 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
   const Walk w(vw.shared());
   const float* pw = vw.pw();
   const uint32_t* pt = vw.pt();
-  const bool rev = w.rev, have0 = ld_once(&vw.shared()->have0) != 0;
+  const bool rev = w.rev;
   const LinArgs& a = A.a;
   const LinPass& p = a.pass[blockIdx.y];
   const int dh = a.dh, seg = ld_once(&vw.shared()->seg);
   const int bh = ld_once(&vw.shared()->b) * a.H + ld_once(&vw.shared()->h);
   const long long st = (long long)dh * dh;
-  const float dec = pw[1], lg = log2f(dec);
   const int tid = threadIdx.x, lane = tid & 31, r = tid & 127, q = r >> 5;
   const int t = tid - 128 * NW, g = t >> 7, c64 = g * 64;
   const bool lo_part = DP == 64 && r < 64;
@@ -640,14 +657,18 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
   const bool mine = !lo_part && srow < dh;
   const uint32_t tinc =
       ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16) + G::cD + c64;
+  // the incoming state: joined in shared memory or by a kernel of its own (in
+  // 4-column groups), or the call's
+  const bool here = a.nseg > 1 && !a.joined;
   if (mine) {
-    const bool joined = a.nseg > 1 && a.joined;
-    const float* src = joined   ? p.seg + ((long long)bh * a.nseg + seg) * st + srow * 4
-                       : p.s_in ? p.s_in + (long long)bh * st
-                                : nullptr;
-    if (src && (joined || !p.s_in_t)) {
-      src += joined ? c64 * dh : srow * dh + c64;
-      const int step = joined ? dh : 1;
+    const bool grouped = a.nseg > 1;
+    const float* src = here      ? reinterpret_cast<const float*>(smem + G::kStage) + srow * 4
+                       : grouped ? p.seg + ((long long)bh * a.nseg + seg) * st + srow * 4
+                       : p.s_in  ? p.s_in + (long long)bh * st
+                                 : nullptr;
+    if (src && (grouped || !p.s_in_t)) {
+      src += grouped ? c64 * dh : srow * dh + c64;
+      const int step = grouped ? dh : 1;
 #pragma unroll
       for (int c = 0; c < 64; c += 4)
         if (c64 + c < dh) load4(src + c * step, S + c);
@@ -656,29 +677,15 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       for (int c = 0; c < 64; ++c)
         if (c64 + c < dh) S[c] = src[(c64 + c) * dh + srow];
     }
-    if (!joined) {
-      if (p.s_in_mul != 1.f && w.n > 0) {  // an empty sequence passes its state on as it is
+    // an empty sequence passes its state on as it is
+    if (!grouped && p.s_in_mul != 1.f && w.n > 0) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) S[c] *= p.s_in_mul;
-      }
-      // the segments before this one, in walk order
-#pragma unroll 1
-      for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1) {
-        const int ms = min(max(w.n - s * a.seg_len, 0), a.seg_len);
-        if (ms == 0) continue;
-        const bool fresh = rev && w.n <= s * a.seg_len + a.seg_len;
-        const float f = decay_pow(lg, ms - (fresh ? 1 : 0));
-        const float* x = p.seg + ((long long)bh * a.nseg + s) * st + c64 * dh + srow * 4;
-#pragma unroll
-        for (int c = 0; c < 64; c += 4)
-          if (c64 + c < dh) {
-            float v[4];
-            load4(x + c * dh, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[c + e] = fmaf(f, S[c + e], v[e]);
-          }
-      }
+      for (int c = 0; c < 64; ++c) S[c] *= p.s_in_mul;
     }
+  }
+  if (here) {  // the stage may be loaded
+    tc::fence_proxy_async_smem();
+    warp_arrive(bar_j, lane);
   }
   float f = 0.f;
   for (int i = 0;; ++i) {
@@ -1001,7 +1008,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     uint64_t* bar = vw.bars();
     if (tid == 0) {
       for (int i = 0; i < 8; ++i) tc::mbar_init(&bar[i], 1);
-      for (int i = 8; i < 13; ++i) tc::mbar_init(&bar[i], 4 * NW);
+      for (int i = 8; i < 14; ++i) tc::mbar_init(&bar[i], 4 * NW);
       tc::fence_mbar_init();
     }
     const int ps = blockIdx.y;
@@ -1014,6 +1021,10 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     const LinArgs& a = A.a;
     const int seg = blockIdx.x % a.nseg, bh = blockIdx.x / a.nseg, b = bh / a.H, h = bh - b * a.H;
     const bool rev = a.pass[ps].rev != 0;
+    if (tid == 0) {
+      const Walk w(a, b, seg, rev);
+      if (w.nch > 0) load_chunk<DP>(A, vw, w, ps, h, b * a.T, 0);
+    }
     if (tid == 32) {
       Shared* sh = vw.shared();
       sh->b = b;
@@ -1036,6 +1047,9 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
         if (d < 32) vw.cw()[rev ? d : 31 - d] = d == 1 ? a.decay[h] : x;
       }
     }
+    if (a.nseg > 1 && !a.joined)
+      join_states(a, a.pass[ps], bh, seg, a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T,
+                  reinterpret_cast<float*>(vw.smem + G::kStage), tid, R::kThreads);
   }
   tc::fence_before_sync();
   __syncthreads();
