@@ -458,23 +458,32 @@ __device__ __forceinline__ void join_states(const LinArgs& a, const LinPass& p, 
       for (int c = 0; c < 8; ++c)
         x[c] = mul * (p.s_in_t ? src[(col + c) * dh + row] : src[row * dh + col + c]);
     }
-#pragma unroll 4
-    for (int i = 0; i < before + (last ? 1 : 0); ++i) {  // in walk order
-      const int s = p.rev ? a.nseg - 1 - i : i;
-      const int m = min(max(n - s * a.seg_len, 0), a.seg_len);
-      const bool fresh = p.rev && n <= s * a.seg_len + a.seg_len;  // holds the last valid token
-      const float* src = p.seg + ((long long)bh * a.nseg + s) * st + at;
-      float v[8];
-      load4(src, v);
-      load4(src + dh * 4, v + 4);
-      if (i == before) {
-        store4(to + at, x);
-        store4(to + at + dh * 4, x + 4);
-      }
-      if (m == 0) continue;
-      const float f = decay_pow(lg, m - (fresh ? 1 : 0));
+    const int count = before + (last ? 1 : 0);
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += 4) {  // in walk order, four segments' loads in flight
+      float v[4][8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[c] = fmaf(f, x[c], v[c]);
+      for (int u = 0; u < 4; ++u) {
+        const int i = min(i0 + u, count - 1), s = p.rev ? a.nseg - 1 - i : i;
+        const float* src = p.seg + ((long long)bh * a.nseg + s) * st + at;
+        load4(src, v[u]);
+        load4(src + dh * 4, v[u] + 4);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u, s = p.rev ? a.nseg - 1 - i : i;
+        if (i >= count) break;
+        if (i == before) {
+          store4(to + at, x);
+          store4(to + at + dh * 4, x + 4);
+        }
+        const int m = min(max(n - s * a.seg_len, 0), a.seg_len);
+        if (m == 0) continue;
+        const bool fresh = p.rev && n <= s * a.seg_len + a.seg_len;  // holds the last valid token
+        const float f = decay_pow(lg, m - (fresh ? 1 : 0));
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[c] = fmaf(f, x[c], v[u][c]);
+      }
     }
     if (last) {
       const float mul = n > 0 ? p.s_out_mul * (p.rev ? dec : 1.f) : 1.f;
