@@ -421,15 +421,15 @@ LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms,
   if (pl.tc) {
     // segments of whole chunks, enough for one CTA in every slot (two per SM up
     // to width 64): the walk is sequential, and a slot left empty is lost.  8 x 1024
-    // tokens of 8 heads of 64 take 25 us so, 31 in one segment, 36 in two or in twice
-    // as many; where a call has one head a slot or so, one segment needs no states
-    // (backward of 4 x 4095, 8 heads of 128: 111 us, 144 in two)
+    // tokens of 8 heads of 64 take 23 us so, 30 in one segment or in twice as many, 32
+    // in two; where a call has one head a slot or so, one segment needs no states
+    // (backward of 4 x 4095, 8 heads of 128: 107 us, 147 in two)
     const long long slots = (long long)sms * (dh <= 64 ? 2 : 1);
     const int chunks = (T + 127) / 128;
     long long n = std::max(1ll, std::min<long long>(slots / heads, chunks));
     // sequences of different lengths: three times as many, of four chunks at least, so
     // that slots whose segment is empty or short take another (4 sequences of up to
-    // 16384 tokens, 8 heads of 128: 164 us for 184; were all of them full, 203 for 190)
+    // 16384 tokens, 8 heads of 128: 159 us for 182; were all of them full, 214 for 188)
     if (ragged && n > 1) n = std::max(n, std::min<long long>(3 * n, chunks / 4));
     const int per = (int)((chunks + n - 1) / n);
     pl.nseg = (chunks + per - 1) / per;

@@ -30,11 +30,11 @@
 // the call returns have K' in three terms, by CTAs of their own (state_cta).
 //
 // What bounds it: at width 128 shared memory, whose bandwidth the operands of the
-// products, the copies of P's, K's and S's making and the loads use to about 70%
-// (3.4 us a chunk, of which 1.0 is loads and products); at width 64 the chain D ->
+// products, the making of P, K' and S's copy and the loads use to about 70%
+// (3.3 us a chunk, of which 1.0 is loads and products); at width 64 the chain D ->
 // S -> B of latencies.  4 sequences of 4095 tokens, 8 heads of 128, backward:
-// 111 us, 193 TFLOP/s of the recurrence's own operations; 8 x 1024 tokens of 8
-// heads of 64, forward: 25 us.
+// 107 us, 200 TFLOP/s of the recurrence's own operations; 8 x 1024 tokens of 8
+// heads of 64, forward: 23 us.
 #include <algorithm>
 
 #include "attn_common.cuh"
@@ -409,7 +409,7 @@ __device__ __forceinline__ void load_chunk(const LinTcArgs& A, const View<DP>& v
 }
 
 // One thread: the loads (the first chunk's is on its way).
-template <int DP>
+template <int DP, bool kSegs>
 __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
   const View<DP> vw(raw);
   LINATTN_BARRIERS(vw);
@@ -422,7 +422,7 @@ __device__ __forceinline__ void role_loads(const LinTcArgs& A, uint8_t* raw, uns
     ++loaded;
   };
   if (w.nch > 1) {
-    if (A.a.nseg > 1 && !A.a.joined) wait(bar_j, 0);  // the joined state is there until then
+    if (kSegs && !A.a.joined) wait(bar_j, 0);  // the joined state is there until then
     if (ok) load();
   }
   // D of chunk i is its last product: its stage takes chunk i + 2
@@ -640,7 +640,7 @@ __device__ __forceinline__ void role_rows(const LinTcArgs& A, uint8_t* raw, unsi
 
 // 4 NW warps, thread = 64 columns of a row of the state; at DP = 64 the lower 64
 // threads keep the sums of the keys' second terms.
-template <int DP>
+template <int DP, bool kSegs>
 __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, unsigned* status) {
   using G = TcGeo<DP>;
   constexpr int NW = Roles<DP>::NW;
@@ -668,9 +668,9 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
       ld_once(&vw.shared()->tmem) + ((uint32_t)(q * 32) << 16) + G::cD + c64;
   // the incoming state: joined in shared memory or by a kernel of its own (in
   // 4-column groups), or the call's
-  const bool here = a.nseg > 1 && !a.joined;
+  const bool here = kSegs && !a.joined;
   if (mine) {
-    const bool grouped = a.nseg > 1;
+    constexpr bool grouped = kSegs;
     const float* src = here      ? reinterpret_cast<const float*>(smem + G::kStage) + srow * 4
                        : grouped ? p.seg + ((long long)bh * a.nseg + seg) * st + srow * 4
                        : p.s_in  ? p.s_in + (long long)bh * st
@@ -1000,14 +1000,17 @@ __global__ void __launch_bounds__(4 * DP + 32, DP == 64 ? 2 : 1)
   state_cta<DP>(A, ps, bh, seg, smem_raw, status);
 }
 
-template <int DP>
+// kSegs: the heads are cut into segments (their join), or not (the outgoing state's
+// CTAs).  A kernel each keeps their code short: as one, the backward of 4 x 4095 tokens
+// of 8 heads of 128 took 115 us for 107.
+template <int DP, bool kSegs>
 __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
     linattn_tc_kernel(const __grid_constant__ LinTcArgs A, unsigned* status) {
   using G = TcGeo<DP>;
   using R = Roles<DP>;
   constexpr int NW = R::NW;
   extern __shared__ uint8_t smem_raw[];
-  if (blockIdx.y == A.a.npass) {  // the outgoing state, beside the walks
+  if (!kSegs && blockIdx.y == A.a.npass) {  // the outgoing state, beside the walks
     state_cta<DP>(A, A.out, blockIdx.x, 0, smem_raw, status);
     return;
   }
@@ -1056,7 +1059,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
         if (d < 32) vw.cw()[rev ? d : 31 - d] = d == 1 ? a.decay[h] : x;
       }
     }
-    if (a.nseg > 1 && !a.joined)
+    if (kSegs && !a.joined)
       join_states(a, a.pass[ps], bh, seg, a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T,
                   reinterpret_cast<float*>(vw.smem + G::kStage), tid, R::kThreads);
   }
@@ -1066,14 +1069,14 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
   if (warp >= 8 * NW) {
     reg_dec<R::kRegIssue>();
     if (tid == 256 * NW) role_products<DP>(A, smem_raw, status);
-    if (tid == 256 * NW + 32) role_loads<DP>(A, smem_raw, status);
+    if (tid == 256 * NW + 32) role_loads<DP, kSegs>(A, smem_raw, status);
     __syncwarp();
   } else if (warp < 4 * NW) {
     reg_dec<R::kRegRows>();
     role_rows<DP>(A, smem_raw, status);
   } else {
     reg_inc<R::kRegState>();
-    role_state<DP>(A, smem_raw, status);
+    role_state<DP, kSegs>(A, smem_raw, status);
   }
   tc::fence_before_sync();
   __syncthreads();
@@ -1086,8 +1089,9 @@ namespace {
 template <int DP>
 cudaError_t tc_launch(const Launch& lc, const LinTcArgs& A) {
   using G = TcGeo<DP>;
-  static std::atomic<unsigned long long> opted{0}, opted_state{0};
-  cudaError_t e = smem_opt_in(linattn_tc_kernel<DP>, G::kSmem, &opted);
+  static std::atomic<unsigned long long> opted{0}, opted_segs{0}, opted_state{0};
+  cudaError_t e = smem_opt_in(linattn_tc_kernel<DP, false>, G::kSmem, &opted);
+  if (e == cudaSuccess) e = smem_opt_in(linattn_tc_kernel<DP, true>, G::kSmem, &opted_segs);
   if (e != cudaSuccess) return e;
   const unsigned heads = (unsigned)A.a.B * A.a.H;
   if ((e = smem_opt_in(linattn_state_kernel<DP>, G::kSmem, &opted_state)) != cudaSuccess) return e;
@@ -1105,7 +1109,7 @@ cudaError_t tc_launch(const Launch& lc, const LinTcArgs& A) {
   bool after = false;
   for (int i = 0; whole && i < A.a.npass; ++i)
     after = after || A.a.pass[i].s_in == A.a.pass[A.out].s_out;
-  e = launch_k(linattn_tc_kernel<DP>,
+  e = launch_k(A.a.nseg > 1 ? linattn_tc_kernel<DP, true> : linattn_tc_kernel<DP, false>,
                dim3(heads * A.a.nseg, A.a.npass + (whole && !after ? 1 : 0)),
                dim3(Roles<DP>::kThreads), G::kSmem, lc.stream, A, lc.status);
   if (e != cudaSuccess) return e;
