@@ -29,10 +29,10 @@
 // mean square).  S itself is a sum of up to T terms, in fp32 throughout.  States that
 // the call returns have K' in three terms, by CTAs of their own (state_cta).
 //
-// What bounds it: at width 128 shared memory, whose bandwidth the operands of the
-// products, the making of P, K' and S's copy and the loads use to about 70%
-// (3.3 us a chunk, of which 1.0 is loads and products); at width 64 the chain D ->
-// S -> B of latencies.  4 sequences of 4095 tokens, 8 heads of 128, backward:
+// What bounds it: at width 128 most of all shared memory (a chunk's loads, products'
+// operands, K' and S's copy are 512 KB, 2.1 us at 128 bytes a cycle, of the 3.3 us
+// that it takes; the tensor cores are busy for 28%); at width 64 the chain D -> S ->
+// B of latencies.  4 sequences of 4095 tokens, 8 heads of 128, backward:
 // 107 us, 200 TFLOP/s of the recurrence's own operations; 8 x 1024 tokens of 8
 // heads of 64, forward: 23 us.
 #include <algorithm>
@@ -793,8 +793,8 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
 // A segment's state is stored with the 4-column groups of all rows together: the
 // threads of a warp hold a row each, and their accesses are consecutive (row-major
 // states made the joins of 8 x 1024 tokens of 8 heads of 64 take 4 us more).
-// Bound by shared memory (K read once, three terms written, six operands read): at
-// DP = 128 a chunk takes 2.2 us, of which 1.6 are that.
+// Bound by shared memory (K read once, three terms written, six operands read, by
+// count of bytes 1.6 us a chunk at DP = 128) and the making of the terms: 2.2 us.
 // The first 4 DP threads hold the state (32 columns of a row each), the warp after
 // them issues.
 template <int DP>
