@@ -18,6 +18,7 @@ import math
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import bcmt as C
 
@@ -140,10 +141,12 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
     in place), decay [H] fp32, lengths [B] int32 (tokens per sequence, default
     T), state [B, H, dh, dh] fp32 (default zero).  scale defaults to
     1/sqrt(dh).  state_out: where the last state goes (default a new tensor; may
-    be ``state``).  Tokens past a sequence's length give zero rows."""
+    be ``state``); autograd sees it as modified in place.  Tokens past a sequence's
+    length give zero rows."""
     dev, dt, decay, lengths, state = _linattn_check(q, k, v, decay, lengths, state)
     shape = q.shape
     B, T, H, dh = shape
+    given = state_out
     if state_out is None:
         state_out = torch.empty((B, H, dh, dh), dtype=_F32, device=dev)
     elif state_out is not state:
@@ -157,6 +160,8 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
     C.check(C.LIB.bcmt_linattn_forward(
         p, pq, lq, pk, lk, pv, lv, decay.data_ptr(), _address(lengths), _address(state),
         o.data_ptr(), H * dh, state_out.data_ptr(), _address(ws), _raw_stream(dev.index)))
+    if given is not None:   # written through its address, which autograd cannot see
+        increment_version(given)
     return o, state_out
 
 
@@ -194,7 +199,9 @@ def linear_attention_step(q, k, v, decay, state, scale: Optional[float] = None, 
                           state_out=None):
     """One token of each sequence: q, k, v [B, 1, H, dh]; updates ``state`` (in
     place unless state_out is given) and returns o [B, 1, H, dh].  active [B]
-    int32: sequences with 0 keep their state and get a zero row."""
+    int32: sequences with 0 keep their state and get a zero row.  A state that a
+    differentiable call read cannot be updated in place before that call's
+    backward (which then raises): pass a copy or a state_out."""
     if q.dim() != 4 or q.shape[1] != 1 or state is None:
         raise ValueError(f"q must be [B, 1, H, dh], not {tuple(q.shape)}, and state a tensor")
     return linear_attention_forward(q, k, v, decay, scale, active, state,
