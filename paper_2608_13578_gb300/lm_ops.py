@@ -4,7 +4,8 @@ dropout.
 
 Marshalling only: each call runs the library's kernels (``include/bcmt.h``) on
 the current CUDA stream.  ``linear_attention``, ``embedding`` and ``dropout``
-are differentiable; the ``*_forward`` / ``*_backward`` / ``*_step`` functions
+are differentiable (the last two, which are linear, any number of times; a second
+derivative of linear attention raises); the ``*_forward`` / ``*_backward`` / ``*_step`` functions
 are the bare calls.  Arguments that the library would misread (devices, types,
 shapes, layouts) raise ``ValueError``; what the library refuses raises
 ``bcmt.BCMTError``.
@@ -18,6 +19,7 @@ import math
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
 from . import bcmt as C
@@ -220,6 +222,7 @@ class LinearAttention(torch.autograd.Function):
         return o, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dlast):
         q, k, v, decay, lengths, state = ctx.saved_tensors
         if do is None and dlast is None:
@@ -299,7 +302,24 @@ class Embedding(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         ids, = ctx.saved_tensors
-        return None, embedding_backward(ids, dout, ctx.V, ctx.scale), None
+        # with a graph of its own where one is wanted (create_graph)
+        grad = EmbeddingGrad.apply if torch.is_grad_enabled() else embedding_backward
+        return None, grad(ids, dout, ctx.V, ctx.scale), None
+
+
+class EmbeddingGrad(torch.autograd.Function):
+    """The table's gradient as a function of dout; its own gradient is the lookup."""
+
+    @staticmethod
+    def forward(ctx, ids, dout, V, scale):
+        ctx.save_for_backward(ids)
+        ctx.scale = scale
+        return embedding_backward(ids, dout, V, scale)
+
+    @staticmethod
+    def backward(ctx, ddw):
+        ids, = ctx.saved_tensors
+        return None, embedding(ids, ddw, ctx.scale), None, None
 
 
 def embedding(ids, weight, scale: float = 1.0):
@@ -352,7 +372,11 @@ class Dropout(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        dx = dropout_backward(dy, *ctx.args, step=ctx.step) if ctx.needs_input_grad[0] else None
+        dx = None
+        if ctx.needs_input_grad[0]:
+            # with a graph of its own where one is wanted (create_graph): the same mask
+            dx = dropout(dy, *ctx.args, step=ctx.step) if torch.is_grad_enabled() \
+                else dropout_backward(dy, *ctx.args, step=ctx.step)
         return dx, None, None, None, dy if ctx.needs_input_grad[4] else None, None
 
 

@@ -49,3 +49,32 @@ def test_a_state_of_its_own_may_be_written(F):
         F.linear_attention_step(d["q"], d["k"], d["v"], d["decay"], s)
         assert torch.equal(s, own)
     F.linear_attention_step(d["q"], d["k"], d["v"], d["decay"], s)   # made there, used here
+
+
+# ---------------------------------------------------- derivatives of derivatives
+def test_penalties_on_gradients(F):
+    """Embedding and dropout are linear: a penalty on their gradients reaches the
+    leaves, as through torch's own operations in float64.  Tolerance: four passes
+    through fp32 arithmetic with sums of up to 40 terms each."""
+    ids = torch.randint(0, 9, (4, 10), generator=torch.Generator().manual_seed(5)).cuda()
+    target = torch.randn(4, 10, 16, device="cuda")
+    w0 = torch.randn(9, 16, device="cuda")
+    keep = F.dropout_forward(torch.ones_like(target), 0.25, 3, 8) != 0
+    grads = []
+    for fn, dt in ((lambda w: F.dropout(F.embedding(ids, w, 1.5), 0.25, 3, 8), torch.float32),
+                   (lambda w: w[ids] * 1.5 * keep / 0.75, torch.float64)):
+        w = w0.detach().clone().to(dt).requires_grad_()
+        loss = ((fn(w) - target.to(dt)) ** 2).sum()
+        g, = torch.autograd.grad(loss, w, create_graph=True)
+        (loss + (g ** 2).sum()).backward()
+        grads.append(w.grad.double())
+    assert (grads[0] - grads[1]).abs().max() <= 4 * 48 * 2.0 ** -24 * grads[1].abs().max()
+
+
+def test_second_derivative_of_linear_attention_raises(F):
+    d, _ = make(1, 40, 2, 64, "fp32", 33)
+    q = d["q"].clone().requires_grad_()
+    o, _ = F.linear_attention(q, d["k"], d["v"], d["decay"])
+    g, = torch.autograd.grad((o ** 2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        ((o ** 2).sum() + (g ** 2).sum()).backward()
