@@ -59,7 +59,10 @@ def _on_its_device(fn):
     """Runs fn with its first tensor's device current (a switch only where it is not)."""
     @functools.wraps(fn)
     def call(*args, **kwargs):
-        first = args[0] if args else next(iter(kwargs.values()))
+        first = args[0] if args else next(
+            (t for t in kwargs.values() if isinstance(t, torch.Tensor)), None)
+        if not isinstance(first, torch.Tensor):
+            raise ValueError(f"a tensor is needed, not {type(first).__name__}")
         if first.is_cuda and first.get_device() != _current_device():
             with torch.cuda.device(first.device):
                 return fn(*args, **kwargs)

@@ -1,0 +1,34 @@
+"""Arguments of the torch-facing language-model operators in every form that Python
+takes (CPU only: the checks of the arguments come before any kernel)."""
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def F():
+    from paper_2608_13578_gb300 import build
+    build.build()
+    from paper_2608_13578_gb300 import lm_ops
+    return lm_ops
+
+
+def test_keywords_in_any_order(F):
+    """The device is that of the first tensor, whichever argument comes first."""
+    q, a = torch.zeros(1, 2, 2, 8), torch.zeros(2)
+    ids, w = torch.zeros(3, dtype=torch.int64), torch.zeros(5, 8)
+    for call in (lambda: F.linear_attention_forward(scale=0.2, q=q, k=q, v=q, decay=a),
+                 lambda: F.linear_attention_forward(lengths=None, state=None, q=q, k=q, v=q, decay=a),
+                 lambda: F.linear_attention_backward(need_dstate=False, do=q, q=q, k=q, v=q, decay=a),
+                 lambda: F.embedding_forward(scale=2.0, ids=ids, weight=w),
+                 lambda: F.embedding_backward(V=5, ids=ids, dout=torch.zeros(3, 8))):
+        with pytest.raises(ValueError, match="CUDA"):
+            call()
+
+
+def test_what_is_no_tensor(F):
+    for call in (lambda: F.embedding_forward([1, 2], torch.zeros(5, 8)),
+                 lambda: F.dropout_forward(1.0, 0.1, 1, 2),
+                 lambda: F.linear_attention_forward(None, None, None, None)):
+        with pytest.raises(ValueError, match="tensor"):
+            call()
