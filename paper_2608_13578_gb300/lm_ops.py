@@ -78,6 +78,16 @@ def _dense(t):
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
+def _number(x, name: str) -> Optional[float]:
+    """x as a Python float (None stays None): the plans are kept by value, and what a
+    call reads from a tensor or array must not change with it later."""
+    if type(x) is float or x is None:
+        return x
+    if isinstance(x, torch.Tensor) and x.requires_grad:
+        raise ValueError(f"{name} is a constant here: it gets no gradient")
+    return float(x)
+
+
 def _buffer(nbytes: int, device) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
@@ -158,7 +168,7 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
         _check(state_out, "state_out", (B, H, dh, dh), _F32, dev)
         if not state_out.is_contiguous():
             raise ValueError("state_out must be dense")
-    p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, False)
+    p, nbytes = _linattn_plan(B, T, H, dh, dt, _number(scale, "scale"), False)
     (q, pq, lq), (k, pk, lk), (v, pv, lv) = _rows(q, shape), _rows(k, shape), _rows(v, shape)
     o = torch.empty(shape, dtype=q.dtype, device=dev)
     ws = _buffer(nbytes, dev) if nbytes else None
@@ -187,7 +197,7 @@ def linear_attention_backward(do, q, k, v, decay, scale: Optional[float] = None,
     if dstate is not None:
         _check(dstate, "dstate", (B, H, dh, dh), _F32, dev)
         dstate = _dense(dstate)
-    p, nbytes = _linattn_plan(B, T, H, dh, dt, scale, True)
+    p, nbytes = _linattn_plan(B, T, H, dh, dt, _number(scale, "scale"), True)
     (do, pd, ldo), (q, pq, lq) = _rows(do, shape), _rows(q, shape)
     (k, pk, lk), (v, pv, lv) = _rows(k, shape), _rows(v, shape)
     dq, dk, dv = (torch.empty(shape, dtype=q.dtype, device=dev) for _ in range(3))
@@ -240,7 +250,7 @@ class LinearAttention(torch.autograd.Function):
 
 def linear_attention(q, k, v, decay, scale: Optional[float] = None, lengths=None, state=None):
     """Differentiable ``linear_attention_forward``: (o, last state)."""
-    return LinearAttention.apply(q, k, v, decay, scale, lengths, state)
+    return LinearAttention.apply(q, k, v, decay, _number(scale, "scale"), lengths, state)
 
 
 # ------------------------------------------------------------------- embedding
@@ -268,7 +278,8 @@ def embedding_forward(ids, weight, scale: float = 1.0):
         raise ValueError(f"weight must be [V, D], not {tuple(weight.shape)}")
     ids = _ids(ids, dev)
     V, D = weight.shape
-    p, _ = _embedding_plan(ids.numel(), V, D, _dtype(weight, "weight"), ids.element_size(), scale)
+    p, _ = _embedding_plan(ids.numel(), V, D, _dtype(weight, "weight"), ids.element_size(),
+                           _number(scale, "scale"))
     out = torch.empty((*ids.shape, D), dtype=weight.dtype, device=dev)
     weight = _dense(weight)
     C.check(C.LIB.bcmt_embedding_forward(p, ids.data_ptr(), weight.data_ptr(), out.data_ptr(),
@@ -284,7 +295,8 @@ def embedding_backward(ids, dout, V: int, scale: float = 1.0):
         raise ValueError(f"dout must be [*ids.shape, D], not {tuple(dout.shape)}")
     ids = _ids(ids, dev)
     D = dout.shape[-1]
-    p, nbytes = _embedding_plan(ids.numel(), V, D, _dtype(dout, "dout"), ids.element_size(), scale)
+    p, nbytes = _embedding_plan(ids.numel(), V, D, _dtype(dout, "dout"), ids.element_size(),
+                                _number(scale, "scale"))
     dw = torch.empty((V, D), dtype=dout.dtype, device=dev)
     ws = _buffer(nbytes, dev)
     dout = _dense(dout)
@@ -327,7 +339,7 @@ class EmbeddingGrad(torch.autograd.Function):
 
 def embedding(ids, weight, scale: float = 1.0):
     """Differentiable ``embedding_forward``."""
-    return Embedding.apply(ids, weight, scale)
+    return Embedding.apply(ids, weight, _number(scale, "scale"))
 
 
 # --------------------------------------------------------------------- dropout
@@ -345,7 +357,8 @@ def _dropout_call(x, p, seed, offset, residual, step):
     x = _dense(x)
     y = torch.empty(x.shape, dtype=x.dtype, device=dev)
     mask = (1 << 64) - 1
-    prm = C.bcmt_dropout_params(x.numel(), dt, 0, p, seed & mask, offset & mask, step)
+    prm = C.bcmt_dropout_params(x.numel(), dt, 0, _number(p, "p"), int(seed) & mask,
+                                 int(offset) & mask, step)
     C.check(C.LIB.bcmt_dropout(ctypes.byref(prm), x.data_ptr(), _address(residual), y.data_ptr(),
                                _raw_stream(dev.index)))
     return y
@@ -385,4 +398,4 @@ class Dropout(torch.autograd.Function):
 
 def dropout(x, p: float, seed: int, offset: int, residual=None, step=None):
     """Differentiable ``dropout_forward``."""
-    return Dropout.apply(x, p, seed, offset, residual, step)
+    return Dropout.apply(x, _number(p, "p"), int(seed), int(offset), residual, step)

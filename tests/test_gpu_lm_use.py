@@ -78,3 +78,46 @@ def test_second_derivative_of_linear_attention_raises(F):
     g, = torch.autograd.grad((o ** 2).sum(), q, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         ((o ** 2).sum() + (g ** 2).sum()).backward()
+
+
+# ------------------------------------------------- numbers given as tensors
+def test_a_number_held_by_a_tensor_is_read_at_each_call(F):
+    """scale and p may be one-element tensors or arrays: each call takes the value of
+    then, and a backward that of its forward."""
+    d, _ = make(1, 40, 2, 64, "fp32", 34)
+    scale = torch.tensor(0.25)
+    ids, w = torch.arange(4, device="cuda"), torch.randn(4, 16, device="cuda")
+    for value in (0.25, 0.5):
+        scale.fill_(value)
+        args = (d["q"], d["k"], d["v"], d["decay"])
+        assert torch.equal(F.linear_attention_forward(*args, scale)[0],
+                           F.linear_attention_forward(*args, value)[0])
+        assert torch.equal(F.linear_attention_backward(d["do"], *args, scale)[2],
+                           F.linear_attention_backward(d["do"], *args, value)[2])
+        assert torch.equal(F.embedding_forward(ids, w, scale), F.embedding_forward(ids, w, value))
+        assert torch.equal(F.embedding_backward(ids, w, 4, scale),
+                           F.embedding_backward(ids, w, 4, value))
+        assert torch.equal(F.dropout_forward(w, scale, 1, 2), F.dropout_forward(w, value, 1, 2))
+
+
+@pytest.mark.parametrize("op", ["linear_attention", "embedding", "dropout"])
+def test_a_backward_takes_the_number_of_its_forward(F, op):
+    d, _ = make(1, 40, 2, 64, "fp32", 35)
+    ids = torch.arange(4, device="cuda")
+    w0 = torch.randn(4, 16, device="cuda")
+
+    def grad(number, after=None):
+        x = (d["q"] if op == "linear_attention" else w0).detach().clone().requires_grad_()
+        if op == "linear_attention":
+            y = F.linear_attention(x, d["k"], d["v"], d["decay"], number)[0]
+        elif op == "embedding":
+            y = F.embedding(ids, x, number)
+        else:
+            y = F.dropout(x, number, 1, 2)
+        if after is not None:
+            number.fill_(after)
+        y.sum().backward()
+        return x.grad
+    assert torch.equal(grad(torch.tensor(0.25), 0.5), grad(0.25))
+    with pytest.raises(ValueError, match="gradient"):
+        grad(torch.tensor(0.25, requires_grad=True))
