@@ -151,8 +151,8 @@ class GPT(nn.Module):
         self.blocks = nn.ModuleList(Block(c) for _ in range(c.layers))
         self.ln_f = nn.LayerNorm(c.D)
         self.head = nn.Linear(c.D, c.vocab, bias=False)
-        # training steps done: part of the dropout's counter, on the device so that
-        # a captured step draws new masks at each replay
+        # calls that drew masks so far: part of the dropout's counter, on the device so
+        # that a captured call draws new masks at each replay
         self.register_buffer("drop_step", torch.zeros(1, dtype=torch.int64), persistent=False)
 
     def embed(self, ids):
@@ -160,17 +160,23 @@ class GPT(nn.Module):
             return lm_ops.embedding(ids, self.tok.weight, self.c.embed_scale)
         return self.tok(ids)
 
-    def _drop(self, x, residual, site: int):
+    def _masks(self):
+        """The dropout of one call of the model: drop(x, residual, site).  Every call has
+        masks of its own; a site's mask can be drawn again (a block run anew for its
+        backward), since the call keeps its own copy of the counter."""
+        step = self.drop_step.clone()
+        self.drop_step += 1
         # places are 2^40 steps apart in the counter's upper half
-        return lm_ops.dropout(x, self.c.dropout, self.c.dropout_seed, site << 40,
-                              residual=residual, step=self.drop_step)
+        return lambda x, residual, site: lm_ops.dropout(
+            x, self.c.dropout, self.c.dropout_seed, site << 40, residual=residual, step=step)
 
     def forward(self, ids):
         x = self.embed(ids) + self.pos[: ids.shape[1]]
         if self.training and self.c.dropout > 0:
-            x = self._drop(x, None, 0)
+            drop = self._masks()
+            x = drop(x, None, 0)
             for i, blk in enumerate(self.blocks):
-                x = blk(x, lambda y, res, s, i=i: self._drop(y, res, 1 + 2 * i + s))
+                x = blk(x, lambda y, res, s, i=i: drop(y, res, 1 + 2 * i + s))
         else:
             for blk in self.blocks:
                 x = blk(x)
@@ -209,8 +215,6 @@ def train_step(model: GPT, opt, ids, targets):
     loss.backward()
     opt.step()
     opt.zero_grad(set_to_none=True)
-    if model.c.dropout > 0:
-        model.drop_step += 1
     if model.c.mixer == "bcmt" and model.c.learn_decay:
         with torch.no_grad():
             for blk in model.blocks:
