@@ -152,8 +152,20 @@ class GPT(nn.Module):
         self.ln_f = nn.LayerNorm(c.D)
         self.head = nn.Linear(c.D, c.vocab, bias=False)
         # calls that drew masks so far: part of the dropout's counter, on the device so
-        # that a captured call draws new masks at each replay
-        self.register_buffer("drop_step", torch.zeros(1, dtype=torch.int64), persistent=False)
+        # that a captured call draws new masks at each replay.  Saved where it is used, so
+        # that a resumed run goes on with new masks
+        self.register_buffer("drop_step", torch.zeros(1, dtype=torch.int64),
+                             persistent=c.dropout > 0)
+
+    def _load_from_state_dict(self, state_dict, prefix, *args):
+        # weights are shared between models with and without dropout, and with files
+        # that hold no counter
+        key, own = prefix + "drop_step", dict(state_dict)
+        if self.c.dropout > 0:
+            own.setdefault(key, self.drop_step)
+        else:
+            own.pop(key, None)
+        super()._load_from_state_dict(own, prefix, *args)
 
     def embed(self, ids):
         if self.c.embed_scale > 0:

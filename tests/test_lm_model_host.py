@@ -74,3 +74,38 @@ def test_a_block_run_anew_draws_the_same_masks(drawn):
         model(ids_of()).square().sum().backward()
         grads.append(torch.cat([p.grad.reshape(-1) for p in model.parameters()]))
     assert len(drawn) > 10 and torch.equal(grads[0], grads[1])
+
+
+# -------------------------------------------------------------- saved models
+def test_a_resumed_run_goes_on_with_new_masks(drawn):
+    model = model_of()
+    model(ids_of()), model(ids_of())
+    saved = {k: v.clone() for k, v in model.state_dict().items()}
+    resumed = model_of(dropout=0.25)
+    resumed.load_state_dict(saved)
+    assert torch.equal(resumed(ids_of()), model(ids_of()))
+    assert [s for _, s in drawn] == [0] * 5 + [1] * 5 + [2] * 10
+
+
+@pytest.mark.parametrize("to", [0.0, 0.25])
+@pytest.mark.parametrize("frm", [0.0, 0.25])
+def test_weights_go_between_models_with_and_without_dropout(drawn, frm, to):
+    a, b = model_of(dropout=frm), model_of(dropout=to)
+    a(ids_of())
+    missing, unexpected = b.load_state_dict(a.state_dict())
+    assert not missing and not unexpected
+    assert int(b.drop_step) == (1 if frm and to else 0)
+    plain = set(model_of(dropout=0.0).state_dict())
+    assert "drop_step" not in plain        # files of models without dropout are as they were
+    with pytest.raises(RuntimeError):      # other names are still looked at
+        b.load_state_dict({**a.state_dict(), "other": torch.zeros(1)})
+    with pytest.raises(RuntimeError):
+        b.load_state_dict({k: v for k, v in a.state_dict().items() if k != "pos"})
+
+
+def test_counters_without_an_entry_stay(drawn):
+    """A file from before the counter was saved loads, and leaves the counter as it is."""
+    model = model_of()
+    model(ids_of())
+    model.load_state_dict({k: v for k, v in model.state_dict().items() if k != "drop_step"})
+    assert int(model.drop_step) == 1
