@@ -136,8 +136,11 @@ class Block(nn.Module):
     def mlp(self, x):
         return self.fc2(F.gelu(self.fc1(self.ln2(x))))
 
-    def recurrent(self, x, state, lengths=None):
+    def recurrent(self, x, state, lengths=None, drop=None):
         m, state = self.mix.recurrent(self.ln1(x), state, lengths)
+        if drop is not None:
+            x = drop(m, x, 0)
+            return drop(self.mlp(x), x, 1), state
         x = x + m
         return x + self.mlp(x), state
 
@@ -182,30 +185,33 @@ class GPT(nn.Module):
         return lambda x, residual, site: lm_ops.dropout(
             x, self.c.dropout, self.c.dropout_seed, site << 40, residual=residual, step=step)
 
+    def _start(self, x):
+        """In training with dropout: (x with it, each block's drop); else (x, Nones)."""
+        if not (self.training and self.c.dropout > 0):
+            return x, [None] * len(self.blocks)
+        drop = self._masks()
+        return drop(x, None, 0), [lambda y, res, s, i=i: drop(y, res, 1 + 2 * i + s)
+                                  for i in range(len(self.blocks))]
+
     def forward(self, ids):
-        x = self.embed(ids) + self.pos[: ids.shape[1]]
-        if self.training and self.c.dropout > 0:
-            drop = self._masks()
-            x = drop(x, None, 0)
-            for i, blk in enumerate(self.blocks):
-                x = blk(x, lambda y, res, s, i=i: drop(y, res, 1 + 2 * i + s))
-        else:
-            for blk in self.blocks:
-                x = blk(x)
+        x, drops = self._start(self.embed(ids) + self.pos[: ids.shape[1]])
+        for blk, drop in zip(self.blocks, drops):
+            x = blk(x) if drop is None else blk(x, drop)
         return self.head(self.ln_f(x))
 
     def recurrent(self, ids, pos, states=None, lengths=None):
         """The model as a recurrence (``mixer="linear"``): tokens ids [B, n] at
         positions pos[b] .. pos[b] + n - 1 on top of the states of an earlier call
         (None: from nothing); lengths [B] int32: valid tokens of each row of ids.
+        Dropout as in ``forward``: in training mode, with masks of this call's own.
         Returns (logits [B, n, vocab], states)."""
         if self.c.mixer != "linear":
             raise ValueError(f"mixer {self.c.mixer!r} has no recurrent form")
         at = pos[:, None] + torch.arange(ids.shape[1], device=ids.device)
-        x = self.embed(ids) + self.pos[at.clamp(max=self.c.T - 1)]
+        x, drops = self._start(self.embed(ids) + self.pos[at.clamp(max=self.c.T - 1)])
         out = []
-        for i, blk in enumerate(self.blocks):
-            x, s = blk.recurrent(x, None if states is None else states[i], lengths)
+        for i, (blk, drop) in enumerate(zip(self.blocks, drops)):
+            x, s = blk.recurrent(x, None if states is None else states[i], lengths, drop)
             out.append(s)
         return self.head(self.ln_f(x)), out
 

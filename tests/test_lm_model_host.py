@@ -38,6 +38,24 @@ def drawn(monkeypatch):
     return calls
 
 
+@pytest.fixture
+def linear(monkeypatch):
+    """Linear attention in float32 torch operations, token by token."""
+    def attention(q, k, v, decay, scale=None, lengths=None, state=None):
+        B, T, H, d = q.shape
+        S = torch.zeros(B, H, d, d) if state is None else state
+        n = torch.full((B,), T) if lengths is None else lengths
+        rows = []
+        for t in range(T):
+            on = (t < n).view(B, 1, 1, 1)
+            S = torch.where(on, decay.view(1, H, 1, 1) * S + k[:, t, :, :, None] * v[:, t, :, None],
+                            S)
+            o = torch.einsum("bhij,bhi->bhj", S, q[:, t]) * (scale or d ** -0.5)
+            rows.append(torch.where(on[..., 0], o, torch.zeros(())))
+        return torch.stack(rows, 1), S
+    monkeypatch.setattr(gpt.lm_ops, "linear_attention", attention)
+
+
 # ------------------------------------------------------------------- masks
 def test_every_call_draws_masks_of_its_own(drawn):
     """A loop of the user's own, or gradients accumulated over several calls, trains
@@ -109,3 +127,20 @@ def test_counters_without_an_entry_stay(drawn):
     model(ids_of())
     model.load_state_dict({k: v for k, v in model.state_dict().items() if k != "drop_step"})
     assert int(model.drop_step) == 1
+
+
+# ---------------------------------------------------------- the recurrent form
+def test_recurrent_form_trains_with_dropout(drawn, linear):
+    """Training carried from one piece of a sequence to the next has the dropout of a
+    whole one: on a whole sequence both forms are the same function."""
+    model = model_of(mixer="linear")
+    zero = torch.zeros(2, dtype=torch.int64)
+    whole = model(ids_of())
+    model.drop_step.zero_()
+    logits, states = model.recurrent(ids_of(), zero)
+    assert torch.equal(logits, whole) and drawn[:5] == drawn[5:]
+    model.recurrent(ids_of(), zero, states)                 # the next piece: new masks
+    assert len(drawn) == 15 and not set(drawn[10:]) & set(drawn[:10])
+    model.eval()
+    a, _ = model.recurrent(ids_of(), zero)
+    assert torch.equal(a, model(ids_of())) and len(drawn) == 15
