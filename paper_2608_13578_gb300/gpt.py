@@ -246,8 +246,19 @@ def generate(model: GPT, ids, new_tokens: int, lengths=None):
     prompts in one pass, then one token of every sequence per step.  lengths [B]
     int32: the prompts' own lengths (default n, each at least 1); positions past
     the model's T share its last position embedding.  Returns
-    [B, new_tokens]."""
+    [B, new_tokens].  What has no meaning (a prompt of no token, a length that is
+    not in 1 .. n) raises ValueError."""
     B, n = ids.shape
+    if model.c.mixer != "linear":
+        raise ValueError(f"mixer {model.c.mixer!r} has no recurrent form")
+    if n < 1 or new_tokens < 0:
+        raise ValueError(f"prompts must have a token and new_tokens be >= 0 (got {n}, {new_tokens})")
+    if lengths is not None:
+        # read back here: a length past the prompts would index past their logits
+        if lengths.shape != (B,) or not all(1 <= x <= n for x in lengths.tolist()):
+            raise ValueError(f"lengths must be [{B}], each in 1 .. {n}")
+    if new_tokens == 0:
+        return ids.new_empty(B, 0)
     was_training = model.training
     model.eval()
     try:

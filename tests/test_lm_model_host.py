@@ -144,3 +144,31 @@ def test_recurrent_form_trains_with_dropout(drawn, linear):
     model.eval()
     a, _ = model.recurrent(ids_of(), zero)
     assert torch.equal(a, model(ids_of())) and len(drawn) == 15
+
+
+# ------------------------------------------------------------------ generation
+@pytest.mark.parametrize("new", [0, 1, 4])
+def test_generate_gives_as_many_tokens_as_asked(linear, new):
+    model = model_of(mixer="linear", dropout=0.0)
+    out = gpt.generate(model, ids_of(6), new)
+    assert out.shape == (2, new) and out.dtype == torch.int64
+    ragged = gpt.generate(model, ids_of(6), new, torch.tensor([6, 2], dtype=torch.int32))
+    assert torch.equal(ragged[0], out[0])
+    alone = gpt.generate(model, ids_of(6)[1:, :2], new)
+    assert torch.equal(ragged[1], alone[0])
+
+
+@pytest.mark.parametrize("lengths", [[6, 0], [7, 6], [-1, 6], [6], [[6, 6]]])
+def test_generate_refuses_lengths_outside_the_prompts(linear, lengths):
+    model = model_of(mixer="linear", dropout=0.0)
+    with pytest.raises(ValueError, match="lengths"):
+        gpt.generate(model, ids_of(6), 3, torch.tensor(lengths, dtype=torch.int32))
+
+
+def test_generate_refuses_empty_prompts_and_negative_counts(linear):
+    model = model_of(mixer="linear", dropout=0.0)
+    for ids, new in ((ids_of(0), 3), (ids_of(6), -1)):
+        with pytest.raises(ValueError, match="new_tokens"):
+            gpt.generate(model, ids, new)
+    with pytest.raises(ValueError, match="recurrent"):
+        gpt.generate(model_of(mixer="dense"), ids_of(6), 0)
