@@ -210,7 +210,9 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
  *            h at column h*dh (dh channels); each row stride ld >= H*dh is a
  *            multiple of 8, so q, k, v may be slices of one projection's rows
  *   decay    [H] fp32, each in [0, 1] (a^0 = 1 for a = 0 too); a constant: no
- *            gradient is computed for it
+ *            gradient is computed for it.  One outside, or NaN, is reported as
+ *            BCMT_ERR_ARG by the next bcmt_device_status (BCMT_FLAG_CHECK: by the
+ *            call); what its head gives then is not defined, the others are right
  *   lengths  [B] int32 device memory, or NULL
  *   state    [B, H, dh, dh] fp32, row = channel of k, column = channel of v
  *   Requirements: B, T, H >= 1; dh a multiple of 8, 8 <= dh <= 128; scale
@@ -300,8 +302,8 @@ bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void
 
 /* Reads and clears the device status word of the current device after
  * synchronising `stream`: BCMT_OK, BCMT_ERR_TIMEOUT if any bounded device-side
- * wait has expired, or BCMT_ERR_ARG if an embedding id was outside its table,
- * since the last read. */
+ * wait has expired, or BCMT_ERR_ARG if an embedding id was outside its table or
+ * a decay of linear attention outside [0, 1], since the last read. */
 bcmt_status bcmt_device_status(void* stream);
 
 /* Message describing the last error of the calling thread ("" if none). */

@@ -603,7 +603,7 @@ bcmt_status check_linattn_workspace(const bcmt_linattn_params* p, int backward, 
   return check_ptr(ws, "workspace");
 }
 LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int* lengths,
-                     int npass, void* workspace, LinPlan* plan) {
+                     int npass, void* workspace, unsigned* status, LinPlan* plan) {
   LinArgs a{};
   a.npass = npass;
   a.B = p->B;
@@ -612,6 +612,7 @@ LinArgs linattn_args(const bcmt_linattn_params* p, const float* decay, const int
   a.dh = p->dh;
   a.decay = decay;
   a.lengths = lengths;
+  a.status = status;
   *plan = linattn_plan(p->dtype, p->B, p->T, p->H, p->dh, npass, device_sms(),
                        g_use_tc_attn, lengths != nullptr);
   a.nseg = plan->nseg;
@@ -693,6 +694,8 @@ bcmt_status bcmt_device_status(void* stream) {
   if (e != cudaSuccess) return cuda_fail(e, "reading device status");
   if (v & kStatusTimeout) return fail(BCMT_ERR_TIMEOUT, "a bounded device-side wait expired");
   if (v & kStatusBadIndex) return fail(BCMT_ERR_ARG, "an embedding id was outside its table");
+  if (v & kStatusBadDecay)
+    return fail(BCMT_ERR_ARG, "a decay of linear attention was outside [0, 1]");
   if (v) return fail(BCMT_ERR_CUDA, "device status 0x%x", v);
   return BCMT_OK;
 }
@@ -1292,7 +1295,7 @@ bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, lo
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};
   LinPlan pl;
-  LinArgs a = linattn_args(p, decay, lengths, 1, workspace, &pl);
+  LinArgs a = linattn_args(p, decay, lengths, 1, workspace, sp, &pl);
   LinPass& f = a.pass[0];
   f.q = q;
   f.ldq = ld_q;
@@ -1337,7 +1340,7 @@ bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o,
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};
   LinPlan pl;
-  LinArgs a = linattn_args(p, decay, lengths, 3, workspace, &pl);
+  LinArgs a = linattn_args(p, decay, lengths, 3, workspace, sp, &pl);
   // dq = pass(do, v, k); dv = reverse pass(k, q, do); dk = reverse pass(v, do, q).
   // The reverse states are kept without the scale (it multiplies the output),
   // so the incoming gradient of the state is divided by it.

@@ -15,7 +15,12 @@ namespace bcmt {
 typedef __nv_bfloat16 bf16;
 
 // Bits OR-ed into the device status word.
-enum : unsigned { kStatusTimeout = 1u, kStatusBadLaunch = 2u, kStatusBadIndex = 4u };
+enum : unsigned {
+  kStatusTimeout = 1u,
+  kStatusBadLaunch = 2u,
+  kStatusBadIndex = 4u,  // an embedding id outside its table
+  kStatusBadDecay = 8u,  // a decay of linear attention outside [0, 1]
+};
 
 // Programmatic dependent launch.  Every kernel of the library is launched with
 // programmatic stream serialisation (launch_k below) and starts with

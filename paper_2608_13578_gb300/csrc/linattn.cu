@@ -86,6 +86,7 @@ __global__ void __launch_bounds__(NW * 32)
   const int seg_lo = seg * a.seg_len, seg_hi = min(a.T, seg_lo + a.seg_len);
   const int t_lo = min(seg_lo, n), t_hi = min(seg_hi, n);
   const float dec = a.decay[h];
+  if (tid == 0) check_decay(dec, a.status);
   const int dh = a.dh;
   const long long tok0 = (long long)b * a.T;
   const T* gq = (const T*)p.q + tok0 * p.ldq + h * dh;
@@ -342,6 +343,7 @@ __global__ void __launch_bounds__(256) linattn_step_kernel(const __grid_constant
   const int col = c0 + quad * 4;
   const bool on = valid_tokens(a, b) > 0;
   const bool col_ok = col < dh;
+  if (tid == 0) check_decay(a.decay[h], a.status);
   const float dec = on ? a.decay[h] : 1.f;
   const T* q = (const T*)p.q + (long long)b * p.ldq + h * dh;
   const T* k = (const T*)p.k + (long long)b * p.ldk + h * dh;

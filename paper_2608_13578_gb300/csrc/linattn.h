@@ -12,6 +12,7 @@
 
 #include <cuda_runtime.h>
 
+#include "common.cuh"
 #include "internal.h"
 
 namespace bcmt {
@@ -42,7 +43,14 @@ struct LinArgs {
   // the tensor-core form's segment states: groups of 4 columns of all rows together,
   // and the join gives the outgoing state too
   int grouped;
+  unsigned* status;       // the device status word
 };
+
+// A decay outside [0, 1] (or NaN) is reported by the walks and the single-token step;
+// what its head then gives is not defined.
+__device__ __forceinline__ void check_decay(float a, unsigned* status) {
+  if (!(a >= 0.f && a <= 1.f)) atomicOr(status, kStatusBadDecay);
+}
 
 // How the passes are cut along the tokens (the same rule for the workspace
 // size and the launch): `tc` tells which kernel runs.

@@ -1048,6 +1048,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
       sh->n = w.n;
       sh->t_lo = w.t_lo;
       sh->t_hi = w.t_hi;
+      check_decay(a.decay[h], status);
     }
     if (tid >= 64 && tid < 193) {
       const int d = tid - 64;

@@ -153,7 +153,8 @@ def linear_attention_forward(q, k, v, decay, scale: Optional[float] = None, leng
     """(o, state_out) of ``S_t = a S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t``.
 
     q, k, v [B, T, H, dh] (bf16 or fp32; slices of one projection's rows are read
-    in place), decay [H] fp32, lengths [B] int32 (tokens per sequence, default
+    in place), decay [H] fp32, each in [0, 1] (others are reported by
+    ``bcmt.bcmt_device_status``), lengths [B] int32 (tokens per sequence, default
     T), state [B, H, dh, dh] fp32 (default zero).  scale defaults to
     1/sqrt(dh).  state_out: where the last state goes (default a new tensor; may
     be ``state``); autograd sees it as modified in place.  Tokens past a sequence's

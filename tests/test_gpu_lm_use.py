@@ -121,3 +121,39 @@ def test_a_backward_takes_the_number_of_its_forward(F, op):
     assert torch.equal(grad(torch.tensor(0.25), 0.5), grad(0.25))
     with pytest.raises(ValueError, match="gradient"):
         grad(torch.tensor(0.25, requires_grad=True))
+
+
+# ------------------------------------------------------------ decays out of range
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [1, 20, 300])
+@pytest.mark.parametrize("bad", [-0.5, -1e-6, 1.0 + 2.0 ** -23, 2.0, float("inf"), float("nan")])
+def test_a_decay_outside_its_range_is_reported(F, bad, T, dtype):
+    from paper_2608_13578_gb300 import bcmt as C
+    good, worse = torch.tensor([0.9, 0.0, 1.0]).cuda(), torch.tensor([0.9, bad, 1.0]).cuda()
+    d, _ = make(2, T, 3, 64, dtype, 36, True)
+
+    def calls(decay):
+        yield F.linear_attention_forward(d["q"], d["k"], d["v"], decay, state=d["s0"])
+        yield F.linear_attention_backward(d["do"], d["q"], d["k"], d["v"], decay, state=d["s0"],
+                                          dstate=d["ds"])
+    for right, wrong in zip(calls(good), calls(worse)):
+        with pytest.raises(C.BCMTError, match="decay") as e:
+            C.bcmt_device_status()
+        assert e.value.code == C.BCMT_ERR_ARG
+        for x, y in zip(right, wrong):     # the other heads are what they were
+            h = 1 if x.shape[1] == 3 and x.shape[2] == 64 else 2
+            keep = torch.tensor([0, 2], device="cuda")
+            assert torch.equal(x.index_select(h, keep), y.index_select(h, keep))
+    list(calls(good))
+    C.bcmt_device_status()                 # the ends of the range are in it
+
+
+def test_a_call_with_the_check_flag_reports_the_decay(F):
+    from paper_2608_13578_gb300 import bcmt as C
+    x = torch.zeros(1, 4, 2, 8, device="cuda")
+    p = C.bcmt_linattn_params(1, 4, 2, 8, C.BCMT_F32, C.BCMT_FLAG_CHECK, 0.5)
+    decay = torch.tensor([0.5, 1.5], device="cuda")
+    ws = torch.empty(C.bcmt_linattn_workspace_size(p, False), dtype=torch.uint8, device="cuda")
+    with pytest.raises(C.BCMTError, match="decay"):
+        C.bcmt_linattn_forward(p, x, 16, x, 16, x, 16, decay, None, None, torch.empty_like(x), 16,
+                               None, ws)
