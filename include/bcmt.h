@@ -283,8 +283,11 @@ bcmt_status bcmt_embedding_backward(const bcmt_embedding_params* p, const void* 
  * backward pass is the same call on dy (residual NULL) with the same seed and
  * offset.  Element i takes 16-bit draw i % 8 of Philox4x32-10 with key `seed`
  * and counter (i / 8, offset) -- word (i % 8) / 2, its low half first -- and is
- * kept iff the draw is at least round(65536 p); a dropped element contributes
- * exactly 0 even where x is infinite or NaN.  Use another offset for each place
+ * kept iff the draw is at least t = round(65536 p), at most 65535 for p < 1; a
+ * dropped element contributes exactly 0 even where x is infinite or NaN.  The
+ * mask's rate r = 1 - t / 65536 is up to 2^-17 off 1 - p: where 1 / (1 - p) is
+ * further than 2^-15 from 1 / r (for some p above 0.75), 1 / r takes its place, so
+ * that the expectation of y is x to within 2^-15 for every p < 1.  Use another offset for each place
  * and step.  `step` (device memory, or NULL) is added to offset when the kernel
  * runs, so a captured graph can draw a new mask at each replay.  y may be x or
  * residual.  Requirements: n >= 0, 0 <= p <= 1.  flags: BCMT_FLAG_CHECK only. */

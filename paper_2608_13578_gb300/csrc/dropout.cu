@@ -97,9 +97,15 @@ cudaError_t dropout(const Launch& lc, int dtype, const void* x, const void* res,
                     long long n, double p, unsigned long long seed, unsigned long long offset,
                     const unsigned long long* step) {
   if (n == 0) return cudaSuccess;
-  // kept iff the 16-bit draw is at least round(65536 p); p = 1 keeps nothing
-  const uint32_t thr = (uint32_t)lrint(p * 65536.0);
-  const float mul = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.f;
+  // kept iff the 16-bit draw is at least round(65536 p); p = 1 keeps nothing, and
+  // nothing else does
+  const uint32_t thr = p < 1.0 ? std::min((uint32_t)lrint(p * 65536.0), 65535u) : 65536u;
+  // The mask keeps (65536 - thr) / 65536, up to 2^-17 off 1 - p.  The scale is 1 / (1 - p)
+  // as long as the expectation is x to within 2^-15 with it (always up to p = 0.75), and
+  // the mask's own beyond: 1 / (1 - p) would be 1.5 times that at p = 0.99999.
+  const double kept = (65536u - thr) / 65536.0;
+  const bool near = fabs(kept - (1.0 - p)) <= (1.0 - p) / 32768.0;
+  const float mul = p < 1.0 ? (float)(1.0 / (near ? 1.0 - p : kept)) : 0.f;
   return dtype == 0 ? typed<float>(lc, x, res, y, n, thr, mul, seed, offset, step)
                     : typed<bf16>(lc, x, res, y, n, thr, mul, seed, offset, step);
 }

@@ -367,7 +367,8 @@ def _dropout_call(x, p, seed, offset, residual, step):
 
 def dropout_forward(x, p: float, seed: int, offset: int, residual=None, step=None):
     """``[residual +] keep * x / (1 - p)``, the mask a function of (seed, offset +
-    step) and the element's index; step: an int64 on the device (for captured
+    step) and the element's index, its rate 1 - p to 2^-17 (where that is too coarse
+    for 1 / (1 - p), near p = 1, the scale is the mask's own); step: an int64 on the device (for captured
     graphs), default 0."""
     return _dropout_call(x, p, seed, offset, residual, step)
 

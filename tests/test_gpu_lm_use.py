@@ -2,9 +2,11 @@
 autograd sees of a state that is written in place, derivatives of derivatives,
 arguments in every form that Python takes."""
 
+import numpy as np
 import pytest
 import torch
 
+from tests import lm_reference as R
 from tests.test_gpu_lm_ops import F, make, no_wait_ran_out  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -157,3 +159,23 @@ def test_a_call_with_the_check_flag_reports_the_decay(F):
     with pytest.raises(C.BCMTError, match="decay"):
         C.bcmt_linattn_forward(p, x, 16, x, 16, x, 16, decay, None, None, torch.empty_like(x), 16,
                                None, ws)
+
+
+# ------------------------------------------------------------- dropout near p = 1
+@pytest.mark.parametrize("p", [0.1, 0.25, 0.6, 0.75, 0.7777, 0.9, 0.99, 0.999, 0.99997, 0.99999,
+                               1 - 2.0 ** -17, 1 - 2.0 ** -30])
+def test_dropout_keeps_the_expectation(F, p):
+    """The kept elements' scale times the mask's rate is 1 to 2^-15 (and half an ulp of
+    fp32), at every p below 1; up to 0.75 the scale is 1 / (1 - p) itself."""
+    n = 1 << 20
+    t = min(round(65536 * p), 65535)
+    keep = R.dropout_keep(n, t / 65536, 77, 5)
+    assert keep.any()
+    for call in (F.dropout_forward, F.dropout_backward):
+        y = call(torch.ones(n, device="cuda"), p, 77, 5).double().cpu().numpy()
+        assert ((y != 0) == keep).all()
+        scale = y[keep]
+        assert (scale == scale[0]).all()
+        assert abs(scale[0] * (65536 - t) / 65536 - 1) <= 2.0 ** -15 + 2.0 ** -23
+        if p <= 0.75:
+            assert scale[0] == np.float32(1 / (1 - p))
