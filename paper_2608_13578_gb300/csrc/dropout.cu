@@ -46,12 +46,14 @@ __device__ __forceinline__ uint32_t draw16(const uint4& w, int e) {
 // A thread takes 8 consecutive elements (one counter); the generator is about
 // 10 integer instructions per element, below what a bf16 element's bytes take:
 // bandwidth-bound: 32767 x 1001 fp32 take 39.0 us (6.7 TB/s), 8192 x 512 bf16 with
-// a residual 5.2.  A dropped element contributes exactly 0, whatever x holds.
+// a residual 5.2.  A dropped element contributes exactly 0, whatever x holds.  y may be x
+// or res (no __restrict__): a thread reads its elements before it writes them, and
+// nobody else's.
 template <class T, bool RES>
 __global__ void __launch_bounds__(256)
-    dropout_kernel(const T* __restrict__ x, const T* __restrict__ res, T* __restrict__ y,
-                   long long n, uint32_t threshold, float mul, unsigned long long seed,
-                   unsigned long long offset, const unsigned long long* __restrict__ step) {
+    dropout_kernel(const T* x, const T* res, T* y, long long n, uint32_t threshold, float mul,
+                   unsigned long long seed, unsigned long long offset,
+                   const unsigned long long* __restrict__ step) {
   pdl_enter();
   if (step) offset += *step;
   const long long groups = (n + 7) / 8, stride = (long long)gridDim.x * 256;

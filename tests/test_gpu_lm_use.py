@@ -179,3 +179,21 @@ def test_dropout_keeps_the_expectation(F, p):
         assert abs(scale[0] * (65536 - t) / 65536 - 1) <= 2.0 ** -15 + 2.0 ** -23
         if p <= 0.75:
             assert scale[0] == np.float32(1 / (1 - p))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [5, 4096, 1000003])
+def test_dropout_in_place(F, n, dtype):
+    """The C entry point takes x or the residual as y: the bits of a call apart."""
+    from paper_2608_13578_gb300 import bcmt as C
+    x, r = (torch.randn(n, device="cuda").to(dtype) for _ in range(2))
+    p = C.bcmt_dropout_params(n, C.BCMT_BF16 if dtype == torch.bfloat16 else C.BCMT_F32, 0, 0.3,
+                              11, 12, None)
+    plain = F.dropout_forward(x, 0.3, 11, 12)
+    added = F.dropout_forward(x, 0.3, 11, 12, residual=r)
+    for y, src, res, want in ((x.clone(), None, None, plain), (x.clone(), None, r, added),
+                              (r.clone(), x, "y", added), (x.clone(), None, "y", None)):
+        if want is None:    # x, residual and y are one
+            want = F.dropout_forward(x, 0.3, 11, 12, residual=x)
+        C.bcmt_dropout(p, y if src is None else src, y if isinstance(res, str) else res, y)
+        assert torch.equal(y, want)
