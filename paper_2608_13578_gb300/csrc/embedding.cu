@@ -13,9 +13,14 @@ namespace {
 
 constexpr int kSortThreads = 256;
 // ids sorted by one CTA of a radix pass: a CTA's scattered stores take a cycle
-// each, so small batches are cut finer; every CTA reads every tile's counts, so
-// large ones are not
+// each, so small batches are cut finer; large ones are not, for their counts' sake
 inline int sort_tile(long long N) { return N <= (1 << 17) ? 1024 : 4096; }
+// More tiles than this, and the counts are scanned by a kernel before each pass
+// (embed_scan_kernel); up to it, every CTA of a pass adds up every tile's counts, which
+// saves the launch and grows with the tiles' square.  Into a table of 40000 x 8, us
+// scanned and not: 16384 ids 27 and 25, 49152 28 and 28, 65536 30 and 35, 262144 53 and
+// 65, 16777216 1538 and 9988.
+constexpr int kScanTiles = 48;
 constexpr int kChunk = 32;       // sorted positions summed by one warp
 
 // The id at i, or -1 where it is outside [0, V).
@@ -101,6 +106,7 @@ struct SortArgs {
   int* key;      // [N] the ids
   int2* pair[2]; // [N] (key, position), sorted by the digits so far
   int* cnt[3];   // [tiles][256] per pass
+  int* total;    // [256], of the pass whose counts have been scanned; null: none are
   int passes;
   uint4* zero;   // the gradient, cleared by parts over the sort's launches
   long long zero_n;
@@ -172,6 +178,49 @@ __device__ __forceinline__ unsigned equal_lanes(int d, unsigned among) {
 }
 }  // namespace
 
+// Before pass p, for many tiles: each tile's counts become, digit by digit, the keys
+// with that digit in the tiles before it, and total[] the keys of all tiles.  In
+// place; a CTA takes 8 digits (a sector of every tile's counts), a thread one digit of
+// a run of consecutive tiles, twice: its sum, then the sums up to each tile.  Without
+// it a pass reads tiles^2 KB: a second and more at the most ids a call takes.
+constexpr int kScanThreads = 1024, kScanDigits = 8;
+__global__ void __launch_bounds__(kScanThreads)
+    embed_scan_kernel(const __grid_constant__ SortArgs a, int p) {
+  constexpr int kRuns = kScanThreads / kScanDigits;
+  __shared__ int sums[kRuns][kScanDigits];
+  pdl_enter();
+  const int d = threadIdx.x % kScanDigits, run = threadIdx.x / kScanDigits;
+  const int digit = blockIdx.x * kScanDigits + d, per = (a.tiles + kRuns - 1) / kRuns;
+  const int lo = min(run * per, a.tiles), hi = min(lo + per, a.tiles);
+  int* c = a.cnt[p] + digit;
+  int sum = 0;
+#pragma unroll 8
+  for (int t = lo; t < hi; ++t) sum += c[(long long)t * 256];
+  sums[run][d] = sum;
+  __syncthreads();
+  if (run == 0) {
+    int before = 0;
+    for (int r = 0; r < kRuns; ++r) {
+      const int x = sums[r][d];
+      sums[r][d] = before;
+      before += x;
+    }
+    a.total[digit] = before;
+  }
+  __syncthreads();
+  int before = sums[run][d];
+  for (int t0 = lo; t0 < hi; t0 += 8) {  // eight loads in flight
+    int x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = t0 + u < hi ? c[(long long)(t0 + u) * 256] : 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (t0 + u < hi) c[(long long)(t0 + u) * 256] = before;
+      before += x[u];
+    }
+  }
+}
+
 // One stable pass: digit `p` of the keys.  Ranks: each warp takes 256
 // consecutive keys, 32 at a time, and ranks equal digits by lane order; the
 // warps' counts are then scanned in warp order and the tiles' in tile order.
@@ -216,14 +265,19 @@ __global__ void __launch_bounds__(kSortThreads)
   }
   // digit tid: keys before this tile's, over all digits and the earlier tiles
   int total = 0, mine = 0;
-  for (int t0 = 0; t0 < a.tiles; t0 += 32) {  // 32 loads in flight
-    int c[32];
+  if (a.total) {
+    total = a.total[tid];
+    mine = a.cnt[p][(long long)blockIdx.x * 256 + tid];
+  } else {
+    for (int t0 = 0; t0 < a.tiles; t0 += 32) {  // 32 loads in flight
+      int c[32];
 #pragma unroll
-    for (int u = 0; u < 32; ++u) c[u] = t0 + u < a.tiles ? a.cnt[p][(t0 + u) * 256 + tid] : 0;
+      for (int u = 0; u < 32; ++u) c[u] = t0 + u < a.tiles ? a.cnt[p][(t0 + u) * 256 + tid] : 0;
 #pragma unroll
-    for (int u = 0; u < 32; ++u) {
-      total += c[u];
-      if (t0 + u < (int)blockIdx.x) mine += c[u];
+      for (int u = 0; u < 32; ++u) {
+        total += c[u];
+        if (t0 + u < (int)blockIdx.x) mine += c[u];
+      }
     }
   }
   int incl = total;
@@ -451,8 +505,9 @@ __global__ void __launch_bounds__(256)
 // ---------------------------------------------------------------- host side
 namespace {
 struct BwdLayout {
-  size_t key, pair[2], cnt[3], part, bytes;
+  size_t key, pair[2], cnt[3], total, part, bytes;
   int tiles, passes, chunks;
+  bool scan;
 };
 BwdLayout bwd_layout(long long N, int V, int D) {
   BwdLayout l{};
@@ -468,6 +523,8 @@ BwdLayout bwd_layout(long long N, int V, int D) {
   l.key = take((size_t)N * 4);
   for (int i = 0; i < 2; ++i) l.pair[i] = take((size_t)N * 8);
   for (int i = 0; i < l.passes; ++i) l.cnt[i] = take((size_t)l.tiles * 256 * 4);
+  l.scan = l.tiles > kScanTiles;
+  if (l.scan) l.total = take(256 * 4);
   l.part = take((size_t)l.chunks * 2 * D * 4);
   l.bytes = off;
   return l;
@@ -496,6 +553,7 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   s.key = reinterpret_cast<int*>(w + l.key);
   for (int i = 0; i < 2; ++i) s.pair[i] = reinterpret_cast<int2*>(w + l.pair[i]);
   for (int i = 0; i < l.passes; ++i) s.cnt[i] = reinterpret_cast<int*>(w + l.cnt[i]);
+  s.total = l.scan ? reinterpret_cast<int*>(w + l.total) : nullptr;
   s.zero = static_cast<uint4*>(dw);
   s.zero_n = (long long)a.V * (a.D / vec_n<T>());
   s.status = lc.status;
@@ -507,6 +565,10 @@ cudaError_t bwd_typed(const Launch& lc, const EmbedArgs& a, const void* dy, void
   if (e != cudaSuccess) return e;
   if (a.N == 0) return cudaGetLastError();
   for (int p = 0; p < l.passes; ++p) {
+    if (l.scan) {
+      e = launch_k(embed_scan_kernel, dim3(256 / kScanDigits), dim3(kScanThreads), 0, lc.stream, s, p);
+      if (e != cudaSuccess) return e;
+    }
     e = fine ? launch_k(embed_sort_kernel<4>, grid, dim3(kSortThreads), 0, lc.stream, s, p)
              : launch_k(embed_sort_kernel<16>, grid, dim3(kSortThreads), 0, lc.stream, s, p);
     if (e != cudaSuccess) return e;

@@ -197,3 +197,42 @@ def test_dropout_in_place(F, n, dtype):
             want = F.dropout_forward(x, 0.3, 11, 12, residual=x)
         C.bcmt_dropout(p, y if src is None else src, y if isinstance(res, str) else res, y)
         assert torch.equal(y, want)
+
+
+# --------------------------------------------------------- table gradient, many ids
+@pytest.mark.parametrize("N,V,kind", [(2097152, 300, "uniform"), (2097153, 300, "uniform"),
+                                      (2500001, 40000, "zipf"), (5000000, 70000, "uniform"),
+                                      (3000000, 200, "same")])
+def test_table_gradient_of_millions_of_ids(F, N, V, kind):
+    """Against float64 sums on the device; tolerance as in test_gpu_lm_ops."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    if kind == "same":
+        ids = torch.full((N,), V - 1, device="cuda")
+    else:
+        u = torch.rand(N, generator=g, device="cuda", dtype=torch.float64)
+        ids = (V * (u ** 6 if kind == "zipf" else u)).long().clamp(max=V - 1)
+    dy = torch.randn(N, 8, generator=g, device="cuda")
+    dw = F.embedding_backward(ids, dy, V, 1.5)
+    ref = torch.zeros(V, 8, dtype=torch.float64, device="cuda").index_add_(0, ids, 1.5 * dy.double())
+    mag = torch.zeros_like(ref).index_add_(0, ids, 1.5 * dy.double().abs())
+    cnt = torch.bincount(ids, minlength=V).view(V, 1)
+    assert ((dw - ref).abs() <= (cnt + 1) * 2.0 ** -24 * mag + 2.0 ** -23 * ref.abs()).all()
+    assert torch.equal(dw, F.embedding_backward(ids, dy, V, 1.5))
+
+
+def test_table_gradient_time_grows_with_the_ids(F):
+    """Eight times the ids take about eight times as long, not 64."""
+    def ms(N):
+        ids = torch.randint(0, 40000, (N,), device="cuda", dtype=torch.int32)
+        dy = torch.zeros(N, 8, device="cuda", dtype=torch.bfloat16)
+        best = float("inf")
+        for _ in range(4):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            F.embedding_backward(ids, dy, 40000)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+    small, large = ms(1 << 23), ms(1 << 26)
+    assert large <= 16 * small, (small, large)
