@@ -220,7 +220,10 @@ bcmt_status bcmt_attention_backward_noalloc(const bcmt_params* p, const void* q,
  *   Arithmetic and states are fp32; with bf16 tensors the tensor-core form
  *   rounds the decayed scores and the state to bf16 where they enter a product
  *   with bf16 rows.  The running state is an fp32 sum whose decayed keys carry 16
- *   bits, in the states that a call returns 24. */
+ *   bits, in the states that a call returns 24.  An infinity or NaN of a valid
+ *   entry reaches the rows that the definition lets it reach and no other: of o
+ *   and dq no row of an earlier token, of dk and dv none of a later one.  No
+ *   output may overlap an input, but for the states as stated below. */
 typedef struct {
   int B, T, H, dh;
   int dtype;       /* bcmt_dtype of q, k, v, o and their gradients */

@@ -780,6 +780,112 @@ __device__ __forceinline__ void role_state(const LinTcArgs& A, uint8_t* raw, uns
   }
 }
 
+// The outputs of the walk that are not finite, again, from the recurrence token by
+// token in fp32 (the rows' threads, at the CTA's end).  In a product over 128 tokens
+// an infinity or NaN of v meets the zero weights of the rows before it, and 0 * inf
+// is NaN: those rows get here what the definition gives them.  Such a value stays in
+// the state, so that one look at the state's last copy and at the last chunk's v finds
+// it in any chunk.  A thread keeps half of a column of the state in shared memory, over
+// the tiles.  The look costs a walk up to 0.4 us, the rest 0.6 us a token.
+template <int DP, bool kSegs>
+__device__ __noinline__ void redo_rows(const LinTcArgs& A, uint8_t* raw) {
+  using G = TcGeo<DP>;
+  constexpr int NT = 128 * Roles<DP>::NW;
+  const View<DP> vw(raw);
+  const Walk w(vw.shared());
+  if (w.nch == 0) return;
+  const int tid = threadIdx.x;
+  __nv_bfloat162 z = __float2bfloat162_rn(0.f);  // 0 * x: 0 or NaN
+  auto look = [&](const uint8_t* at) {
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      z = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&vv[e]), __float2bfloat162_rn(0.f), z);
+  };
+  // (rows past the end have been cleared)
+  const uint8_t* sV = vw.smem + ((w.nch - 1) & 1) * G::kStage + 2 * G::kTile;
+#pragma unroll
+  for (int x = tid * 16; x < (int)G::kTile; x += NT * 16) look(sV + x);
+#pragma unroll
+  for (int x = tid * 16; x < (int)G::kState; x += NT * 16) look(vw.state() + x);
+  // true for all threads if it is for one; a barrier between them
+  auto any = [&](bool x) {
+    uint32_t r = x;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %0, 0;\n\t"
+        "barrier.cta.red.or.pred q, 1, %1, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "+r"(r)
+        : "n"(NT)
+        : "memory");
+    return r != 0;
+  };
+  if (!any(!(__low2float(z) + __high2float(z) == 0.f))) return;
+  const LinArgs& a = A.a;
+  const LinPass& p = a.pass[blockIdx.y];
+  const int dh = a.dh, st = dh * dh, h = ld_once(&vw.shared()->h), b = ld_once(&vw.shared()->b);
+  const int seg = ld_once(&vw.shared()->seg), bh = b * a.H + h;
+  const float dec = a.decay[h], lg = log2f(dec);
+  float* S = reinterpret_cast<float*>(vw.smem);  // [dh][dh]
+  float* part = reinterpret_cast<float*>(vw.smem + G::kStage);
+  const float* segs = p.seg + (long long)bh * a.nseg * st;
+#pragma unroll 1
+  for (int e = tid; e < st; e += NT) {  // the state coming into the segment
+    const int i = e / dh, j = e - i * dh, at = (j >> 2) * dh * 4 + i * 4 + (j & 3);
+    float x = 0.f;
+    if (kSegs && a.joined) {
+      x = segs[seg * st + at];
+    } else {
+      if (p.s_in)
+        x = (w.n > 0 ? p.s_in_mul : 1.f) * p.s_in[(long long)bh * st + (p.s_in_t ? j * dh + i : e)];
+#pragma unroll 1
+      for (int y = 0; kSegs && y < (w.rev ? a.nseg - 1 - seg : seg); ++y) {
+        const int s = w.rev ? a.nseg - 1 - y : y, m = min(max(w.n - s * a.seg_len, 0), a.seg_len);
+        const bool fresh = w.rev && w.n <= s * a.seg_len + a.seg_len;
+        if (m > 0) x = fmaf(decay_pow(lg, m - (fresh ? 1 : 0)), x, segs[s * st + at]);
+      }
+    }
+    S[e] = x;
+  }
+  any(false);
+  const int j = tid % DP, mid = (dh / 2 + 7) / 8 * 8;
+  const bool first = tid < DP;
+  const bf16 *q = (const bf16*)p.q, *k = (const bf16*)p.k, *v = (const bf16*)p.v;
+  float y = 0.f;
+#pragma unroll 1
+  for (int x = 0; x < w.t_hi - w.t_lo; ++x) {
+    // a column whose state is not finite gives no finite output any more
+    if (x % 32 == 31 && !any(j < dh && isfinite(y))) return;
+    const int t = w.rev ? w.t_hi - 1 - x : w.t_lo + x;
+    const long long tok = (long long)b * a.T + t;
+    const float f = w.rev && t == w.n - 1 ? 1.f : dec;
+    float acc = 0.f;
+    if (j < dh) {
+      const float vj = to_f(v[tok * p.ldv + h * dh + j]);
+#pragma unroll 1
+      for (int i = first ? 0 : mid; i < (first ? mid : dh); i += 8) {
+        float kk[8], qq[8], s[8];
+        load8(k + tok * p.ldk + h * dh + i, kk);
+        load8(q + tok * p.ldq + h * dh + i, qq);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = S[(i + e) * dh + j];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y = fmaf(f, s[e], kk[e] * vj);
+          S[(i + e) * dh + j] = y;
+          acc = fmaf(qq[e], y, acc);
+        }
+      }
+      if (!first) part[(x & 1) * DP + j] = acc;
+    }
+    any(false);
+    if (j < dh && first) {
+      bf16* o = (bf16*)p.o + tok * p.ldo + h * dh + j;
+      if (!isfinite(to_f(*o))) *o = from_f<bf16>((acc + part[(x & 1) * DP + j]) * p.out_mul);
+    }
+  }
+}
+
 // ------------------------------------------------------------------ states
 // The state that a segment adds (from zero, before the segments' join) or, with
 // one segment, the outgoing state: product D alone.  A state that the call returns
@@ -1082,6 +1188,7 @@ __global__ void __launch_bounds__(Roles<DP>::kThreads, DP == 64 ? 2 : 1)
   tc::fence_before_sync();
   __syncthreads();
   if (warp == 8 * NW) tc::tmem_dealloc(View<DP>(smem_raw).shared()->tmem, G::kCols);
+  if (warp < 4 * NW) redo_rows<DP, kSegs>(A, smem_raw);
 }
 
 // ---------------------------------------------------------------- host side

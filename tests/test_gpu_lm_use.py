@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import lm_reference as R
-from tests.test_gpu_lm_ops import F, make, no_wait_ran_out  # noqa: F401
+from tests.test_gpu_lm_ops import F, make, no_wait_ran_out, tolerances  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -236,3 +236,59 @@ def test_table_gradient_time_grows_with_the_ids(F):
         return best
     small, large = ms(1 << 23), ms(1 << 26)
     assert large <= 16 * small, (small, large)
+
+
+# --------------------------------------------------------- values that are not finite
+def same_where_finite(name, got, ref, tol):
+    """Finite exactly where the definition is, and within tol of its largest entry there."""
+    got = got.detach().double().cpu().numpy()
+    ok = np.isfinite(ref)
+    assert (np.isfinite(got) == ok).all(), (name, int((np.isfinite(got) != ok).sum()))
+    if ok.any():
+        assert np.abs(got[ok] - ref[ok]).max() <= tol * np.abs(ref[ok]).max(), name
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("where", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("B,H,dh,T,at,dtype,ragged", [
+    (1, 2, 64, 300, 150, "bf16", False), (2, 2, 128, 260, 259, "bf16", False),
+    (1, 2, 40, 700, 0, "bf16", False), (1, 3, 128, 1500, 1100, "bf16", True),
+    (32, 10, 64, 385, 200, "bf16", True), (40, 4, 96, 300, 77, "bf16", False),
+    (1, 2, 64, 300, 150, "fp32", False), (1, 2, 64, 20, 11, "bf16", False),
+])
+@pytest.mark.filterwarnings("ignore::RuntimeWarning")
+def test_what_is_not_finite_stays_where_it_belongs(F, B, H, dh, T, at, dtype, ragged, where, value):
+    """An infinity or NaN of one entry reaches the rows and channels that the definition
+    lets it reach: no earlier row of an output, no later one of a gradient."""
+    lengths = [T - 3 * (b % 7) if b else T for b in range(B)] if ragged else None
+    d, r = make(B, T, H, dh, dtype, 41, True, lengths)
+    for x in (d, r):
+        x[where][0, at, H - 1, 5] = value
+    some = sorted({0, B - 1})
+    r = {x: y if x == "decay" or y is None else y[some] for x, y in r.items()}
+    o, S = F.linear_attention_forward(d["q"], d["k"], d["v"], d["decay"], None, d["n"], d["s0"])
+    got = F.linear_attention_backward(d["do"], d["q"], d["k"], d["v"], d["decay"], None, d["n"],
+                                      d["s0"], d["ds"])
+    ro, rS = R.linear_attention(r["q"], r["k"], r["v"], r["decay"], dh ** -0.5, r["n"], r["s0"])
+    ref = R.linear_attention_grads(r["do"], r["q"], r["k"], r["v"], r["decay"], dh ** -0.5, r["n"],
+                                   r["s0"], r["ds"])
+    to, ts = tolerances(dtype, T, dh)
+    for name, x, y, t in zip(("o", "state", "dq", "dk", "dv", "d_state"), (o, S, *got),
+                             (ro, rS, *ref), (to, ts, to, to, to, ts)):
+        same_where_finite(name, x[some], y, t)
+
+
+def test_rows_before_a_value_that_is_not_finite_keep_their_bits(F):
+    """The rows that it does not reach are those of a call without it, where the kernel
+    had them finite: other chunks of 128 tokens, and other heads and channels."""
+    d, _ = make(2, 700, 2, 64, "bf16", 42)
+    want, _ = F.linear_attention_forward(d["q"], d["k"], d["v"], d["decay"])
+    d["v"][1, 300, 0, 7] = float("nan")
+    o, _ = F.linear_attention_forward(d["q"], d["k"], d["v"], d["decay"])
+    bad = torch.zeros_like(o, dtype=torch.bool)
+    bad[1, 300:, 0, 7] = True
+    redone = torch.zeros_like(bad)
+    redone[1, 256:300, 0, 7] = True
+    assert o[bad].isnan().all() and torch.equal(o[~bad & ~redone], want[~bad & ~redone])
+    scale = want.float().abs().max()
+    assert (o[redone].float() - want[redone].float()).abs().max() <= 4 * 2.0 ** -9 * scale
