@@ -292,3 +292,32 @@ def test_rows_before_a_value_that_is_not_finite_keep_their_bits(F):
     assert o[bad].isnan().all() and torch.equal(o[~bad & ~redone], want[~bad & ~redone])
     scale = want.float().abs().max()
     assert (o[redone].float() - want[redone].float()).abs().max() <= 4 * 2.0 ** -9 * scale
+
+
+# ------------------------------------------------------------------- the model
+def test_a_captured_training_forward_draws_new_masks(F):
+    """Replays of one captured call of a model with dropout move its counter on."""
+    from paper_2608_13578_gb300 import gpt
+    c = gpt.GPTConfig(vocab=64, D=64, H=2, layers=1, mlp=64, L=16, T=32, mixer="linear",
+                      embed_scale=1.0, dropout=0.3)
+    model = gpt.build(c, dtype=torch.float32)
+    ids = torch.randint(0, 64, (2, 32), generator=torch.Generator().manual_seed(1)).cuda()
+    with torch.no_grad():
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            model(ids)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = model(ids)
+        model.drop_step.zero_()
+        replayed = []
+        for _ in range(3):
+            graph.replay()
+            replayed.append(out.clone())
+        assert int(model.drop_step) == 3
+        model.drop_step.zero_()
+        for got in replayed:
+            assert torch.equal(got, model(ids))
+        assert not torch.equal(replayed[0], replayed[1])
