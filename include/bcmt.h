@@ -246,7 +246,9 @@ bcmt_status bcmt_linattn_forward(const bcmt_linattn_params* p, const void* q, lo
 /* Gradients of sum(d_o * o) + sum(d_state_out * state_out) with respect to q, k,
  * v and state_in, from the forward's inputs (nothing else is kept).
  * d_state_out NULL: zero; d_state_in NULL: not computed (it must not be
- * d_state_out's or state_in's buffer).  Rows t >= n of dq, dk, dv are zero. */
+ * d_state_out's or state_in's buffer).  Rows t >= n of dq, dk, dv are zero.
+ * d_state_out / scale must stay within fp32: with d_state_out, a scale whose
+ * reciprocal does not is refused. */
 bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o, long ld_do,
                                   const void* q, long ld_q, const void* k, long ld_k,
                                   const void* v, long ld_v, const float* decay,

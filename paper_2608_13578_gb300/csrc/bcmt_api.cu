@@ -1335,6 +1335,8 @@ bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o,
   BCMT_TRY(check_opt(d_state_in, "d_state_in"));
   if (d_state_in && (d_state_in == d_state_out || d_state_in == state_in))
     return fail(BCMT_ERR_ARG, "d_state_in must have a buffer of its own");
+  if (d_state_out && !isfinite(1.f / p->scale))  // the reverse states start at their ratio
+    return fail(BCMT_ERR_ARG, "scale %g is too small for a gradient of the last state", p->scale);
   BCMT_TRY(check_linattn_workspace(p, 1, workspace));
   unsigned* sp = status_ptr();
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");

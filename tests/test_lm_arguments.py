@@ -32,3 +32,19 @@ def test_what_is_no_tensor(F):
                  lambda: F.linear_attention_forward(None, None, None, None)):
         with pytest.raises(ValueError, match="tensor"):
             call()
+
+
+@pytest.mark.parametrize("scale,refused", [(1e-39, True), (-1e-40, True), (2e-38, False), (0.1, False)])
+def test_backward_refuses_a_scale_without_a_reciprocal(F, scale, refused):
+    """With a gradient of the last state: the reverse states start at its ratio to the
+    scale, which would be infinite."""
+    from paper_2608_13578_gb300 import bcmt as C
+    A, p = 1 << 20, C.bcmt_linattn_params(1, 2, 1, 8, C.BCMT_F32, 0, scale)
+
+    def code(dstate):   # the last argument but one is checked after the scale
+        with pytest.raises(C.BCMTError) as e:
+            C.bcmt_linattn_backward(p, A, 8, A, 8, A, 8, A, 8, A, None, None, dstate, A, 8, A, 8,
+                                    A, 8, None, A + 8, 0)
+        return e.value.code
+    assert code(A) == (C.BCMT_ERR_ARG if refused else C.BCMT_ERR_ALIGN)
+    assert code(None) == C.BCMT_ERR_ALIGN
