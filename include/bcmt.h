@@ -259,7 +259,8 @@ bcmt_status bcmt_linattn_backward(const bcmt_linattn_params* p, const void* d_o,
 
 /* Scaled embedding lookup out[i] = scale * weight[ids[i]] and its gradient
  * d_weight[v] = scale * (sum of d_out[i] over the i with ids[i] = v), the sum in
- * fp32 in the order of i: the same bits at every run.  weight, d_weight [V, D];
+ * fp32 in an order that ids alone decide (runs of up to 32 in the order of i, then
+ * their sums): the same bits at every run.  weight, d_weight [V, D];
  * out, d_out [N, D]; ids [N] int32 (id_bytes 4) or int64 (8).  An id outside
  * [0, V) gives a zero row and no gradient, and is reported as BCMT_ERR_ARG by
  * the next bcmt_device_status (BCMT_FLAG_CHECK: by the call).  Every row of

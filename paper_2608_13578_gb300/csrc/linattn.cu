@@ -59,7 +59,7 @@ __device__ __forceinline__ void load_run(const float* p, float* v) {
 // four columns (4 shuffles).  Rows are taken in pairs by the packed fp32
 // instructions: 1.5 instructions per state element and token.  Bound by those and
 // the latency of the sums: 4 x 4096 tokens of 8 heads of width 64 take 154 us (183
-// without pairs), 2 x 2048 of width 128 take 142 us (167).
+// without pairs; their backward 453), 2 x 2048 of width 128 take 142 us (167).
 // `local`: states only, from zero, into pass.seg (the first launch of a
 // segmented walk).
 template <class T, int DK, int NW>
@@ -425,7 +425,7 @@ LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms,
     // to width 64): the walk is sequential, and a slot left empty is lost.  8 x 1024
     // tokens of 8 heads of 64 take 23 us so, 30 in one segment or in twice as many, 32
     // in two; where a call has one head a slot or so, one segment needs no states
-    // (backward of 4 x 4095, 8 heads of 128: 107 us, 147 in two)
+    // (backward of 4 x 4095, 8 heads of 128: 109 us, 147 in two)
     const long long slots = (long long)sms * (dh <= 64 ? 2 : 1);
     const int chunks = (T + 127) / 128;
     long long n = std::max(1ll, std::min<long long>(slots / heads, chunks));
@@ -438,8 +438,10 @@ LinPlan linattn_plan(int dtype, int B, int T, int H, int dh, int npass, int sms,
     pl.seg_len = per * 128;
     return pl;
   }
-  // enough CTAs for eight on each SM, by segments of at least 24 tokens: the walk
-  // is sequential, and one segment's latency is the pass's.  Two CTAs an SM and 64
+  // CTAs for eight on each SM, by segments of at least 24 tokens: the walk is
+  // sequential, and one segment's latency is the pass's.  Eight fit up to width 32; by
+  // their registers (fp32) 5 of width 64 do and 3 of width 128, so that there the CTAs
+  // come in 1.6 and 2.7 waves.  Two CTAs an SM and 64
   // tokens took 277 us for 183 at 4 x 4096 of width 64, 39 for 31 at 1 x 200 of 4
   // heads of width 128; segments of 32 and of 24 tokens differ by 2 to 4 us in small calls
   const long long ctas = heads * (dh > 64 ? 2 : 1);

@@ -33,8 +33,8 @@
 // operands, K' and S's copy are 512 KB, 2.1 us at 128 bytes a cycle, of the 3.3 us
 // that it takes; the tensor cores are busy for 28%); at width 64 the chain D -> S ->
 // B of latencies.  4 sequences of 4095 tokens, 8 heads of 128, backward:
-// 107 us, 200 TFLOP/s of the recurrence's own operations; 8 x 1024 tokens of 8
-// heads of 64, forward: 23 us.
+// 109 us, 197 TFLOP/s of the recurrence's own operations; 8 x 1024 tokens of 8
+// heads of 64, forward: 23.5 us.
 #include <algorithm>
 
 #include "attn_common.cuh"
@@ -791,6 +791,7 @@ template <int DP, bool kSegs>
 __device__ __noinline__ void redo_rows(const LinTcArgs& A, uint8_t* raw) {
   using G = TcGeo<DP>;
   constexpr int NT = 128 * Roles<DP>::NW;
+  static_assert(NT == 2 * DP && DP * DP * 4 <= G::kStage, "two threads a column, the state in a stage");
   const View<DP> vw(raw);
   const Walk w(vw.shared());
   if (w.nch == 0) return;

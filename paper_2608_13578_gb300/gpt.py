@@ -21,7 +21,8 @@ not grow with the length.
 
 ``embed_scale`` and ``dropout`` put the library's scaled embedding (with its
 gradient by sorted tokens) and its counter-based dropout in place of PyTorch's
-embedding and of no dropout; both are off by default.
+embedding and of no dropout; both are off by default.  The masks come from a counter
+that every call in training mode moves on, and that is saved with the model.
 """
 
 from __future__ import annotations
