@@ -309,10 +309,146 @@ typedef struct {
 bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void* residual,
                          void* y, void* stream);
 
+/* The end of a block and the norm before the next, over rows of D channels:
+ *     z = post(branch), or branch;   h = alpha * x + gate * z;   n = pre(h),
+ * post and pre both layer norms, (v - mean) / sqrt(var + eps) * weight [+ bias], or
+ * both root-mean-square norms, v / sqrt(mean v^2 + eps) * weight [+ bias].
+ *
+ *   branch, x, h, n .. [rows, D] of dtype, dense
+ *   weight, bias .. [D] of wtype: the pre norm; bias may be NULL (0)
+ *   post_weight, post_bias .. [D] of wtype: the post norm; post_weight NULL: none
+ *   gate     [gates, D] of dtype, row i for rows i * rows / gates and on (gates
+ *            divides rows: 1 for all rows, the number of sequences, rows); NULL: 1
+ *
+ * Statistics and everything between the loads and the stores are fp32; n is the
+ * norm of h before its rounding.  Requirements: rows >= 0, 1 <= D <= 8192,
+ * rows * D <= 2^40, alpha finite, eps >= 0 and finite.  flags: BCMT_FLAG_CHECK
+ * only.  h may be x or branch; no other output may overlap an input. */
+typedef struct {
+  long long rows;
+  int D;
+  int dtype, wtype; /* bcmt_dtype */
+  int rms;          /* 0: layer norms, 1: root-mean-square norms */
+  long long gates;  /* rows of the gate (0 where gate is NULL) */
+  unsigned flags;
+  float alpha, eps;
+} bcmt_norm_params;
+
+bcmt_status bcmt_residual_norm_forward(const bcmt_norm_params* p, const void* branch,
+                                       const void* x, const void* weight, const void* bias,
+                                       const void* post_weight, const void* post_bias,
+                                       const void* gate, void* h, void* n, void* stream);
+
+/* Bytes of workspace of the backward call (post: with a post norm), free to
+ * reuse between calls; 0 for invalid parameters. */
+size_t bcmt_residual_norm_workspace_size(const bcmt_norm_params* p, int post);
+/* Gradients of sum(dh * h) + sum(dn * n) from the forward's branch, weights and
+ * gate and its h; dh NULL: zero.  The outputs have the shape and type of what
+ * they belong to; each but dbranch may be NULL (not computed).  Column sums
+ * are fp32 in an order that the sizes alone decide. */
+bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* dh, const void* dn,
+                                        const void* branch, const void* h, const void* weight,
+                                        const void* post_weight, const void* post_bias,
+                                        const void* gate, void* dbranch, void* dx, void* dweight,
+                                        void* dbias, void* dpost_weight, void* dpost_bias,
+                                        void* dgate, void* workspace, void* stream);
+
+/* One AdamW step over `count` tensors in one launch (384 tensors a launch):
+ *     m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,   g times *grad_scale,
+ *     p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps),
+ * p taken from, and written to, the float32 master too where there is one (dtype
+ * bf16, all tensors or none).  bits 32: m and v are float32.  bits 8: signed and
+ * unsigned bytes with one float32 scale per 256 consecutive elements of the
+ * tensor (the last block may be shorter): m = c |c| s with c in -127 .. 127 and
+ * s = max |m| / 127^2, sqrt(v) = c^2 r with c in 0 .. 255 and r = sqrt(max v) /
+ * 255^2 of the block, each c the nearest in c (rounded up at the middle; at least
+ * 1 where v > 0); a block with s < 2^-100, r < 2^-60 is held as zeros there.  What
+ * decides a code is rounded to fp32 at each operation.  All zeros are states of 0.
+ * A gradient that is not finite makes its element's state, in 8 bits its block's
+ * scales, not finite.  step_ptr and lr_ptr (device memory, or NULL) take the
+ * place of step and lr when the kernel runs, for captured graphs.
+ * Requirements: buffers of a tensor and of different tensors do not overlap;
+ * 0 <= beta < 1; lr, eps, weight_decay >= 0 and finite; step >= 1.  flags:
+ * BCMT_FLAG_CHECK only.  `tensors` is read during the call (host memory). */
+typedef struct {
+  int count;
+  int dtype; /* bcmt_dtype of p and g */
+  int bits;  /* 32 or 8 */
+  unsigned flags;
+  long long step;
+  double lr, beta1, beta2, eps, weight_decay;
+  const float* grad_scale; /* device memory, or NULL: 1 */
+  const long long* step_ptr;
+  const float* lr_ptr;
+} bcmt_adamw_params;
+
+typedef struct {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* master;  /* or NULL */
+  float* m_scale; /* bits 8: [ceil(n / 256)] */
+  float* v_scale;
+  long long n;
+} bcmt_adamw_tensor;
+
+bcmt_status bcmt_adamw_step(const bcmt_adamw_params* p, const bcmt_adamw_tensor* tensors,
+                            void* stream);
+/* The float32 values m, v [n] that 8-bit states of n elements stand for. */
+bcmt_status bcmt_adamw_values(const void* m_codes, const float* m_scale, const void* v_codes,
+                              const float* v_scale, float* m, float* v, long long n, void* stream);
+
+/* A step of beam search.  For each of N searches, over its K beams k and the V
+ * tokens v, cand[k, v] = scores[k] + logits[k, v] - log sum_u exp(logits[k, u]); a
+ * beam that has ended has one candidate, token `eos` at scores[k].  The K largest
+ * candidates, equal ones by the lower k V + v, become the beams: their scores,
+ * parents (k), tokens (v) and whether they have ended (the parent had, or v is
+ * eos).  Logits of -inf are tokens ruled out and scores of -inf beams that are not
+ * there: their candidates, -inf too, come last, in the order of k V + v.  What
+ * decides is held in 64 bits.  A beam with a logit or score that is NaN or +inf
+ * counts as not there and is reported as BCMT_ERR_ARG by the next
+ * bcmt_device_status (BCMT_FLAG_CHECK: by the call); the logits of beams that have
+ * ended, or have a score of -inf, are not read.
+ *
+ *   logits   [N, K, V] of dtype, rows of a stride ld >= V elements
+ *   scores, scores_out [N, K] fp32;   finished [N, K] bytes, or NULL: none has
+ *   parents, tokens [N, K] 64-bit;    finished_out [N, K] bytes
+ *   Requirements: N >= 0, 1 <= K <= 32, 1 <= V < 2^24, N * K <= 2^22; eos < V, negative
+ *   for none (not with finished).  flags: BCMT_FLAG_CHECK only.  scores_out may
+ *   be scores and finished_out finished. */
+typedef struct {
+  int N, K, V;
+  int dtype;
+  int eos;
+  unsigned flags;
+  long long ld;
+} bcmt_beam_params;
+
+/* Bytes of workspace of bcmt_beam_select; 0 for invalid parameters. */
+size_t bcmt_beam_workspace_size(const bcmt_beam_params* p);
+bcmt_status bcmt_beam_select(const bcmt_beam_params* p, const void* logits, const float* scores,
+                             const void* finished, float* scores_out, long long* parents,
+                             long long* tokens, void* finished_out, void* workspace, void* stream);
+
+/* dst[n, k] = src[n, parents[n, k]] for `count` tensors of N x K rows of
+ * row_bytes bytes each (dense; src and dst do not overlap), one launch for up to
+ * 128.  A parent outside [0, K) gives a row of zeros and is reported as
+ * BCMT_ERR_ARG by the next bcmt_device_status.  N * K <= 2^22, K <= 32. */
+typedef struct {
+  const void* src;
+  void* dst;
+  long long row_bytes;
+} bcmt_beam_tensor;
+bcmt_status bcmt_beam_reorder(const long long* parents, int N, int K,
+                              const bcmt_beam_tensor* tensors, int count, unsigned flags,
+                              void* stream);
+
 /* Reads and clears the device status word of the current device after
  * synchronising `stream`: BCMT_OK, BCMT_ERR_TIMEOUT if any bounded device-side
- * wait has expired, or BCMT_ERR_ARG if an embedding id was outside its table or
- * a decay of linear attention outside [0, 1], since the last read. */
+ * wait has expired, or BCMT_ERR_ARG if an embedding id was outside its table,
+ * a decay of linear attention outside [0, 1], a logit or score of beam search NaN
+ * or +inf, or a parent outside its beams, since the last read. */
 bcmt_status bcmt_device_status(void* stream);
 
 /* Message describing the last error of the calling thread ("" if none). */

@@ -64,11 +64,44 @@ class bcmt_dropout_params(ctypes.Structure):
                 ("offset", ctypes.c_ulonglong), ("step", ctypes.c_void_p)]
 
 
+class bcmt_norm_params(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("D", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("wtype", ctypes.c_int), ("rms", ctypes.c_int), ("gates", ctypes.c_longlong),
+                ("flags", ctypes.c_uint), ("alpha", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class bcmt_adamw_params(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int), ("dtype", ctypes.c_int), ("bits", ctypes.c_int),
+                ("flags", ctypes.c_uint), ("step", ctypes.c_longlong), ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_void_p),
+                ("step_ptr", ctypes.c_void_p), ("lr_ptr", ctypes.c_void_p)]
+
+
+class bcmt_adamw_tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "master", "m_scale",
+                                               "v_scale")] + [("n", ctypes.c_longlong)]
+
+
+class bcmt_beam_params(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int), ("K", ctypes.c_int), ("V", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("eos", ctypes.c_int), ("flags", ctypes.c_uint),
+                ("ld", ctypes.c_longlong)]
+
+
+class bcmt_beam_tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p),
+                ("row_bytes", ctypes.c_longlong)]
+
+
 _VP = ctypes.c_void_p
 _P = ctypes.POINTER(bcmt_params)
 _PL = ctypes.POINTER(bcmt_linattn_params)
 _PE = ctypes.POINTER(bcmt_embedding_params)
 _PD = ctypes.POINTER(bcmt_dropout_params)
+_PN = ctypes.POINTER(bcmt_norm_params)
+_PA = ctypes.POINTER(bcmt_adamw_params)
+_PB = ctypes.POINTER(bcmt_beam_params)
 
 
 def _load():
@@ -117,6 +150,23 @@ def _load():
     lib.bcmt_embedding_backward.restype = ctypes.c_int
     lib.bcmt_dropout.argtypes = [_PD] + [_VP] * 4
     lib.bcmt_dropout.restype = ctypes.c_int
+    lib.bcmt_residual_norm_forward.argtypes = [_PN] + [_VP] * 10
+    lib.bcmt_residual_norm_forward.restype = ctypes.c_int
+    lib.bcmt_residual_norm_workspace_size.argtypes = [_PN, ctypes.c_int]
+    lib.bcmt_residual_norm_workspace_size.restype = ctypes.c_size_t
+    lib.bcmt_residual_norm_backward.argtypes = [_PN] + [_VP] * 17
+    lib.bcmt_residual_norm_backward.restype = ctypes.c_int
+    lib.bcmt_adamw_step.argtypes = [_PA, _VP, _VP]
+    lib.bcmt_adamw_step.restype = ctypes.c_int
+    lib.bcmt_adamw_values.argtypes = [_VP] * 6 + [ctypes.c_longlong, _VP]
+    lib.bcmt_adamw_values.restype = ctypes.c_int
+    lib.bcmt_beam_workspace_size.argtypes = [_PB]
+    lib.bcmt_beam_workspace_size.restype = ctypes.c_size_t
+    lib.bcmt_beam_select.argtypes = [_PB] + [_VP] * 9
+    lib.bcmt_beam_select.restype = ctypes.c_int
+    lib.bcmt_beam_reorder.argtypes = [_VP, ctypes.c_int, ctypes.c_int, _VP, ctypes.c_int,
+                                      ctypes.c_uint, _VP]
+    lib.bcmt_beam_reorder.restype = ctypes.c_int
     lib.bcmt_test_set_tensor_cores.argtypes = [ctypes.c_int, ctypes.c_int]
     lib.bcmt_test_set_tensor_cores.restype = ctypes.c_int
     lib.bcmt_test_gemm.argtypes = [ctypes.c_int] * 6 + [_VP, ctypes.c_long, ctypes.c_long, _VP,
@@ -144,7 +194,9 @@ EXPORTED = ("bcmt_workspace_size", "bcmt_scratch_size", "bcmt_forward", "bcmt_ba
             "bcmt_decode_state_size", "bcmt_decode_reset", "bcmt_decode_step",
             "bcmt_linattn_workspace_size", "bcmt_linattn_forward", "bcmt_linattn_backward",
             "bcmt_embedding_workspace_size", "bcmt_embedding_forward", "bcmt_embedding_backward",
-            "bcmt_dropout",
+            "bcmt_dropout", "bcmt_residual_norm_forward", "bcmt_residual_norm_workspace_size",
+            "bcmt_residual_norm_backward", "bcmt_adamw_step", "bcmt_adamw_values",
+            "bcmt_beam_workspace_size", "bcmt_beam_select", "bcmt_beam_reorder",
             "bcmt_test_set_tensor_cores", "bcmt_test_gemm", "bcmt_test_gemm_group", "bcmt_test_attn",
             "bcmt_test_wait_expiry")
 
@@ -271,6 +323,53 @@ def bcmt_embedding_backward(p: bcmt_embedding_params, ids, d_out, d_weight, work
 
 def bcmt_dropout(p: bcmt_dropout_params, x, residual, y, stream=None) -> None:
     _check(LIB.bcmt_dropout(ctypes.byref(p), _ptr(x), _ptr(residual), _ptr(y), _stream(stream)))
+
+
+def bcmt_residual_norm_forward(p: bcmt_norm_params, branch, x, weight, bias, post_weight, post_bias,
+                               gate, h, n, stream=None) -> None:
+    _check(LIB.bcmt_residual_norm_forward(ctypes.byref(p), _ptr(branch), _ptr(x), _ptr(weight),
+                                          _ptr(bias), _ptr(post_weight), _ptr(post_bias), _ptr(gate),
+                                          _ptr(h), _ptr(n), _stream(stream)))
+
+
+def bcmt_residual_norm_workspace_size(p: bcmt_norm_params, post: bool) -> int:
+    return LIB.bcmt_residual_norm_workspace_size(ctypes.byref(p), int(post))
+
+
+def bcmt_residual_norm_backward(p: bcmt_norm_params, dh, dn, branch, h, weight, post_weight,
+                                post_bias, gate, dbranch, dx, dweight, dbias, dpost_weight,
+                                dpost_bias, dgate, workspace, stream=None) -> None:
+    _check(LIB.bcmt_residual_norm_backward(
+        ctypes.byref(p), _ptr(dh), _ptr(dn), _ptr(branch), _ptr(h), _ptr(weight), _ptr(post_weight),
+        _ptr(post_bias), _ptr(gate), _ptr(dbranch), _ptr(dx), _ptr(dweight), _ptr(dbias),
+        _ptr(dpost_weight), _ptr(dpost_bias), _ptr(dgate), _ptr(workspace), _stream(stream)))
+
+
+def bcmt_adamw_step(p: bcmt_adamw_params, tensors, stream=None) -> None:
+    """tensors: a ctypes array of bcmt_adamw_tensor, or its address."""
+    _check(LIB.bcmt_adamw_step(ctypes.byref(p), tensors, _stream(stream)))
+
+
+def bcmt_adamw_values(m_codes, m_scale, v_codes, v_scale, m, v, n: int, stream=None) -> None:
+    _check(LIB.bcmt_adamw_values(_ptr(m_codes), _ptr(m_scale), _ptr(v_codes), _ptr(v_scale),
+                                 _ptr(m), _ptr(v), n, _stream(stream)))
+
+
+def bcmt_beam_workspace_size(p: bcmt_beam_params) -> int:
+    return LIB.bcmt_beam_workspace_size(ctypes.byref(p))
+
+
+def bcmt_beam_select(p: bcmt_beam_params, logits, scores, finished, scores_out, parents, tokens,
+                     finished_out, workspace, stream=None) -> None:
+    _check(LIB.bcmt_beam_select(ctypes.byref(p), _ptr(logits), _ptr(scores), _ptr(finished),
+                                _ptr(scores_out), _ptr(parents), _ptr(tokens), _ptr(finished_out),
+                                _ptr(workspace), _stream(stream)))
+
+
+def bcmt_beam_reorder(parents, N: int, K: int, tensors, count: int, flags: int = 0,
+                      stream=None) -> None:
+    """tensors: a ctypes array of bcmt_beam_tensor, or its address."""
+    _check(LIB.bcmt_beam_reorder(_ptr(parents), N, K, tensors, count, flags, _stream(stream)))
 
 
 def bcmt_profile_reset() -> None:

@@ -15,9 +15,12 @@
 
 #include "../../include/bcmt.h"
 #include "../../include/bcmt_testing.h"
+#include "adamw.h"
+#include "beam.h"
 #include "common.cuh"
 #include "internal.h"
 #include "linattn.h"
+#include "norms.h"
 #include "tc.cuh"
 
 namespace bcmt {
@@ -645,6 +648,90 @@ bcmt_status check_ids(const bcmt_embedding_params* p, const void* ids) {
     return fail(BCMT_ERR_ALIGN, "ids is not aligned to its %d-byte elements", p->id_bytes);
   return BCMT_OK;
 }
+bcmt_status check_norm(const bcmt_norm_params* p) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  BCMT_TRY(check_dtype(p->wtype));
+  if (p->rms != 0 && p->rms != 1) return fail(BCMT_ERR_ARG, "rms must be 0 or 1 (got %d)", p->rms);
+  if (p->rows < 0 || p->rows > (1ll << 30))
+    return fail(BCMT_ERR_SHAPE, "rows = %lld must be in [0, 2^30]", p->rows);
+  if (p->D < 1) return fail(BCMT_ERR_SHAPE, "D = %d must be >= 1", p->D);
+  if (p->D > kNormMaxD)
+    return fail(BCMT_ERR_UNSUPPORTED, "D = %d: rows of up to %d channels", p->D, kNormMaxD);
+  if (p->gates < 0 || (p->gates > 0 && p->rows % p->gates != 0))
+    return fail(BCMT_ERR_SHAPE, "gates = %lld must divide rows = %lld", p->gates, p->rows);
+  if (!isfinite(p->alpha)) return fail(BCMT_ERR_ARG, "alpha must be finite");
+  if (!isfinite(p->eps) || p->eps < 0.f) return fail(BCMT_ERR_ARG, "eps must be finite and >= 0");
+  return check_flags(p->flags);
+}
+bcmt_status check_norm_weights(const bcmt_norm_params* p, const void* weight, const void* bias,
+                               const void* post_weight, const void* post_bias, const void* gate) {
+  BCMT_TRY(check_ptr(weight, "weight"));
+  BCMT_TRY(check_opt(bias, "bias"));
+  BCMT_TRY(check_opt(post_weight, "post_weight"));
+  BCMT_TRY(check_opt(post_bias, "post_bias"));
+  if (post_bias && !post_weight) return fail(BCMT_ERR_ARG, "post_bias without post_weight");
+  BCMT_TRY(check_opt(gate, "gate"));
+  if (gate ? p->gates < 1 : p->gates != 0)
+    return fail(BCMT_ERR_ARG, "gates = %lld %s a gate", p->gates, gate ? "with" : "without");
+  return BCMT_OK;
+}
+
+bcmt_status check_adamw(const bcmt_adamw_params* p, const bcmt_adamw_tensor* t) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  if (p->bits != 32 && p->bits != 8)
+    return fail(BCMT_ERR_ARG, "bits must be 32 or 8 (got %d)", p->bits);
+  if (p->count < 0) return fail(BCMT_ERR_ARG, "count = %d must be >= 0", p->count);
+  if (!(p->beta1 >= 0.0 && p->beta1 < 1.0 && p->beta2 >= 0.0 && p->beta2 < 1.0))
+    return fail(BCMT_ERR_ARG, "betas %g, %g must be in [0, 1)", p->beta1, p->beta2);
+  if (!(p->lr >= 0.0 && isfinite(p->lr) && p->eps >= 0.0 && isfinite(p->eps) &&
+        p->weight_decay >= 0.0 && isfinite(p->weight_decay)))
+    return fail(BCMT_ERR_ARG, "lr, eps and weight_decay must be finite and >= 0");
+  if (p->step < 1 && !p->step_ptr) return fail(BCMT_ERR_ARG, "step = %lld must be >= 1", p->step);
+  if (reinterpret_cast<uintptr_t>(p->step_ptr) % 8 || reinterpret_cast<uintptr_t>(p->lr_ptr) % 4 ||
+      reinterpret_cast<uintptr_t>(p->grad_scale) % 4)
+    return fail(BCMT_ERR_ALIGN, "step_ptr, lr_ptr or grad_scale is not aligned to its type");
+  BCMT_TRY(check_flags(p->flags));
+  if (p->count > 0 && !t) return fail(BCMT_ERR_ARG, "tensors is NULL");
+  const uintptr_t es = p->dtype == BCMT_F32 ? 4 : 2;
+  for (int i = 0; i < p->count; ++i) {
+    if (t[i].n < 0 || t[i].n > (1ll << 40))
+      return fail(BCMT_ERR_SHAPE, "tensor %d: n = %lld must be in [0, 2^40]", i, t[i].n);
+    if (t[i].n == 0) continue;
+    if (!t[i].p || !t[i].g || !t[i].m || !t[i].v)
+      return fail(BCMT_ERR_ARG, "tensor %d: p, g, m or v is NULL", i);
+    if ((t[i].master != nullptr) != (t[0].master != nullptr))
+      return fail(BCMT_ERR_ARG, "tensor %d: masters for all tensors or none", i);
+    if (t[i].master && p->dtype == BCMT_F32)
+      return fail(BCMT_ERR_ARG, "tensor %d: float32 parameters have no masters", i);
+    if (p->bits == 8 && (!t[i].m_scale || !t[i].v_scale))
+      return fail(BCMT_ERR_ARG, "tensor %d: m_scale or v_scale is NULL", i);
+    uintptr_t words = reinterpret_cast<uintptr_t>(t[i].master);
+    if (p->bits == 8) words |= reinterpret_cast<uintptr_t>(t[i].m_scale) | reinterpret_cast<uintptr_t>(t[i].v_scale);
+    else words |= reinterpret_cast<uintptr_t>(t[i].m) | reinterpret_cast<uintptr_t>(t[i].v);
+    if (words % 4 || (reinterpret_cast<uintptr_t>(t[i].p) | reinterpret_cast<uintptr_t>(t[i].g)) % es)
+      return fail(BCMT_ERR_ALIGN, "tensor %d: a buffer is not aligned to its type", i);
+  }
+  return BCMT_OK;
+}
+
+bcmt_status check_beam(const bcmt_beam_params* p) {
+  if (!p) return fail(BCMT_ERR_ARG, "params is NULL");
+  BCMT_TRY(check_dtype(p->dtype));
+  if (p->N < 0) return fail(BCMT_ERR_SHAPE, "N = %d must be >= 0", p->N);
+  if (p->K < 1 || p->K > kBeamMaxK)
+    return fail(BCMT_ERR_SHAPE, "K = %d must be in [1, %d]", p->K, kBeamMaxK);
+  if (p->V < 1 || p->V >= (1 << 24)) return fail(BCMT_ERR_SHAPE, "V = %d must be in [1, 2^24)", p->V);
+  if ((long long)p->N * p->K > (1ll << 22))
+    return fail(BCMT_ERR_SHAPE, "N * K = %lld beams are too many", (long long)p->N * p->K);
+  // a CTA of the grid per chunk of a row
+  if ((long long)p->N * p->K * ((p->V + 2047) / 2048) > 0x7fffffffll)
+    return fail(BCMT_ERR_SHAPE, "N * K * V is too large");
+  if (p->eos >= p->V) return fail(BCMT_ERR_ARG, "eos = %d must be below V = %d", p->eos, p->V);
+  if (p->ld < p->V) return fail(BCMT_ERR_ARG, "row stride %lld must be >= V = %d", p->ld, p->V);
+  return check_flags(p->flags);
+}
 bcmt_status finish_flags(unsigned flags, cudaStream_t s) {
   return (flags & BCMT_FLAG_CHECK) ? bcmt_device_status(s) : BCMT_OK;
 }
@@ -696,6 +783,9 @@ bcmt_status bcmt_device_status(void* stream) {
   if (v & kStatusBadIndex) return fail(BCMT_ERR_ARG, "an embedding id was outside its table");
   if (v & kStatusBadDecay)
     return fail(BCMT_ERR_ARG, "a decay of linear attention was outside [0, 1]");
+  if (v & kStatusBadLogit)
+    return fail(BCMT_ERR_ARG, "a logit or score of beam search was NaN or +inf");
+  if (v & kStatusBadParent) return fail(BCMT_ERR_ARG, "a parent was outside its search's beams");
   if (v) return fail(BCMT_ERR_CUDA, "device status 0x%x", v);
   return BCMT_OK;
 }
@@ -1432,6 +1522,207 @@ bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void
   cudaError_t e = dropout(lc, p->dtype, x, residual, y, p->n, p->p, p->seed, p->offset, p->step);
   if (e != cudaSuccess) return cuda_fail(e, "dropout");
   return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_residual_norm_forward(const bcmt_norm_params* p, const void* branch,
+                                       const void* x, const void* weight, const void* bias,
+                                       const void* post_weight, const void* post_bias,
+                                       const void* gate, void* h, void* n, void* stream) {
+  BCMT_TRY(check_norm(p));
+  BCMT_TRY(check_norm_weights(p, weight, bias, post_weight, post_bias, gate));
+  if (p->rows > 0) {
+    BCMT_TRY(check_ptr(branch, "branch"));
+    BCMT_TRY(check_ptr(x, "x"));
+    BCMT_TRY(check_ptr(h, "h"));
+    BCMT_TRY(check_ptr(n, "n"));
+  }
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  NormFwd a{p->rows, p->D, p->rms == 0, p->wtype == BCMT_BF16,
+            p->gates > 0 ? std::max(1ll, p->rows / p->gates) : 1, p->alpha, p->eps, branch, x,
+            weight, bias, post_weight, post_bias, gate, h, n};
+  cudaError_t e = norm_forward(lc, p->dtype, a);
+  if (e != cudaSuccess) return cuda_fail(e, "residual norm forward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+size_t bcmt_residual_norm_workspace_size(const bcmt_norm_params* p, int post) {
+  if (check_norm(p) != BCMT_OK) return 0;
+  if (p->rows == 0) return 256;
+  const NormPlan pl = norm_plan(p->rows, p->D, p->gates, post != 0, device_sms());
+  return al256(pl.part_bytes) + al256(std::max<size_t>(256, pl.gate_bytes));
+}
+
+bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* dh, const void* dn,
+                                        const void* branch, const void* h, const void* weight,
+                                        const void* post_weight, const void* post_bias,
+                                        const void* gate, void* dbranch, void* dx, void* dweight,
+                                        void* dbias, void* dpost_weight, void* dpost_bias,
+                                        void* dgate, void* workspace, void* stream) {
+  BCMT_TRY(check_norm(p));
+  BCMT_TRY(check_norm_weights(p, weight, nullptr, post_weight, post_bias, gate));
+  if (p->rows > 0) {
+    BCMT_TRY(check_opt(dh, "dh"));
+    BCMT_TRY(check_ptr(dn, "dn"));
+    BCMT_TRY(check_ptr(branch, "branch"));
+    BCMT_TRY(check_ptr(h, "h"));
+    BCMT_TRY(check_ptr(dbranch, "dbranch"));
+    BCMT_TRY(check_opt(dx, "dx"));
+    BCMT_TRY(check_ptr(workspace, "workspace"));
+  }
+  BCMT_TRY(check_opt(dweight, "dweight"));
+  BCMT_TRY(check_opt(dbias, "dbias"));
+  BCMT_TRY(check_opt(dpost_weight, "dpost_weight"));
+  BCMT_TRY(check_opt(dpost_bias, "dpost_bias"));
+  BCMT_TRY(check_opt(dgate, "dgate"));
+  if ((dpost_weight || dpost_bias) && !post_weight)
+    return fail(BCMT_ERR_ARG, "gradients of a post norm without post_weight");
+  if (dgate && !gate) return fail(BCMT_ERR_ARG, "dgate without a gate");
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  cudaError_t e = cudaSuccess;
+  if (p->rows == 0) {
+    const size_t wb = (size_t)p->D * (p->wtype == BCMT_BF16 ? 2 : 4);
+    for (void* out : {dweight, dbias, dpost_weight, dpost_bias})
+      if (out && e == cudaSuccess) e = fill_zero(lc, out, wb);
+    if (dgate && e == cudaSuccess)
+      e = fill_zero(lc, dgate, (size_t)p->gates * p->D * (p->dtype == BCMT_BF16 ? 2 : 4));
+  } else {
+    const NormPlan pl = norm_plan(p->rows, p->D, p->gates, post_weight != nullptr, device_sms());
+    NormBwd a{};
+    a.D = p->D;
+    a.layer = p->rms == 0;
+    a.w_bf16 = p->wtype == BCMT_BF16;
+    a.group_rows = p->gates > 0 ? p->rows / p->gates : 1;
+    a.alpha = p->alpha;
+    a.eps = p->eps;
+    a.dh = dh;
+    a.dn = dn;
+    a.branch = branch;
+    a.h = h;
+    a.weight = weight;
+    a.post_weight = post_weight;
+    a.post_bias = post_bias;
+    a.gate = gate;
+    a.dbranch = dbranch;
+    a.dx = dx;
+    a.dgate = dgate;
+    a.part = static_cast<float*>(workspace);
+    a.gate_part = a.part + al256(pl.part_bytes) / 4;
+    NormJoin j{p->D, p->wtype == BCMT_BF16, p->dtype == BCMT_BF16,
+               {dweight, dbias, dpost_weight, dpost_bias}, dgate, a.part, a.gate_part, 0, 0, 0};
+    e = norm_backward(lc, p->dtype, pl, a, j);
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "residual norm backward");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_adamw_step(const bcmt_adamw_params* p, const bcmt_adamw_tensor* tensors,
+                            void* stream) {
+  BCMT_TRY(check_adamw(p, tensors));
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  const double t = (double)p->step;
+  const double bc1 = -expm1(t * log(p->beta1)), bc2 = -expm1(t * log(p->beta2));
+  const AdamwHyper h{(float)p->beta1, (float)(1.0 - p->beta1), (float)p->beta2,
+                     (float)(1.0 - p->beta2), (float)p->eps, (float)p->lr, (float)p->weight_decay,
+                     (float)(p->lr / bc1), (float)(1.0 - p->lr * p->weight_decay),
+                     (float)(1.0 / sqrt(bc2)), log(p->beta1), log(p->beta2), p->step, p->step_ptr,
+                     p->lr_ptr, p->grad_scale};
+  static_assert(sizeof(AdamwTensor) == sizeof(bcmt_adamw_tensor), "the same layout");
+  bool master = false;
+  for (int i = 0; i < p->count; ++i) master |= tensors[i].master != nullptr;
+  cudaError_t e = adamw_step(lc, p->dtype, p->bits, master, h,
+                             reinterpret_cast<const AdamwTensor*>(tensors), p->count);
+  if (e != cudaSuccess) return cuda_fail(e, "AdamW step");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_adamw_values(const void* m_codes, const float* m_scale, const void* v_codes,
+                              const float* v_scale, float* m, float* v, long long n, void* stream) {
+  if (n < 0) return fail(BCMT_ERR_SHAPE, "n = %lld must be >= 0", n);
+  if (n > 0) {
+    BCMT_TRY(check_ptr(m_codes, "m_codes"));
+    BCMT_TRY(check_ptr(m_scale, "m_scale"));
+    BCMT_TRY(check_ptr(v_codes, "v_codes"));
+    BCMT_TRY(check_ptr(v_scale, "v_scale"));
+    BCMT_TRY(check_ptr(m, "m"));
+    BCMT_TRY(check_ptr(v, "v"));
+  }
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  cudaError_t e = adamw_values(lc, static_cast<const uint8_t*>(m_codes), m_scale,
+                               static_cast<const uint8_t*>(v_codes), v_scale, m, v, n);
+  if (e != cudaSuccess) return cuda_fail(e, "AdamW values");
+  return BCMT_OK;
+}
+
+size_t bcmt_beam_workspace_size(const bcmt_beam_params* p) {
+  if (check_beam(p) != BCMT_OK) return 0;
+  return al256(std::max<size_t>(256, beam_workspace(p->N, p->K, p->V, device_sms())));
+}
+
+bcmt_status bcmt_beam_select(const bcmt_beam_params* p, const void* logits, const float* scores,
+                             const void* finished, float* scores_out, long long* parents,
+                             long long* tokens, void* finished_out, void* workspace, void* stream) {
+  BCMT_TRY(check_beam(p));
+  if (finished && p->eos < 0) return fail(BCMT_ERR_ARG, "finished beams need an end token (eos >= 0)");
+  if (p->N > 0) {
+    if (!logits || !scores || !scores_out || !parents || !tokens || !finished_out)
+      return fail(BCMT_ERR_ARG, "logits, scores or an output is NULL");
+    const uintptr_t es = p->dtype == BCMT_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es ||
+        (reinterpret_cast<uintptr_t>(scores) | reinterpret_cast<uintptr_t>(scores_out)) % 4 ||
+        (reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(tokens)) % 8)
+      return fail(BCMT_ERR_ALIGN, "a buffer is not aligned to its type");
+    BCMT_TRY(check_ptr(workspace, "workspace"));
+  }
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  const BeamArgs a{p->N, p->K, p->V, p->eos, logits, p->ld, scores,
+                   static_cast<const uint8_t*>(finished), scores_out, parents, tokens,
+                   static_cast<uint8_t*>(finished_out), workspace};
+  cudaError_t e = beam_select(lc, p->dtype, device_sms(), a);
+  if (e != cudaSuccess) return cuda_fail(e, "beam selection");
+  return finish_flags(p->flags, lc.stream);
+}
+
+bcmt_status bcmt_beam_reorder(const long long* parents, int N, int K,
+                              const bcmt_beam_tensor* tensors, int count, unsigned flags,
+                              void* stream) {
+  if (N < 0 || K < 1 || K > kBeamMaxK || (long long)N * K > (1ll << 22))
+    return fail(BCMT_ERR_SHAPE, "N = %d, K = %d must be N >= 0, K in [1, %d], N * K <= 2^22", N, K,
+                kBeamMaxK);
+  if (count < 0) return fail(BCMT_ERR_ARG, "count = %d must be >= 0", count);
+  BCMT_TRY(check_flags(flags));
+  if (count > 0 && !tensors) return fail(BCMT_ERR_ARG, "tensors is NULL");
+  if (N > 0 && count > 0) {
+    if (!parents) return fail(BCMT_ERR_ARG, "parents is NULL");
+    if (reinterpret_cast<uintptr_t>(parents) % 8) return fail(BCMT_ERR_ALIGN, "parents is not 8-byte aligned");
+  }
+  for (int i = 0; i < count; ++i) {
+    const bcmt_beam_tensor& t = tensors[i];
+    if (t.row_bytes < 0 || t.row_bytes > (1ll << 40) / std::max(1, N))
+      return fail(BCMT_ERR_SHAPE, "tensor %d: row_bytes = %lld", i, t.row_bytes);
+    if (t.row_bytes == 0 || N == 0) continue;
+    if (!t.src || !t.dst) return fail(BCMT_ERR_ARG, "tensor %d: src or dst is NULL", i);
+    const uintptr_t s = reinterpret_cast<uintptr_t>(t.src), d = reinterpret_cast<uintptr_t>(t.dst);
+    const uintptr_t bytes = (uintptr_t)N * K * t.row_bytes;
+    if (s < d + bytes && d < s + bytes)
+      return fail(BCMT_ERR_ARG, "tensor %d: src and dst overlap", i);
+  }
+  unsigned* sp = status_ptr();
+  if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
+  Launch lc{static_cast<cudaStream_t>(stream), sp};
+  static_assert(sizeof(ReorderTensor) == sizeof(bcmt_beam_tensor), "the same layout");
+  cudaError_t e = beam_reorder(lc, parents, N, K, reinterpret_cast<const ReorderTensor*>(tensors), count);
+  if (e != cudaSuccess) return cuda_fail(e, "beam reordering");
+  return finish_flags(flags, lc.stream);
 }
 
 int bcmt_profile_read(const char** names, int* launches, double* ms, int cap) {

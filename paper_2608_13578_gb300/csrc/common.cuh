@@ -20,6 +20,8 @@ enum : unsigned {
   kStatusBadLaunch = 2u,
   kStatusBadIndex = 4u,  // an embedding id outside its table
   kStatusBadDecay = 8u,  // a decay of linear attention outside [0, 1]
+  kStatusBadLogit = 16u,   // a logit or score of beam search that is NaN or +inf
+  kStatusBadParent = 32u,  // a parent outside its search's beams
 };
 
 // Programmatic dependent launch.  Every kernel of the library is launched with

@@ -1,0 +1,152 @@
+// Rows of D channels over the threads of a warp or CTA: loads, stores and sums over a
+// row, shared by the kernels of the norms around a block.
+#pragma once
+
+#include "common.cuh"
+
+namespace bcmt {
+
+namespace {
+
+// Eight elements as they are stored.
+template <class T> struct Raw8;
+template <> struct Raw8<float> {
+  float4 a, b;
+};
+template <> struct Raw8<bf16> {
+  uint4 a;
+};
+__device__ __forceinline__ void widen(const Raw8<float>& r, float* v) {
+  v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
+  v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
+}
+__device__ __forceinline__ void widen(const Raw8<bf16>& r, float* v) { unpack8(r.a, v); }
+__device__ __forceinline__ void zero(Raw8<float>& r) {
+  r.a = r.b = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ void zero(Raw8<bf16>& r) { r.a = make_uint4(0, 0, 0, 0); }
+__device__ __forceinline__ void fetch(const float* p, Raw8<float>& r) {
+  r.a = *reinterpret_cast<const float4*>(p);
+  r.b = *reinterpret_cast<const float4*>(p + 4);
+}
+__device__ __forceinline__ void fetch(const bf16* p, Raw8<bf16>& r) {
+  r.a = *reinterpret_cast<const uint4*>(p);
+}
+__device__ __forceinline__ void gather8(const float* p, int step, int n, Raw8<float>& r) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? p[(long)e * step] : 0.f;
+  r.a = make_float4(v[0], v[1], v[2], v[3]);
+  r.b = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void gather8(const bf16* p, int step, int n, Raw8<bf16>& r) {
+  const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+  uint32_t v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < n ? q[(long)e * step] : 0u;
+  r.a = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// The eight columns of a row that thread t of `tpr` takes in its j-th turn: VEC, eight
+// consecutive ones in one 16-byte (fp32: two) access, for D a multiple of 8; else every
+// tpr-th column, so that a warp's accesses are consecutive.  `count`: how many of them
+// are below D.
+template <bool VEC>
+struct Cols {
+  int first, step, count;
+  __device__ __forceinline__ Cols(int t, int tpr, int j, int D) {
+    if (VEC) {
+      first = (t + j * tpr) * 8;
+      step = 1;
+      count = first < D ? 8 : 0;
+    } else {
+      first = t + j * 8 * tpr;
+      step = tpr;
+      count = first < D ? min(8, (D - first + tpr - 1) / tpr) : 0;
+    }
+  }
+};
+
+template <bool VEC, class T>
+__device__ __forceinline__ void read8(const T* row, const Cols<VEC>& c, bool live, Raw8<T>& r) {
+  if (VEC) {
+    if (live && c.count) fetch(row + c.first, r);
+    else zero(r);
+  } else {
+    gather8(row + c.first, c.step, live ? c.count : 0, r);
+  }
+}
+// A vector of weights (either type), zeros past D.
+template <bool VEC>
+__device__ __forceinline__ void read_weight(const void* w, bool is_bf16, const Cols<VEC>& c,
+                                            float* v) {
+  if (is_bf16) {
+    Raw8<bf16> r;
+    read8<VEC>(static_cast<const bf16*>(w), c, true, r);
+    widen(r, v);
+  } else {
+    Raw8<float> r;
+    read8<VEC>(static_cast<const float*>(w), c, true, r);
+    widen(r, v);
+  }
+}
+template <bool VEC, class T>
+__device__ __forceinline__ void write8(T* row, const Cols<VEC>& c, const float* v) {
+  if (VEC) {
+    if (c.count) store8(row + c.first, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < c.count) row[c.first + (long)e * c.step] = from_f<T>(v[e]);
+  }
+}
+
+// Sums of NV values over the threads of a row, given to all of them.  TPR <= 32: lanes
+// of a warp.  Else the row's warps add through shared memory, `slot` alternating between
+// two buffers of NV floats per warp so that one barrier a sum is enough.
+template <int TPR, int NV>
+__device__ __forceinline__ void lane_sums(float (&v)[NV]) {
+#pragma unroll
+  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  }
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+constexpr int kMaxWarps = 16, kMaxSums = 4;
+struct RowShared {
+  float4 sums[2][kMaxWarps];
+};
+template <int TPR, int NV>
+__device__ __forceinline__ void row_sums(float (&v)[NV], RowShared& sh, int& slot, int warp0,
+                                         int nw, int bar) {
+  static_assert(NV <= kMaxSums, "");
+  lane_sums<TPR, NV>(v);
+  if (TPR > 32) {
+    float4* s = sh.sums[slot];
+    slot ^= 1;
+    if ((threadIdx.x & 31) == 0) {
+      float4 f = make_float4(v[0], NV > 1 ? v[NV > 1 ? 1 : 0] : 0.f, NV > 2 ? v[NV > 2 ? 2 : 0] : 0.f,
+                             NV > 3 ? v[NV > 3 ? 3 : 0] : 0.f);
+      s[threadIdx.x >> 5] = f;
+    }
+    bar_sync(bar, nw * 32);
+    float4 a = s[warp0];
+    for (int w = 1; w < nw; ++w) {
+      const float4 b = s[warp0 + w];
+      a.x += b.x;
+      if (NV > 1) a.y += b.y;
+      if (NV > 2) a.z += b.z;
+      if (NV > 3) a.w += b.w;
+    }
+    const float f[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = f[i];
+  }
+}
+
+}  // namespace
+
+}  // namespace bcmt

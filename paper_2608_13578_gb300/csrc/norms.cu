@@ -1,0 +1,254 @@
+// The end of a block of the language model and the norm before the next one:
+//   z = post(y) or y,   h = alpha x + g z,   n = pre(h)
+// over rows of D channels, and the gradients.  post and pre are layer norms
+// (v - mean) r w + b with r = 1 / sqrt(mean (v - mean)^2 + eps), or root-mean-square
+// norms (mean = 0); the gate g is a row of D channels for every group of consecutive
+// rows (one for all, one per sequence, one per row), or absent.
+//
+// Backward, with hh = (h - mean) r the normalised rows and all means over a row:
+//   e  = dn w,   s = dh + r (e - mean(e) - hh mean(e hh))          (the sum's gradient)
+//   dx = alpha s,   dg = sum over the gate's rows of s z,   dz = g s
+//   dy = r_y (dz pw - mean(dz pw) - yh mean(dz pw yh)),
+//   dw = sum dn hh,  db = sum dn,  dpw = sum dz yh,  dpb = sum dz  (over the rows)
+// (mean(e) and mean(dz pw) only in layer norms).  Both passes read each row once into
+// registers and take the statistics there: the mean first, then the squares around it.
+// Everything between the loads and the stores is fp32, rounded once to the stored type.
+#include <algorithm>
+
+#include "internal.h"
+#include "norm_rows.cuh"
+#include "norms.h"
+
+namespace bcmt {
+
+// Forward: a row belongs to TPR threads, each with J times eight of its columns; the row
+// stays in registers between its loads and its stores.
+template <class T, int TPR, int J, bool VEC>
+__global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_fwd_kernel(const NormFwd a) {
+  __shared__ RowShared sh;
+  constexpr int E = 8 * J;
+  pdl_enter();
+  const int t = threadIdx.x % TPR;
+  const long long row = (long long)blockIdx.x * (blockDim.x / TPR) + threadIdx.x / TPR;
+  const bool live = row < a.rows;
+  const int D = a.D, warp0 = (threadIdx.x / TPR) * (TPR / 32), bar = 1 + threadIdx.x / TPR;
+  const long long at = (live ? row : 0) * D;
+  int slot = 0;
+  float z[E];
+  Raw8<T> xr[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const Cols<VEC> c(t, TPR, j, D);
+    Raw8<T> y;
+    read8<VEC>(static_cast<const T*>(a.branch) + at, c, live, y);
+    read8<VEC>(static_cast<const T*>(a.x) + at, c, live, xr[j]);
+    widen(y, z + 8 * j);
+  }
+  const float inv = 1.f / D;
+  // mean and 1 / deviation of the row in z
+  auto stats = [&](float& mean, float& r) {
+    mean = 0.f;
+    if (a.layer) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[0] += z[e];
+      row_sums<TPR, 1>(s, sh, slot, warp0, TPR / 32, bar);
+      mean = s[0] * inv;
+    }
+    float q[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const Cols<VEC> c(t, TPR, j, D);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = z[8 * j + e] - mean;
+        q[0] += e < c.count ? d * d : 0.f;
+      }
+    }
+    row_sums<TPR, 1>(q, sh, slot, warp0, TPR / 32, bar);
+    r = 1.f / sqrtf(q[0] * inv + a.eps);
+  };
+  float mean, r;
+  if (a.post_weight) {
+    stats(mean, r);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const Cols<VEC> c(t, TPR, j, D);
+      float w[8], b[8] = {};
+      read_weight<VEC>(a.post_weight, a.w_bf16, c, w);
+      if (a.post_bias) read_weight<VEC>(a.post_bias, a.w_bf16, c, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[8 * j + e] = (z[8 * j + e] - mean) * r * w[e] + b[e];
+    }
+  }
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (live ? row : 0) / a.group_rows * D
+                         : nullptr;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const Cols<VEC> c(t, TPR, j, D);
+    float x[8];
+    widen(xr[j], x);
+    if (gate) {
+      Raw8<T> gr;
+      float g[8];
+      read8<VEC>(gate, c, live, gr);
+      widen(gr, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[8 * j + e] *= g[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[8 * j + e] = fmaf(a.alpha, x[e], z[8 * j + e]);
+    if (live) write8<VEC>(static_cast<T*>(a.h) + at, c, z + 8 * j);
+  }
+  stats(mean, r);
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const Cols<VEC> c(t, TPR, j, D);
+    float w[8], b[8] = {}, n[8];
+    read_weight<VEC>(a.weight, a.w_bf16, c, w);
+    if (a.bias) read_weight<VEC>(a.bias, a.w_bf16, c, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n[e] = (z[8 * j + e] - mean) * r * w[e] + b[e];
+    if (live) write8<VEC>(static_cast<T*>(a.n) + at, c, n);
+  }
+}
+
+// Sums of the CTAs' and segments' parts: blockIdx.y is one of the four vectors of
+// weights, or 4 + a gate; a CTA adds 32 columns with 8 lines of threads, each over every
+// eighth part, then the lines in order.
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormJoin a) {
+  __shared__ float s[8][33];
+  pdl_enter();
+  const int col = blockIdx.x * 32 + (threadIdx.x & 31), line = threadIdx.x >> 5;
+  const long long y = blockIdx.y + (long long)a.first;
+  const float* in;
+  long long n, stride;
+  void* out;
+  bool is_bf16;
+  if (y < 4) {
+    in = a.part + y * a.D;
+    n = a.nparts;
+    stride = 4ll * a.D;
+    out = a.out[y];
+    is_bf16 = a.w_bf16;
+  } else {
+    in = a.gate_part + (y - 4) * a.segs_per_group * a.D;
+    n = a.segs_per_group;
+    stride = a.D;
+    out = a.dgate;
+    is_bf16 = a.t_bf16;
+  }
+  if (!out) return;
+  float v = 0.f;
+  if (col < a.D) {
+#pragma unroll 4
+    for (long long i = line; i < n; i += 8) v += in[i * stride + col];
+  }
+  s[line][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (line == 0 && col < a.D) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+    const long long at = y < 4 ? col : (y - 4) * a.D + col;
+    if (is_bf16) static_cast<bf16*>(out)[at] = from_f<bf16>(v);
+    else static_cast<float*>(out)[at] = v;
+  }
+}
+
+namespace {
+
+template <class T, int TPR, int J>
+cudaError_t fwd_shape(const Launch& lc, const NormFwd& a) {
+  constexpr int threads = TPR > 128 ? TPR : 128, rows = threads / TPR;
+  const dim3 grid((unsigned)((a.rows + rows - 1) / rows));
+  return a.D % 8 == 0 ? launch_k(norm_fwd_kernel<T, TPR, J, true>, grid, dim3(threads), 0, lc.stream, a)
+                      : launch_k(norm_fwd_kernel<T, TPR, J, false>, grid, dim3(threads), 0, lc.stream, a);
+}
+template <class T>
+cudaError_t fwd_typed(const Launch& lc, const NormFwd& a) {
+  if (a.D <= 128) return fwd_shape<T, 16, 1>(lc, a);
+  if (a.D <= 256) return fwd_shape<T, 32, 1>(lc, a);
+  if (a.D <= 512) return fwd_shape<T, 32, 2>(lc, a);
+  if (a.D <= 1024) return fwd_shape<T, 32, 4>(lc, a);
+  if (a.D <= 2048) return fwd_shape<T, 64, 4>(lc, a);
+  if (a.D <= 4096) return fwd_shape<T, 128, 4>(lc, a);
+  return fwd_shape<T, 256, 4>(lc, a);
+}
+
+}  // namespace
+
+NormPlan norm_plan(long long rows, int D, long long groups, bool post, int sms) {
+  NormPlan p{};
+  if (rows < 1) return p;
+  const int need = (D + 7) / 8;   // threads of eight columns
+  int ctas_per_sm;
+  if (need <= 32) {
+    p.tpr = need <= 16 ? 16 : 32;
+    p.threads = 256;
+    ctas_per_sm = 2;
+  } else if (need <= 256) {
+    p.tpr = (need + 31) / 32 * 32;
+    p.threads = 256 / p.tpr * p.tpr;
+    ctas_per_sm = 2;
+  } else {
+    p.wide = need > 512;
+    p.tpr = ((p.wide ? (need + 1) / 2 : need) + 31) / 32 * 32;
+    p.threads = p.tpr;
+    ctas_per_sm = 1;
+  }
+  p.rows_per_cta = p.threads / p.tpr;
+  p.smem = p.wide ? (post ? 5 : 3) * 2 * 8 * 512 * 4 : p.rows_per_cta > 1 ? 8 * 512 * 4 : 0;
+  p.ctas = (int)std::min<long long>((rows + p.rows_per_cta - 1) / p.rows_per_cta,
+                                    (long long)sms * ctas_per_sm);
+  // segments: each gate's rows in equal parts, so that the workers' longest walk is
+  // short; where rows have gates of their own (or none), all rows are one group
+  const long long g = groups == 0 || groups == rows ? 1 : groups, gr = rows / g;
+  const long long workers = (long long)p.ctas * p.rows_per_cta;
+  long long best = -1;
+  for (long long turns = (g + workers - 1) / workers, i = 0; i < 8; ++i, ++turns) {
+    const long long s = std::min(gr, turns * workers / g), len = (gr + s - 1) / s;
+    if (best < 0 || turns * len < best) {
+      best = turns * len;
+      p.segs_per_group = (gr + len - 1) / len;
+      p.seg_rows = len;
+      p.turns = (int)((g * p.segs_per_group + workers - 1) / workers);
+    }
+  }
+  p.seg_group_rows = gr;
+  p.nseg = g * p.segs_per_group;
+  p.part_bytes = (size_t)p.ctas * 4 * D * 4;
+  p.gate_bytes = groups > 0 && groups < rows && p.segs_per_group > 1 ? (size_t)p.nseg * D * 4 : 0;
+  return p;
+}
+
+cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a) {
+  if (a.rows == 0) return cudaSuccess;
+  return dtype == 0 ? fwd_typed<float>(lc, a) : fwd_typed<bf16>(lc, a);
+}
+
+cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormBwd a,
+                          const NormJoin& j) {
+  if (pl.ctas == 0) return cudaSuccess;
+  a.tpr = pl.tpr;
+  a.rows_per_cta = pl.rows_per_cta;
+  a.seg_rows = pl.seg_rows;
+  a.segs_per_group = pl.segs_per_group;
+  a.seg_group_rows = pl.seg_group_rows;
+  a.nseg = pl.nseg;
+  a.turns = pl.turns;
+  cudaError_t e = dtype == 0 ? norm_bwd_f32(lc, a, pl) : norm_bwd_bf16(lc, a, pl);
+  if (e != cudaSuccess) return e;
+  // gates beyond the grid's second axis take further launches
+  const long long gates = pl.gate_bytes ? pl.nseg / pl.segs_per_group : 0, all = 4 + gates;
+  for (long long y = 0; y < all && e == cudaSuccess; y += 65535) {
+    NormJoin q = j;
+    q.first = y;
+    q.nparts = pl.ctas;
+    q.segs_per_group = pl.segs_per_group;
+    e = launch_k(norm_join_kernel, dim3((a.D + 31) / 32, (unsigned)std::min<long long>(65535, all - y)),
+                 dim3(256), 0, lc.stream, q);
+  }
+  return e;
+}
+
+}  // namespace bcmt

@@ -1,0 +1,175 @@
+"""The end of a block of the language model fused with the norm before the next:
+``h = residual_scale * x + gate * post(branch)``, ``n = pre(h)``.
+
+Marshalling only, as in ``lm_ops``: each call runs the library's kernels
+(``include/bcmt.h``) on the current CUDA stream.  ``residual_norm`` is
+differentiable (once); ``residual_norm_forward`` and ``residual_norm_backward`` are
+the bare calls.  Arguments that the library would misread raise ``ValueError``;
+what the library refuses raises ``bcmt.BCMTError``.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import Optional
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import bcmt as C
+from .lm_ops import (_address, _buffer, _check, _dense, _device, _dtype, _number, _on_its_device,
+                     _raw_stream)
+
+KINDS = ("layer", "rms")
+
+
+@functools.lru_cache(maxsize=4096)
+def _plan(rows, D, dt, wt, rms, gates, alpha, eps, post):
+    """(parameters by reference, bytes of the backward's workspace)."""
+    p = C.bcmt_norm_params(rows, D, dt, wt, rms, gates, 0, alpha, eps)
+    return ctypes.byref(p), C.bcmt_residual_norm_workspace_size(p, post)
+
+
+def _gates(gate, shape) -> int:
+    """Rows of a gate that broadcasts to ``shape``: [D], or the leading dimensions of
+    ``shape``, ones, and D, so that consecutive rows share one."""
+    g = tuple(gate.shape)
+    if g == tuple(shape):
+        return gate.numel() // shape[-1] if shape[-1] else 0
+    full = (1,) * (len(shape) - len(g)) + g
+    i = len(full) - 1
+    while i > 0 and full[i - 1] == 1:
+        i -= 1
+    if len(g) < 1 or len(full) != len(shape) or full[-1] != shape[-1] or full[:i] != tuple(shape[:i]):
+        raise ValueError(f"gate must be [D] or leading dimensions of {tuple(shape)}, ones and D, "
+                         f"not {g}")
+    n = 1
+    for d in full[:i]:
+        n *= d
+    return n
+
+
+def _arguments(branch, weight, bias, post_weight, post_bias, gate, kind):
+    """(device, dtype, weights' dtype, rows of the gate), after the checks of what both
+    passes take."""
+    dev = _device(branch)
+    dt = _dtype(branch, "branch")
+    if branch.dim() < 1:
+        raise ValueError("branch must be [..., D]")
+    if kind not in KINDS:
+        raise ValueError(f"kind must be one of {KINDS}, not {kind!r}")
+    wt = _dtype(weight, "weight")
+    D = branch.shape[-1]
+    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"),
+                    (post_bias, "post_bias")):
+        if t is not None:
+            _check(t, name, (D,), weight.dtype, dev)
+    if post_bias is not None and post_weight is None:
+        raise ValueError("post_bias without post_weight")
+    gates = 0
+    if gate is not None:
+        gates = _gates(gate, branch.shape)
+        _check(gate, "gate", gate.shape, branch.dtype, dev)
+    return dev, dt, wt, gates
+
+
+@_on_its_device
+def residual_norm_forward(branch, x, weight, bias=None, *, post_weight=None, post_bias=None,
+                          gate=None, residual_scale: float = 1.0, kind: str = "layer",
+                          eps: float = 1e-5):
+    """(h, n) of ``h = residual_scale * x + gate * post(branch)``, ``n = pre(h)``.
+
+    branch, x [..., D] (bf16 or fp32; 1 <= D <= 8192); weight, bias [D] of the pre norm and
+    post_weight, post_bias [D] of the post norm, all of one type (bf16 or fp32; no
+    post_weight: no post norm); kind: both are layer norms ("layer") or root-mean-square
+    norms ("rms").  gate: [D], or one for every leading index ([B, 1, D] for branch
+    [B, T, D]), or of branch's shape; default 1."""
+    dev, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
+    shape = branch.shape
+    _check(x, "x", shape, branch.dtype, dev)
+    D = shape[-1]
+    rows = branch.numel() // D if D else 0
+    p, _ = _plan(rows, D, dt, wt, int(kind == "rms"), gates, _number(residual_scale, "residual_scale"),
+                 _number(eps, "eps"), post_weight is not None)
+    branch, x, weight, bias = _dense(branch), _dense(x), _dense(weight), _dense(bias)
+    post_weight, post_bias, gate = _dense(post_weight), _dense(post_bias), _dense(gate)
+    h = torch.empty(shape, dtype=branch.dtype, device=dev)
+    n = torch.empty(shape, dtype=branch.dtype, device=dev)
+    C.check(C.LIB.bcmt_residual_norm_forward(
+        p, branch.data_ptr(), x.data_ptr(), weight.data_ptr(), _address(bias),
+        _address(post_weight), _address(post_bias), _address(gate), h.data_ptr(), n.data_ptr(),
+        _raw_stream(dev.index)))
+    return h, n
+
+
+@_on_its_device
+def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=None,
+                           post_bias=None, gate=None, residual_scale: float = 1.0,
+                           kind: str = "layer", eps: float = 1e-5):
+    """(dbranch, dx, dweight, dbias, dpost_weight, dpost_bias, dgate) from the forward's
+    arguments, its h and the gradients dh (None: zero) and dn of its results; None for what
+    was not given.  dbranch and dx are one tensor where they are equal (no post norm, no gate,
+    residual_scale 1)."""
+    dev, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
+    shape, dtype = branch.shape, branch.dtype
+    _check(dn, "dn", shape, dtype, dev)
+    _check(h, "h", shape, dtype, dev)
+    if dh is not None:
+        _check(dh, "dh", shape, dtype, dev)
+    D = shape[-1]
+    rows = branch.numel() // D if D else 0
+    alpha = _number(residual_scale, "residual_scale")
+    p, nbytes = _plan(rows, D, dt, wt, int(kind == "rms"), gates, alpha, _number(eps, "eps"),
+                      post_weight is not None)
+    dh, dn, branch, h = _dense(dh), _dense(dn), _dense(branch), _dense(h)
+    weight, post_weight, post_bias = _dense(weight), _dense(post_weight), _dense(post_bias)
+    one = post_weight is None and gate is None and alpha == 1.0
+    new = functools.partial(torch.empty, device=dev)
+    dbranch = new(shape, dtype=dtype)
+    dx = None if one else new(shape, dtype=dtype)
+    dw, db, dpw, dpb = (None if t is None else new((D,), dtype=weight.dtype)
+                        for t in (weight, bias, post_weight, post_bias))
+    dgate = None if gate is None else new(gate.shape, dtype=dtype)
+    gate = _dense(gate)
+    ws = _buffer(max(256, nbytes), dev)
+    C.check(C.LIB.bcmt_residual_norm_backward(
+        p, _address(dh), dn.data_ptr(), branch.data_ptr(), h.data_ptr(), weight.data_ptr(),
+        _address(post_weight), _address(post_bias), _address(gate), dbranch.data_ptr(),
+        _address(dx), dw.data_ptr(), _address(db), _address(dpw), _address(dpb), _address(dgate),
+        ws.data_ptr(), _raw_stream(dev.index)))
+    return dbranch, dbranch if one else dx, dw, db, dpw, dpb, dgate
+
+
+class ResidualNorm(torch.autograd.Function):
+    """(h, n) with branch, x, the norms' weights and the gate as differentiable inputs."""
+
+    @staticmethod
+    def forward(ctx, branch, x, weight, bias, post_weight, post_bias, gate, alpha, kind, eps):
+        h, n = residual_norm_forward(branch, x, weight, bias, post_weight=post_weight,
+                                     post_bias=post_bias, gate=gate, residual_scale=alpha,
+                                     kind=kind, eps=eps)
+        ctx.save_for_backward(branch, h, weight, bias, post_weight, post_bias, gate)
+        ctx.args = (alpha, kind, eps)
+        ctx.set_materialize_grads(False)
+        return h, n
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, dn):
+        branch, h, weight, bias, post_weight, post_bias, gate = ctx.saved_tensors
+        alpha, kind, eps = ctx.args
+        if dh is None and dn is None:
+            return (None,) * 10
+        if dn is None:
+            dn = torch.zeros_like(h)
+        return residual_norm_backward(
+            dh, dn, branch, h, weight, bias, post_weight=post_weight, post_bias=post_bias,
+            gate=gate, residual_scale=alpha, kind=kind, eps=eps) + (None,) * 3
+
+
+def residual_norm(branch, x, weight, bias=None, *, post_weight=None, post_bias=None, gate=None,
+                  residual_scale: float = 1.0, kind: str = "layer", eps: float = 1e-5):
+    """Differentiable ``residual_norm_forward``."""
+    return ResidualNorm.apply(branch, x, weight, bias, post_weight, post_bias, gate,
+                              _number(residual_scale, "residual_scale"), kind, _number(eps, "eps"))

@@ -1,0 +1,286 @@
+"""AdamW over many tensors in one launch, with states in 32 or in 8 bits.
+
+``AdamWPlan`` is the bare call over a list of tensors, ``AdamW`` a
+``torch.optim.Optimizer`` around it.  8-bit states are signed and unsigned bytes with
+one float32 scale for every 256 consecutive elements of a tensor (``include/bcmt.h`` has
+the code); ``adamw8_values`` gives the values that they stand for.  Everything runs on
+the current CUDA stream; arguments that the library would misread raise ``ValueError``,
+what it refuses raises ``bcmt.BCMTError``.
+"""
+
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import numpy as np
+import torch
+from torch.autograd.graph import increment_version
+
+from . import bcmt as C
+from .lm_ops import _address, _check, _current_device, _dense, _device, _dtype, _on_its_device, \
+    _raw_stream
+
+_F32 = torch.float32
+BLOCK = 256   # elements that share a scale of 8-bit states
+_P, _G, _M, _V, _W, _MS, _VS, _N = range(8)   # fields of bcmt_adamw_tensor
+
+
+def _overlap(tensors):
+    """Whether two of the (dense) tensors share memory."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                   for t in tensors if t.numel())
+    return any(a[1] > b[0] for a, b in zip(spans, spans[1:]))
+
+
+class AdamWPlan:
+    """One AdamW step over the tensors of ``params`` (bf16 or fp32, all of one type, dense),
+    which it updates in place with their states: m and v fp32 of the same shapes, or, with
+    m_scales and v_scales, int8 and uint8 of as many elements with [ceil(n / 256)] fp32 scales.
+    masters: fp32 values of bf16 params, which are then what is updated and params their
+    rounding.  States start as zeros.  The plan holds the tensors, and reads their addresses
+    at each step."""
+
+    def __init__(self, params, m, v, *, masters=None, m_scales=None, v_scales=None):
+        params, m, v = list(params), list(m), list(v)
+        lists = [params, m, v]
+        self.bits = 32 if m_scales is None and v_scales is None else 8
+        if (m_scales is None) != (v_scales is None):
+            raise ValueError("m_scales and v_scales belong together")
+        self._columns = [_P, _M, _V]
+        for t, column in ((masters, _W), (m_scales, _MS), (v_scales, _VS)):
+            if t is not None:
+                lists.append(list(t))
+                self._columns.append(column)
+        if any(len(t) != len(params) for t in lists):
+            raise ValueError("params, states, masters and scales must be lists of one length")
+        if not params:
+            raise ValueError("params must have a tensor")
+        if not all(isinstance(t, torch.Tensor) for x in lists for t in x):
+            raise ValueError("params, states, masters and scales must be tensors")
+        self.device = _device(params[0])
+        self.dtype = params[0].dtype
+        self._dt = _dtype(params[0], "params")
+        if masters is not None and self.dtype == _F32:
+            raise ValueError("float32 params have no masters")
+        self._lists, self._all = lists, [t for x in lists for t in x]
+        self._check()
+        self._table = np.zeros((len(params), 8), dtype=np.int64)
+        self._address = self._table.ctypes.data
+        self._shapes = [p.shape for p in params]
+        self._sizes = np.array([p.numel() for p in params], dtype=np.int64)
+        self._at = None
+
+    def _check(self):
+        dev = self.device
+        for column, tensors in zip(self._columns, self._lists):
+            name = ("params", "", "m", "v", "masters", "m_scales", "v_scales")[column]
+            for p, t in zip(self._lists[0], tensors):
+                shape, dtype = p.shape, self.dtype if column == _P else _F32
+                if column in (_MS, _VS):
+                    shape = (-(-p.numel() // BLOCK),)
+                elif self.bits == 8 and column in (_M, _V):
+                    shape, dtype = t.shape, torch.int8 if column == _M else torch.uint8
+                    if t.numel() != p.numel():
+                        raise ValueError(f"{name} must have {p.numel()} elements, not {t.numel()}")
+                _check(t, name, shape, dtype, dev)
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be dense")
+        if _overlap(self._all):
+            raise ValueError("params, states, masters and scales must not share memory")
+
+    def _refresh(self):
+        at = [t.data_ptr() for t in self._all]
+        if at != self._at:
+            self._check()
+            n = len(self._shapes)
+            for i, column in enumerate(self._columns):
+                self._table[:, column] = at[i * n:(i + 1) * n]
+            self._at = at
+
+    @torch.no_grad()
+    def step(self, grads, *, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+             step, grad_scale: Optional[torch.Tensor] = None):
+        """One step, the ``step``-th (from 1), with ``grads`` of the params' shapes and type
+        (None: that tensor is left as it is).  step: an int, or one int64 on the device, and lr a
+        number, or one float32 on the device, both then read when the kernel runs (captured
+        graphs); grad_scale: one float32 on the device that the gradients are multiplied by."""
+        dev = self.device
+        if dev.index != _current_device():
+            with torch.cuda.device(dev):
+                return self.step(grads, lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
+                                 step=step, grad_scale=grad_scale)
+        self._refresh()
+        if len(grads) != len(self._shapes):
+            raise ValueError(f"{len(self._shapes)} gradients are needed, not {len(grads)}")
+        at, kept, dtype, holes = [], [], self.dtype, False
+        for g, shape in zip(grads, self._shapes):
+            if g is None:
+                at.append(0)
+                holes = True
+                continue
+            if g.shape != shape or g.dtype != dtype or g.device != dev:
+                _check(g, "grads", shape, dtype, dev)
+            if not g.is_contiguous():
+                g = g.contiguous()
+                kept.append(g)
+            at.append(g.data_ptr())
+        self._table[:, _G] = at
+        self._table[:, _N] = np.where(self._table[:, _G] != 0, self._sizes, 0) if holes else self._sizes
+        step_ptr = lr_ptr = None
+        if isinstance(step, torch.Tensor) and step.is_cuda:
+            _one(step, "step", torch.int64, dev)
+            step, step_ptr = 1, step.data_ptr()
+        if isinstance(lr, torch.Tensor) and lr.is_cuda:
+            _one(lr, "lr", _F32, dev)
+            lr, lr_ptr = 0.0, lr.data_ptr()
+        if grad_scale is not None:
+            _one(grad_scale, "grad_scale", _F32, dev)
+            grad_scale = grad_scale.data_ptr()
+        p = C.bcmt_adamw_params(len(at), self._dt, self.bits, 0, int(step), float(lr), betas[0],
+                                betas[1], eps, weight_decay, grad_scale, step_ptr, lr_ptr)
+        C.check(C.LIB.bcmt_adamw_step(ctypes.byref(p), self._address, _raw_stream(dev.index)))
+        # written through their addresses, which autograd cannot see
+        increment_version(self._all)
+
+
+def _one(t, name, dtype, dev):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.numel() != 1 or t.device != dev:
+        raise ValueError(f"{name} must be one {dtype} on {dev}")
+
+
+def _codes(t, name, dtype, dev):
+    if t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be dense {dtype} on {dev}")
+    return _dense(t)
+
+
+@_on_its_device
+def adamw8_values(m, m_scale, v, v_scale):
+    """The fp32 values (m, v) that 8-bit states stand for: m int8 and v uint8 of one shape,
+    scales [ceil(n / 256)] fp32."""
+    dev = _device(m)
+    m, v = _codes(m, "m", torch.int8, dev), _codes(v, "v", torch.uint8, dev)
+    if v.shape != m.shape:
+        raise ValueError(f"v must be {tuple(m.shape)}, not {tuple(v.shape)}")
+    blocks = (-(-m.numel() // BLOCK),)
+    _check(m_scale, "m_scale", blocks, _F32, dev)
+    _check(v_scale, "v_scale", blocks, _F32, dev)
+    m_scale, v_scale = _dense(m_scale), _dense(v_scale)
+    mo = torch.empty(m.shape, dtype=_F32, device=dev)
+    vo = torch.empty(m.shape, dtype=_F32, device=dev)
+    C.check(C.LIB.bcmt_adamw_values(m.data_ptr(), m_scale.data_ptr(), v.data_ptr(),
+                                    v_scale.data_ptr(), mo.data_ptr(), vo.data_ptr(), m.numel(),
+                                    _raw_stream(dev.index)))
+    return mo, vo
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW with every tensor of a parameter group in one launch.
+
+    bits: 32, or 8 for states in 8 bits; masters: float32 values of bf16 parameters are kept
+    and updated.  capturable: the count of steps is kept on the device, so that a captured
+    ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
+    a float32 on the device, the rate can change between replays too.  ``step`` takes a
+    grad_scale (one float32 on the device, as from clipping by the norm)."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 1e-2, *, bits: int = 32, masters: bool = False,
+                 capturable: bool = False):
+        if bits not in (32, 8):
+            raise ValueError(f"bits must be 32 or 8, not {bits}")
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
+                                      bits=bits, masters=masters, capturable=capturable))
+        self._plans = {}
+
+    def _init(self, p, group):
+        s = self.state[p]
+        if s:
+            return
+        flat = torch.preserve_format if p.is_contiguous() else torch.contiguous_format
+        if group["bits"] == 8:
+            blocks = -(-p.numel() // BLOCK)
+            s["exp_avg"] = torch.zeros(p.shape, dtype=torch.int8, device=p.device)
+            s["exp_avg_sq"] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device)
+            s["exp_avg_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
+            s["exp_avg_sq_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
+        else:
+            s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
+            s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
+        if group["masters"] and p.dtype != _F32:
+            s["master"] = p.detach().to(_F32)
+        # one count for the group where it is on the device
+        s["step"] = self._count(group, p.device) if group["capturable"] else 0
+
+    def _count(self, group, device):
+        for p in group["params"]:
+            if "step" in self.state.get(p, {}):
+                return self.state[p]["step"]
+        return torch.zeros((), dtype=torch.int64, device=device)
+
+    def _plan(self, key, group, params):
+        states = [self.state[p] for p in params]
+        names = ["exp_avg", "exp_avg_sq"] + (["exp_avg_scale", "exp_avg_sq_scale"]
+                                             if group["bits"] == 8 else [])
+        names += ["master"] if "master" in states[0] else []
+        ids = [id(p) for p in params] + [id(s[k]) for s in states for k in names]
+        plan = self._plans.get(key)
+        if plan is None or plan[0] != ids:
+            of = {k: [s[k] for s in states] for k in names}
+            plan = (ids, AdamWPlan(params, of["exp_avg"], of["exp_avg_sq"], masters=of.get("master"),
+                                   m_scales=of.get("exp_avg_scale"),
+                                   v_scales=of.get("exp_avg_sq_scale")))
+            self._plans[key] = plan
+        return plan[1]
+
+    @torch.no_grad()
+    def step(self, closure=None, *, grad_scale: Optional[torch.Tensor] = None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for i, group in enumerate(self.param_groups):
+            kinds = {}
+            for p in group["params"]:
+                if p.grad is not None:
+                    self._init(p, group)
+                    kinds.setdefault((p.dtype, p.device), []).append(p)
+            how = dict(lr=group["lr"], betas=group["betas"], eps=group["eps"],
+                       weight_decay=group["weight_decay"], grad_scale=grad_scale)
+            counted = False
+            for kind, params in kinds.items():
+                plan = self._plan((i, kind), group, params)
+                grads = [p.grad for p in params]
+                if group["capturable"]:
+                    count = self.state[params[0]]["step"]
+                    if not counted:
+                        count += 1
+                        counted = True
+                    plan.step(grads, step=count, **how)
+                    continue
+                for p in params:
+                    self.state[p]["step"] += 1
+                steps = [self.state[p]["step"] for p in params]
+                if steps.count(steps[0]) == len(steps):
+                    plan.step(grads, step=steps[0], **how)
+                else:   # parameters that had no gradient in some steps are behind
+                    for n in sorted(set(steps)):
+                        plan.step([g if k == n else None for g, k in zip(grads, steps)], step=n, **how)
+        return loss
+
+    @torch.no_grad()
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # the states in their own types (the base class gives them the parameters')
+        params = [p for g in self.param_groups for p in g["params"]]
+        ids = [k for g in state_dict["param_groups"] for k in g["params"]]
+        counts = {}
+        for p, k in zip(params, ids):
+            for name, x in state_dict["state"].get(k, {}).items():
+                if isinstance(x, torch.Tensor):
+                    if name == "step":   # one tensor for those that shared one
+                        x = counts.setdefault(id(x), x.detach().to(p.device, copy=True))
+                    else:
+                        x = x.detach().to(p.device, copy=True)
+                self.state[p][name] = x
+        self._plans.clear()
