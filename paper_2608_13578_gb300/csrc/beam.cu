@@ -24,19 +24,87 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
+// Sums of exponentials are integers in units of 2^-48: exact, whatever the order of the
+// additions (a chunk's is below 2^62).
+constexpr float kUnit = 281474976710656.f;   // 2^48
 struct ChunkHead {
-  double sum;   // of exp(x - max) over the chunk
-  float max;    // -inf: no entry above it
-  int n;        // entries in the list
+  unsigned long long sum;   // of exp(x - max) over the chunk
+  float max;                // -inf: no entry above it; NaN: a logit is NaN or +inf
+  int n;                    // entries in the list
 };
 struct Entry {
   float x;
   int v;
 };
 
+// The sum a + b as a float and what it lacks.
+__device__ __forceinline__ float two_sum(float a, float b, float& rest) {
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  rest = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
+  return s;
+}
+// exp(x - ref), x - ref from -86 to 0, as 2^n (h + l) to within 2^-32: the 64-bit units of
+// this chip are too slow for it (a fp64 exponential took most of the merge's time).
+// x - ref = n ln 2 + r with r in two floats, and exp(r) = 1 + r + r^2/2 + r^3/6 + ..., the
+// first four terms in two floats, Taylor's next six in one.
+__device__ __forceinline__ void exp_wide(float x, float ref, float& h, float& l, int& n) {
+  float lo, t;
+  const float hi = two_sum(x, -ref, lo);
+  const float fn = rintf(__fmul_rn(hi, 1.44269504f));
+  n = (int)fn;
+  // ln 2 = 90852 / 2^17 + kLn2b, the first exact in every product with n
+  constexpr double kLn2 = 0.693147180559945309417;
+  constexpr float kLn2a = 90852.f / 131072.f, kLn2b = (float)(kLn2 - 90852.0 / 131072.0),
+                  kLn2c = (float)(kLn2 - 90852.0 / 131072.0 - (double)kLn2b);
+  const float r1 = __fmaf_rn(-fn, kLn2a, hi);
+  const float p = __fmul_rn(fn, kLn2b), pe = __fmaf_rn(fn, kLn2b, -p);
+  float u;
+  const float s0 = two_sum(r1, -p, u), s = two_sum(s0, u + (lo - pe - fn * kLn2c), t);
+  // r^2 and r^3 / 6 as two floats
+  const float a = __fmul_rn(s, s), ae = __fmaf_rn(s, s, -a) + 2.f * s * t;
+  const float b = __fmul_rn(a, s), be = __fmaf_rn(a, s, -b) + ae * s + a * t;
+  constexpr float kSixth = (float)(1.0 / 6.0), kSixthRest = (float)(1.0 / 6.0 - (double)kSixth);
+  const float m = __fmul_rn(b, kSixth), me = __fmaf_rn(b, kSixth, -m) + b * kSixthRest + be * kSixth;
+  float q = 1.f / 3628800.f;
+  q = fmaf(q, s, 1.f / 362880.f);
+  q = fmaf(q, s, 1.f / 40320.f);
+  q = fmaf(q, s, 1.f / 5040.f);
+  q = fmaf(q, s, 1.f / 720.f);
+  q = fmaf(q, s, 1.f / 120.f);
+  q = fmaf(q, s, 1.f / 24.f);
+  float e0, e1, e2, e3;
+  h = two_sum(1.f, s, e0);
+  h = two_sum(h, 0.5f * a, e1);
+  h = two_sum(h, m, e2);
+  h = two_sum(h, a * a * q, e3);
+  l = ((e0 + e1) + (e2 + e3)) + (t + (0.5f * ae + me));
+}
+__device__ __forceinline__ unsigned long long exp_units(float x, float ref) {
+  if (!(x - ref > -34.f)) return 0;   // below half a unit
+  float h, l;
+  int n;
+  exp_wide(x, ref, h, l, n);
+  const float scale = __int_as_float((n + 48 + 127) << 23);
+  return (unsigned long long)(__float2ll_rn(h * scale) + __float2ll_rn(l * scale));
+}
+__device__ __forceinline__ double exp_double(float x, float ref) {
+  if (!(x - ref > -86.f)) return 0.0;
+  float h, l;
+  int n;
+  exp_wide(x, ref, h, l, n);
+  const float scale = __int_as_float((n + 127) << 23);
+  return (double)(h * scale) + (double)(l * scale);
+}
+
 template <class T, int E, bool VEC>
 __device__ __forceinline__ int column(int j, int e) {   // of element e of group j, in the chunk
   return VEC ? (j * kThreads + (int)threadIdx.x) * 8 + e : (j * 8 + e) * kThreads + (int)threadIdx.x;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // Sorted over the lanes, the largest first.
@@ -76,8 +144,8 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   constexpr int J = E / 8, kCap = 2 * kBeamMaxK * E;
   __shared__ float tops[kWarps][32];
   __shared__ Entry list[kCap];
-  __shared__ double sums[kWarps];
-  __shared__ unsigned long long listed;
+  __shared__ unsigned long long total;
+  __shared__ int bad;
   __shared__ float thr;
   __shared__ int cnt, tie;
   pdl_enter();
@@ -134,7 +202,8 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   }
   if (threadIdx.x == 0) {
     cnt = 0;
-    listed = 0;
+    total = 0;
+    bad = 0;
   }
   tops[warp][lane] = warp_sort(top);
   __syncthreads();
@@ -160,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   for (int j = 0; j < J; ++j) {
     if (!(gmax[j] >= limit) || none) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += exp2f((v[8 * j + e] - ref) * kLog2e);
+      for (int e = 0; e < 8; ++e) s += exp2_fast((v[8 * j + e] - ref) * kLog2e);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -169,14 +238,14 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
           const int at = atomicAdd(&cnt, 1);
           if (at < kCap) list[at] = Entry{u, column<T, E, VEC>(j, e)};
         } else {
-          s += exp2f((u - ref) * kLog2e);
+          s += exp2_fast((u - ref) * kLog2e);
         }
       }
     }
   }
   __syncthreads();
   int n = cnt;
-  double d = s;
+  unsigned long long part = 0;
   if (n > kCap) {
     // many elements equal to the threshold: the lowest places among them
     __syncthreads();
@@ -200,7 +269,7 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
     }
     __syncthreads();
     const int limit_at = tie;
-    const double one = exp((double)limit - (double)ref);
+    const unsigned long long one = exp_units(limit, ref);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int c = column<T, E, VEC>(i / 8, i % 8);
@@ -208,18 +277,16 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
         const int at = atomicAdd(&cnt, 1);
         if (at < kCap) list[at] = Entry{v[i], c};
       } else if (v[i] == limit) {
-        d += one;
+        part += one;
       }
     }
     __syncthreads();
     n = min(cnt, kCap);
   }
-  // the list's part of the sum in units of 2^-52: an integer, whatever the order in which
-  // the entries came here
+  // the list in order, and its exponentials
   Entry* out = reinterpret_cast<Entry*>(static_cast<char*>(a.ws) +
                                         (size_t)a.N * a.K * nchunk * sizeof(ChunkHead)) +
                (row * nchunk + chunk) * a.K;
-  unsigned long long part = 0;
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const Entry m = list[i];
     int rank = 0;
@@ -227,40 +294,43 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
       const Entry o = list[k];
       rank += o.x > m.x || (o.x == m.x && o.v < m.v);
     }
-    part += (unsigned long long)(exp((double)m.x - (double)ref) * 0x1p52);
+    part += exp_units(m.x, ref);
     if (rank < a.K) out[rank] = Entry{m.x, base + m.v};
   }
-  if (part) atomicAdd(&listed, part);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-  if (lane == 0) sums[warp] = d;
+  // the others' sum of this warp; not finite where a logit is NaN or +inf
+  s = warp_sum(s);
+  if (lane == 0) {
+    if (s < 1e9f) part += (unsigned long long)__float2ll_rn(s * kUnit);
+    else bad = 1;
+  }
+  if (part) atomicAdd(&total, part);
   __syncthreads();
   if (threadIdx.x == 0) {
-    d = (double)listed * 0x1p-52;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) d += sums[w];
-    static_cast<ChunkHead*>(a.ws)[row * nchunk + chunk] = ChunkHead{d, mx, min(n, a.K)};
+    const bool ok = !bad && mx < INFINITY;
+    static_cast<ChunkHead*>(a.ws)[row * nchunk + chunk] =
+        ChunkHead{total, ok ? mx : __int_as_float(0x7fffffff), min(n, a.K)};
   }
 }
 
 namespace {
 
-// A candidate: the value in 64 bits and its place k V + v.  Places are below 2^31.
+// A candidate: a 64-bit key that orders as its value, the larger the better, and its
+// place, the lower the better.  Comparisons are of integers.
 struct Cand {
-  double c;
+  long long key;
   int at;
 };
+constexpr int kNoPlace = 0x7fffffff;
+constexpr long long kNoKey = -0x7fffffffffffffffll - 1;
+
 __device__ __forceinline__ bool before(const Cand& a, const Cand& b) {
-  return a.c > b.c || (a.c == b.c && a.at < b.at);
+  return a.key > b.key || (a.key == b.key && a.at < b.at);
 }
 __device__ __forceinline__ Cand shfl(const Cand& a, int from) {
-  return Cand{__shfl_sync(0xffffffffu, a.c, from), __shfl_sync(0xffffffffu, a.at, from)};
+  return Cand{__shfl_sync(0xffffffffu, a.key, from), __shfl_sync(0xffffffffu, a.at, from)};
 }
-// The best 32 of two lists that are sorted over the lanes, sorted again.
-__device__ __forceinline__ Cand merge(const Cand& a, const Cand& b) {
+__device__ __forceinline__ Cand settle(Cand v) {   // a bitonic sequence over the lanes, sorted
   const int lane = threadIdx.x & 31;
-  Cand v = shfl(b, 31 - lane);
-  if (before(a, v)) v = a;
 #pragma unroll
   for (int j = 16; j > 0; j >>= 1) {
     const Cand o = shfl(v, lane ^ j);
@@ -268,122 +338,131 @@ __device__ __forceinline__ Cand merge(const Cand& a, const Cand& b) {
   }
   return v;
 }
-constexpr int kNoPlace = 0x7fffffff;
+__device__ __forceinline__ Cand sorted(Cand v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1) {
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const Cand o = shfl(v, lane ^ j);
+      if (before(o, v) == (((lane & j) == 0) == ((lane & k) == 0))) v = o;
+    }
+  }
+  return v;
+}
+// The best 32 of two lists that are sorted over the lanes, sorted again.
+__device__ __forceinline__ Cand merge(const Cand& a, const Cand& b) {
+  Cand v = shfl(b, 31 - (threadIdx.x & 31));
+  if (before(a, v)) v = a;
+  return settle(v);
+}
+// Floats and doubles (no NaN, no -0) as integers of the same order.
+__device__ __forceinline__ int ordered(float x) {
+  const int b = __float_as_int(x + 0.f);
+  return b < 0 ? b ^ 0x7fffffff : b;
+}
+__device__ __forceinline__ long long ordered(double x) {
+  const long long b = __double_as_longlong(x);
+  return b < 0 ? b ^ 0x7fffffffffffffffll : b;
+}
+__device__ __forceinline__ double value(long long key) {
+  return __longlong_as_double(key < 0 ? key ^ 0x7fffffffffffffffll : key);
+}
 
 }  // namespace
 
-// One search: the sums of its beams, then the lists of its chunks, each warp a part of
-// them, then the warps' lists in pairs.
-__global__ void __launch_bounds__(1024) beam_merge_kernel(const BeamArgs a, int nchunk,
-                                                          unsigned* status) {
-  __shared__ double tops[kBeamMaxK], logs[kBeamMaxK], base[kBeamMaxK];
-  __shared__ int kind[kBeamMaxK];   // 0: candidates in the lists, 1: ended, 2: none
-  __shared__ Cand lists[32][32];
+// One search, one warp a beam: the sum of its row and the best K of its chunks' lists,
+// then the beams' lists in pairs.
+__global__ void __launch_bounds__(32 * kBeamMaxK) beam_merge_kernel(const BeamArgs a, int nchunk,
+                                                                    unsigned* status) {
+  __shared__ Cand lists[kBeamMaxK][32];
   pdl_enter();
-  const int n = blockIdx.x, K = a.K, lane = threadIdx.x & 31, warp = threadIdx.x >> 5,
-            warps = blockDim.x >> 5;
-  const ChunkHead* heads = static_cast<const ChunkHead*>(a.ws) + (size_t)n * K * nchunk;
-  const Entry* entries = reinterpret_cast<const Entry*>(
-                             static_cast<const char*>(a.ws) +
-                             (size_t)a.N * K * nchunk * sizeof(ChunkHead)) +
-                         (size_t)n * K * nchunk * K;
-  for (int k = warp; k < K; k += warps) {
-    const float score = a.scores[(size_t)n * K + k];
-    const bool ended = a.finished && a.finished[(size_t)n * K + k];
-    int what = !(score > -INFINITY && score < INFINITY) ? 2 : ended ? 1 : 0;
-    double top = 0.0, total = 1.0;
-    if (what == 0) {
-      float m = -INFINITY;
-      for (int c = lane; c < nchunk; c += 32) m = fmaxf(m, heads[k * nchunk + c].max);
-      m = warp_max(m);
-      double s = 0.0;
-      for (int c = lane; c < nchunk; c += 32) {
-        const ChunkHead h = heads[k * nchunk + c];
-        // a chunk without a finite element adds its 0, or the NaN that it holds
-        s += h.max == -INFINITY ? h.sum : h.sum * exp((double)h.max - (double)m);
+  const int n = blockIdx.x, K = a.K, lane = threadIdx.x & 31, k = threadIdx.x >> 5;
+  const size_t row = (size_t)n * K + k;
+  const ChunkHead* heads = static_cast<const ChunkHead*>(a.ws) + row * nchunk;
+  const Entry* entries = reinterpret_cast<const Entry*>(static_cast<const char*>(a.ws) +
+                                                        (size_t)a.N * K * nchunk * sizeof(ChunkHead)) +
+                         row * nchunk * K;
+  const float score = a.scores[row];
+  const bool ended = a.finished && a.finished[row];
+  const bool there = score > -INFINITY && score < INFINITY;
+  if (lane == 0 && !(score < INFINITY)) atomicOr(status, kStatusBadLogit);
+  Cand best{kNoKey, kNoPlace};
+  if (there && ended) {
+    if (lane == 0) best = Cand{ordered((double)score), k * a.V + a.eos};
+  } else if (there) {
+    // the best of the lists by logit; the first 32 heads stay for the sum
+    ChunkHead h{0, -INFINITY, 0};
+    if (lane < nchunk) h = heads[lane];
+    const int total = nchunk * K;
+    Cand last = best;
+    for (int i = 0; i < total; i += 32) {
+      const int l = (i + lane) / K;
+      Cand c{kNoKey, kNoPlace};
+      if (i + lane < total) {
+        const Entry e = entries[i + lane];
+        if (i + lane - l * K < heads[l].n) c = Cand{ordered(e.x), e.v};
       }
+      if (!__any_sync(0xffffffffu, before(c, last))) continue;
+      best = i == 0 ? sorted(c) : merge(best, sorted(c));
+      last = shfl(best, K - 1);
+    }
+    float m = h.max;
+    bool ok = m == m;
+    for (int c = lane + 32; c < nchunk; c += 32) {
+      ok = ok && heads[c].max == heads[c].max;
+      m = fmaxf(m, heads[c].max);
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok && lane == 0) atomicOr(status, kStatusBadLogit);
+    m = warp_max(m);
+    if (ok && m > -INFINITY) {
+      double s = (double)h.sum * exp_double(h.max, m);
+      for (int c = lane + 32; c < nchunk; c += 32) s += (double)heads[c].sum * exp_double(heads[c].max, m);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (!(s < INFINITY) || !(m < INFINITY)) {
-        what = 2;   // a logit is NaN or +inf
-        if (lane == 0) atomicOr(status, kStatusBadLogit);
-      } else if (m == -INFINITY) {
-        what = 2;
-      } else {
-        top = m;
-        total = s;
+      s *= 0x1p-48;
+      // log s: a float y near it, and log(s exp(-y)) from its series
+      const float y = logf((float)s);
+      const double z = s * exp_double(-y, 0.f) - 1.0;
+      const double log_s = (double)y + (z - 0.5 * z * z);
+      if (best.at != kNoPlace) {
+        const float x = __int_as_float((int)best.key < 0 ? (int)best.key ^ 0x7fffffff : (int)best.key);
+        best = Cand{ordered((double)score + (((double)x - (double)m) - log_s)), k * a.V + best.at};
       }
-    }
-    if (lane == 0) {
-      if (!(score < INFINITY)) atomicOr(status, kStatusBadLogit);
-      kind[k] = what;
-      tops[k] = top;
-      logs[k] = log(total);
-      base[k] = score;
+    } else {
+      best = Cand{kNoKey, kNoPlace};
     }
   }
-  __syncthreads();
-  Cand best{-INFINITY, kNoPlace};
-  if (warp == 0) {   // ended beams: one candidate each
-    Cand c{-INFINITY, kNoPlace};
-    if (lane < K && kind[lane] == 1) c = Cand{base[lane], lane * a.V + a.eos};
-    // in order: each lane to the number of those before it
-    int rank = 0;
-    for (int i = 0; i < 32; ++i) {
-      const Cand o = shfl(c, i);
-      rank += before(o, c) || (o.c == c.c && o.at == c.at && i < lane);
-    }
-    for (int i = 0; i < 32; ++i) {
-      const int r = __shfl_sync(0xffffffffu, rank, i);
-      const Cand o = shfl(c, i);
-      if (lane == r) best = o;
-    }
-  }
-  Cand last = shfl(best, K - 1);
-  for (int l = warp; l < K * nchunk; l += warps) {
-    const int k = l / nchunk;
-    if (kind[k] != 0) continue;
-    const int cnt = heads[l].n;
-    Cand c{-INFINITY, kNoPlace};
-    if (lane < cnt) {
-      const Entry e = entries[(size_t)l * K + lane];
-      c = Cand{base[k] + (((double)e.x - tops[k]) - logs[k]), k * a.V + e.v};
-    }
-    // the list's first is its best: nothing to do where that is past the K-th so far
-    if (!before(shfl(c, 0), last)) continue;
-    best = merge(best, c);
-    last = shfl(best, K - 1);
-  }
-  lists[warp][lane] = best;
-  for (int m = 1; m < warps; m *= 2) {
+  lists[k][lane] = best;
+  for (int m = 1; m < K; m *= 2) {
     __syncthreads();
-    if (warp % (2 * m) == 0 && warp + m < warps) {
-      best = merge(best, lists[warp + m][lane]);
-      lists[warp][lane] = best;
+    if (k % (2 * m) == 0 && k + m < K) {
+      best = merge(best, lists[k + m][lane]);
+      lists[k][lane] = best;
     }
   }
-  if (warp != 0) return;
-  // places of -inf fill what is left, the lowest first: the places below 2 K that are not
-  // among the selected, in order
+  if (k != 0) return;
+  // places of -inf fill what is left, the lowest first: those that are not among the selected
   const int have = __popc(__ballot_sync(0xffffffffu, lane < K && best.at != kNoPlace));
   int place = best.at;
-  if (have < K) {
-    int filled = 0;
-    for (int at = 0; filled < K - have; ++at) {
-      const bool taken = __ballot_sync(0xffffffffu, lane < have && place == at) != 0;
-      if (taken) continue;
-      if (lane == have + filled) place = at;
-      ++filled;
-    }
+  for (int at = 0, filled = 0; filled < K - have; ++at) {
+    if (__any_sync(0xffffffffu, lane < have && place == at)) continue;
+    if (lane == have + filled) place = at;
+    ++filled;
   }
   if (lane < K) {
     const size_t o = (size_t)n * K + lane;
-    const int k = place / a.V, v = place - k * a.V;
-    a.scores_out[o] = (float)best.c;
-    a.parents[o] = k;
+    const int parent = place / a.V, v = place - parent * a.V;
+    const bool was = a.finished && a.finished[(size_t)n * K + parent];
+    a.scores_out[o] = lane < have ? (float)value(best.key) : -INFINITY;
+    a.parents[o] = parent;
     a.tokens[o] = v;
-    a.finished_out[o] = (a.finished && a.finished[(size_t)n * K + k]) || v == a.eos;
+    lists[0][lane].at = was || v == a.eos;
   }
+  // finished_out may be finished: written after all of it has been read
+  __syncwarp();
+  if (lane < K) a.finished_out[(size_t)n * K + lane] = (uint8_t)lists[0][lane].at;
 }
 
 namespace {
@@ -471,8 +550,7 @@ cudaError_t beam_select(const Launch& lc, int dtype, int sms, const BeamArgs& a)
                     : e == 32  ? chunks<bf16, 32>(lc, a, nchunk)
                                : chunks<bf16, 8>(lc, a, nchunk);
   if (err != cudaSuccess) return err;
-  const int warps = std::min(32, std::max(1, a.K * nchunk > 64 ? 32 : std::min(8, a.K * nchunk)));
-  return launch_k(beam_merge_kernel, dim3(a.N), dim3(warps * 32), 0, lc.stream, a, nchunk, lc.status);
+  return launch_k(beam_merge_kernel, dim3(a.N), dim3(a.K * 32), 0, lc.stream, a, nchunk, lc.status);
 }
 
 cudaError_t beam_reorder(const Launch& lc, const long long* parents, int N, int K,

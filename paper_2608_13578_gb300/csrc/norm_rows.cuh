@@ -101,50 +101,83 @@ __device__ __forceinline__ void write8(T* row, const Cols<VEC>& c, const float* 
   }
 }
 
-// Sums of NV values over the threads of a row, given to all of them.  TPR <= 32: lanes
-// of a warp.  Else the row's warps add through shared memory, `slot` alternating between
-// two buffers of NV floats per warp so that one barrier a sum is enough.
-template <int TPR, int NV>
-__device__ __forceinline__ void lane_sums(float (&v)[NV]) {
-#pragma unroll
-  for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-  }
-}
+// Sums of NV (1, 2 or 4) values over the threads of a row, given to all of them.  Each
+// step of a warp's sum halves the values while there is more than one (a lane keeps one
+// half of them and hands the other to its partner), then the lanes: 4 values take 6
+// exchanges, not 20.  Up to 32 threads: lanes of a warp.  More: the row's warps add
+// through shared memory, `slot` alternating between two buffers, so that one barrier a
+// sum is enough.
 __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
-constexpr int kMaxWarps = 16, kMaxSums = 4;
+constexpr int kMaxWarps = 16;
 struct RowShared {
   float4 sums[2][kMaxWarps];
 };
 template <int TPR, int NV>
 __device__ __forceinline__ void row_sums(float (&v)[NV], RowShared& sh, int& slot, int warp0,
                                          int nw, int bar) {
-  static_assert(NV <= kMaxSums, "");
-  lane_sums<TPR, NV>(v);
-  if (TPR > 32) {
-    float4* s = sh.sums[slot];
+  static_assert(NV == 1 || NV == 2 || NV == 4, "");
+  const int lane = threadIdx.x & 31;
+  constexpr int W = TPR < 32 ? TPR : 32;
+  float a[2], s;
+  if (NV == 4) {
+    const bool up = lane & 2;   // keeps values 2, 3
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float give = up ? v[i] : v[NV == 4 ? 2 + i : 0], keep = up ? v[NV == 4 ? 2 + i : 0] : v[i];
+      a[i] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
+    }
+  } else {
+    a[0] = v[0];
+    a[1] = NV == 2 ? v[NV == 2 ? 1 : 0] : 0.f;
+  }
+  if (NV >= 2) {
+    const bool up = lane & 1;   // keeps the second of its values
+    const float give = up ? a[0] : a[1], keep = up ? a[1] : a[0];
+    s = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+  } else {
+    s = a[0];
+  }
+#pragma unroll
+  for (int o = W / 2; o >= NV; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (TPR <= 32) {
+    // lane i (of every NV) holds the sum of value i
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = NV == 1 ? s : __shfl_sync(0xffffffffu, s, (lane & ~(NV - 1)) | i);
+  } else {
+    float4* buf = sh.sums[slot];
     slot ^= 1;
-    if ((threadIdx.x & 31) == 0) {
-      float4 f = make_float4(v[0], NV > 1 ? v[NV > 1 ? 1 : 0] : 0.f, NV > 2 ? v[NV > 2 ? 2 : 0] : 0.f,
-                             NV > 3 ? v[NV > 3 ? 3 : 0] : 0.f);
-      s[threadIdx.x >> 5] = f;
-    }
+    if (lane < NV) reinterpret_cast<float*>(buf + (threadIdx.x >> 5))[lane] = s;
     bar_sync(bar, nw * 32);
-    float4 a = s[warp0];
+    float4 t = buf[warp0];
     for (int w = 1; w < nw; ++w) {
-      const float4 b = s[warp0 + w];
-      a.x += b.x;
-      if (NV > 1) a.y += b.y;
-      if (NV > 2) a.z += b.z;
-      if (NV > 3) a.w += b.w;
+      const float4 b = buf[warp0 + w];
+      t.x += b.x;
+      if (NV > 1) t.y += b.y;
+      if (NV > 2) t.z += b.z;
+      if (NV > 2) t.w += b.w;
     }
-    const float f[4] = {a.x, a.y, a.z, a.w};
+    const float f[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = f[i];
   }
+}
+
+// Asynchronous copies of a thread's own elements to its own place in shared memory: what
+// a thread waits for, it has issued itself, so no barrier is needed.
+__device__ __forceinline__ void copy_async16(void* s, const void* g) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(s)),
+               "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_async4(void* s, const void* g) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(s)),
+               "l"(g) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
 }  // namespace

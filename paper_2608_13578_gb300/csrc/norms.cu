@@ -197,7 +197,6 @@ NormPlan norm_plan(long long rows, int D, long long groups, bool post, int sms) 
     ctas_per_sm = 1;
   }
   p.rows_per_cta = p.threads / p.tpr;
-  p.smem = p.wide ? (post ? 5 : 3) * 2 * 8 * 512 * 4 : p.rows_per_cta > 1 ? 8 * 512 * 4 : 0;
   p.ctas = (int)std::min<long long>((rows + p.rows_per_cta - 1) / p.rows_per_cta,
                                     (long long)sms * ctas_per_sm);
   // segments: each gate's rows in equal parts, so that the workers' longest walk is

@@ -38,7 +38,7 @@ struct NormJoin {
 // How a backward call is cut: threads of a row, rows at a time in a CTA, CTAs, and the
 // segments of rows that its workers walk.
 struct NormPlan {
-  int tpr, threads, rows_per_cta, ctas, smem, turns;
+  int tpr, threads, rows_per_cta, ctas, turns;
   bool wide;
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
   size_t part_bytes, gate_bytes;
