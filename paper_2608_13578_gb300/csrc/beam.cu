@@ -520,11 +520,12 @@ __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant
 
 namespace {
 
-// Elements per thread of a chunk: 32 where that gives every SM work, else 8, for more
-// CTAs on few rows.
+// Elements per thread of a chunk: 16 where that gives every SM work, else 8, for more
+// CTAs on few rows.  (32 have half the lists, but 200 registers' worth of latency a CTA:
+// 64 x 8 x 32000 take the same time, 40 x 5 x 50257 of fp32 four us more.)
 int chunk_elements(int N, int K, int V, int sms) {
-  const long long big = (V + 32 * kThreads - 1) / (32 * kThreads);
-  return (long long)N * K * big >= sms ? 32 : 8;
+  const long long big = (V + 16 * kThreads - 1) / (16 * kThreads);
+  return (long long)N * K * big >= sms ? 16 : 8;
 }
 
 template <class T, int E>
@@ -546,8 +547,8 @@ cudaError_t beam_select(const Launch& lc, int dtype, int sms, const BeamArgs& a)
   if (a.N == 0) return cudaSuccess;
   const int e = chunk_elements(a.N, a.K, a.V, sms);
   const int nchunk = (a.V + e * kThreads - 1) / (e * kThreads);
-  cudaError_t err = dtype == 0 ? e == 32 ? chunks<float, 32>(lc, a, nchunk) : chunks<float, 8>(lc, a, nchunk)
-                    : e == 32  ? chunks<bf16, 32>(lc, a, nchunk)
+  cudaError_t err = dtype == 0 ? e == 16 ? chunks<float, 16>(lc, a, nchunk) : chunks<float, 8>(lc, a, nchunk)
+                    : e == 16  ? chunks<bf16, 16>(lc, a, nchunk)
                                : chunks<bf16, 8>(lc, a, nchunk);
   if (err != cudaSuccess) return err;
   return launch_k(beam_merge_kernel, dim3(a.N), dim3(a.K * 32), 0, lc.stream, a, nchunk, lc.status);

@@ -47,6 +47,46 @@ __device__ __forceinline__ void gather8(const bf16* p, int step, int n, Raw8<bf1
   r.a = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
+// Two floats in one register pair, for the packed instructions: half the issue slots of
+// single ones.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float x, float y) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+  return p;
+}
+__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
+__device__ __forceinline__ void split(Pair p, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p));
+}
+__device__ __forceinline__ float fold(Pair p) {
+  float x, y;
+  split(p, x, y);
+  return x + y;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+template <class T>
+__device__ __forceinline__ void widen2(const Raw8<T>& r, Pair* p) {
+  float v[8];
+  widen(r, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = pair(v[2 * i], v[2 * i + 1]);
+}
+
 // The eight columns of a row that thread t of `tpr` takes in its j-th turn: VEC, eight
 // consecutive ones in one 16-byte (fp32: two) access, for D a multiple of 8; else every
 // tpr-th column, so that a warp's accesses are consecutive.  `count`: how many of them
@@ -99,6 +139,14 @@ __device__ __forceinline__ void write8(T* row, const Cols<VEC>& c, const float* 
     for (int e = 0; e < 8; ++e)
       if (e < c.count) row[c.first + (long)e * c.step] = from_f<T>(v[e]);
   }
+}
+
+template <bool VEC, class T>
+__device__ __forceinline__ void write8(T* row, const Cols<VEC>& c, const Pair* p) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split(p[i], v[2 * i], v[2 * i + 1]);
+  write8<VEC>(row, c, v);
 }
 
 // Sums of NV (1, 2 or 4) values over the threads of a row, given to all of them.  Each
