@@ -321,8 +321,8 @@ bcmt_status bcmt_dropout(const bcmt_dropout_params* p, const void* x, const void
  *            divides rows: 1 for all rows, the number of sequences, rows); NULL: 1
  *
  * Statistics and everything between the loads and the stores are fp32; n is the
- * norm of h before its rounding.  Requirements: rows >= 0, 1 <= D <= 8192,
- * rows * D <= 2^40, alpha finite, eps >= 0 and finite.  flags: BCMT_FLAG_CHECK
+ * norm of h before its rounding.  Requirements: 0 <= rows <= 2^30, 1 <= D <= 8192,
+ * alpha finite, eps >= 0 and finite.  flags: BCMT_FLAG_CHECK
  * only.  h may be x or branch; no other output may overlap an input. */
 typedef struct {
   long long rows;
@@ -432,8 +432,8 @@ bcmt_status bcmt_beam_select(const bcmt_beam_params* p, const void* logits, cons
                              long long* tokens, void* finished_out, void* workspace, void* stream);
 
 /* dst[n, k] = src[n, parents[n, k]] for `count` tensors of N x K rows of
- * row_bytes bytes each (dense; src and dst do not overlap), one launch for up to
- * 128.  A parent outside [0, K) gives a row of zeros and is reported as
+ * row_bytes bytes each (dense; no dst overlaps a src or another dst), one launch for
+ * up to 128.  A parent outside [0, K) gives a row of zeros and is reported as
  * BCMT_ERR_ARG by the next bcmt_device_status.  N * K <= 2^22, K <= 32. */
 typedef struct {
   const void* src;

@@ -10,9 +10,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
+from array import array
 from typing import Optional
 
-import numpy as np
 import torch
 from torch.autograd.graph import increment_version
 
@@ -41,7 +41,7 @@ def beam_select(logits, scores, finished=None, eos: Optional[int] = None):
     dev = _device(logits)
     if logits.dim() != 3:
         raise ValueError(f"logits must be [N, K, V], not {tuple(logits.shape)}")
-    if logits.requires_grad and torch.is_grad_enabled():
+    if (logits.requires_grad or scores.requires_grad) and torch.is_grad_enabled():
         raise ValueError("beam_select is not differentiable: call it under torch.no_grad")
     dt = _dtype(logits, "logits")
     N, K, V = logits.shape
@@ -72,7 +72,7 @@ def beam_select(logits, scores, finished=None, eos: Optional[int] = None):
 
 def beam_reorder(tensors, parents, out=None):
     """``t[n, parents[n, k]]`` for every t of ``tensors`` ([N, K, ...] or [N * K, ...], any type):
-    a list of new tensors, or those of ``out`` (dense, apart from ``tensors``).  A parent
+    a list of new tensors, or those of ``out`` (dense; they may not share memory with ``tensors`` or each other).  A parent
     outside its beams gives zeros and is reported by ``bcmt.bcmt_device_status``."""
     if not isinstance(parents, torch.Tensor):
         raise ValueError(f"parents must be a tensor, not {type(parents).__name__}")
@@ -83,49 +83,38 @@ def beam_reorder(tensors, parents, out=None):
     if parents.dim() != 2 or parents.dtype != torch.int64:
         raise ValueError(f"parents must be int64 [N, K], not {parents.dtype} {tuple(parents.shape)}")
     N, K = parents.shape
-    tensors = list(tensors)
+    NK, at = N * K, dev.index
     parents = parents.contiguous()
-    rows = []
-    for t in tensors:
-        if t.device != dev or not (t.shape[:2] == (N, K) or (t.dim() >= 1 and t.shape[0] == N * K)):
+    grad, rows, table = torch.is_grad_enabled(), [], array("q")
+    tensors = list(tensors)
+    fresh = out is None
+    out = [None] * len(tensors) if fresh else list(out)
+    if len(out) != len(tensors):
+        raise ValueError(f"out must have {len(tensors)} tensors, not {len(out)}")
+    for i, t in enumerate(tensors):
+        shape = t.shape
+        n = t.numel()
+        if (t.device.index != at or t.device.type != dev.type or not shape
+                or not (shape[0] == NK or (len(shape) > 1 and shape[0] == N and shape[1] == K))):
             raise ValueError(f"tensors must be [N, K, ...] or [N K, ...] on {dev}, not "
-                             f"{tuple(t.shape)} on {t.device}")
-        if t.requires_grad and torch.is_grad_enabled():
+                             f"{tuple(shape)} on {t.device}")
+        if grad and t.requires_grad:
             raise ValueError("beam_reorder is not differentiable: call it under torch.no_grad")
-        rows.append(t.contiguous())
-    if out is None:
-        out = [torch.empty_like(t) for t in rows]
-    else:
-        out = list(out)
-        if len(out) != len(tensors):
-            raise ValueError(f"out must have {len(tensors)} tensors, not {len(out)}")
-        for t, o in zip(tensors, out):
-            _check(o, "out", t.shape, t.dtype, dev)
-            if not o.is_contiguous():
+        if not t.is_contiguous():
+            t = t.contiguous()
+            rows.append(t)   # alive until the launch
+        if fresh:
+            o = out[i] = torch.empty_like(t)
+        else:
+            o = out[i]
+            if o.shape != shape or o.dtype != t.dtype or o.device != t.device or not o.is_contiguous():
+                _check(o, "out", shape, t.dtype, dev)
                 raise ValueError("out must be dense")
-        increment_version(out)   # written through its address, which autograd cannot see
-    if not out or N * K == 0:
+        table.extend((t.data_ptr(), o.data_ptr(), n // NK * t.element_size() if n else 0))
+    if not out or NK == 0:
         return out
-    table = np.empty((len(out), 3), dtype=np.int64)
-    table[:, 0] = [t.data_ptr() for t in rows]
-    table[:, 1] = [o.data_ptr() for o in out]
-    table[:, 2] = [t.numel() // (N * K) * t.element_size() for t in rows]
-    # what one launch writes, no other tensor of it may read
-    src = sorted((a, a + N * K * n) for a, _, n in table.tolist() if n)
-    dst = sorted((b, b + N * K * n) for _, b, n in table.tolist() if n)
-    if any(a[1] > b[0] for a, b in zip(dst, dst[1:])) or _meet(src, dst):
-        raise ValueError("out must not share memory with tensors or within itself")
-    C.check(C.LIB.bcmt_beam_reorder(parents.data_ptr(), N, K, table.ctypes.data, len(out), 0,
-                                    _raw_stream(dev.index)))
+    C.check(C.LIB.bcmt_beam_reorder(parents.data_ptr(), N, K, table.buffer_info()[0], len(out), 0,
+                                    _raw_stream(at)))
+    if not fresh:
+        increment_version(out)   # written through its address, which autograd cannot see
     return out
-
-
-def _meet(a, b) -> bool:
-    """Whether a range of a (sorted) overlaps one of b (sorted, apart from one another)."""
-    i = 0
-    for lo, hi in a:
-        while i < len(b) and b[i][1] <= lo:
-            i += 1
-        if i < len(b) and b[i][0] < hi:
-            return True
-    return False

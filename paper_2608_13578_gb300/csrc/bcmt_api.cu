@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <new>
 #include <array>
 #include <memory>
 #include <mutex>
@@ -695,13 +696,15 @@ bcmt_status check_adamw(const bcmt_adamw_params* p, const bcmt_adamw_tensor* t) 
   BCMT_TRY(check_flags(p->flags));
   if (p->count > 0 && !t) return fail(BCMT_ERR_ARG, "tensors is NULL");
   const uintptr_t es = p->dtype == BCMT_F32 ? 4 : 2;
+  int first = -1;   // the first tensor that has elements
   for (int i = 0; i < p->count; ++i) {
     if (t[i].n < 0 || t[i].n > (1ll << 40))
       return fail(BCMT_ERR_SHAPE, "tensor %d: n = %lld must be in [0, 2^40]", i, t[i].n);
     if (t[i].n == 0) continue;
     if (!t[i].p || !t[i].g || !t[i].m || !t[i].v)
       return fail(BCMT_ERR_ARG, "tensor %d: p, g, m or v is NULL", i);
-    if ((t[i].master != nullptr) != (t[0].master != nullptr))
+    if (first < 0) first = i;
+    if ((t[i].master != nullptr) != (t[first].master != nullptr))
       return fail(BCMT_ERR_ARG, "tensor %d: masters for all tensors or none", i);
     if (t[i].master && p->dtype == BCMT_F32)
       return fail(BCMT_ERR_ARG, "tensor %d: float32 parameters have no masters", i);
@@ -714,6 +717,34 @@ bcmt_status check_adamw(const bcmt_adamw_params* p, const bcmt_adamw_tensor* t) 
       return fail(BCMT_ERR_ALIGN, "tensor %d: a buffer is not aligned to its type", i);
   }
   return BCMT_OK;
+}
+
+// What one copy of a reordering writes, no copy reads and no other writes.
+struct Span {
+  uintptr_t from, to;
+  bool written;
+};
+bcmt_status check_apart(const bcmt_beam_tensor* t, int count, uintptr_t rows) {
+  Span few[256];
+  Span* s = count <= 128 ? few : new (std::nothrow) Span[2 * (size_t)count];
+  if (!s) return fail(BCMT_ERR_ARG, "no host memory for %d tensors", count);
+  int n = 0;
+  for (int i = 0; i < count; ++i) {
+    if (rows * t[i].row_bytes == 0) continue;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(t[i].src), b = reinterpret_cast<uintptr_t>(t[i].dst);
+    s[n++] = Span{a, a + rows * t[i].row_bytes, false};
+    s[n++] = Span{b, b + rows * t[i].row_bytes, true};
+  }
+  std::sort(s, s + n, [](const Span& a, const Span& b) { return a.from < b.from; });
+  uintptr_t read = 0, written = 0;   // the ends so far
+  bool apart = true;
+  for (int i = 0; i < n; ++i) {
+    apart = apart && s[i].from >= written && (!s[i].written || s[i].from >= read);
+    uintptr_t& end = s[i].written ? written : read;
+    end = std::max(end, s[i].to);
+  }
+  if (s != few) delete[] s;
+  return apart ? BCMT_OK : fail(BCMT_ERR_ARG, "a destination overlaps a source or another destination");
 }
 
 bcmt_status check_beam(const bcmt_beam_params* p) {
@@ -1609,6 +1640,8 @@ bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* d
     a.dbranch = dbranch;
     a.dx = dx;
     a.dgate = dgate;
+    a.wanted = (dweight != nullptr) | (dbias != nullptr) << 1 | (dpost_weight != nullptr) << 2 |
+               (dpost_bias != nullptr) << 3;
     a.part = static_cast<float*>(workspace);
     a.gate_part = a.part + al256(pl.part_bytes) / 4;
     NormJoin j{p->D, p->wtype == BCMT_BF16, p->dtype == BCMT_BF16,
@@ -1634,7 +1667,7 @@ bcmt_status bcmt_adamw_step(const bcmt_adamw_params* p, const bcmt_adamw_tensor*
                      p->lr_ptr, p->grad_scale};
   static_assert(sizeof(AdamwTensor) == sizeof(bcmt_adamw_tensor), "the same layout");
   bool master = false;
-  for (int i = 0; i < p->count; ++i) master |= tensors[i].master != nullptr;
+  for (int i = 0; i < p->count; ++i) master |= tensors[i].n > 0 && tensors[i].master;
   cudaError_t e = adamw_step(lc, p->dtype, p->bits, master, h,
                              reinterpret_cast<const AdamwTensor*>(tensors), p->count);
   if (e != cudaSuccess) return cuda_fail(e, "AdamW step");
@@ -1711,11 +1744,8 @@ bcmt_status bcmt_beam_reorder(const long long* parents, int N, int K,
       return fail(BCMT_ERR_SHAPE, "tensor %d: row_bytes = %lld", i, t.row_bytes);
     if (t.row_bytes == 0 || N == 0) continue;
     if (!t.src || !t.dst) return fail(BCMT_ERR_ARG, "tensor %d: src or dst is NULL", i);
-    const uintptr_t s = reinterpret_cast<uintptr_t>(t.src), d = reinterpret_cast<uintptr_t>(t.dst);
-    const uintptr_t bytes = (uintptr_t)N * K * t.row_bytes;
-    if (s < d + bytes && d < s + bytes)
-      return fail(BCMT_ERR_ARG, "tensor %d: src and dst overlap", i);
   }
+  BCMT_TRY(check_apart(tensors, count, (uintptr_t)N * K));
   unsigned* sp = status_ptr();
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};

@@ -521,8 +521,7 @@ __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant
 namespace {
 
 // Elements per thread of a chunk: 16 where that gives every SM work, else 8, for more
-// CTAs on few rows.  (32 have half the lists, but 200 registers' worth of latency a CTA:
-// 64 x 8 x 32000 take the same time, 40 x 5 x 50257 of fp32 four us more.)
+// CTAs on few rows.
 int chunk_elements(int N, int K, int V, int sms) {
   const long long big = (V + 16 * kThreads - 1) / (16 * kThreads);
   return (long long)N * K * big >= sms ? 16 : 8;

@@ -20,6 +20,7 @@ struct NormBwd {
   float alpha, eps;
   const void *dh, *dn, *branch, *h, *weight, *post_weight, *post_bias, *gate;  // dh may be NULL
   void *dbranch, *dx, *dgate;   // dx, dgate may be NULL
+  int wanted;                   // bits: which of dw, db, dpw, dpb
   float *part, *gate_part;      // sums of each CTA [ctas, 4, D], of each segment [nseg, D]
   // from the plan
   int tpr, rows_per_cta, turns;

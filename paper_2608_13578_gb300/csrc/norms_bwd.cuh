@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) norm_bwd_kernel(const NormBwd a
   const int last = POST ? 4 : 2;
 #pragma unroll
   for (int i = 0; i < last; ++i) {
-    if ((i & 1) && !a.layer) continue;
+    if (!(a.wanted >> i & 1)) continue;
     float* part = a.part + ((long long)blockIdx.x * 4 + i) * D;
     // where vector i of this CTA's threads lies
     const Pair* at = i >= 2 ? tot + (i - 2) * Q * THREADS : SMEM_ACC ? dyn + i * Q * THREADS : dyn;

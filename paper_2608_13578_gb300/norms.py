@@ -18,7 +18,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import bcmt as C
-from .lm_ops import (_address, _buffer, _check, _dense, _device, _dtype, _number, _on_its_device,
+from .lm_ops import (_address, _buffer, _check, _current_device, _dense, _device, _dtype, _number, _on_its_device,
                      _raw_stream)
 
 KINDS = ("layer", "rms")
@@ -103,7 +103,6 @@ def residual_norm_forward(branch, x, weight, bias=None, *, post_weight=None, pos
     return h, n
 
 
-@_on_its_device
 def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=None,
                            post_bias=None, gate=None, residual_scale: float = 1.0,
                            kind: str = "layer", eps: float = 1e-5):
@@ -111,6 +110,12 @@ def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=
     arguments, its h and the gradients dh (None: zero) and dn of its results; None for what
     was not given.  dbranch and dx are one tensor where they are equal (no post norm, no gate,
     residual_scale 1)."""
+    # (dh may be None: the device is that of branch)
+    if isinstance(branch, torch.Tensor) and branch.is_cuda and branch.get_device() != _current_device():
+        with torch.cuda.device(branch.device):
+            return residual_norm_backward(
+                dh, dn, branch, h, weight, bias, post_weight=post_weight, post_bias=post_bias,
+                gate=gate, residual_scale=residual_scale, kind=kind, eps=eps)
     dev, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
     shape, dtype = branch.shape, branch.dtype
     _check(dn, "dn", shape, dtype, dev)

@@ -119,8 +119,9 @@ class AdamWPlan:
                 at.append(0)
                 holes = True
                 continue
-            if g.shape != shape or g.dtype != dtype or g.device != dev:
+            if g.shape != shape or g.dtype != dtype or g.device != dev or g.layout != torch.strided:
                 _check(g, "grads", shape, dtype, dev)
+                raise ValueError("grads must be dense tensors, not sparse ones")
             if not g.is_contiguous():
                 g = g.contiguous()
                 kept.append(g)
@@ -192,6 +193,13 @@ class AdamW(torch.optim.Optimizer):
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
                                       bits=bits, masters=masters, capturable=capturable))
         self._plans = {}
+
+    def __setstate__(self, state):   # a copy, or groups out of a file
+        super().__setstate__(state)
+        self._plans = {}
+        for group in self.param_groups:
+            for k in ("bits", "masters", "capturable"):
+                group.setdefault(k, self.defaults.get(k))
 
     def _init(self, p, group):
         s = self.state[p]
@@ -272,15 +280,15 @@ class AdamW(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
         # the states in their own types (the base class gives them the parameters')
-        params = [p for g in self.param_groups for p in g["params"]]
-        ids = [k for g in state_dict["param_groups"] for k in g["params"]]
-        counts = {}
-        for p, k in zip(params, ids):
-            for name, x in state_dict["state"].get(k, {}).items():
-                if isinstance(x, torch.Tensor):
-                    if name == "step":   # one tensor for those that shared one
-                        x = counts.setdefault(id(x), x.detach().to(p.device, copy=True))
-                    else:
+        for group, saved in zip(self.param_groups, state_dict["param_groups"]):
+            count = {}   # one count for the group where it is on the device
+            for p, k in zip(group["params"], saved["params"]):
+                for name, x in state_dict["state"].get(k, {}).items():
+                    if name == "step":
+                        x = int(x)
+                        if group["capturable"]:
+                            x = count.setdefault(p.device, torch.tensor(x, device=p.device))
+                    elif isinstance(x, torch.Tensor):
                         x = x.detach().to(p.device, copy=True)
-                self.state[p][name] = x
+                    self.state[p][name] = x
         self._plans.clear()
