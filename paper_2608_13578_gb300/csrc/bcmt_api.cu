@@ -1581,7 +1581,7 @@ bcmt_status bcmt_residual_norm_forward(const bcmt_norm_params* p, const void* br
 size_t bcmt_residual_norm_workspace_size(const bcmt_norm_params* p, int post) {
   if (check_norm(p) != BCMT_OK) return 0;
   if (p->rows == 0) return 256;
-  const NormPlan pl = norm_plan(p->rows, p->D, p->gates, post != 0, device_sms());
+  const NormPlan pl = norm_plan(p->rows, p->D, p->dtype == BCMT_F32 ? 4 : 2, p->gates, post != 0, device_sms());
   return al256(pl.part_bytes) + al256(std::max<size_t>(256, pl.gate_bytes));
 }
 
@@ -1621,12 +1621,13 @@ bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* d
     if (dgate && e == cudaSuccess)
       e = fill_zero(lc, dgate, (size_t)p->gates * p->D * (p->dtype == BCMT_BF16 ? 2 : 4));
   } else {
-    const NormPlan pl = norm_plan(p->rows, p->D, p->gates, post_weight != nullptr, device_sms());
+    const NormPlan pl = norm_plan(p->rows, p->D, p->dtype == BCMT_F32 ? 4 : 2, p->gates,
+                                  post_weight != nullptr, device_sms());
     NormBwd a{};
     a.D = p->D;
     a.layer = p->rms == 0;
     a.w_bf16 = p->wtype == BCMT_BF16;
-    a.group_rows = p->gates > 0 ? p->rows / p->gates : 1;
+    a.rows = p->rows;
     a.alpha = p->alpha;
     a.eps = p->eps;
     a.dh = dh;

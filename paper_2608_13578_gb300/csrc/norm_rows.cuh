@@ -79,6 +79,32 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+// Loads from shared memory that are not kept from an earlier one of the same place: where a
+// value is read anew, its registers are meant to be free in between.
+__device__ __forceinline__ uint32_t shared_address(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void load_shared(uint32_t p, Pair& x, Pair& y) {
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(x), "=l"(y) : "r"(p) : "memory");
+}
+__device__ __forceinline__ void load_shared(uint32_t p, uint4& v) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(p) : "memory");
+}
+template <class T> __device__ __forceinline__ float load_shared(uint32_t p);
+template <> __device__ __forceinline__ float load_shared<float>(uint32_t p) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p) : "memory");
+  return v;
+}
+template <> __device__ __forceinline__ float load_shared<bf16>(uint32_t p) {
+  unsigned short v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p) : "memory");
+  return __uint_as_float((uint32_t)v << 16);
+}
+__device__ __forceinline__ void store_shared(uint32_t p, Pair x, Pair y) {
+  asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(p), "l"(x), "l"(y) : "memory");
+}
 template <class T>
 __device__ __forceinline__ void widen2(const Raw8<T>& r, Pair* p) {
   float v[8];
@@ -94,6 +120,8 @@ __device__ __forceinline__ void widen2(const Raw8<T>& r, Pair* p) {
 template <bool VEC>
 struct Cols {
   int first, step, count;
+  __device__ __forceinline__ Cols(int first_, int step_, int count_)
+      : first(first_), step(step_), count(count_) {}
   __device__ __forceinline__ Cols(int t, int tpr, int j, int D) {
     if (VEC) {
       first = (t + j * tpr) * 8;
@@ -198,29 +226,22 @@ __device__ __forceinline__ void row_sums(float (&v)[NV], RowShared& sh, int& slo
     slot ^= 1;
     if (lane < NV) reinterpret_cast<float*>(buf + (threadIdx.x >> 5))[lane] = s;
     bar_sync(bar, nw * 32);
-    float4 t = buf[warp0];
-    for (int w = 1; w < nw; ++w) {
-      const float4 b = buf[warp0 + w];
-      t.x += b.x;
-      if (NV > 1) t.y += b.y;
-      if (NV > 2) t.z += b.z;
-      if (NV > 2) t.w += b.w;
-    }
-    const float f[4] = {t.x, t.y, t.z, t.w};
+    // lane: a value (lane mod NV) of a warp; the warps' together, in the same order in every lane
+    float f = 0.f;
+#pragma unroll 1
+    for (int w = lane / NV; w < nw; w += 32 / NV)
+      f += reinterpret_cast<const float*>(buf + warp0 + w)[lane & (NV - 1)];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = f[i];
+    for (int o = 16; o >= NV; o >>= 1) f += __shfl_xor_sync(0xffffffffu, f, o);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = NV == 1 ? f : __shfl_sync(0xffffffffu, f, i);
   }
 }
 
-// Asynchronous copies of a thread's own elements to its own place in shared memory: what
-// a thread waits for, it has issued itself, so no barrier is needed.
-__device__ __forceinline__ void copy_async16(void* s, const void* g) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(s)),
-               "l"(g) : "memory");
-}
-__device__ __forceinline__ void copy_async4(void* s, const void* g) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(s)),
-               "l"(g) : "memory");
+// Asynchronous copies to shared memory: a thread waits for those that it has issued.
+// 16 bytes, of which the first n are read and the others are zeros.
+__device__ __forceinline__ void copy_async16(uint32_t s, const void* g, int n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(s), "l"(g), "r"(n) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>

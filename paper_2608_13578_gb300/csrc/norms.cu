@@ -14,6 +14,7 @@
 // registers and take the statistics there: the mean first, then the squares around it.
 // Everything between the loads and the stores is fp32, rounded once to the stored type.
 #include <algorithm>
+#include <stdlib.h>
 
 #include "internal.h"
 #include "norm_rows.cuh"
@@ -177,46 +178,79 @@ cudaError_t fwd_typed(const Launch& lc, const NormFwd& a) {
 
 }  // namespace
 
-NormPlan norm_plan(long long rows, int D, long long groups, bool post, int sms) {
+NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, int sms) {
   NormPlan p{};
   if (rows < 1) return p;
-  const int need = (D + 7) / 8;   // threads of eight columns
-  int ctas_per_sm;
-  if (need <= 32) {
-    p.tpr = need <= 16 ? 16 : 32;
-    p.threads = 256;
-    ctas_per_sm = 2;
-  } else if (need <= 256) {
-    p.tpr = (need + 31) / 32 * 32;
-    p.threads = 256 / p.tpr * p.tpr;
-    ctas_per_sm = 2;
-  } else {
-    p.wide = need > 512;
-    p.tpr = ((p.wide ? (need + 1) / 2 : need) + 31) / 32 * 32;
-    p.threads = p.tpr;
-    ctas_per_sm = 1;
+  p.mode = groups == 0 ? kGateNone : groups == rows ? kGateRows : groups == 1 ? kGateOne : kGateGroups;
+  // threads of a row: 8, 16 or one warp of 8 J columns a lane, or the warps that cost least
+  // by a count of instructions (190 a group of eight columns, 180 for the sums)
+  p.tpr = D <= 64 ? 8 : D <= 128 ? 16 : 32;
+  p.J = 1;
+  const int most = norm_max_warps(2) / (post ? 2 : 1);
+  for (int J = 2, best = 1 << 30; D > 256 && J <= 4; ++J) {
+    const int n = (D + 256 * J - 1) / (256 * J), cost = n * (J * 190 + 180);
+    static const char* only = getenv("NORM_J");
+    if (only && J != atoi(only) && D <= 6144) continue;
+    // more than two groups take too many registers without the roles, four with them
+    if (n <= most && cost < best && (J < 3 || (post && (J == 3 || best == 1 << 30)))) {
+      best = cost;
+      p.J = J;
+      p.tpr = n * 32;
+    }
   }
-  p.rows_per_cta = p.threads / p.tpr;
-  p.ctas = (int)std::min<long long>((rows + p.rows_per_cta - 1) / p.rows_per_cta,
-                                    (long long)sms * ctas_per_sm);
-  // segments: each gate's rows in equal parts, so that the workers' longest walk is
-  // short; where rows have gates of their own (or none), all rows are one group
-  const long long g = groups == 0 || groups == rows ? 1 : groups, gr = rows / g;
-  const long long workers = (long long)p.ctas * p.rows_per_cta;
+  const int R = p.tpr < 32 ? 32 / p.tpr : 1, wt = std::max(32, p.tpr), roles = post ? 2 : 1;
+  // segments are of whole steps of R rows
+  const long long g = p.mode == kGateGroups ? groups : 1, gr = rows / g, gs = (gr + R - 1) / R;
+  // workers of a CTA: as many as there are steps for, registers and shared memory allow; the
+  // rings are to hold the next step at least
+  static const char* ww = getenv("NORM_W");
+  const int arrays = p.mode == kGateRows ? 5 : 4;
+  p.gp_smem = p.mode != kGateRows && (post || p.mode != kGateNone);
+  p.tot_smem = post && p.mode == kGateGroups;
+  p.pw_smem = post && p.mode == kGateRows;
+  long long W = std::min<long long>(norm_max_warps(p.J) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
+  W = std::max(1ll, W);
+  if (ww) W = std::min<long long>(W, atoi(ww));
+  const bool vec = D % 8 == 0;
+  long long stage16 = 0, rest16 = 0;
+  auto size = [&](int stages, int slots) {   // whether it fits
+    const long long nt = W * wt;
+    p.stages = stages;
+    p.ds_slots = slots;
+    stage16 = vec ? (long long)arrays * p.J * (es / 2) * nt : arrays * W * (((long long)R * D * es + 30) / 16);
+    rest16 = (p.pw_smem ? 6 : 2) * p.J * wt + (post ? slots * 2 * p.J * nt : 0) +
+             (p.gp_smem ? 2 * p.J * nt : 0) + (p.tot_smem ? 4 * p.J * nt : 0);
+    // the CTA's sums go through the rings at the end
+    p.ring16 = (int)std::max(stages * stage16, 2ll * p.J * nt * roles);
+    p.smem = (int)(p.ring16 + rest16) * 16;
+    return p.smem <= kNormSmem;
+  };
+  while (!size(2, 2) && W > 1) --W;
+  if (p.smem <= kNormSmem) {
+    if (!size(3, 2)) size(2, 2);
+  } else if (!size(2, 1) && !size(1, 1)) {
+    p.tot_smem = p.pw_smem = false;
+    size(1, 1);
+  }
+  p.threads = (int)(W * wt) * roles;
+  p.ctas = (int)std::min<long long>((g * gs + W - 1) / W, sms);
+  // each gate's steps in equal parts, so that the workers' longest walk is short; a gate for
+  // all rows (or none): a segment a worker
+  const long long workers = p.ctas * W;
   long long best = -1;
-  for (long long turns = (g + workers - 1) / workers, i = 0; i < 8; ++i, ++turns) {
-    const long long s = std::min(gr, turns * workers / g), len = (gr + s - 1) / s;
+  for (long long turns = (g + workers - 1) / workers, i = 0; i < (g == 1 ? 1 : 8); ++i, ++turns) {
+    const long long s = std::min(gs, std::max(1ll, turns * workers / g)), len = (gs + s - 1) / s;
     if (best < 0 || turns * len < best) {
       best = turns * len;
-      p.segs_per_group = (gr + len - 1) / len;
-      p.seg_rows = len;
-      p.turns = (int)((g * p.segs_per_group + workers - 1) / workers);
+      p.segs_per_group = (gs + len - 1) / len;
+      p.seg_rows = len * R;
     }
   }
   p.seg_group_rows = gr;
   p.nseg = g * p.segs_per_group;
   p.part_bytes = (size_t)p.ctas * 4 * D * 4;
-  p.gate_bytes = groups > 0 && groups < rows && p.segs_per_group > 1 ? (size_t)p.nseg * D * 4 : 0;
+  p.gate_bytes = (p.mode == kGateOne || p.mode == kGateGroups) && p.segs_per_group > 1
+                     ? (size_t)p.nseg * D * 4 : 0;
   return p;
 }
 
@@ -229,13 +263,20 @@ cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormB
                           const NormJoin& j) {
   if (pl.ctas == 0) return cudaSuccess;
   a.tpr = pl.tpr;
-  a.rows_per_cta = pl.rows_per_cta;
+  a.stages = pl.stages;
+  a.mode = pl.mode;
+  a.ring16 = pl.ring16;
+  a.ds_slots = pl.ds_slots;
+  a.gp_smem = pl.gp_smem;
+  a.tot_smem = pl.tot_smem;
+  a.pw_smem = pl.pw_smem;
   a.seg_rows = pl.seg_rows;
   a.segs_per_group = pl.segs_per_group;
   a.seg_group_rows = pl.seg_group_rows;
   a.nseg = pl.nseg;
-  a.turns = pl.turns;
-  cudaError_t e = dtype == 0 ? norm_bwd_f32(lc, a, pl) : norm_bwd_bf16(lc, a, pl);
+  const auto kernel = dtype == 0 ? a.post_weight ? norm_bwd_f32_post : norm_bwd_f32
+                                 : a.post_weight ? norm_bwd_bf16_post : norm_bwd_bf16;
+  cudaError_t e = kernel(lc, a, pl);
   if (e != cudaSuccess) return e;
   // gates beyond the grid's second axis take further launches
   const long long gates = pl.gate_bytes ? pl.nseg / pl.segs_per_group : 0, all = 4 + gates;

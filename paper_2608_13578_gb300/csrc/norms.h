@@ -14,16 +14,20 @@ struct NormFwd {
   void *h, *n;
 };
 
+// How rows share the gate: none, one for all, one for groups of rows, one per row.
+enum NormMode { kGateNone, kGateOne, kGateGroups, kGateRows };
+
 struct NormBwd {
+  long long rows;
   int D, layer, w_bf16;
-  long long group_rows;
   float alpha, eps;
   const void *dh, *dn, *branch, *h, *weight, *post_weight, *post_bias, *gate;  // dh may be NULL
   void *dbranch, *dx, *dgate;   // dx, dgate may be NULL
   int wanted;                   // bits: which of dw, db, dpw, dpb
   float *part, *gate_part;      // sums of each CTA [ctas, 4, D], of each segment [nseg, D]
   // from the plan
-  int tpr, rows_per_cta, turns;
+  int tpr, stages, mode, ring16, ds_slots;
+  bool gp_smem, tot_smem, pw_smem;
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
 };
 
@@ -36,18 +40,23 @@ struct NormJoin {
   long long first, nparts, segs_per_group;
 };
 
-// How a backward call is cut: threads of a row, rows at a time in a CTA, CTAs, and the
-// segments of rows that its workers walk.
+// How a backward call is cut: threads of a row with 8 J columns each, threads of a CTA,
+// CTAs, its shared memory, and the segments of rows that its workers walk.
 struct NormPlan {
-  int tpr, threads, rows_per_cta, ctas, turns;
-  bool wide;
+  int tpr, J, threads, ctas, stages, mode, ring16, ds_slots, smem;
+  bool gp_smem, tot_smem, pw_smem;
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
   size_t part_bytes, gate_bytes;
 };
 constexpr int kNormMaxD = 8192;
-NormPlan norm_plan(long long rows, int D, long long groups, bool post, int sms);
+constexpr int kNormSmem = 227 * 1024 - 1024;   // of a CTA, beside the sums' buffers
+// Warps of a CTA whose threads have 8 J columns: 96 and 128 registers a thread.
+constexpr int norm_max_warps(int J) { return J == 1 ? 20 : 16; }
+NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, int sms);
 cudaError_t norm_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norm_bwd_f32_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norm_bwd_bf16_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a);
 cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormBwd a,
                           const NormJoin& j);
