@@ -1645,8 +1645,9 @@ bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* d
                (dpost_bias != nullptr) << 3;
     a.part = static_cast<float*>(workspace);
     a.gate_part = a.part + al256(pl.part_bytes) / 4;
-    NormJoin j{p->D, p->wtype == BCMT_BF16, p->dtype == BCMT_BF16,
-               {dweight, dbias, dpost_weight, dpost_bias}, dgate, a.part, a.gate_part, 0, 0, 0};
+    NormJoin j{p->D, p->wtype == BCMT_BF16, p->dtype == BCMT_BF16, 0,
+               {dweight, dbias, dpost_weight, dpost_bias}, dgate, nullptr, nullptr, nullptr,
+               a.part, a.gate_part, 0, 0, 0};
     e = norm_backward(lc, p->dtype, pl, a, j);
   }
   if (e != cudaSuccess) return cuda_fail(e, "residual norm backward");

@@ -20,7 +20,14 @@ __device__ __forceinline__ void widen(const Raw8<float>& r, float* v) {
   v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w;
   v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
 }
-__device__ __forceinline__ void widen(const Raw8<bf16>& r, float* v) { unpack8(r.a, v); }
+__device__ __forceinline__ void widen(const Raw8<bf16>& r, float* v) {
+  const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
 __device__ __forceinline__ void zero(Raw8<float>& r) {
   r.a = r.b = make_float4(0.f, 0.f, 0.f, 0.f);
 }
@@ -79,6 +86,12 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
+__device__ __forceinline__ Pair shfl_xor(Pair p, int o) {
+  float x, y;
+  split(p, x, y);
+  return pair(__shfl_xor_sync(0xffffffffu, x, o), __shfl_xor_sync(0xffffffffu, y, o));
+}
+
 // Loads from shared memory that are not kept from an earlier one of the same place: where a
 // value is read anew, its registers are meant to be free in between.
 __device__ __forceinline__ uint32_t shared_address(const void* p) {

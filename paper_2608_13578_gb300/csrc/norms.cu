@@ -14,7 +14,6 @@
 // registers and take the statistics there: the mean first, then the squares around it.
 // Everything between the loads and the stores is fp32, rounded once to the stored type.
 #include <algorithm>
-#include <stdlib.h>
 
 #include "internal.h"
 #include "norm_rows.cuh"
@@ -114,46 +113,55 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_fwd_kernel(const N
   }
 }
 
-// Sums of the CTAs' and segments' parts: blockIdx.y is one of the four vectors of
-// weights, or 4 + a gate; a CTA adds 32 columns with 8 lines of threads, each over every
-// eighth part, then the lines in order.
-__global__ void __launch_bounds__(256) norm_join_kernel(const NormJoin a) {
-  __shared__ float s[8][33];
+// Sums of the CTAs' and segments' parts: blockIdx.y is one of the four vectors of weights
+// (with one gate for all rows the last two are A and B), or 4 + a gate; a CTA adds 32
+// columns with 16 lines of threads, each over every 16th part, then the lines in order.
+__global__ void __launch_bounds__(512) norm_join_kernel(const NormJoin a) {
+  __shared__ float s[16][33];
   pdl_enter();
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), line = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, col = blockIdx.x * 32 + lane, line = threadIdx.x >> 5;
   const long long y = blockIdx.y + (long long)a.first;
-  const float* in;
-  long long n, stride;
-  void* out;
-  bool is_bf16;
-  if (y < 4) {
-    in = a.part + y * a.D;
-    n = a.nparts;
-    stride = 4ll * a.D;
-    out = a.out[y];
-    is_bf16 = a.w_bf16;
-  } else {
-    in = a.gate_part + (y - 4) * a.segs_per_group * a.D;
-    n = a.segs_per_group;
-    stride = a.D;
-    out = a.dgate;
-    is_bf16 = a.t_bf16;
-  }
+  const bool one = a.mode == kGateOne;
+  void* const out = y < 4 ? a.out[y] : a.dgate;
   if (!out) return;
-  float v = 0.f;
-  if (col < a.D) {
-#pragma unroll 4
-    for (long long i = line; i < n; i += 8) v += in[i * stride + col];
-  }
-  s[line][threadIdx.x & 31] = v;
-  __syncthreads();
-  if (line == 0 && col < a.D) {
+  auto sum = [&](const float* in, long long n, long long stride) {   // in line 0
+    float v = 0.f;
+    if (col < a.D) {
+#pragma unroll 8
+      for (long long i = line; i < n; i += 16) v += in[i * stride + col];
+    }
+    __syncthreads();
+    s[line][lane] = v;
+    __syncthreads();
+    if (line == 0) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
-    const long long at = y < 4 ? col : (y - 4) * a.D + col;
-    if (is_bf16) static_cast<bf16*>(out)[at] = from_f<bf16>(v);
-    else static_cast<float*>(out)[at] = v;
+      for (int i = 1; i < 16; ++i) v += s[i][lane];
+    }
+    return v;
+  };
+  auto part = [&](int i) { return sum(a.part + (long long)i * a.D, a.nparts, 4ll * a.D); };
+  auto weight = [&](const void* w, bool is_bf16) {
+    return is_bf16 ? to_f(static_cast<const bf16*>(w)[col]) : static_cast<const float*>(w)[col];
+  };
+  const bool on = line == 0 && col < a.D;
+  float v;
+  if (y < 4) {
+    v = part((int)y);
+    if (on && one && y >= 2) v *= weight(a.gate, a.t_bf16);
+  } else if (one) {
+    v = part(2);
+    if (a.post_weight && on) v *= weight(a.post_weight, a.w_bf16);
+    if (a.post_bias) {
+      const float b = part(3);
+      if (on) v = fmaf(weight(a.post_bias, a.w_bf16), b, v);
+    }
+  } else {
+    v = sum(a.gate_part + (y - 4) * a.segs_per_group * a.D, a.segs_per_group, a.D);
   }
+  if (!on) return;
+  const long long at = y < 4 ? col : (y - 4) * a.D + col;
+  if (y < 4 ? a.w_bf16 : a.t_bf16) static_cast<bf16*>(out)[at] = from_f<bf16>(v);
+  else static_cast<float*>(out)[at] = v;
 }
 
 namespace {
@@ -189,8 +197,6 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   const int most = norm_max_warps(2) / (post ? 2 : 1);
   for (int J = 2, best = 1 << 30; D > 256 && J <= 4; ++J) {
     const int n = (D + 256 * J - 1) / (256 * J), cost = n * (J * 190 + 180);
-    static const char* only = getenv("NORM_J");
-    if (only && J != atoi(only) && D <= 6144) continue;
     // more than two groups take too many registers without the roles, four with them
     if (n <= most && cost < best && (J < 3 || (post && (J == 3 || best == 1 << 30)))) {
       best = cost;
@@ -203,14 +209,12 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   const long long g = p.mode == kGateGroups ? groups : 1, gr = rows / g, gs = (gr + R - 1) / R;
   // workers of a CTA: as many as there are steps for, registers and shared memory allow; the
   // rings are to hold the next step at least
-  static const char* ww = getenv("NORM_W");
   const int arrays = p.mode == kGateRows ? 5 : 4;
   p.gp_smem = p.mode != kGateRows && (post || p.mode != kGateNone);
   p.tot_smem = post && p.mode == kGateGroups;
   p.pw_smem = post && p.mode == kGateRows;
   long long W = std::min<long long>(norm_max_warps(p.J) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
   W = std::max(1ll, W);
-  if (ww) W = std::min<long long>(W, atoi(ww));
   const bool vec = D % 8 == 0;
   long long stage16 = 0, rest16 = 0;
   auto size = [&](int stages, int slots) {   // whether it fits
@@ -249,8 +253,7 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   p.seg_group_rows = gr;
   p.nseg = g * p.segs_per_group;
   p.part_bytes = (size_t)p.ctas * 4 * D * 4;
-  p.gate_bytes = (p.mode == kGateOne || p.mode == kGateGroups) && p.segs_per_group > 1
-                     ? (size_t)p.nseg * D * 4 : 0;
+  p.gate_bytes = p.mode == kGateGroups && p.segs_per_group > 1 ? (size_t)p.nseg * D * 4 : 0;
   return p;
 }
 
@@ -270,6 +273,7 @@ cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormB
   a.gp_smem = pl.gp_smem;
   a.tot_smem = pl.tot_smem;
   a.pw_smem = pl.pw_smem;
+  if (pl.mode == kGateOne && a.dgate) a.wanted |= a.post_bias ? 12 : 4;
   a.seg_rows = pl.seg_rows;
   a.segs_per_group = pl.segs_per_group;
   a.seg_group_rows = pl.seg_group_rows;
@@ -279,14 +283,19 @@ cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormB
   cudaError_t e = kernel(lc, a, pl);
   if (e != cudaSuccess) return e;
   // gates beyond the grid's second axis take further launches
-  const long long gates = pl.gate_bytes ? pl.nseg / pl.segs_per_group : 0, all = 4 + gates;
+  const long long gates = pl.mode == kGateOne ? 1 : pl.gate_bytes ? pl.nseg / pl.segs_per_group : 0;
+  const long long all = (gates ? 4 + gates : a.post_weight ? 4 : 2);
   for (long long y = 0; y < all && e == cudaSuccess; y += 65535) {
     NormJoin q = j;
     q.first = y;
     q.nparts = pl.ctas;
     q.segs_per_group = pl.segs_per_group;
+    q.mode = pl.mode;
+    q.gate = a.gate;
+    q.post_weight = a.post_weight;
+    q.post_bias = a.post_bias;
     e = launch_k(norm_join_kernel, dim3((a.D + 31) / 32, (unsigned)std::min<long long>(65535, all - y)),
-                 dim3(256), 0, lc.stream, q);
+                 dim3(512), 0, lc.stream, q);
   }
   return e;
 }

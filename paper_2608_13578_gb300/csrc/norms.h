@@ -31,11 +31,13 @@ struct NormBwd {
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
 };
 
-// Sums of the parts: dw, db, dpw, dpb (NULL: not wanted) and the gates' gradient.
+// Sums of the parts: dw, db, dpw, dpb (NULL: not wanted) and the gates' gradient (with one
+// gate: from the last two, which it also scales).
 struct NormJoin {
-  int D, w_bf16, t_bf16;
+  int D, w_bf16, t_bf16, mode;
   void* out[4];
   void* dgate;
+  const void *gate, *post_weight, *post_bias;
   const float *part, *gate_part;
   long long first, nparts, segs_per_group;
 };

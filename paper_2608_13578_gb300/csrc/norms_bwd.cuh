@@ -25,7 +25,7 @@ namespace bcmt {
 //
 // With A = sum ds yh and B = sum ds over the rows of one gate, its gradient is pw A + pb B,
 // and it adds g A to dpw and g B to dpb: the sums take A and B, and what depends on the
-// gate is done once for its segment.  A gate per row (ROWS) comes through the ring too, and
+// gate is done once for its segment (a gate for all rows: when the CTAs' sums are joined).  A gate per row (ROWS) comes through the ring too, and
 // the sums take g ds.
 enum { kRolePre, kRolePost, kRoleAll };
 
@@ -476,7 +476,7 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
         advance();
       }
     }
-    if (!LAST || ROWS || a.mode == kGateNone) continue;
+    if (!LAST || ROWS || a.mode != kGateGroups) continue;
     // A and B of the gate's segment that ends here: the gate's gradient, and dpw and dpb
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -486,35 +486,27 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
       for (int i = 0; i < 4; ++i) s0[i] = acc[kA][4 * j + i];
       if (POST) {
         Pair g[4], pw[4], s1[4];
-        gate_row(j, a.mode == kGateGroups ? grp : 0, g);
+        gate_row(j, grp, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) s1[i] = acc[1][4 * j + i];
-        if (a.mode == kGateOne) {   // the only segment of the worker
+        Pair u[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            acc[0][4 * j + i] = mul2(s0[i], g[i]);
-            acc[1][4 * j + i] = mul2(s1[i], g[i]);
+        for (int i = 0; i < 2; ++i) {
+          float* part = a.part + ((long long)blockIdx.x * 4 + 2 + i) * D;
+          if (a.tot_smem) {
+            get2(tot + i * V + 2 * j * G, u);
+          } else {
+            Raw8<float> r;
+            read8<VEC>(part, c, true, r);
+            widen2(r, u);
           }
-        } else {
-          Pair u[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float* part = a.part + ((long long)blockIdx.x * 4 + 2 + i) * D;
-            if (a.tot_smem) {
-              get2(tot + i * V + 2 * j * G, u);
-            } else {
-              Raw8<float> r;
-              read8<VEC>(part, c, true, r);
-              widen2(r, u);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              u[e] = fma2(acc[i][4 * j + e], g[e], u[e]);
-              acc[i][4 * j + e] = 0;
-            }
-            if (a.tot_smem) put2(tot + i * V + 2 * j * G, u);
-            else write8<VEC>(part, c, u);
+          for (int e = 0; e < 4; ++e) {
+            u[e] = fma2(acc[i][4 * j + e], g[e], u[e]);
+            acc[i][4 * j + e] = 0;
           }
+          if (a.tot_smem) put2(tot + i * V + 2 * j * G, u);
+          else write8<VEC>(part, c, u);
         }
         vector(a.post_weight, j, pw);
 #pragma unroll
@@ -534,7 +526,7 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
 #pragma unroll
         for (int o = TPR; o < 32; o <<= 1)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s0[i] = add2(s0[i], __shfl_xor_sync(0xffffffffu, s0[i], o));
+          for (int i = 0; i < 4; ++i) s0[i] = add2(s0[i], shfl_xor(s0[i], o));
       }
       if (sub == 0) {
         if (a.segs_per_group == 1) write8<VEC>(static_cast<T*>(a.dgate) + seg * D, c, s0);
@@ -544,30 +536,39 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
   }
   if (ROLE == kRolePre && handed) bar_sync(handover, 2 * wt);
   copy_wait<0>();
-  // the CTA's sums (dw, db | dpw, dpb): its rows' added through shared memory
+  // the CTA's sums (dw, db | dpw, dpb, or for one gate A, B): its rows' added through shared
+  // memory
   const uint32_t buf0 = base + (ROLE == kRolePost ? nwarps * V : 0);
+  constexpr bool kTotals = ROLE == kRolePost && !ROWS;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < NACC; ++i) {
     const int v = i + (ROLE == kRolePost ? 2 : 0);
-    const bool totals = ROLE == kRolePost && !ROWS && a.mode == kGateGroups;
+    const bool want = (a.wanted >> v & 1) && !(kTotals && a.mode == kGateGroups && !a.tot_smem);
     __syncthreads();
-    if (!totals) {
+    if (want) {
 #pragma unroll
-      for (int j = 0; j < J; ++j) put2(buf0 + wid * V + lane * 16 + 2 * j * G, acc[i] + 4 * j);
+      for (int j = 0; j < J; ++j) {
+        Pair* p = acc[i] + 4 * j;
+        if (kTotals && a.tot_smem) get2(tot + (i & 1) * V + 2 * j * G, p);
+        if (R > 1) {   // rows side by side in a warp
+#pragma unroll
+          for (int o = TPR; o < 32; o <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = add2(p[e], shfl_xor(p[e], o));
+        }
+        put2(buf0 + wid * V + lane * 16 + 2 * j * G, p);
+      }
     }
     __syncthreads();
-    if (tid < tpr && (a.wanted >> v & 1) && !(totals && !a.tot_smem)) {
-      const uint32_t from = totals ? tot0 + i * V : buf0, warp_bytes = totals ? 2 * V : V;
+    if (tid < tpr && want) {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         Pair s[4] = {0, 0, 0, 0}, u[4];
-        for (int k = wr; k < nwarps; k += wt / 32)
+        for (int k = wr; k < nwarps; k += wt / 32) {
+          get2(buf0 + k * V + 2 * j * G + lane * 16, u);
 #pragma unroll
-          for (int r = 0; r < R; ++r) {
-            get2(from + k * warp_bytes + 2 * j * G + (lane + r * TPR % 32) * 16, u);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] = add2(s[e], u[e]);
-          }
+          for (int e = 0; e < 4; ++e) s[e] = add2(s[e], u[e]);
+        }
         write8<VEC>(a.part + ((long long)blockIdx.x * 4 + v) * D, columns(j), s);
       }
     }

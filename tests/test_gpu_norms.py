@@ -128,6 +128,21 @@ def test_constant_rows_and_offsets(N, D):
     check(N, t, dh, dn, 1.0, "layer")
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("D", [16, 100, 264, 768, 1001, 4096])
+def test_rows_whose_first_element_stands_out(N, D, dtype):
+    """The backward takes a row's squares less its first element: an outlier there, a row of
+    nothing else, and one that hides a small deviation behind a large mean."""
+    t, dh, dn = make((3, 5, D), dtype, F, "layer", True, (3, 1, D))
+    for y in (t["branch"], t["x"]):
+        y[0, 0, 0] = 1e4
+        y[1, 2] = 0.0
+        y[1, 2, 0] = -3e3
+        y[2, 1] = 0.01 * y[2, 1] + 64.0
+        y[2, 1, 0] = 0.0
+    check(N, t, dh, dn, 1.0, "layer")
+
+
 @pytest.mark.parametrize("D", [24, 1001])
 def test_not_finite_rows_stay_apart(N, D):
     t, dh, dn = make((3, 9, D), BF, BF, "rms", True, (3, 1, D), bias=False, post_bias=False)
