@@ -19,6 +19,7 @@
 #include "adamw.h"
 #include "common.cuh"
 #include "internal.h"
+#include "pairs.cuh"
 
 namespace bcmt {
 
@@ -130,50 +131,101 @@ namespace {
 __device__ __forceinline__ float byte_float(uint32_t word, int i) {
   return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440u | i));
 }
-// Four codes of m (two's complement) and of v as the values that they stand for.
-__device__ __forceinline__ void decode_m(uint32_t word, float s, float* m) {
+// Four codes of m (two's complement) and of v as the values that they stand for, in pairs
+// (one instruction for two operations, each rounded as it is alone).
+__device__ __forceinline__ void decode_m(uint32_t word, float s, Pair* m) {
   word ^= 0x80808080u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float c = byte_float(word, i) - 8388736.f;
-    m[i] = __fmul_rn(c * fabsf(c), s);
+  for (int i = 0; i < 2; ++i) {
+    float x, y;
+    split(add2(pair(byte_float(word, 2 * i), byte_float(word, 2 * i + 1)), both(-8388736.f)), x, y);
+    m[i] = mul2(pair(x * fabsf(x), y * fabsf(y)), both(s));
   }
 }
-__device__ __forceinline__ void decode_v(uint32_t word, float r, float* v) {
+__device__ __forceinline__ void decode_v(uint32_t word, float r, Pair* v) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float c = byte_float(word, i) - 8388608.f, q = __fmul_rn(c * c, r);
-    v[i] = __fmul_rn(q, q);
+  for (int i = 0; i < 2; ++i) {
+    const Pair c = add2(pair(byte_float(word, 2 * i), byte_float(word, 2 * i + 1)), both(-8388608.f));
+    const Pair q = mul2(mul2(c, c), both(r));
+    v[i] = mul2(q, q);
   }
 }
-constexpr float kToInt = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer
-// The number of thresholds up to x.  The root is within 2^-21 of its value, and a little
-// more is added, so that its rounding is the count or one more: the threshold decides.
-__device__ __forceinline__ float count_m(float x) {
-  float k = __fadd_rn(__fadd_rn(__fmul_rn(root(x), 1.f + 1.f / (1 << 19)), kToInt), -kToInt);
-  const float h = k - 0.5f;
-  if (__fmul_rn(h, h) > x) k -= 1.f;
-  return fmaxf(k, 0.f);
+// A sum of products that stay rounded: one at a time (a packed product and a packed sum came out
+// as one rounding).
+__device__ __forceinline__ Pair sum2(Pair a, Pair b) {
+  float a0, a1, b0, b1;
+  split(a, a0, a1);
+  split(b, b0, b1);
+  return pair(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
 }
-__device__ __forceinline__ float count_v(float y) {
-  float k = __fadd_rn(__fadd_rn(__fmul_rn(root(root(y)), 1.f + 1.f / (1 << 19)), kToInt), -kToInt);
-  const float h = k - 0.5f, q = __fmul_rn(h, h);
-  if (__fmul_rn(q, q) > y) k -= 1.f;
-  return fmaxf(k, 0.f);
+__device__ __forceinline__ float root_ftz(float x) {
+  float y;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-__device__ __forceinline__ uint32_t pack4(const float* k) {
-  uint32_t b[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(k[i], kToInt));
-  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+__device__ __forceinline__ float reciprocal_ftz(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float x, float y) {   // NaN where one is
+  float z;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+  return z;
+}
+// A count of thresholds as the float 1.5 * 2^23 + count, whose last byte is the code: what is
+// added to the root, rounded to an integer there, is the count or one more (the roots below are
+// within 2^-20 of their values, and 2^-18 of them is added): the threshold decides.
+constexpr float kToInt = 12582912.f, kMore = 1.f + 1.f / (1 << 18);
+__device__ __forceinline__ void round2(Pair roots, Pair& t, Pair& k) {
+  t = fma2(roots, both(kMore), both(kToInt));
+  k = add2(t, both(-kToInt));
+}
+// Signed codes of m: x = |m| / s.  The threshold's square keeps the sign of k - 1/2, so that 0
+// stays.
+__device__ __forceinline__ void code_m(Pair m, float si, float& c0, float& c1) {
+  float a, b, k0, k1;
+  split(m, a, b);
+  const float xa = fabsf(a) * si, xb = fabsf(b) * si;
+  Pair t, k;
+  round2(pair(copysignf(root_ftz(xa), a), copysignf(root_ftz(xb), b)), t, k);
+  split(t, c0, c1);
+  split(k, k0, k1);
+  const float ha = fabsf(k0) - 0.5f, hb = fabsf(k1) - 0.5f;
+  if (ha * fabsf(ha) > xa) c0 -= copysignf(1.f, a);
+  if (hb * fabsf(hb) > xb) c1 -= copysignf(1.f, b);
+}
+// Codes of v: y = (v / r) / r; roots: of v.  least: kToInt + 1, the code of a v above 0 (kToInt in
+// a block of zeros).
+__device__ __forceinline__ void code_v(Pair v, Pair roots, float qi, float least, float& c0, float& c1) {
+  const Pair q2 = both(qi), y = mul2(mul2(v, q2), q2);
+  float a, b, ya, yb, r0, r1, h0, h1;
+  split(v, a, b);
+  split(y, ya, yb);
+  split(mul2(roots, q2), r0, r1);
+  Pair t, k;
+  round2(pair(root_ftz(r0), root_ftz(r1)), t, k);
+  split(t, c0, c1);
+  Pair h = add2(k, both(-0.5f));
+  h = mul2(h, h);
+  split(mul2(h, h), h0, h1);
+  if (h0 > ya) c0 -= 1.f;
+  if (h1 > yb) c1 -= 1.f;
+  c0 = fmaxf(c0, a > 0.f ? least : kToInt);
+  c1 = fmaxf(c1, b > 0.f ? least : kToInt);
+}
+__device__ __forceinline__ uint32_t pack4(const float* t) {
+  return __byte_perm(__byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040),
+                     __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040), 0x5410);
 }
 
 }  // namespace
 
 // States in 8 bits: a warp takes a block of 256 elements, eight per lane, whose largest
-// values are a maximum over the warp.  About 70 instructions an element against 10 bytes
-// (bf16): the arithmetic takes about as long as the bytes.
-template <class T, bool MASTER, int CAP>
+// values are a maximum over the warp.  About 50 instructions an element against 10 bytes
+// (bf16): the arithmetic takes about as long as the bytes.  FTZ: a v below 2^-126 has no root
+// (see adamw_step, which chooses).
+template <class T, bool MASTER, bool FTZ, int CAP>
 __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ AdamwTable<CAP> a) {
   pdl_enter();
   long long at;
@@ -195,7 +247,7 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
     const float s0 = t.m_scale[blk], r0 = t.v_scale[blk];
     const bool whole = t.vec && b0 + kBlock <= t.n;
     const int left = (int)min(8ll, max(0ll, t.n - i));
-    float pv[8], gv[8], m[8], v[8];
+    float pv[8], gv[8];
     uint2 mw = make_uint2(0, 0), vw = make_uint2(0, 0);
     if (whole) {
       if (MASTER) load8(w + i, pv);
@@ -203,7 +255,7 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
       load8(g + i, gv);
       mw = *reinterpret_cast<const uint2*>(mc + i);
       vw = *reinterpret_cast<const uint2*>(vc + i);
-    } else {
+    } else {   // zeros past the end, whose moments stay zeros
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool on = e < left;
@@ -214,35 +266,47 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
         (e < 4 ? vw.x : vw.y) |= vb << 8 * (e & 3);
       }
     }
+    Pair m[4], v[4], roots[4];
     decode_m(mw.x, s0, m);
-    decode_m(mw.y, s0, m + 4);
+    decode_m(mw.y, s0, m + 2);
     decode_v(vw.x, r0, v);
-    decode_v(vw.y, r0, v + 4);
-    // the largest as bits: the order of the values, with NaN above infinity
-    uint32_t mm = 0, vm = 0;
+    decode_v(vw.y, r0, v + 2);
+    float mm = 0.f, vm = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      moments(h, gv[e] * gs, m[e], v[e]);
-      pv[e] = weight(h, r, pv[e], m[e], v[e]);
-      if (whole || e < left) {
-        mm = max(mm, __float_as_uint(m[e]) & 0x7fffffffu);
-        vm = max(vm, __float_as_uint(v[e]));
-      }
+    for (int e = 0; e < 4; ++e) {
+      const Pair x = mul2(pair(gv[2 * e], gv[2 * e + 1]), both(gs));
+      m[e] = sum2(mul2(m[e], both(h.b1)), mul2(x, both(h.omb1)));
+      v[e] = sum2(mul2(v[e], both(h.b2)), mul2(mul2(x, both(h.omb2)), x));
+      float m0, m1, v0, v1;
+      split(m[e], m0, m1);
+      split(v[e], v0, v1);
+      // p keep - rate m / (root(v) ib2 + eps)
+      float d0, d1, q0, q1;
+      roots[e] = FTZ ? pair(root_ftz(v0), root_ftz(v1)) : pair(root(v0), root(v1));
+      split(fma2(roots[e], both(r.ib2), both(h.eps)), d0, d1);
+      const Pair q = FTZ ? mul2(m[e], pair(reciprocal_ftz(d0), reciprocal_ftz(d1)))
+                         : pair(__fdividef(m0, d0), __fdividef(m1, d1));
+      split(fma2(q, both(-r.rate), mul2(pair(pv[2 * e], pv[2 * e + 1]), both(r.keep))), q0, q1);
+      pv[2 * e] = q0;
+      pv[2 * e + 1] = q1;
+      mm = max_nan(mm, max_nan(fabsf(m0), fabsf(m1)));
+      vm = max_nan(vm, max_nan(v0, v1));
     }
-    mm = __reduce_max_sync(0xffffffffu, mm);
-    vm = __reduce_max_sync(0xffffffffu, vm);
-    float s = __fmul_rn(__uint_as_float(mm), (float)(1.0 / 16129.0));
-    float q = __fmul_rn(__fsqrt_rn(__uint_as_float(vm)), (float)(1.0 / 65025.0));
+    // the largest as bits: the order of the values, with NaN above infinity
+    const uint32_t mb = __reduce_max_sync(0xffffffffu, __float_as_uint(mm));
+    const uint32_t vb = __reduce_max_sync(0xffffffffu, __float_as_uint(vm));
+    float s = __fmul_rn(__uint_as_float(mb), (float)(1.0 / 16129.0));
+    float q = __fmul_rn(__fsqrt_rn(__uint_as_float(vb)), (float)(1.0 / 65025.0));
     // below these the reciprocal (its square) is no float: held as zeros
     if (s < 0x1p-100f) s = 0.f;
     if (q < 0x1p-60f) q = 0.f;
     const float si = s == 0.f ? 0.f : __frcp_rn(s), qi = q == 0.f ? 0.f : __frcp_rn(q);
+    const float least = qi > 0.f ? kToInt + 1.f : kToInt;
     float cm[8], cv[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      cm[e] = copysignf(count_m(__fmul_rn(fabsf(m[e]), si)), m[e]);
-      cv[e] = count_v(__fmul_rn(__fmul_rn(v[e], qi), qi));
-      cv[e] = v[e] > 0.f && qi > 0.f ? fmaxf(cv[e], 1.f) : cv[e];
+    for (int e = 0; e < 4; ++e) {
+      code_m(m[e], si, cm[2 * e], cm[2 * e + 1]);
+      code_v(v[e], roots[e], qi, least, cv[2 * e], cv[2 * e + 1]);
     }
     mw = make_uint2(pack4(cm), pack4(cm + 4));
     vw = make_uint2(pack4(cv), pack4(cv + 4));
@@ -278,9 +342,18 @@ __global__ void __launch_bounds__(kThreads)
   for (long long i = ((long long)blockIdx.x * kThreads + threadIdx.x) * 4; i < n; i += step) {
     const float s = ms[i / kBlock], r = vs[i / kBlock];
     float a[4], b[4];
+    auto decode = [&](uint32_t mw, uint32_t vw) {
+      Pair x[2], y[2];
+      decode_m(mw, s, x);
+      decode_v(vw, r, y);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        split(x[e], a[2 * e], a[2 * e + 1]);
+        split(y[e], b[2 * e], b[2 * e + 1]);
+      }
+    };
     if (i + 4 <= n) {
-      decode_m(*reinterpret_cast<const uint32_t*>(mc + i), s, a);
-      decode_v(*reinterpret_cast<const uint32_t*>(vc + i), r, b);
+      decode(*reinterpret_cast<const uint32_t*>(mc + i), *reinterpret_cast<const uint32_t*>(vc + i));
       store4(m + i, a);
       store4(v + i, b);
     } else {
@@ -289,8 +362,7 @@ __global__ void __launch_bounds__(kThreads)
         mw |= (uint32_t)mc[i + e] << 8 * e;
         vw |= (uint32_t)vc[i + e] << 8 * e;
       }
-      decode_m(mw, s, a);
-      decode_v(vw, r, b);
+      decode(mw, vw);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (i + e < n) {
@@ -303,6 +375,12 @@ __global__ void __launch_bounds__(kThreads)
 
 namespace {
 
+// Whether the root of a v below 2^-126 may count as 0: where it is less than 2^-24 of eps at
+// every step (1 / sqrt(1 - b2^t) is largest at the first).
+bool small_roots_do_not_count(const AdamwHyper& h) {
+  return h.eps * 0x1p-24 >= 0x1p-63 / sqrt(1.0 - exp(h.log_b2));
+}
+
 template <class T, bool MASTER, int CAP>
 cudaError_t launch_table(const Launch& lc, int bits, const AdamwHyper& h, const AdamwEntry* e,
                          int count, unsigned blocks) {
@@ -310,7 +388,9 @@ cudaError_t launch_table(const Launch& lc, int bits, const AdamwHyper& h, const 
   std::copy(e, e + count, a.e);
   a.h = h;
   a.count = count;
-  return bits == 8 ? launch_k(adamw8_kernel<T, MASTER, CAP>, dim3(blocks), dim3(kThreads), 0, lc.stream, a)
+  if (bits == 8 && small_roots_do_not_count(h))
+    return launch_k(adamw8_kernel<T, MASTER, true, CAP>, dim3(blocks), dim3(kThreads), 0, lc.stream, a);
+  return bits == 8 ? launch_k(adamw8_kernel<T, MASTER, false, CAP>, dim3(blocks), dim3(kThreads), 0, lc.stream, a)
                    : launch_k(adamw_kernel<T, MASTER, CAP>, dim3(blocks), dim3(kThreads), 0, lc.stream, a);
 }
 // The table travels with the launch: the smallest that holds it, 384 tensors a launch.

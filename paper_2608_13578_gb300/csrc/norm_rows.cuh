@@ -3,6 +3,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "pairs.cuh"
 
 namespace bcmt {
 
@@ -54,38 +55,6 @@ __device__ __forceinline__ void gather8(const bf16* p, int step, int n, Raw8<bf1
   r.a = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
-// Two floats in one register pair, for the packed instructions: half the issue slots of
-// single ones.
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair(float x, float y) {
-  Pair p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
-  return p;
-}
-__device__ __forceinline__ Pair both(float x) { return pair(x, x); }
-__device__ __forceinline__ void split(Pair p, float& x, float& y) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p));
-}
-__device__ __forceinline__ float fold(Pair p) {
-  float x, y;
-  split(p, x, y);
-  return x + y;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-  Pair d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-  Pair d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-  Pair d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
 __device__ __forceinline__ Pair shfl_xor(Pair p, int o) {
   float x, y;
   split(p, x, y);
