@@ -19,14 +19,15 @@
 #include "adamw.h"
 #include "common.cuh"
 #include "internal.h"
-#include "pairs.cuh"
+#include "norm_rows.cuh"
 
 namespace bcmt {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;   // elements of a CTA
+constexpr int kChunk = 4096;   // elements of a CTA; with 8-bit states, where a launch has many,
+                               // twice that, which spreads what a CTA begins with over more
 constexpr int kBlock = 256;    // elements that share a scale
 
 struct Rates {
@@ -70,7 +71,7 @@ __device__ __forceinline__ int find(const AdamwTable<CAP>& a, long long& at) {
     if (a.e[mid].first <= blockIdx.x) lo = mid;
     else hi = mid - 1;
   }
-  at = (long long)(blockIdx.x - a.e[lo].first) * kChunk;
+  at = (long long)(blockIdx.x - a.e[lo].first) * a.chunk;
   return lo;
 }
 
@@ -239,33 +240,56 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
   uint8_t* __restrict__ mc = static_cast<uint8_t*>(t.m);
   uint8_t* __restrict__ vc = static_cast<uint8_t*>(t.v);
   float* __restrict__ w = t.master;
+  // a block as it is stored, fetched while the one before it is computed
+  struct Stored {
+    float s, r;
+    Raw8<T> p, g;
+    Raw8<float> w;
+    uint2 m, v;
+  };
+  const long long end = min(t.n, at + a.chunk);
+  auto fetch_block = [&](long long b0, Stored& x) {
+    if (b0 >= end) return;
+    const long long i = b0 + lane * 8;
+    x.s = t.m_scale[b0 / kBlock];
+    x.r = t.v_scale[b0 / kBlock];
+    if (t.vec && b0 + kBlock <= t.n) {
+      if (MASTER) fetch(w + i, x.w);
+      else fetch(p + i, x.p);
+      fetch(g + i, x.g);
+      x.m = *reinterpret_cast<const uint2*>(mc + i);
+      x.v = *reinterpret_cast<const uint2*>(vc + i);
+    } else {   // zeros past the end, whose moments stay zeros
+      const int left = (int)min(8ll, max(0ll, t.n - i));
+      if (MASTER) gather8(w + i, 1, left, x.w);
+      else gather8(p + i, 1, left, x.p);
+      gather8(g + i, 1, left, x.g);
+      x.m = x.v = make_uint2(0, 0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t mb = e < left ? mc[i + e] : 0u, vb = e < left ? vc[i + e] : 0u;
+        (e < 4 ? x.m.x : x.m.y) |= mb << 8 * (e & 3);
+        (e < 4 ? x.v.x : x.v.y) |= vb << 8 * (e & 3);
+      }
+    }
+  };
+  const long long first = at + (threadIdx.x >> 5) * kBlock;
+  constexpr int kStep = kThreads / 32 * kBlock;
+  Stored next;
+  fetch_block(first, next);
 #pragma unroll 1
-  for (int u = 0; u < kChunk / (kBlock * kThreads / 32); ++u) {
-    const long long b0 = at + (u * (kThreads / 32) + (int)(threadIdx.x >> 5)) * kBlock;
-    if (b0 >= t.n) return;   // the whole warp
+  for (long long b0 = first; b0 < end; b0 += kStep) {   // whole warps
+    const Stored x = next;
+    fetch_block(b0 + kStep, next);
     const long long blk = b0 / kBlock, i = b0 + lane * 8;
-    const float s0 = t.m_scale[blk], r0 = t.v_scale[blk];
     const bool whole = t.vec && b0 + kBlock <= t.n;
     const int left = (int)min(8ll, max(0ll, t.n - i));
     float pv[8], gv[8];
-    uint2 mw = make_uint2(0, 0), vw = make_uint2(0, 0);
-    if (whole) {
-      if (MASTER) load8(w + i, pv);
-      else load8(p + i, pv);
-      load8(g + i, gv);
-      mw = *reinterpret_cast<const uint2*>(mc + i);
-      vw = *reinterpret_cast<const uint2*>(vc + i);
-    } else {   // zeros past the end, whose moments stay zeros
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool on = e < left;
-        pv[e] = on ? (MASTER ? w[i + e] : to_f(p[i + e])) : 0.f;
-        gv[e] = on ? to_f(g[i + e]) : 0.f;
-        const uint32_t mb = on ? mc[i + e] : 0u, vb = on ? vc[i + e] : 0u;
-        (e < 4 ? mw.x : mw.y) |= mb << 8 * (e & 3);
-        (e < 4 ? vw.x : vw.y) |= vb << 8 * (e & 3);
-      }
-    }
+    if (MASTER) widen(x.w, pv);
+    else widen(x.p, pv);
+    widen(x.g, gv);
+    uint2 mw = x.m, vw = x.v;
+    const float s0 = x.s, r0 = x.r;
     Pair m[4], v[4], roots[4];
     decode_m(mw.x, s0, m);
     decode_m(mw.y, s0, m + 2);
@@ -383,8 +407,9 @@ bool small_roots_do_not_count(const AdamwHyper& h) {
 
 template <class T, bool MASTER, int CAP>
 cudaError_t launch_table(const Launch& lc, int bits, const AdamwHyper& h, const AdamwEntry* e,
-                         int count, unsigned blocks) {
+                         int count, unsigned blocks, int chunk) {
   AdamwTable<CAP> a;
+  a.chunk = chunk;
   std::copy(e, e + count, a.e);
   a.h = h;
   a.count = count;
@@ -396,10 +421,10 @@ cudaError_t launch_table(const Launch& lc, int bits, const AdamwHyper& h, const 
 // The table travels with the launch: the smallest that holds it, 384 tensors a launch.
 template <class T, bool MASTER>
 cudaError_t launch_typed(const Launch& lc, int bits, const AdamwHyper& h, const AdamwEntry* e,
-                         int count, unsigned blocks) {
-  if (count <= 32) return launch_table<T, MASTER, 32>(lc, bits, h, e, count, blocks);
-  if (count <= 128) return launch_table<T, MASTER, 128>(lc, bits, h, e, count, blocks);
-  return launch_table<T, MASTER, 384>(lc, bits, h, e, count, blocks);
+                         int count, unsigned blocks, int chunk) {
+  if (count <= 32) return launch_table<T, MASTER, 32>(lc, bits, h, e, count, blocks, chunk);
+  if (count <= 128) return launch_table<T, MASTER, 128>(lc, bits, h, e, count, blocks, chunk);
+  return launch_table<T, MASTER, 384>(lc, bits, h, e, count, blocks, chunk);
 }
 
 }  // namespace
@@ -410,17 +435,20 @@ cudaError_t adamw_step(const Launch& lc, int dtype, int bits, bool master, const
   int k = 0;
   unsigned long long blocks = 0;
   cudaError_t err = cudaSuccess;
+  long long all = 0;
+  for (int i = 0; i < count; ++i) all += t[i].n;
+  const int chunk = bits == 8 && all > (1ll << 24) ? 2 * kChunk : kChunk;
   auto flush = [&] {
     if (k > 0)
-      err = dtype == 0 ? launch_typed<float, false>(lc, bits, h, e, k, (unsigned)blocks)
-            : master   ? launch_typed<bf16, true>(lc, bits, h, e, k, (unsigned)blocks)
-                       : launch_typed<bf16, false>(lc, bits, h, e, k, (unsigned)blocks);
+      err = dtype == 0 ? launch_typed<float, false>(lc, bits, h, e, k, (unsigned)blocks, chunk)
+            : master   ? launch_typed<bf16, true>(lc, bits, h, e, k, (unsigned)blocks, chunk)
+                       : launch_typed<bf16, false>(lc, bits, h, e, k, (unsigned)blocks, chunk);
     k = 0;
     blocks = 0;
   };
   for (int i = 0; i < count && err == cudaSuccess; ++i) {
     if (t[i].n == 0) continue;
-    const unsigned long long need = (unsigned long long)((t[i].n + kChunk - 1) / kChunk);
+    const unsigned long long need = (unsigned long long)((t[i].n + chunk - 1) / chunk);
     if (k == 384 || blocks + need > 0x7fffffffull) flush();
     // 16-byte accesses of p and master, 8- or 16-byte ones of the rest
     const uintptr_t at = (uintptr_t)t[i].p | (uintptr_t)t[i].g | (uintptr_t)t[i].m |

@@ -38,7 +38,7 @@ template <int CAP>
 struct AdamwTable {
   AdamwEntry e[CAP];
   AdamwHyper h;
-  int count;
+  int count, chunk;   // tensors; elements of a CTA
 };
 
 cudaError_t adamw_step(const Launch& lc, int dtype, int bits, bool master, const AdamwHyper& h,
