@@ -138,7 +138,11 @@ __device__ __forceinline__ float warp_merge(float a, float b) {
 // One chunk of one row.  The threshold is the K-th largest of the threads' maxima: at
 // least K elements reach it, and those above it belong to fewer than K threads.  Elements
 // equal to it are taken too; where they are too many (rows of one value), those up to the
-// K-th lowest place among the threads' first ones, which are in K threads.
+// K-th lowest place among the threads' first ones, which are in K threads.  Up to kCoarseK
+// beams the maxima of every eight threads give a threshold that is found in one sort, and
+// lets few more elements through (K = 8: 9 of 4096; 64 x 8 x 32000: 32 -> 30 us); where they are
+// too many, the other follows.
+constexpr int kCoarseK = 16;
 template <class T, int E, bool VEC>
 __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, int nchunk) {
   constexpr int J = E / 8, kCap = 2 * kBeamMaxK * E;
@@ -146,8 +150,8 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   __shared__ Entry list[kCap];
   __shared__ unsigned long long total;
   __shared__ int bad;
-  __shared__ float thr;
-  __shared__ int cnt, tie;
+  __shared__ float thr, most;
+  __shared__ int cnt;
   pdl_enter();
   const long long row = blockIdx.x / nchunk;
   const int chunk = blockIdx.x - (int)(row * nchunk);
@@ -157,7 +161,7 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   const int base = chunk * E * kThreads, V = a.V, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const T* x = static_cast<const T*>(a.logits) + row * a.ld + base;
   const int left = V - base;
-  float v[E], gmax[J], top = -INFINITY;
+  float v[E], top = -INFINITY;
   if (VEC) {
     if (sizeof(T) == 2) {
       uint4 raw[J];
@@ -194,68 +198,15 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
     }
   }
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    gmax[j] = v[8 * j];
-#pragma unroll
-    for (int e = 1; e < 8; ++e) gmax[j] = fmaxf(gmax[j], v[8 * j + e]);
-    top = fmaxf(top, gmax[j]);
-  }
+  for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);
   if (threadIdx.x == 0) {
     cnt = 0;
     total = 0;
     bad = 0;
   }
-  tops[warp][lane] = warp_sort(top);
-  __syncthreads();
-  if (warp == 0) {
-    float s[kWarps];
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) s[w] = tops[w][lane];
-#pragma unroll
-    for (int n = kWarps / 2; n > 0; n >>= 1)
-#pragma unroll
-      for (int w = 0; w < n; ++w) s[w] = warp_merge(s[w], s[w + n]);
-    if (lane == a.K - 1) thr = s[0];
-    if (lane == 0) tops[0][0] = s[0];
-  }
-  __syncthreads();
-  const float limit = thr, mx = tops[0][0];
-  // exp(x - max) = 2^(x log2 e - max log2 e); where nothing is finite, 0 or NaN
-  constexpr float kLog2e = 1.4426950408889634f;
-  const bool none = mx == -INFINITY;
-  const float ref = none ? 0.f : mx;
-  float s = 0.f;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    if (!(gmax[j] >= limit) || none) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += exp2_fast((v[8 * j + e] - ref) * kLog2e);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = v[8 * j + e];
-        if (u >= limit && u > -INFINITY) {
-          const int at = atomicAdd(&cnt, 1);
-          if (at < kCap) list[at] = Entry{u, column<T, E, VEC>(j, e)};
-        } else {
-          s += exp2_fast((u - ref) * kLog2e);
-        }
-      }
-    }
-  }
-  __syncthreads();
-  int n = cnt;
-  unsigned long long part = 0;
-  if (n > kCap) {
-    // many elements equal to the threshold: the lowest places among them
-    __syncthreads();
-    int first = 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (v[i] == limit) first = min(first, column<T, E, VEC>(i / 8, i % 8));
-    // the K-th smallest of the threads' first places (as floats: below 2^24)
-    tops[warp][lane] = warp_sort(first == 0x7fffffff ? -INFINITY : -(float)first);
-    if (threadIdx.x == 0) cnt = 0;
+  // the K-th largest of the threads' values, in every thread; top: the largest
+  auto kth = [&](float value, float& largest) {
+    tops[warp][lane] = warp_sort(value);
     __syncthreads();
     if (warp == 0) {
       float p[kWarps];
@@ -265,10 +216,93 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
       for (int m = kWarps / 2; m > 0; m >>= 1)
 #pragma unroll
         for (int w = 0; w < m; ++w) p[w] = warp_merge(p[w], p[w + m]);
-      if (lane == a.K - 1) tie = p[0] == -INFINITY ? 0x7fffffff : (int)-p[0];
+      if (lane == a.K - 1) thr = p[0];
+      if (lane == 0) most = p[0];
     }
     __syncthreads();
-    const int limit_at = tie;
+    largest = most;
+    return thr;
+  };
+  float limit, mx;
+  const bool coarse = a.K <= kCoarseK;
+  if (coarse) {   // of the largest of every eight threads
+    float g = top;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if ((lane & 7) == 0) tops[0][warp * 4 + lane / 8] = g;
+    __syncthreads();
+    if (warp == 0) {
+      g = warp_sort(tops[0][lane]);
+      if (lane == a.K - 1) thr = g;
+      if (lane == 0) most = g;
+    }
+    __syncthreads();
+    limit = thr;
+    mx = most;
+  } else {
+    limit = kth(top, mx);
+  }
+  // exp(x - max) = 2^(x log2 e - max log2 e); where nothing is finite, 0 or NaN
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  // elements from the threshold up go into the list (a thread's one after another, a place in it
+  // for a warp by one atomic addition), the others into the sum
+  float s;
+  auto collect = [&] {
+    int mine = 0;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const bool hit = v[i] >= limit && v[i] > -INFINITY;
+      mine += hit;
+      const float e = exp2_fast((v[i] - ref) * kLog2e);
+      s += hit ? 0.f : e;
+    }
+    if (__any_sync(0xffffffffu, mine)) {
+      int before = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += up;
+      }
+      int from = 0;
+      if (lane == 31) from = atomicAdd(&cnt, before);
+      from = __shfl_sync(0xffffffffu, from, 31) + before - mine;
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (v[i] >= limit && v[i] > -INFINITY) {
+            if (from < kCap) list[from] = Entry{v[i], column<T, E, VEC>(i / 8, i % 8)};
+            ++from;
+          }
+      }
+    }
+    __syncthreads();
+    return cnt;
+  };
+  int n = collect();
+  unsigned long long part = 0;
+  auto empty = [&] {
+    __syncthreads();
+    if (threadIdx.x == 0) cnt = 0;
+    __syncthreads();
+  };
+  if (n > kCap && coarse) {
+    empty();
+    limit = kth(top, mx);
+    n = collect();
+  }
+  if (n > kCap) {
+    // many elements equal to the threshold: the lowest places among them, up to the K-th
+    // lowest of the threads' first places (as floats: below 2^24)
+    int first = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (v[i] == limit) first = min(first, column<T, E, VEC>(i / 8, i % 8));
+    empty();
+    float lowest;
+    const float place = kth(first == 0x7fffffff ? -INFINITY : -(float)first, lowest);
+    const int limit_at = place == -INFINITY ? 0x7fffffff : (int)-place;
     const unsigned long long one = exp_units(limit, ref);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -287,16 +321,20 @@ __global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, 
   Entry* out = reinterpret_cast<Entry*>(static_cast<char*>(a.ws) +
                                         (size_t)a.N * a.K * nchunk * sizeof(ChunkHead)) +
                (row * nchunk + chunk) * a.K;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const Entry m = list[i];
+  // eight threads find an entry's rank
+  for (int i0 = 0; i0 < n; i0 += kThreads / 8) {
+    const int i = i0 + threadIdx.x / 8;
+    const Entry m = i < n ? list[i] : Entry{0.f, 0};
     int rank = 0;
-    for (int k = 0; k < n; ++k) {
+    for (int k = threadIdx.x & 7; k < n; k += 8) {
       const Entry o = list[k];
       rank += o.x > m.x || (o.x == m.x && o.v < m.v);
     }
-    part += exp_units(m.x, ref);
-    if (rank < a.K) out[rank] = Entry{m.x, base + m.v};
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+    if ((threadIdx.x & 7) == 0 && i < n && rank < a.K) out[rank] = Entry{m.x, base + m.v};
   }
+  for (int i = threadIdx.x; i < n; i += kThreads) part += exp_units(list[i].x, ref);
   // the others' sum of this warp; not finite where a logit is NaN or +inf
   s = warp_sum(s);
   if (lane == 0) {
@@ -338,23 +376,38 @@ __device__ __forceinline__ Cand settle(Cand v) {   // a bitonic sequence over th
   }
   return v;
 }
-__device__ __forceinline__ Cand sorted(Cand v) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1) {
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const Cand o = shfl(v, lane ^ j);
-      if (before(o, v) == (((lane & j) == 0) == ((lane & k) == 0))) v = o;
-    }
-  }
-  return v;
-}
 // The best 32 of two lists that are sorted over the lanes, sorted again.
 __device__ __forceinline__ Cand merge(const Cand& a, const Cand& b) {
   Cand v = shfl(b, 31 - (threadIdx.x & 31));
   if (before(a, v)) v = a;
   return settle(v);
+}
+// Entries of one beam: the logit's order above, the lower place the better below.
+typedef unsigned long long Packed;
+__device__ __forceinline__ Packed settle(Packed v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) {
+    const Packed o = __shfl_xor_sync(0xffffffffu, v, j);
+    if ((o > v) == ((lane & j) == 0)) v = o;
+  }
+  return v;
+}
+__device__ __forceinline__ Packed sorted(Packed v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1) {
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const Packed o = __shfl_xor_sync(0xffffffffu, v, j);
+      if ((o > v) == (((lane & j) == 0) == ((lane & k) == 0))) v = o;
+    }
+  }
+  return v;
+}
+__device__ __forceinline__ Packed merge(Packed a, Packed b) {
+  const Packed v = __shfl_sync(0xffffffffu, b, 31 - (threadIdx.x & 31));
+  return settle(a > v ? a : v);
 }
 // Floats and doubles (no NaN, no -0) as integers of the same order.
 __device__ __forceinline__ int ordered(float x) {
@@ -394,18 +447,23 @@ __global__ void __launch_bounds__(32 * kBeamMaxK) beam_merge_kernel(const BeamAr
     // the best of the lists by logit; the first 32 heads stay for the sum
     ChunkHead h{0, -INFINITY, 0};
     if (lane < nchunk) h = heads[lane];
+    // (the lists' first entries, then their second ones and so on: up to 32 lists, where no entry
+    // of a turn is among the best, none that follows is)
     const int total = nchunk * K;
-    Cand last = best;
+    Packed found = 0, last = 0;
     for (int i = 0; i < total; i += 32) {
-      const int l = (i + lane) / K;
-      Cand c{kNoKey, kNoPlace};
-      if (i + lane < total) {
-        const Entry e = entries[i + lane];
-        if (i + lane - l * K < heads[l].n) c = Cand{ordered(e.x), e.v};
+      const int rank = (i + lane) / nchunk, l = i + lane - rank * nchunk;
+      Packed c = 0;
+      if (i + lane < total && rank < heads[l].n) {
+        const Entry e = entries[l * K + rank];
+        c = (Packed)((uint32_t)ordered(e.x) ^ 0x80000000u) << 32 | ~(uint32_t)e.v;
       }
-      if (!__any_sync(0xffffffffu, before(c, last))) continue;
-      best = i == 0 ? sorted(c) : merge(best, sorted(c));
-      last = shfl(best, K - 1);
+      if (!__any_sync(0xffffffffu, c > last)) {
+        if (nchunk <= 32) break;
+        continue;
+      }
+      found = i == 0 ? sorted(c) : merge(found, sorted(c));
+      last = __shfl_sync(0xffffffffu, found, K - 1);
     }
     float m = h.max;
     bool ok = m == m;
@@ -426,12 +484,12 @@ __global__ void __launch_bounds__(32 * kBeamMaxK) beam_merge_kernel(const BeamAr
       const float y = logf((float)s);
       const double z = s * exp_double(-y, 0.f) - 1.0;
       const double log_s = (double)y + (z - 0.5 * z * z);
-      if (best.at != kNoPlace) {
-        const float x = __int_as_float((int)best.key < 0 ? (int)best.key ^ 0x7fffffff : (int)best.key);
-        best = Cand{ordered((double)score + (((double)x - (double)m) - log_s)), k * a.V + best.at};
+      if (found) {
+        const int o = (int)((uint32_t)(found >> 32) ^ 0x80000000u);
+        const float x = __int_as_float(o < 0 ? o ^ 0x7fffffff : o);
+        best = Cand{ordered((double)score + (((double)x - (double)m) - log_s)),
+                    k * a.V + (int)~(uint32_t)found};
       }
-    } else {
-      best = Cand{kNoKey, kNoPlace};
     }
   }
   lists[k][lane] = best;

@@ -232,7 +232,7 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   while (!size(2, 2) && W > 1) --W;
   if (p.smem <= kNormSmem) {
     if (!size(3, 2)) size(2, 2);
-  } else if (!size(2, 1) && !size(1, 1)) {
+  } else if (!size(1, 2) && !size(2, 1) && !size(1, 1)) {
     p.tot_smem = p.pw_smem = false;
     size(1, 1);
   }
