@@ -83,7 +83,7 @@ def beam_reorder(tensors, parents, out=None):
     if parents.dim() != 2 or parents.dtype != torch.int64:
         raise ValueError(f"parents must be int64 [N, K], not {parents.dtype} {tuple(parents.shape)}")
     N, K = parents.shape
-    NK, at = N * K, dev.index
+    NK, at, index = N * K, dev.index, parents.get_device()
     parents = parents.contiguous()
     grad, rows, table = torch.is_grad_enabled(), [], array("q")
     tensors = list(tensors)
@@ -94,8 +94,8 @@ def beam_reorder(tensors, parents, out=None):
     for i, t in enumerate(tensors):
         shape = t.shape
         n = t.numel()
-        if (t.device.index != at or t.device.type != dev.type or not shape
-                or not (shape[0] == NK or (len(shape) > 1 and shape[0] == N and shape[1] == K))):
+        if (t.get_device() != index or not shape
+                or not (shape[0] == NK or (shape[0] == N and len(shape) > 1 and shape[1] == K))):
             raise ValueError(f"tensors must be [N, K, ...] or [N K, ...] on {dev}, not "
                              f"{tuple(shape)} on {t.device}")
         if grad and t.requires_grad:
@@ -107,7 +107,8 @@ def beam_reorder(tensors, parents, out=None):
             o = out[i] = torch.empty_like(t)
         else:
             o = out[i]
-            if o.shape != shape or o.dtype != t.dtype or o.device != t.device or not o.is_contiguous():
+            if (o.shape != shape or o.dtype is not t.dtype or o.get_device() != index
+                    or not o.is_contiguous()):
                 _check(o, "out", shape, t.dtype, dev)
                 raise ValueError("out must be dense")
         table.extend((t.data_ptr(), o.data_ptr(), n // NK * t.element_size() if n else 0))

@@ -50,28 +50,37 @@ def _gates(gate, shape) -> int:
     return n
 
 
+def _same(t, name, shape, dtype, dev):
+    """``_check`` for a tensor on a CUDA device, quicker where it is right."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev.index:
+        _check(t, name, shape, dtype, dev)
+
+
 def _arguments(branch, weight, bias, post_weight, post_bias, gate, kind):
-    """(device, dtype, weights' dtype, rows of the gate), after the checks of what both
+    """(device, shape, dtype, weights' dtype, rows of the gate), after the checks of what both
     passes take."""
-    dev = _device(branch)
+    dev, shape, dtype = _device(branch), branch.shape, weight.dtype
     dt = _dtype(branch, "branch")
-    if branch.dim() < 1:
+    if not shape:
         raise ValueError("branch must be [..., D]")
     if kind not in KINDS:
         raise ValueError(f"kind must be one of {KINDS}, not {kind!r}")
     wt = _dtype(weight, "weight")
-    D = branch.shape[-1]
-    for t, name in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight"),
-                    (post_bias, "post_bias")):
-        if t is not None:
-            _check(t, name, (D,), weight.dtype, dev)
-    if post_bias is not None and post_weight is None:
-        raise ValueError("post_bias without post_weight")
+    vector = shape[-1:]
+    _same(weight, "weight", vector, dtype, dev)
+    if bias is not None:
+        _same(bias, "bias", vector, dtype, dev)
+    if post_weight is not None:
+        _same(post_weight, "post_weight", vector, dtype, dev)
+    if post_bias is not None:
+        _same(post_bias, "post_bias", vector, dtype, dev)
+        if post_weight is None:
+            raise ValueError("post_bias without post_weight")
     gates = 0
     if gate is not None:
-        gates = _gates(gate, branch.shape)
-        _check(gate, "gate", gate.shape, branch.dtype, dev)
-    return dev, dt, wt, gates
+        gates = _gates(gate, shape)
+        _same(gate, "gate", gate.shape, branch.dtype, dev)
+    return dev, shape, dt, wt, gates
 
 
 @_on_its_device
@@ -85,17 +94,15 @@ def residual_norm_forward(branch, x, weight, bias=None, *, post_weight=None, pos
     post_weight: no post norm); kind: both are layer norms ("layer") or root-mean-square
     norms ("rms").  gate: [D], or one for every leading index ([B, 1, D] for branch
     [B, T, D]), or of branch's shape; default 1."""
-    dev, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
-    shape = branch.shape
-    _check(x, "x", shape, branch.dtype, dev)
+    dev, shape, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
+    _same(x, "x", shape, branch.dtype, dev)
     D = shape[-1]
     rows = branch.numel() // D if D else 0
     p, _ = _plan(rows, D, dt, wt, int(kind == "rms"), gates, _number(residual_scale, "residual_scale"),
                  _number(eps, "eps"), post_weight is not None)
     branch, x, weight, bias = _dense(branch), _dense(x), _dense(weight), _dense(bias)
     post_weight, post_bias, gate = _dense(post_weight), _dense(post_bias), _dense(gate)
-    h = torch.empty(shape, dtype=branch.dtype, device=dev)
-    n = torch.empty(shape, dtype=branch.dtype, device=dev)
+    h, n = torch.empty_like(branch), torch.empty_like(branch)
     C.check(C.LIB.bcmt_residual_norm_forward(
         p, branch.data_ptr(), x.data_ptr(), weight.data_ptr(), _address(bias),
         _address(post_weight), _address(post_bias), _address(gate), h.data_ptr(), n.data_ptr(),
@@ -116,12 +123,12 @@ def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=
             return residual_norm_backward(
                 dh, dn, branch, h, weight, bias, post_weight=post_weight, post_bias=post_bias,
                 gate=gate, residual_scale=residual_scale, kind=kind, eps=eps)
-    dev, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
-    shape, dtype = branch.shape, branch.dtype
-    _check(dn, "dn", shape, dtype, dev)
-    _check(h, "h", shape, dtype, dev)
+    dev, shape, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
+    dtype = branch.dtype
+    _same(dn, "dn", shape, dtype, dev)
+    _same(h, "h", shape, dtype, dev)
     if dh is not None:
-        _check(dh, "dh", shape, dtype, dev)
+        _same(dh, "dh", shape, dtype, dev)
     D = shape[-1]
     rows = branch.numel() // D if D else 0
     alpha = _number(residual_scale, "residual_scale")
@@ -130,13 +137,15 @@ def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=
     dh, dn, branch, h = _dense(dh), _dense(dn), _dense(branch), _dense(h)
     weight, post_weight, post_bias = _dense(weight), _dense(post_weight), _dense(post_bias)
     one = post_weight is None and gate is None and alpha == 1.0
-    new = functools.partial(torch.empty, device=dev)
-    dbranch = new(shape, dtype=dtype)
-    dx = None if one else new(shape, dtype=dtype)
-    dw, db, dpw, dpb = (None if t is None else new((D,), dtype=weight.dtype)
-                        for t in (weight, bias, post_weight, post_bias))
-    dgate = None if gate is None else new(gate.shape, dtype=dtype)
     gate = _dense(gate)
+    like = torch.empty_like
+    dbranch = like(branch)
+    dx = None if one else like(branch)
+    dw = like(weight)
+    db = None if bias is None else like(weight)
+    dpw = None if post_weight is None else like(weight)
+    dpb = None if post_bias is None else like(weight)
+    dgate = None if gate is None else like(gate)
     ws = _buffer(max(256, nbytes), dev)
     C.check(C.LIB.bcmt_residual_norm_backward(
         p, _address(dh), dn.data_ptr(), branch.data_ptr(), h.data_ptr(), weight.data_ptr(),

@@ -70,6 +70,8 @@ class AdamWPlan:
         self._shapes = [p.shape for p in params]
         self._sizes = np.array([p.numel() for p in params], dtype=np.int64)
         self._at = None
+        self._table[:, _N] = self._sizes
+        self._holes = False
 
     def _check(self):
         dev = self.device
@@ -98,6 +100,29 @@ class AdamWPlan:
                 self._table[:, column] = at[i * n:(i + 1) * n]
             self._at = at
 
+    def _addresses(self, grads, dev):
+        """(the gradients' addresses, 0 for None; copies that are to live until the launch)."""
+        try:    # most often all are there, dense and right
+            if ([g.shape for g in grads] == self._shapes and {g.dtype for g in grads} == {self.dtype}
+                    and {g.get_device() for g in grads} == {dev.index}
+                    and False not in [g.is_contiguous() for g in grads]):
+                return [g.data_ptr() for g in grads], None
+        except (AttributeError, RuntimeError):
+            pass
+        at, kept = [], []
+        for g, shape in zip(grads, self._shapes):
+            if g is None:
+                at.append(0)
+                continue
+            if g.layout is not torch.strided:
+                raise ValueError("grads must be dense tensors, not sparse ones")
+            _check(g, "grads", shape, self.dtype, dev)
+            if not g.is_contiguous():
+                g = g.contiguous()
+                kept.append(g)
+            at.append(g.data_ptr())
+        return at, kept
+
     @torch.no_grad()
     def step(self, grads, *, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
              step, grad_scale: Optional[torch.Tensor] = None):
@@ -113,21 +138,13 @@ class AdamWPlan:
         self._refresh()
         if len(grads) != len(self._shapes):
             raise ValueError(f"{len(self._shapes)} gradients are needed, not {len(grads)}")
-        at, kept, dtype, holes = [], [], self.dtype, False
-        for g, shape in zip(grads, self._shapes):
-            if g is None:
-                at.append(0)
-                holes = True
-                continue
-            if g.shape != shape or g.dtype != dtype or g.device != dev or g.layout != torch.strided:
-                _check(g, "grads", shape, dtype, dev)
-                raise ValueError("grads must be dense tensors, not sparse ones")
-            if not g.is_contiguous():
-                g = g.contiguous()
-                kept.append(g)
-            at.append(g.data_ptr())
-        self._table[:, _G] = at
-        self._table[:, _N] = np.where(self._table[:, _G] != 0, self._sizes, 0) if holes else self._sizes
+        at, kept = self._addresses(grads, dev)
+        table = self._table
+        table[:, _G] = at
+        holes = 0 in at
+        if holes or self._holes:
+            table[:, _N] = np.where(table[:, _G] != 0, self._sizes, 0)
+            self._holes = holes
         step_ptr = lr_ptr = None
         if isinstance(step, torch.Tensor) and step.is_cuda:
             _one(step, "step", torch.int64, dev)
