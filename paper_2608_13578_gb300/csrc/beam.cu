@@ -144,7 +144,7 @@ __device__ __forceinline__ float warp_merge(float a, float b) {
 // too many, the other follows.
 constexpr int kCoarseK = 16;
 template <class T, int E, bool VEC>
-__global__ void __launch_bounds__(kThreads) beam_chunk_kernel(const BeamArgs a, int nchunk) {
+__global__ void __launch_bounds__(kThreads, E == 16 ? 4 : 5) beam_chunk_kernel(const BeamArgs a, int nchunk) {
   constexpr int J = E / 8, kCap = 2 * kBeamMaxK * E;
   __shared__ float tops[kWarps][32];
   __shared__ Entry list[kCap];

@@ -207,49 +207,56 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   const int R = p.tpr < 32 ? 32 / p.tpr : 1, wt = std::max(32, p.tpr), roles = post ? 2 : 1;
   // segments are of whole steps of R rows
   const long long g = p.mode == kGateGroups ? groups : 1, gr = rows / g, gs = (gr + R - 1) / R;
-  // workers of a CTA: as many as there are steps for, registers and shared memory allow; the
-  // rings are to hold the next step at least
   const int arrays = p.mode == kGateRows ? 5 : 4;
-  p.gp_smem = p.mode != kGateRows && (post || p.mode != kGateNone);
-  p.tot_smem = post && p.mode == kGateGroups;
-  p.pw_smem = post && p.mode == kGateRows;
-  long long W = std::min<long long>(norm_max_warps(p.J) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
-  W = std::max(1ll, W);
   const bool vec = D % 8 == 0;
-  long long stage16 = 0, rest16 = 0;
-  auto size = [&](int stages, int slots) {   // whether it fits
-    const long long nt = W * wt;
-    p.stages = stages;
-    p.ds_slots = slots;
-    stage16 = vec ? (long long)arrays * p.J * (es / 2) * nt : arrays * W * (((long long)R * D * es + 30) / 16);
-    rest16 = (p.pw_smem ? 6 : 2) * p.J * wt + (post ? slots * 2 * p.J * nt : 0) +
-             (p.gp_smem ? 2 * p.J * nt : 0) + (p.tot_smem ? 4 * p.J * nt : 0);
-    // the CTA's sums go through the rings at the end
-    p.ring16 = (int)std::max(stages * stage16, 2ll * p.J * nt * roles);
-    p.smem = (int)(p.ring16 + rest16) * 16;
-    return p.smem <= kNormSmem;
-  };
-  while (!size(2, 2) && W > 1) --W;
-  if (p.smem <= kNormSmem) {
-    if (!size(3, 2)) size(2, 2);
-  } else if (!size(1, 2) && !size(2, 1) && !size(1, 1)) {
-    p.tot_smem = p.pw_smem = false;
-    size(1, 1);
-  }
-  p.threads = (int)(W * wt) * roles;
-  p.ctas = (int)std::min<long long>((g * gs + W - 1) / W, sms);
-  // each gate's steps in equal parts, so that the workers' longest walk is short; a gate for
-  // all rows (or none): a segment a worker
-  const long long workers = p.ctas * W;
-  long long best = -1;
-  for (long long turns = (g + workers - 1) / workers, i = 0; i < (g == 1 ? 1 : 8); ++i, ++turns) {
-    const long long s = std::min(gs, std::max(1ll, turns * workers / g)), len = (gs + s - 1) / s;
-    if (best < 0 || turns * len < best) {
-      best = turns * len;
-      p.segs_per_group = (gs + len - 1) / len;
-      p.seg_rows = len * R;
+  // workers of a CTA: as many as there are steps for, registers and shared memory allow; the
+  // rings are to hold the next step at least.  totals: whether workers walk several gates'
+  // segments and keep totals of dpw and dpb over them
+  auto cut = [&](bool totals) {
+    p.gp_smem = p.mode != kGateRows && (post || p.mode != kGateNone);
+    p.tot_smem = totals;
+    p.pw_smem = post && p.mode == kGateRows;
+    p.one_seg = !totals;
+    long long W = std::min<long long>(norm_max_warps(p.J) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
+    W = std::max(1ll, W);
+    auto size = [&](int stages, int slots) {   // whether it fits
+      const long long nt = W * wt;
+      p.stages = stages;
+      p.ds_slots = slots;
+      const long long stage16 = vec ? (long long)arrays * p.J * (es / 2) * nt
+                                    : arrays * W * (((long long)R * D * es + 30) / 16);
+      const long long rest16 = (p.pw_smem ? 6 : 2) * p.J * wt + (post ? slots * 2 * p.J * nt : 0) +
+                               (p.gp_smem ? 2 * p.J * nt : 0) + (p.tot_smem ? 4 * p.J * nt : 0);
+      // the CTA's sums go through the rings at the end
+      p.ring16 = (int)std::max(stages * stage16, 2ll * p.J * nt * roles);
+      p.smem = (int)(p.ring16 + rest16) * 16;
+      return p.smem <= kNormSmem;
+    };
+    while (!size(2, 2) && W > 1) --W;
+    if (p.smem <= kNormSmem) {
+      if (!size(3, 2)) size(2, 2);
+    } else if (!size(1, 2) && !size(2, 1) && !size(1, 1)) {
+      p.tot_smem = p.pw_smem = false;
+      size(1, 1);
     }
-  }
+    p.threads = (int)(W * wt) * roles;
+    p.ctas = (int)std::min<long long>((g * gs + W - 1) / W, sms);
+    // each gate's steps in equal parts, so that the workers' longest walk is short; a gate for
+    // all rows (or none): a segment a worker
+    const long long workers = p.ctas * W;
+    long long best = -1;
+    for (long long turns = (g + workers - 1) / workers, i = 0; i < (totals ? 8 : 1); ++i, ++turns) {
+      const long long s = std::min(gs, std::max(1ll, turns * workers / g)), len = (gs + s - 1) / s;
+      if (best < 0 || turns * len < best) {
+        best = turns * len;
+        p.segs_per_group = (gs + len - 1) / len;
+        p.seg_rows = len * R;
+      }
+    }
+    // one segment a worker at most, the longest walk within an eighth of the mean
+    return g * p.segs_per_group <= workers && best * workers * 8 <= g * gs * 9 + workers * 8;
+  };
+  if (!cut(false) && post && p.mode == kGateGroups) cut(true);
   p.seg_group_rows = gr;
   p.nseg = g * p.segs_per_group;
   p.part_bytes = (size_t)p.ctas * 4 * D * 4;
@@ -273,6 +280,7 @@ cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormB
   a.gp_smem = pl.gp_smem;
   a.tot_smem = pl.tot_smem;
   a.pw_smem = pl.pw_smem;
+  a.one_seg = pl.one_seg;
   if (pl.mode == kGateOne && a.dgate) a.wanted |= a.post_bias ? 12 : 4;
   a.seg_rows = pl.seg_rows;
   a.segs_per_group = pl.segs_per_group;

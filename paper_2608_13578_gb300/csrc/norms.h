@@ -27,7 +27,7 @@ struct NormBwd {
   float *part, *gate_part;      // sums of each CTA [ctas, 4, D], of each segment [nseg, D]
   // from the plan
   int tpr, stages, mode, ring16, ds_slots;
-  bool gp_smem, tot_smem, pw_smem;
+  bool gp_smem, tot_smem, pw_smem, one_seg;
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
 };
 
@@ -46,7 +46,7 @@ struct NormJoin {
 // CTAs, its shared memory, and the segments of rows that its workers walk.
 struct NormPlan {
   int tpr, J, threads, ctas, stages, mode, ring16, ds_slots, smem;
-  bool gp_smem, tot_smem, pw_smem;
+  bool gp_smem, tot_smem, pw_smem, one_seg;
   long long seg_rows, segs_per_group, seg_group_rows, nseg;
   size_t part_bytes, gate_bytes;
 };

@@ -135,7 +135,7 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
       put2(gps + 2 * j * G, v);
     }
   };
-  if (ROLE == kRolePost && !ROWS && a.mode == kGateGroups) {
+  if (ROLE == kRolePost && !ROWS && a.mode == kGateGroups && !a.one_seg) {
     const Pair z[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < J; ++j)
@@ -492,6 +492,11 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
         Pair u[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+          if (a.one_seg) {   // the worker's only segment
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][4 * j + e] = mul2(acc[i][4 * j + e], g[e]);
+            continue;
+          }
           float* part = a.part + ((long long)blockIdx.x * 4 + 2 + i) * D;
           if (a.tot_smem) {
             get2(tot + i * V + 2 * j * G, u);
@@ -543,7 +548,7 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
 #pragma unroll
   for (int i = 0; i < NACC; ++i) {
     const int v = i + (ROLE == kRolePost ? 2 : 0);
-    const bool want = (a.wanted >> v & 1) && !(kTotals && a.mode == kGateGroups && !a.tot_smem);
+    const bool want = (a.wanted >> v & 1) && !(kTotals && a.mode == kGateGroups && !a.tot_smem && !a.one_seg);
     __syncthreads();
     if (want) {
 #pragma unroll
