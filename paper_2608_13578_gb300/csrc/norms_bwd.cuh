@@ -27,6 +27,12 @@ namespace bcmt {
 // and it adds g A to dpw and g B to dpb: the sums take A and B, and what depends on the
 // gate is done once for its segment (a gate for all rows: when the CTAs' sums are joined).  A gate per row (ROWS) comes through the ring too, and
 // the sums take g ds.
+//
+// What bounds it: the latency of a row's sums with 16 warps an SM (128 registers a thread), and
+// issue slots (1200 instructions for both roles of a row of 768).  Measured, both kernels of a
+// call: 16384 x 768 bf16 42 us (22.7 at the copy's rate), 16384 x 4096 165 us (121), 4095 x 1001
+// fp32 with a gate per row 31 us (20), 65536 x 64 18 us (7.6), 8192 x 8192 without a post norm
+// 142 us (121).  One role with 8 columns a lane took 57, 211, 106 and 88 us for the first four.
 enum { kRolePre, kRolePost, kRoleAll };
 
 template <class T, int TPR, int J, bool VEC, bool ROWS, int ROLE>
