@@ -432,7 +432,7 @@ bcmt_status bcmt_beam_select(const bcmt_beam_params* p, const void* logits, cons
                              long long* tokens, void* finished_out, void* workspace, void* stream);
 
 /* dst[n, k] = src[n, parents[n, k]] for `count` tensors of N x K rows of
- * row_bytes bytes each (dense; no dst overlaps a src or another dst), one launch for
+ * row_bytes bytes each (dense; no dst overlaps a src, parents or another dst), one launch for
  * up to 128.  A parent outside [0, K) gives a row of zeros and is reported as
  * BCMT_ERR_ARG by the next bcmt_device_status.  N * K <= 2^22, K <= 32. */
 typedef struct {

@@ -72,8 +72,9 @@ def beam_select(logits, scores, finished=None, eos: Optional[int] = None):
 
 def beam_reorder(tensors, parents, out=None):
     """``t[n, parents[n, k]]`` for every t of ``tensors`` ([N, K, ...] or [N * K, ...], any type):
-    a list of new tensors, or those of ``out`` (dense; they may not share memory with ``tensors`` or each other).  A parent
-    outside its beams gives zeros and is reported by ``bcmt.bcmt_device_status``."""
+    a list of new tensors, or those of ``out`` (dense; they may not share memory with ``tensors``,
+    ``parents`` or each other).  A parent outside its beams gives zeros and is reported by
+    ``bcmt.bcmt_device_status``."""
     if not isinstance(parents, torch.Tensor):
         raise ValueError(f"parents must be a tensor, not {type(parents).__name__}")
     dev = _device(parents)

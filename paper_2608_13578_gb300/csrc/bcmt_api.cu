@@ -724,11 +724,13 @@ struct Span {
   uintptr_t from, to;
   bool written;
 };
-bcmt_status check_apart(const bcmt_beam_tensor* t, int count, uintptr_t rows) {
-  Span few[256];
-  Span* s = count <= 128 ? few : new (std::nothrow) Span[2 * (size_t)count];
+bcmt_status check_apart(const bcmt_beam_tensor* t, int count, uintptr_t rows, const long long* parents) {
+  Span few[257];
+  Span* s = count <= 128 ? few : new (std::nothrow) Span[2 * (size_t)count + 1];
   if (!s) return fail(BCMT_ERR_ARG, "no host memory for %d tensors", count);
   int n = 0;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(parents);
+  if (rows > 0) s[n++] = Span{p, p + 8 * rows, false};
   for (int i = 0; i < count; ++i) {
     if (rows * t[i].row_bytes == 0) continue;
     const uintptr_t a = reinterpret_cast<uintptr_t>(t[i].src), b = reinterpret_cast<uintptr_t>(t[i].dst);
@@ -744,7 +746,8 @@ bcmt_status check_apart(const bcmt_beam_tensor* t, int count, uintptr_t rows) {
     end = std::max(end, s[i].to);
   }
   if (s != few) delete[] s;
-  return apart ? BCMT_OK : fail(BCMT_ERR_ARG, "a destination overlaps a source or another destination");
+  return apart ? BCMT_OK
+               : fail(BCMT_ERR_ARG, "a destination overlaps a source, the parents or another destination");
 }
 
 bcmt_status check_beam(const bcmt_beam_params* p) {
@@ -1747,7 +1750,7 @@ bcmt_status bcmt_beam_reorder(const long long* parents, int N, int K,
     if (t.row_bytes == 0 || N == 0) continue;
     if (!t.src || !t.dst) return fail(BCMT_ERR_ARG, "tensor %d: src or dst is NULL", i);
   }
-  BCMT_TRY(check_apart(tensors, count, (uintptr_t)N * K));
+  BCMT_TRY(check_apart(tensors, count, (uintptr_t)N * K, parents));
   unsigned* sp = status_ptr();
   if (!sp) return fail(BCMT_ERR_CUDA, "no CUDA device / device status word unavailable");
   Launch lc{static_cast<cudaStream_t>(stream), sp};

@@ -11,6 +11,7 @@ what it refuses raises ``bcmt.BCMTError``.
 from __future__ import annotations
 
 import ctypes
+from operator import attrgetter
 from typing import Optional
 
 import numpy as np
@@ -23,6 +24,10 @@ from .lm_ops import _address, _check, _current_device, _dense, _device, _dtype, 
 
 _F32 = torch.float32
 BLOCK = 256   # elements that share a scale of 8-bit states
+# what a step asks of every tensor, for map()
+_SHAPE, _DTYPE = attrgetter("shape"), attrgetter("dtype")
+_POINTER, _INDEX, _IS_DENSE = (torch.Tensor.data_ptr, torch.Tensor.get_device,
+                               torch.Tensor.is_contiguous)
 _P, _G, _M, _V, _W, _MS, _VS, _N = range(8)   # fields of bcmt_adamw_tensor
 
 
@@ -92,7 +97,7 @@ class AdamWPlan:
             raise ValueError("params, states, masters and scales must not share memory")
 
     def _refresh(self):
-        at = [t.data_ptr() for t in self._all]
+        at = list(map(_POINTER, self._all))
         if at != self._at:
             self._check()
             n = len(self._shapes)
@@ -103,11 +108,11 @@ class AdamWPlan:
     def _addresses(self, grads, dev):
         """(the gradients' addresses, 0 for None; copies that are to live until the launch)."""
         try:    # most often all are there, dense and right
-            if ([g.shape for g in grads] == self._shapes and {g.dtype for g in grads} == {self.dtype}
-                    and {g.get_device() for g in grads} == {dev.index}
-                    and False not in [g.is_contiguous() for g in grads]):
-                return [g.data_ptr() for g in grads], None
-        except (AttributeError, RuntimeError):
+            if (list(map(_SHAPE, grads)) == self._shapes and set(map(_DTYPE, grads)) == {self.dtype}
+                    and set(map(_INDEX, grads)) == {dev.index}
+                    and False not in map(_IS_DENSE, grads)):
+                return list(map(_POINTER, grads)), None
+        except (AttributeError, TypeError, RuntimeError):
             pass
         at, kept = [], []
         for g, shape in zip(grads, self._shapes):

@@ -282,6 +282,7 @@ def test_beam_reorder_tables(C):
                  [(A, far, 16), (far + 1000, A + 90, 16)], [(A, far, 16), (A + 1000, far + 95, 16)],
                  [(far + 50, A, 16), (A + 1000, far + 20, 16)]):
         assert code(C, table(*rows)) == C.BCMT_ERR_ARG, rows
+    assert code(C, lambda: ok(parents=far + 40)) == C.BCMT_ERR_ARG      # written by a copy
     assert code(C, table((A, far, -1))) == C.BCMT_ERR_SHAPE
     assert code(C, lambda: C.bcmt_beam_reorder(A, 2, 3, None, 1, 0, 0)) == C.BCMT_ERR_ARG
     assert code(C, lambda: C.bcmt_beam_reorder(A, 2, 3, None, -1, 0, 0)) == C.BCMT_ERR_ARG

@@ -223,6 +223,13 @@ def test_reorder(B, N, K):
         assert torch.equal(a, want) and torch.equal(b, want)
 
 
+def test_no_searches(B):
+    out = B.beam_select(torch.zeros(0, 3, 10, device="cuda"), torch.zeros(0, 3, device="cuda"))
+    assert all(t.shape == (0, 3) for t in out)
+    a, = B.beam_reorder([torch.zeros(0, 3, 4, device="cuda")], out[1])
+    assert a.shape == (0, 3, 4)
+
+
 def test_reorder_many(B):
     parents = torch.tensor([[1, 1, 0]], device="cuda")
     tensors = [torch.arange(3 * (1 + i % 5), device="cuda").view(1, 3, -1) + i for i in range(300)]

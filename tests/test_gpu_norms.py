@@ -111,6 +111,24 @@ def test_many_rows(N, dtype, rows, D, gates):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("rows,D,gates", [(3000, 64, 1500), (4100, 100, 2050), (3000, 768, 1500), (900, 1001, 450),
+                                          (800, 5000, 400), (480, 7676, 160), (480, 8192, 160)])
+def test_more_gates_than_workers(N, dtype, post, rows, D, gates):
+    """Workers that walk the segments of several gates, a few rows each."""
+    t, dh, dn = make((gates, rows // gates, D), dtype, dtype, "layer", post, (gates, 1, D))
+    check(N, t, dh, dn, 1.0, "layer")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("post,post_bias", [(True, True), (True, False), (False, False)])
+@pytest.mark.parametrize("rows,D", [(1, 72), (5, 2056), (7, 5001), (160, 6152), (3, 7676), (160, 8191), (157, 8192)])
+def test_gates_of_every_row(N, dtype, post, post_bias, rows, D):
+    t, dh, dn = make((rows, D), dtype, F, "layer", post, (rows, D), post_bias=post_bias)
+    check(N, t, dh, dn, 1.0, "layer")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("D", [40, 321, 1024, 6000])
 def test_no_gradient_of_the_sum(N, D, dtype):
     t, _, dn = make((2, 6, D), dtype, dtype, "layer", True, (2, 1, D))
