@@ -1576,7 +1576,7 @@ bcmt_status bcmt_residual_norm_forward(const bcmt_norm_params* p, const void* br
   NormFwd a{p->rows, p->D, p->rms == 0, p->wtype == BCMT_BF16,
             p->gates > 0 ? std::max(1ll, p->rows / p->gates) : 1, p->alpha, p->eps, branch, x,
             weight, bias, post_weight, post_bias, gate, h, n};
-  cudaError_t e = norm_forward(lc, p->dtype, a);
+  cudaError_t e = norm_forward(lc, p->dtype, a, device_sms());
   if (e != cudaSuccess) return cuda_fail(e, "residual norm forward");
   return finish_flags(p->flags, lc.stream);
 }

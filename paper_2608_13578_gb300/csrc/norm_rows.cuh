@@ -168,7 +168,7 @@ __device__ __forceinline__ void write8(T* row, const Cols<VEC>& c, const Pair* p
 __device__ __forceinline__ void bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
-constexpr int kMaxWarps = 16;
+constexpr int kMaxWarps = 24;
 struct RowShared {
   float4 sums[2][kMaxWarps];
 };

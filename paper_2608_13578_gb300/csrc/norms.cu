@@ -14,6 +14,7 @@
 // global memory and take the mean first, then the squares around it.  Everything between
 // the loads and the stores is fp32, rounded once to the stored type.
 #include <algorithm>
+#include <atomic>
 
 #include "internal.h"
 #include "norm_rows.cuh"
@@ -24,9 +25,9 @@ namespace bcmt {
 // Forward: a row belongs to TPR threads, each with J times eight of its columns; the row
 // stays in registers between its loads and its stores.  Up to 1024 columns a row is one
 // warp's, so that its sums need no barrier.  Bytes and the launch decide: 8192 x 512 bf16
-// 7.2 us (5.1 at the copy's rate), 8192 x 4096 60 us (40), 16384 x 768 fp32 38 us (30); rows
-// that are no multiples of 16 bytes go element by element and are bound by the load and
-// store units (16384 x 1001 bf16: 67 us, 20).
+// 7.2 us (5.1 at the copy's rate), 8192 x 4096 59 us (40), 16384 x 768 fp32 36 us (30).  Few
+// rows that are no multiples of 16 bytes, or short ones, go element by element (65000 x 201 bf16:
+// 46 us, 16).
 template <class T, int TPR, int J, bool VEC>
 __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_fwd_kernel(const NormFwd a) {
   __shared__ RowShared sh;
@@ -117,6 +118,189 @@ __global__ void __launch_bounds__(TPR > 128 ? TPR : 128) norm_fwd_kernel(const N
   }
 }
 
+// Forward over many rows whose width is no multiple of 16 bytes: workers (one warp a row, or
+// several) walk rows that come through a ring in shared memory as the 16-byte pieces that they
+// lie in, as in the backward; the norms' weights, and the gate where all rows share it, stay in
+// shared memory in fp32, so that an element costs one load of each array and a quarter of a
+// load of each vector.  Issue slots decide in bf16, whose elements are half as wide: 16384 x 1001
+// bf16 50 us (20 at the copy's rate; element by element from global memory 88), fp32 48 us (39;
+// 60); 8192 x 4099 bf16 72 us (40; 162).
+constexpr int kNormWalkJ = 2;   // groups of eight columns a lane: 72 registers, 24 warps
+template <class T, int TPR>
+__global__ void __launch_bounds__(kMaxWarps * 32, 1) norm_fwd_walk_kernel(const __grid_constant__ NormFwd a,
+                                                              const __grid_constant__ NormWalk pl) {
+  extern __shared__ float4 dyn4[];
+  __shared__ RowShared sh;
+  constexpr int J = kNormWalkJ, E = 8 * J, ES = sizeof(T);
+  pdl_enter();
+  const int tid = threadIdx.x, nt = blockDim.x, wt = TPR > 32 ? pl.tpr : 32, W = nt / wt;
+  const int worker = tid / wt, t = tid - worker * wt, lane = tid & 31, wr = t >> 5;
+  const int nw = wt / 32, warp0 = worker * nw, bar = 1 + worker, D = a.D, S = pl.stages;
+  const float inv = 1.f / D;
+  const int col0 = wr * 256 * J + lane;
+  int slot = 0;
+  auto columns = [&](int j) {
+    const int first = col0 + 256 * j;
+    return Cols<false>(first, 32, max(0, min(8, (D - first + 31) / 32)));
+  };
+  const int slot16 = (D * ES + 30) / 16;
+  const uint32_t base = shared_address(dyn4), stage_bytes = 2 * slot16 * 16;
+  const uint32_t ring = base + worker * S * stage_bytes, ring_end = ring + S * stage_bytes;
+  // vectors: post weight, post bias, gate, weight, bias; a lane's 16 bytes beside the next one's
+  constexpr int V = 2 * J * 512;
+  const uint32_t vectors = base + W * S * stage_bytes + wr * 5 * V + lane * 16;
+  const bool one = a.gate && a.group_rows >= a.rows;
+  if (worker == 0) {
+    const void* const src[5] = {a.post_weight, a.post_bias, one ? a.gate : nullptr, a.weight, a.bias};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+#pragma unroll 1
+      for (int j = 0; j < J; ++j) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i == 0 || i == 2 ? 1.f : 0.f;
+        if (src[i]) read_weight<false>(src[i], i == 2 ? ES == 2 : a.w_bf16, columns(j), v);
+        store_shared(vectors + i * V + 2 * j * 512, pair(v[0], v[1]), pair(v[2], v[3]));
+        store_shared(vectors + i * V + 2 * j * 512 + 512, pair(v[4], v[5]), pair(v[6], v[7]));
+      }
+    }
+  }
+  auto vector = [&](int i, int j, float* v) {
+    Pair p[4];
+    load_shared(vectors + i * V + 2 * j * 512, p[0], p[1]);
+    load_shared(vectors + i * V + 2 * j * 512 + 512, p[2], p[3]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split(p[e], v[2 * e], v[2 * e + 1]);
+  };
+  auto request = [&](uint32_t stage, long long row) {
+    if (row < a.rows) {
+      const long long all = a.rows * D * ES, from = row * D * ES, first = from & ~15ll;
+      const int n = (int)((from - first) + D * ES + 15) / 16;
+      const int left = (int)min((long long)n * 16, all - first);   // the last piece of all may be shorter
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const char* p = static_cast<const char*>(x ? a.x : a.branch) + first;
+        for (int i = t; i < n; i += wt) copy_async16(stage + (x * slot16 + i) * 16, p + 16 * i, min(16, left - 16 * i));
+      }
+    }
+    copy_commit();
+  };
+  auto take = [&](uint32_t stage, int x, int j, long long row, int count, float* v) {
+    const uint32_t at = stage + x * slot16 * 16 + (uint32_t)((row * D * ES) & 15) + (col0 + 256 * j) * ES;
+    if (count == 8) {   // all groups but a row's last
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = load_shared<T>(at + e * 32 * ES);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < count ? load_shared<T>(at + e * 32 * ES) : 0.f;
+    }
+  };
+  auto put = [&](T* row, const Cols<false>& c, const float* v) {
+    T* p = row + c.first;
+    if (c.count == 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e * 32] = from_f<T>(v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < c.count) p[e * 32] = from_f<T>(v[e]);
+    }
+  };
+  const long long step = (long long)gridDim.x * W;
+  long long row = (long long)blockIdx.x * W + worker, ahead = row;
+  uint32_t in = ring, cur = ring;
+  auto advance = [&] {
+    request(in, ahead);
+    ahead += step;
+    in = in + stage_bytes == ring_end ? ring : in + stage_bytes;
+  };
+  for (int i = 0; i < S - 1; ++i) advance();
+  __syncthreads();   // the vectors
+  float z[E];
+  auto stats = [&](float& mean, float& r) {
+    mean = 0.f;
+    if (a.layer) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[0] += z[e];
+      row_sums<TPR, 1>(s, sh, slot, warp0, nw, bar);
+      mean = s[0] * inv;
+    }
+    float q[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int count = columns(j).count;
+      if (count == 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = z[8 * j + e] - mean;
+          q[0] = fmaf(d, d, q[0]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = z[8 * j + e] - mean;
+          q[0] += e < count ? d * d : 0.f;
+        }
+      }
+    }
+    row_sums<TPR, 1>(q, sh, slot, warp0, nw, bar);
+    r = 1.f / sqrtf(q[0] * inv + a.eps);
+  };
+#pragma unroll 1
+  for (; row < a.rows; row += step) {
+    if (S > 2) copy_wait<1>();
+    else copy_wait<0>();
+    if (TPR > 32) bar_sync(bar, wt);   // others' copies are here, and have left the stage before
+    else __syncwarp();
+    advance();
+    const uint32_t stage = cur;
+    cur = cur + stage_bytes == ring_end ? ring : cur + stage_bytes;
+    const long long at = row * D;
+#pragma unroll
+    for (int j = 0; j < J; ++j) take(stage, 0, j, row, columns(j).count, z + 8 * j);
+    float mean, r;
+    if (a.post_weight) stats(mean, r);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const Cols<false> c = columns(j);
+      float v[8], u[8];
+      if (a.post_weight) {
+        vector(0, j, v);
+        vector(1, j, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[8 * j + e] = (z[8 * j + e] - mean) * r * v[e] + u[e];
+      }
+      if (a.gate) {
+        if (one) {
+          vector(2, j, v);
+        } else {
+          Raw8<T> g;
+          read8<false>(static_cast<const T*>(a.gate) + row / a.group_rows * D, c, true, g);
+          widen(g, v);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[8 * j + e] *= v[e];
+      }
+      take(stage, 1, j, row, c.count, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[8 * j + e] = fmaf(a.alpha, v[e], z[8 * j + e]);
+      put(static_cast<T*>(a.h) + at, c, z + 8 * j);
+    }
+    stats(mean, r);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float v[8], u[8];
+      vector(3, j, v);
+      vector(4, j, u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (z[8 * j + e] - mean) * r * v[e] + u[e];
+      put(static_cast<T*>(a.n) + at, columns(j), v);
+    }
+  }
+  copy_wait<0>();
+}
+
 // Sums of the CTAs' and segments' parts: blockIdx.y is one of the four vectors of weights
 // (with one gate for all rows the last two are A and B), or 4 + a gate; a CTA adds 32
 // columns with 16 lines of threads, each over every 16th part, then the lines in order.
@@ -188,6 +372,38 @@ cudaError_t fwd_typed(const Launch& lc, const NormFwd& a) {
   if (a.D <= 2048) return fwd_shape<T, 64, 4>(lc, a);
   if (a.D <= 4096) return fwd_shape<T, 128, 4>(lc, a);
   return fwd_shape<T, 256, 4>(lc, a);
+}
+
+template <class T, int TPR>
+cudaError_t walk_launch(const Launch& lc, const NormFwd& a, const NormWalk& w) {
+  static std::atomic<unsigned long long> done{0};
+  auto k = norm_fwd_walk_kernel<T, TPR>;
+  cudaError_t e = smem_opt_in(k, kNormSmem, &done);
+  if (e != cudaSuccess) return e;
+  return launch_k(k, dim3(w.ctas), dim3(w.threads), w.smem, lc.stream, a, w);
+}
+
+// Whether, and how, a forward call walks: rows that are no multiples of 16 bytes, at least four
+// for every worker.  (Up to 256 channels a warp a row alone is quicker: 65000 x 201 bf16 46 us,
+// walked 57.)
+bool walk_plan(const NormFwd& a, int es, int sms, NormWalk& w) {
+  if (a.D % 8 == 0 || a.D <= 256) return false;
+  w.tpr = (a.D + 256 * kNormWalkJ - 1) / (256 * kNormWalkJ) * 32;
+  for (int W = kMaxWarps * 32 / w.tpr; W >= 1; --W) {
+    const int row = 2 * ((a.D * es + 30) / 16) * 16, vectors = 5 * 2 * kNormWalkJ * 16 * w.tpr;
+    for (w.stages = 3; w.stages >= 2; --w.stages) {
+      w.smem = W * w.stages * row + vectors;
+      if (w.smem > kNormSmem) continue;
+      w.threads = W * w.tpr;
+      w.ctas = sms;
+      return a.rows >= 4ll * W * sms;
+    }
+  }
+  return false;
+}
+template <class T>
+cudaError_t walk_typed(const Launch& lc, const NormFwd& a, const NormWalk& w) {
+  return w.tpr == 32 ? walk_launch<T, 32>(lc, a, w) : walk_launch<T, 64>(lc, a, w);
 }
 
 }  // namespace
@@ -270,8 +486,11 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   return p;
 }
 
-cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a) {
+cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a, int sms) {
   if (a.rows == 0) return cudaSuccess;
+  NormWalk w;
+  if (walk_plan(a, dtype == 0 ? 4 : 2, sms, w))
+    return dtype == 0 ? walk_typed<float>(lc, a, w) : walk_typed<bf16>(lc, a, w);
   return dtype == 0 ? fwd_typed<float>(lc, a) : fwd_typed<bf16>(lc, a);
 }
 

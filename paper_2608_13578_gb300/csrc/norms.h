@@ -14,6 +14,11 @@ struct NormFwd {
   void *h, *n;
 };
 
+// How a forward call walks its rows.
+struct NormWalk {
+  int tpr, threads, ctas, stages, smem;
+};
+
 // How rows share the gate: none, one for all, one for groups of rows, one per row.
 enum NormMode { kGateNone, kGateOne, kGateGroups, kGateRows };
 
@@ -59,7 +64,7 @@ cudaError_t norm_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl)
 cudaError_t norm_bwd_f32_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_bwd_bf16_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
-cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a);
+cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a, int sms);
 cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormBwd a,
                           const NormJoin& j);
 

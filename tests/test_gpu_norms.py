@@ -111,6 +111,24 @@ def test_many_rows(N, dtype, rows, D, gates):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("kind,post,gated", [("layer", True, 1), ("rms", True, 8), ("layer", False, 0),
+                                             ("rms", False, None)])
+@pytest.mark.parametrize("rows,D", [(9800, 131), (9736, 257), (9728, 511), (4872, 1001), (2440, 2047), (1232, 4095),
+                                    (1600, 5001), (1216, 8191)])
+def test_forward_over_many_odd_rows(N, dtype, kind, post, gated, rows, D):
+    """Rows that come in pieces, the last of which is cut short; gated: gates (None: one for
+    every row, 0: without)."""
+    gates = rows if gated is None else gated
+    shape = (gates, rows // gates, D) if gates else (rows, D)
+    t, _, _ = make(shape, dtype, F, kind, post, (gates, 1, D) if gates else None)
+    h, n = forward(N, t, 0.9, kind)
+    kw = dict(post_weight=t["post_weight"], post_bias=t["post_bias"], gate=t["gate"], kind=kind, alpha=0.9)
+    (rh, rn), (bh, bn) = R.norm_forward(t["branch"], t["x"], t["weight"], t["bias"], **kw)
+    close(h, rh, bh, ROUNDINGS, "h")
+    close(n, rn, bn, ROUNDINGS, "n")
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("post", [True, False])
 @pytest.mark.parametrize("rows,D,gates", [(3000, 64, 1500), (4100, 100, 2050), (3000, 768, 1500), (900, 1001, 450),
                                           (800, 5000, 400), (480, 7676, 160), (480, 8192, 160)])
