@@ -416,7 +416,7 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   // by a count of instructions (190 a group of eight columns, 180 for the sums)
   p.tpr = D <= 64 ? 8 : D <= 128 ? 16 : 32;
   p.J = 1;
-  const int most = norm_max_warps(2) / (post ? 2 : 1);
+  const int most = 16 / (post ? 2 : 1);
   for (int J = 2, best = 1 << 30; D > 256 && J <= 4; ++J) {
     const int n = (D + 256 * J - 1) / (256 * J), cost = n * (J * 190 + 180);
     // more than two groups take too many registers without the roles, four with them
@@ -439,7 +439,7 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
     p.tot_smem = totals;
     p.pw_smem = post && p.mode == kGateRows;
     p.one_seg = !totals;
-    long long W = std::min<long long>(norm_max_warps(p.J) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
+    long long W = std::min<long long>(norm_max_warps(p.J, p.tpr <= 32) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
     W = std::max(1ll, W);
     auto size = [&](int stages, int slots) {   // whether it fits
       const long long nt = W * wt;

@@ -57,8 +57,10 @@ struct NormPlan {
 };
 constexpr int kNormMaxD = 8192;
 constexpr int kNormSmem = 227 * 1024 - 1024;   // of a CTA, beside the sums' buffers
-// Warps of a CTA whose threads have 8 J columns: 96 and 128 registers a thread.
-constexpr int norm_max_warps(int J) { return J == 1 ? 20 : 16; }
+// Warps of a CTA whose threads have 8 J columns, one warp a row or several: 96, 128, and for
+// rows of 24 columns a lane of one warp 168 registers a thread (16384 x 768: 40 us, with 16 warps
+// of 128 registers 42).
+constexpr int norm_max_warps(int J, bool one) { return J == 1 ? 20 : one && J == 3 ? 12 : 16; }
 NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, int sms);
 cudaError_t norm_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_bwd_f32_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);

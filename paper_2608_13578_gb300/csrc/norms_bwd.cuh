@@ -18,7 +18,8 @@ namespace bcmt {
 //
 // A thread's columns are the same in every row, so the columns' sums stay in its registers
 // and reach global memory once per CTA, the gate's once per segment.  A lane has 8 J columns,
-// up to 32: what a sum over a row costs is shared by more of them.  Rows come through rings
+// up to 32: what a sum over a row costs is shared by more of them (a single warp with all of
+// 1024 columns, 32 a lane, is slower than two: 4095 x 1001 fp32 57 us for 31).  Rows come through rings
 // in shared memory by asynchronous copies.  VEC (16-byte rows): a thread copies its own
 // columns to its own places and needs no barrier.  Else the role's threads copy the 16-byte
 // pieces that a row lies in, and read elements.
@@ -28,9 +29,9 @@ namespace bcmt {
 // gate is done once for its segment (a gate for all rows: when the CTAs' sums are joined).  A gate per row (ROWS) comes through the ring too, and
 // the sums take g ds.
 //
-// What bounds it: the latency of a row's sums with 16 warps an SM (128 registers a thread), and
-// issue slots (1200 instructions for both roles of a row of 768).  Measured, both kernels of a
-// call: 16384 x 768 bf16 42 us (22.7 at the copy's rate), 16384 x 4096 165 us (121), 4095 x 1001
+// What bounds it: the latency of a row's sums with 12 to 20 warps an SM (168 to 96 registers a
+// thread), and issue slots (990 instructions for both roles of a row of 768).  Measured, both
+// kernels of a call: 16384 x 768 bf16 40 us (22.7 at the copy's rate), 16384 x 4096 165 us (121), 4095 x 1001
 // fp32 with a gate per row 31 us (20), 65536 x 64 18 us (7.6), 8192 x 8192 without a post norm
 // 142 us (121).  One role with 8 columns a lane took 57, 211, 106 and 88 us for the first four.
 enum { kRolePre, kRolePost, kRoleAll };
@@ -46,7 +47,7 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
   constexpr int NPRE = ROLE == kRolePost ? 0 : 3, NA = NPRE + (LAST ? 1 + ROWS : 0);
   constexpr int kBranch = NPRE, kGate = NPRE + 1;
   constexpr int kA = ROLE == kRoleAll ? 2 : 0;     // where A is
-  constexpr bool KEEP = ROLE == kRolePre ? J <= 3 : J <= 2;   // a row stays in registers
+  constexpr bool KEEP = TPR == 32 || J <= (ROLE == kRolePre ? 3 : 2);   // a row stays in registers
 
   const int nt = POST ? blockDim.x / 2 : blockDim.x;   // threads of a role
   const int tid = threadIdx.x - (ROLE == kRolePost ? nt : 0);
@@ -601,7 +602,7 @@ namespace {
 template <class T, int TPR, int J, bool VEC, bool POST, bool ROWS>
 cudaError_t bwd_launch(const Launch& lc, const NormBwd& a, const NormPlan& pl) {
   static std::atomic<unsigned long long> done{0};
-  auto k = norm_bwd_kernel<T, TPR, J, VEC, POST, ROWS, norm_max_warps(J) * 32>;
+  auto k = norm_bwd_kernel<T, TPR, J, VEC, POST, ROWS, norm_max_warps(J, TPR <= 32) * 32>;
   cudaError_t e = smem_opt_in(k, kNormSmem, &done);
   if (e != cudaSuccess) return e;
   return launch_k(k, dim3(pl.ctas), dim3(pl.threads), pl.smem, lc.stream, a);
