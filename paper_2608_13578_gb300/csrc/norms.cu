@@ -511,9 +511,11 @@ cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormB
   a.segs_per_group = pl.segs_per_group;
   a.seg_group_rows = pl.seg_group_rows;
   a.nseg = pl.nseg;
-  const auto kernel = dtype == 0 ? a.post_weight ? norm_bwd_f32_post : norm_bwd_f32
-                                 : a.post_weight ? norm_bwd_bf16_post : norm_bwd_bf16;
-  cudaError_t e = kernel(lc, a, pl);
+  // by type; without a post norm, with one, with one and a gate per row
+  static constexpr decltype(&norms_bwd_f32) kCalls[2][3] = {
+      {norms_bwd_f32, norms_bwd_f32_post, norms_bwd_f32_post_rows},
+      {norms_bwd_bf16, norms_bwd_bf16_post, norms_bwd_bf16_post_rows}};
+  cudaError_t e = kCalls[dtype != 0][a.post_weight ? 1 + (pl.mode == kGateRows) : 0](lc, a, pl);
   if (e != cudaSuccess) return e;
   // gates beyond the grid's second axis take further launches
   const long long gates = pl.mode == kGateOne ? 1 : pl.gate_bytes ? pl.nseg / pl.segs_per_group : 0;

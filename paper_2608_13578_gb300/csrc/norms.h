@@ -62,10 +62,12 @@ constexpr int kNormSmem = 227 * 1024 - 1024;   // of a CTA, beside the sums' buf
 // of 128 registers 42).
 constexpr int norm_max_warps(int J, bool one) { return J == 1 ? 20 : one && J == 3 ? 12 : 16; }
 NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, int sms);
-cudaError_t norm_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl);
-cudaError_t norm_bwd_f32_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
-cudaError_t norm_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl);
-cudaError_t norm_bwd_bf16_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_f32_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_f32_post_rows(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_bf16_post(const Launch& lc, const NormBwd& a, const NormPlan& pl);
+cudaError_t norms_bwd_bf16_post_rows(const Launch& lc, const NormBwd& a, const NormPlan& pl);
 cudaError_t norm_forward(const Launch& lc, int dtype, const NormFwd& a, int sms);
 cudaError_t norm_backward(const Launch& lc, int dtype, const NormPlan& pl, NormBwd a,
                           const NormJoin& j);

@@ -4,7 +4,7 @@
 
 namespace bcmt {
 
-cudaError_t norm_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl) {
+cudaError_t norms_bwd_bf16(const Launch& lc, const NormBwd& a, const NormPlan& pl) {
   return pl.mode == kGateRows ? bwd_typed<bf16, false, true>(lc, a, pl) : bwd_typed<bf16, false, false>(lc, a, pl);
 }
 

@@ -4,7 +4,7 @@
 
 namespace bcmt {
 
-cudaError_t norm_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl) {
+cudaError_t norms_bwd_f32(const Launch& lc, const NormBwd& a, const NormPlan& pl) {
   return pl.mode == kGateRows ? bwd_typed<float, false, true>(lc, a, pl) : bwd_typed<float, false, false>(lc, a, pl);
 }
 
