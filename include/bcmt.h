@@ -366,7 +366,7 @@ bcmt_status bcmt_residual_norm_backward(const bcmt_norm_params* p, const void* d
  * decides a code is rounded to fp32 at each operation.  All zeros are states of 0.
  * A gradient that is not finite makes its element's state, in 8 bits its block's
  * scales, not finite.  step_ptr and lr_ptr (device memory, or NULL) take the
- * place of step and lr when the kernel runs, for captured graphs.
+ * place of step (>= 1 there too) and lr when the kernel runs, for captured graphs.
  * Requirements: buffers of a tensor and of different tensors do not overlap;
  * 0 <= beta < 1; lr, eps, weight_decay >= 0 and finite; step >= 1.  flags:
  * BCMT_FLAG_CHECK only.  `tensors` is read during the call (host memory). */

@@ -317,8 +317,14 @@ __global__ void __launch_bounds__(512) norm_join_kernel(const NormJoin a) {
   auto sum = [&](const float* in, long long n, long long stride) {   // in line 0
     float v = 0.f;
     if (col < a.D) {
-#pragma unroll 8
-      for (long long i = line; i < n; i += 16) v += in[i * stride + col];
+      // ten loads at a time: the parts of up to 160 CTAs are one turn
+      for (long long i = line; i < n; i += 160) {
+        float u[10];
+#pragma unroll
+        for (int k = 0; k < 10; ++k) u[k] = i + 16 * k < n ? in[(i + 16 * k) * stride + col] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 10; ++k) v += u[k];
+      }
     }
     __syncthreads();
     s[line][lane] = v;
