@@ -37,7 +37,7 @@ struct Entry {
   int v;
 };
 
-// The sum a + b as a float and what it lacks.
+// The sum a + b as a float and what it lacks (Knuth's two-sum).
 __device__ __forceinline__ float two_sum(float a, float b, float& rest) {
   const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
   rest = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
@@ -45,7 +45,7 @@ __device__ __forceinline__ float two_sum(float a, float b, float& rest) {
 }
 // exp(x - ref), x - ref from -86 to 0, as 2^n (h + l) to within 2^-32: the 64-bit units of
 // this chip are too slow for it (a fp64 exponential took most of the merge's time).
-// x - ref = n ln 2 + r with r in two floats, and exp(r) = 1 + r + r^2/2 + r^3/6 + ..., the
+// x - ref = n ln 2 + r with r in two floats (as Cody and Waite reduce, ln 2 split in three), and exp(r) = 1 + r + r^2/2 + r^3/6 + ..., the
 // first four terms in two floats, Taylor's next six in one.
 __device__ __forceinline__ void exp_wide(float x, float ref, float& h, float& l, int& n) {
   float lo, t;
