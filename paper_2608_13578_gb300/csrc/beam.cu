@@ -45,8 +45,9 @@ __device__ __forceinline__ float two_sum(float a, float b, float& rest) {
 }
 // exp(x - ref), x - ref from -86 to 0, as 2^n (h + l) to within 2^-32: the 64-bit units of
 // this chip are too slow for it (a fp64 exponential took most of the merge's time).
-// x - ref = n ln 2 + r with r in two floats (as Cody and Waite reduce, ln 2 split in three), and exp(r) = 1 + r + r^2/2 + r^3/6 + ..., the
-// first four terms in two floats, Taylor's next six in one.
+// x - ref = n ln 2 + r with r in two floats (as Cody and Waite reduce, ln 2 split in
+// three), and exp(r) = 1 + r + r^2/2 + r^3/6 + ..., the first four terms in two floats,
+// Taylor's next seven in one.
 __device__ __forceinline__ void exp_wide(float x, float ref, float& h, float& l, int& n) {
   float lo, t;
   const float hi = two_sum(x, -ref, lo);
@@ -539,8 +540,8 @@ constexpr int kPiece = 4096;   // bytes of a row that a CTA copies
 }  // namespace
 
 // A CTA copies one piece of the rows of one search: beams with a parent in common read
-// it while it is in the caches (64 x 8 beams of 6 layers of 8 x 64 x 64: 96 us, 6.9 TB/s).  Rows of 16-byte multiples in 16-byte steps, others in
-// single bytes.
+// it while it is in the caches (64 x 8 beams of 6 layers of 8 x 64 x 64: 96 us, 6.9 TB/s).
+// Rows of 16-byte multiples in 16-byte steps, others in single bytes.
 __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant__ ReorderTable a) {
   pdl_enter();
   int lo = 0, hi = a.count - 1;

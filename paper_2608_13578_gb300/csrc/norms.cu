@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 1) norm_fwd_walk_kernel(const 
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const char* p = static_cast<const char*>(x ? a.x : a.branch) + first;
-        for (int i = t; i < n; i += wt) copy_async16(stage + (x * slot16 + i) * 16, p + 16 * i, min(16, left - 16 * i));
+        for (int i = t; i < n; i += wt)
+          copy_async16(stage + (x * slot16 + i) * 16, p + 16 * i, min(16, left - 16 * i));
       }
     }
     copy_commit();
@@ -445,8 +446,8 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
     p.tot_smem = totals;
     p.pw_smem = post && p.mode == kGateRows;
     p.one_seg = !totals;
-    long long W = std::min<long long>(norm_max_warps(p.J, p.tpr <= 32) * 32 / (wt * roles), (g * gs + sms - 1) / sms);
-    W = std::max(1ll, W);
+    long long W = norm_max_warps(p.J, p.tpr <= 32) * 32 / (wt * roles);
+    W = std::max(1ll, std::min(W, (g * gs + sms - 1) / sms));
     auto size = [&](int stages, int slots) {   // whether it fits
       const long long nt = W * wt;
       p.stages = stages;

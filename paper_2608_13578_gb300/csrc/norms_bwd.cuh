@@ -26,8 +26,8 @@ namespace bcmt {
 //
 // With A = sum ds yh and B = sum ds over the rows of one gate, its gradient is pw A + pb B,
 // and it adds g A to dpw and g B to dpb: the sums take A and B, and what depends on the
-// gate is done once for its segment (a gate for all rows: when the CTAs' sums are joined).  A gate per row (ROWS) comes through the ring too, and
-// the sums take g ds.
+// gate is done once for its segment (a gate for all rows: when the CTAs' sums are joined).
+// A gate per row (ROWS) comes through the ring too, and the sums take g ds.
 //
 // What bounds it: the latency of a row's sums with 12 to 20 warps an SM (168 to 96 registers a
 // thread), and issue slots (990 instructions for both roles of a row of 768).  Measured, both
@@ -82,7 +82,8 @@ __device__ __forceinline__ void norm_bwd_role(const NormBwd& a, float4* dyn4, Ro
   const int slot16 = VEC ? 0 : (R * D * ES + 30) / 16;    // of one array of one worker
   const uint32_t stage_bytes = VEC ? STAGE : NA * slot16 * 16;
   const uint32_t base = shared_address(dyn4);
-  const uint32_t ring = base + (ROLE == kRolePost ? S * 3 * (VEC ? J * PIECES * 512 * nwarps : slot16 * 16 * W) : 0) +
+  const uint32_t first_ring = S * 3 * (VEC ? J * PIECES * 512 * nwarps : slot16 * 16 * W);
+  const uint32_t ring = base + (ROLE == kRolePost ? first_ring : 0) +
                         (VEC ? wid * S * STAGE + lane * 16 : worker * S * stage_bytes);
   const uint32_t dss = base + a.ring16 * 16 + wid * a.ds_slots * V + lane * 16;
   const uint32_t ws0 = base + a.ring16 * 16 + (POST ? nwarps * a.ds_slots * V : 0);

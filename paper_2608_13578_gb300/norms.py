@@ -18,8 +18,8 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import bcmt as C
-from .lm_ops import (_address, _buffer, _check, _current_device, _dense, _device, _dtype, _number, _on_its_device,
-                     _raw_stream)
+from .lm_ops import (_address, _buffer, _check, _current_device, _dense, _device, _dtype, _number,
+                     _on_its_device, _raw_stream)
 
 KINDS = ("layer", "rms")
 
