@@ -198,6 +198,17 @@ def adamw8_values(m, m_scale, v, v_scale):
     return mo, vo
 
 
+def _options(group):
+    """Refuses what would change the step in a group of torch's optimizers, and has no place here."""
+    for name in ("maximize", "amsgrad", "differentiable"):
+        if group.get(name):
+            raise ValueError(f"this AdamW has no {name}")
+    if not group.get("decoupled_weight_decay", True) and group["weight_decay"] != 0:
+        raise ValueError("decoupled_weight_decay=False: the weight decay of AdamW is decoupled")
+    if group.get("bits", 32) not in (32, 8):
+        raise ValueError(f"bits must be 32 or 8, not {group['bits']}")
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW with every tensor of a parameter group in one launch.
 
@@ -205,13 +216,14 @@ class AdamW(torch.optim.Optimizer):
     and updated.  capturable: the count of steps is kept on the device, so that a captured
     ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
     a float32 on the device, the rate can change between replays too.  ``step`` takes a
-    grad_scale (one float32 on the device, as from clipping by the norm)."""
+    grad_scale (one float32 on the device, as from clipping by the norm).  Groups, and files of
+    other optimizers, that ask for a step of another kind (maximize, amsgrad, differentiable, a
+    weight decay that is not decoupled) raise ValueError."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 1e-2, *, bits: int = 32, masters: bool = False,
                  capturable: bool = False):
-        if bits not in (32, 8):
-            raise ValueError(f"bits must be 32 or 8, not {bits}")
+        _options(dict(bits=bits))
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay,
                                       bits=bits, masters=masters, capturable=capturable))
         self._plans = {}
@@ -222,6 +234,11 @@ class AdamW(torch.optim.Optimizer):
         for group in self.param_groups:
             for k in ("bits", "masters", "capturable"):
                 group.setdefault(k, self.defaults.get(k))
+
+    def add_param_group(self, param_group):
+        if isinstance(param_group, dict):   # (torch refuses anything else)
+            _options({**self.defaults, **param_group})
+        super().add_param_group(param_group)
 
     def _init(self, p, group):
         s = self.state[p]
@@ -266,6 +283,8 @@ class AdamW(torch.optim.Optimizer):
     @torch.no_grad()
     def step(self, closure=None, *, grad_scale: Optional[torch.Tensor] = None):
         loss = None
+        for group in self.param_groups:
+            _options(group)
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
@@ -300,6 +319,8 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def load_state_dict(self, state_dict):
+        for group in state_dict["param_groups"]:
+            _options(group)
         super().load_state_dict(state_dict)
         # the states in their own types (the base class gives them the parameters')
         for group, saved in zip(self.param_groups, state_dict["param_groups"]):

@@ -1,0 +1,84 @@
+"""Host side of the library's AdamW (CPU only): the options of its groups, files of other
+optimizers, counts of steps.  Plans are replaced by ones that record their calls."""
+
+import copy
+
+import pytest
+import torch
+
+from paper_2608_13578_gb300 import optim
+
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """(params, their lists of states by name, what a step was called with) of every step."""
+    got = []
+
+    class Plan:
+        def __init__(self, params, m, v, **lists):
+            self.params, self.lists = params, dict(m=m, v=v, **lists)
+
+        def step(self, grads, **how):
+            got.append((self.params, self.lists, {**how, "grads": grads, "step": how["step"]}))
+    monkeypatch.setattr(optim, "AdamWPlan", Plan)
+    return got
+
+
+def params(*shapes, dtype=F, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    ps = [torch.nn.Parameter(torch.randn(s, generator=g).to(dtype)) for s in shapes]
+    for p in ps:
+        p.grad = torch.randn(p.shape, generator=g).to(dtype)
+    return ps
+
+
+# ------------------------------------------------------------- options of a group
+IGNORED = [dict(maximize=True), dict(amsgrad=True), dict(differentiable=True),
+           dict(decoupled_weight_decay=False, weight_decay=0.1), dict(bits=16)]
+
+
+@pytest.mark.parametrize("option", IGNORED, ids=lambda o: next(iter(o)))
+def test_options_that_would_be_ignored(calls, option):
+    """A group with an option of torch's that changes the step, and that this one has not,
+    is refused wherever it comes from, and nothing is changed by it."""
+    name = next(iter(option))
+    p, q = params(3, 4)
+    with pytest.raises(ValueError, match=name):
+        optim.AdamW([dict(params=[p], **option)])
+    opt = optim.AdamW([p], lr=0.5)
+    with pytest.raises(ValueError, match=name):
+        opt.add_param_group(dict(params=[q], **option))
+    assert len(opt.param_groups) == 1
+    file = opt.state_dict()
+    file["param_groups"][0].update(option, lr=0.1)
+    with pytest.raises(ValueError, match=name):
+        opt.load_state_dict(file)
+    assert opt.param_groups[0]["lr"] == 0.5
+    opt.param_groups[0].update(option)
+    with pytest.raises(ValueError, match=name):
+        opt.step()
+    assert not calls
+
+
+@pytest.mark.parametrize("option", [dict(maximize=True), dict(amsgrad=True)], ids=lambda o: next(iter(o)))
+def test_a_file_of_torch_with_such_an_option(calls, option):
+    (p,) = params(3)
+    old = torch.optim.AdamW([p], **option)
+    old.step()
+    opt = optim.AdamW([p])
+    with pytest.raises(ValueError, match=next(iter(option))):
+        opt.load_state_dict(old.state_dict())
+    assert not opt.state
+
+
+def test_options_that_are_only_hints(calls):
+    """foreach, fused and the switches that are off are taken as they are."""
+    (p,) = params(3)
+    old = torch.optim.AdamW([p], foreach=True)
+    old.step()
+    opt = optim.AdamW([dict(params=[p], maximize=False, amsgrad=False, fused=True)])
+    opt.load_state_dict(old.state_dict())
+    opt.step()
+    assert len(calls) == 1 and calls[0][2]["step"] == 2
