@@ -216,7 +216,8 @@ class AdamW(torch.optim.Optimizer):
     and updated.  capturable: the count of steps is kept on the device, so that a captured
     ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
     a float32 on the device, the rate can change between replays too.  ``step`` takes a
-    grad_scale (one float32 on the device, as from clipping by the norm).  Groups, and files of
+    grad_scale (one float32 on the device, as from clipping by the norm).  Files of
+    torch.optim.AdamW load; bits and masters, and capturable=True, stay as they are.  Groups, and files of
     other optimizers, that ask for a step of another kind (maximize, amsgrad, differentiable, a
     weight decay that is not decoupled) raise ValueError."""
 
@@ -319,8 +320,13 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def load_state_dict(self, state_dict):
-        for group in state_dict["param_groups"]:
-            _options(group)
+        groups = list(state_dict["param_groups"])
+        for i, (saved, group) in enumerate(zip(groups, self.param_groups)):
+            if "bits" not in saved:   # of another optimizer: what it does not know stays
+                groups[i] = saved = {**saved, "bits": group["bits"], "masters": group["masters"],
+                                     "capturable": group["capturable"] or saved.get("capturable", False)}
+            _options(saved)
+        state_dict = {**state_dict, "param_groups": groups}
         super().load_state_dict(state_dict)
         # the states in their own types (the base class gives them the parameters')
         for group, saved in zip(self.param_groups, state_dict["param_groups"]):

@@ -82,3 +82,38 @@ def test_options_that_are_only_hints(calls):
     opt.load_state_dict(old.state_dict())
     opt.step()
     assert len(calls) == 1 and calls[0][2]["step"] == 2
+
+
+# ------------------------------------------------------ files of torch's optimizer
+def torch_file(ps, steps=3, **kw):
+    """The states of torch's AdamW after some steps over ps, which it moves."""
+    old = torch.optim.AdamW(ps, **kw)
+    for _ in range(steps):
+        old.step()
+    return copy.deepcopy(old.state_dict())
+
+
+def test_a_file_of_torch_leaves_what_it_does_not_know(calls):
+    """bits, masters and capturable of each group stay as they were made: torch's files do not
+    have the first two, and their capturable=False would freeze the count of a captured step."""
+    p, q = params((4, 5), 7)
+    opt = optim.AdamW([dict(params=[p], capturable=True), dict(params=[q], masters=True)], lr=0.5)
+    opt.load_state_dict(torch_file([dict(params=[p]), dict(params=[q])], lr=0.25))
+    first, second = opt.param_groups
+    assert (first["bits"], first["masters"], first["capturable"], first["lr"]) == (32, False, True, 0.25)
+    assert (second["bits"], second["masters"], second["capturable"]) == (32, True, False)
+    assert isinstance(opt.state[p]["step"], torch.Tensor) and opt.state[q]["step"] == 3
+    opt.step()
+    assert [int(c[2]["step"]) for c in calls] == [4, 4]
+    # a file of this class says what its groups are
+    other = optim.AdamW([dict(params=[p]), dict(params=[q])])
+    other.load_state_dict(opt.state_dict())
+    assert [g["capturable"] for g in other.param_groups] == [True, False]
+    assert [g["masters"] for g in other.param_groups] == [False, True]
+
+
+def test_files_of_another_length(calls):
+    p, q = params(3, 4)
+    opt = optim.AdamW([p])
+    with pytest.raises(ValueError, match="group"):
+        opt.load_state_dict(torch_file([dict(params=[p]), dict(params=[q])]))
