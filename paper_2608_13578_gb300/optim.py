@@ -209,6 +209,30 @@ def _options(group):
         raise ValueError(f"bits must be 32 or 8, not {group['bits']}")
 
 
+def _states(bits):
+    """Names and types of a parameter's states."""
+    if bits == 8:
+        return {"exp_avg": torch.int8, "exp_avg_sq": torch.uint8, "exp_avg_scale": _F32,
+                "exp_avg_sq_scale": _F32}
+    return {"exp_avg": _F32, "exp_avg_sq": _F32}
+
+
+def _check_file(group, states):
+    """Refuses a file's states that are not those of its (completed) group."""
+    names = _states(group["bits"])
+    for k in group["params"]:
+        s = states.get(k)
+        if not s:
+            continue
+        lacking = [n for n in (*names, "step") if n not in s]
+        # floats of another width are taken, as torch's files of bf16 parameters have them
+        lacking += [f"{n} as {t}" for n, t in names.items()
+                    if n in s and s[n].dtype != t and not (t.is_floating_point and s[n].is_floating_point())]
+        if lacking:
+            raise ValueError(f"parameter {k} of the file has no {', '.join(lacking)}: the group's states "
+                             f"are in {group['bits']} bits")
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW with every tensor of a parameter group in one launch.
 
@@ -217,9 +241,9 @@ class AdamW(torch.optim.Optimizer):
     ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
     a float32 on the device, the rate can change between replays too.  ``step`` takes a
     grad_scale (one float32 on the device, as from clipping by the norm).  Files of
-    torch.optim.AdamW load; bits and masters, and capturable=True, stay as they are.  Groups, and files of
-    other optimizers, that ask for a step of another kind (maximize, amsgrad, differentiable, a
-    weight decay that is not decoupled) raise ValueError."""
+    torch.optim.AdamW load where bits is 32; masters, and capturable=True, stay as they are.
+    Groups and files that ask for a step of another kind (maximize, amsgrad, differentiable, a
+    weight decay that is not decoupled) or lack the group's states raise ValueError."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 1e-2, *, bits: int = 32, masters: bool = False,
@@ -268,8 +292,7 @@ class AdamW(torch.optim.Optimizer):
 
     def _plan(self, key, group, params):
         states = [self.state[p] for p in params]
-        names = ["exp_avg", "exp_avg_sq"] + (["exp_avg_scale", "exp_avg_sq_scale"]
-                                             if group["bits"] == 8 else [])
+        names = list(_states(group["bits"]))
         names += ["master"] if "master" in states[0] else []
         ids = [id(p) for p in params] + [id(s[k]) for s in states for k in names]
         plan = self._plans.get(key)
@@ -326,6 +349,7 @@ class AdamW(torch.optim.Optimizer):
                 groups[i] = saved = {**saved, "bits": group["bits"], "masters": group["masters"],
                                      "capturable": group["capturable"] or saved.get("capturable", False)}
             _options(saved)
+            _check_file(saved, state_dict["state"])
         state_dict = {**state_dict, "param_groups": groups}
         super().load_state_dict(state_dict)
         # the states in their own types (the base class gives them the parameters')

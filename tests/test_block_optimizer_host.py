@@ -117,3 +117,47 @@ def test_files_of_another_length(calls):
     opt = optim.AdamW([p])
     with pytest.raises(ValueError, match="group"):
         opt.load_state_dict(torch_file([dict(params=[p]), dict(params=[q])]))
+
+
+def test_files_without_the_states_are_refused(calls):
+    """States of another kind than the group's are refused by name, before anything changes."""
+    p, q = params((4, 5), 7)
+    file = torch_file([p, q], lr=0.25)
+    opt = optim.AdamW([p, q], lr=0.5, bits=8)
+    with pytest.raises(ValueError, match="exp_avg_scale.*8 bits"):
+        opt.load_state_dict(file)
+    with pytest.raises(ValueError, match="exp_avg"):
+        optim.AdamW([p, q]).load_state_dict(copy.deepcopy(torch.optim.SGD([p, q], lr=1.0, momentum=0.9).state_dict())
+                                            | {"state": {0: dict(momentum_buffer=torch.zeros(4, 5))}})
+    assert not opt.state and opt.param_groups[0]["lr"] == 0.5
+    # one parameter of several, and codes where the group wants floats
+    opt = optim.AdamW([p, q])
+    opt.step()
+    for name in ("exp_avg", "exp_avg_sq", "step"):
+        file = opt.state_dict()
+        file["state"][1] = {k: x for k, x in file["state"][1].items() if k != name}
+        with pytest.raises(ValueError, match=name):
+            optim.AdamW([p, q]).load_state_dict(file)
+    eight = optim.AdamW([p, q], bits=8)
+    eight.step()
+    file = eight.state_dict()
+    file["param_groups"][0]["bits"] = 32
+    with pytest.raises(ValueError, match="32 bits"):
+        optim.AdamW([p, q]).load_state_dict(file)
+    file = opt.state_dict()
+    file["param_groups"][0]["bits"] = 8
+    for s in file["state"].values():
+        s["exp_avg_scale"] = s["exp_avg_sq_scale"] = torch.zeros(1)
+    with pytest.raises(ValueError, match="8 bits"):
+        optim.AdamW([p, q]).load_state_dict(file)
+
+
+def test_a_parameter_that_the_file_has_no_states_of(calls):
+    p, q = params(3, 4)
+    grad, q.grad = q.grad, None
+    file = torch_file([p, q])
+    opt = optim.AdamW([p, q])
+    opt.load_state_dict(file)
+    q.grad = grad
+    opt.step()
+    assert [c[2]["step"] for c in calls] == [1, 4]
