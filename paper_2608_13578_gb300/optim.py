@@ -217,6 +217,10 @@ def _states(bits):
     return {"exp_avg": _F32, "exp_avg_sq": _F32}
 
 
+def _has_master(group, p):
+    return group["masters"] and p.dtype != _F32
+
+
 def _check_file(group, states):
     """Refuses a file's states that are not those of its (completed) group."""
     names = _states(group["bits"])
@@ -241,7 +245,8 @@ class AdamW(torch.optim.Optimizer):
     ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
     a float32 on the device, the rate can change between replays too.  ``step`` takes a
     grad_scale (one float32 on the device, as from clipping by the norm).  Files of
-    torch.optim.AdamW load where bits is 32; masters, and capturable=True, stay as they are.
+    torch.optim.AdamW load where bits is 32; masters (then begun from the parameters) and
+    capturable=True stay as they are.
     Groups and files that ask for a step of another kind (maximize, amsgrad, differentiable, a
     weight decay that is not decoupled) or lack the group's states raise ValueError."""
 
@@ -267,22 +272,21 @@ class AdamW(torch.optim.Optimizer):
 
     def _init(self, p, group):
         s = self.state[p]
-        if s:
-            return
-        flat = torch.preserve_format if p.is_contiguous() else torch.contiguous_format
-        if group["bits"] == 8:
-            blocks = -(-p.numel() // BLOCK)
-            s["exp_avg"] = torch.zeros(p.shape, dtype=torch.int8, device=p.device)
-            s["exp_avg_sq"] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device)
-            s["exp_avg_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
-            s["exp_avg_sq_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
-        else:
-            s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
-            s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
-        if group["masters"] and p.dtype != _F32:
+        if not s:
+            flat = torch.preserve_format if p.is_contiguous() else torch.contiguous_format
+            if group["bits"] == 8:
+                blocks = -(-p.numel() // BLOCK)
+                s["exp_avg"] = torch.zeros(p.shape, dtype=torch.int8, device=p.device)
+                s["exp_avg_sq"] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device)
+                s["exp_avg_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
+                s["exp_avg_sq_scale"] = torch.zeros(blocks, dtype=_F32, device=p.device)
+            else:
+                s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
+                s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
+            # one count for the group where it is on the device
+            s["step"] = self._count(group, p.device) if group["capturable"] else 0
+        if "master" not in s and _has_master(group, p):   # (a file may have states without)
             s["master"] = p.detach().to(_F32)
-        # one count for the group where it is on the device
-        s["step"] = self._count(group, p.device) if group["capturable"] else 0
 
     def _count(self, group, device):
         for p in group["params"]:
@@ -293,7 +297,7 @@ class AdamW(torch.optim.Optimizer):
     def _plan(self, key, group, params):
         states = [self.state[p] for p in params]
         names = list(_states(group["bits"]))
-        names += ["master"] if "master" in states[0] else []
+        names += ["master"] if _has_master(group, params[0]) else []
         ids = [id(p) for p in params] + [id(s[k]) for s in states for k in names]
         plan = self._plans.get(key)
         if plan is None or plan[0] != ids:

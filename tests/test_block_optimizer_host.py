@@ -161,3 +161,42 @@ def test_a_parameter_that_the_file_has_no_states_of(calls):
     q.grad = grad
     opt.step()
     assert [c[2]["step"] for c in calls] == [1, 4]
+
+
+def test_masters_of_a_file_that_has_none(calls):
+    """Every bf16 parameter of a group with masters gets one, whether the file has its states
+    or not and whichever comes first."""
+    for without in (0, 1, None):
+        p, q = params((4, 5), 7, dtype=BF)
+        if without is not None:
+            kept = (p, q)[without].grad
+            (p, q)[without].grad = None
+        file = torch_file([p, q])
+        if without is not None:
+            (p, q)[without].grad = kept
+        calls.clear()
+        opt = optim.AdamW([p, q], masters=True)
+        opt.load_state_dict(file)
+        opt.step()
+        seen = {id(x) for c in calls for x in c[1]["masters"]}
+        assert seen == {id(opt.state[x]["master"]) for x in (p, q)}
+        for x in (p, q):
+            assert torch.equal(opt.state[x]["master"], x.detach().float()) and opt.state[x]["master"].dtype == F
+        # they are kept from then on
+        for x in (p, q):
+            opt.state[x]["master"].add_(1.0)
+        before = [opt.state[x]["master"] for x in (p, q)]
+        opt.step()
+        assert all(opt.state[x]["master"] is m for x, m in zip((p, q), before))
+        again = optim.AdamW([p, q], masters=True)
+        again.load_state_dict(opt.state_dict())
+        again.step()
+        assert all(torch.equal(again.state[x]["master"], m) for x, m in zip((p, q), before))
+
+
+def test_no_masters_where_none_are_kept(calls):
+    p, q = params(3, 4)
+    r, s = params(3, 4, dtype=BF)
+    opt = optim.AdamW([dict(params=[p, q], masters=True), dict(params=[r, s])])
+    opt.step()
+    assert [c[1].get("masters") for c in calls] == [None, None]
