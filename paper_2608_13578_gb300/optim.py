@@ -356,7 +356,8 @@ class AdamW(torch.optim.Optimizer):
             _check_file(saved, state_dict["state"])
         state_dict = {**state_dict, "param_groups": groups}
         super().load_state_dict(state_dict)
-        # the states in their own types (the base class gives them the parameters')
+        # the states in their own types (the base class gives them the parameters'): all floats are
+        # float32, moments that torch kept in bf16 too
         for group, saved in zip(self.param_groups, state_dict["param_groups"]):
             count = {}   # one count for the group where it is on the device
             for p, k in zip(group["params"], saved["params"]):
@@ -366,6 +367,6 @@ class AdamW(torch.optim.Optimizer):
                         if group["capturable"]:
                             x = count.setdefault(p.device, torch.tensor(x, device=p.device))
                     elif isinstance(x, torch.Tensor):
-                        x = x.detach().to(p.device, copy=True)
+                        x = x.detach().to(p.device, _F32 if x.is_floating_point() else x.dtype, copy=True)
                     self.state[p][name] = x
         self._plans.clear()

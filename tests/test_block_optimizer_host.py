@@ -200,3 +200,23 @@ def test_no_masters_where_none_are_kept(calls):
     opt = optim.AdamW([dict(params=[p, q], masters=True), dict(params=[r, s])])
     opt.step()
     assert [c[1].get("masters") for c in calls] == [None, None]
+
+
+@pytest.mark.parametrize("masters", [False, True])
+def test_moments_of_another_width(calls, masters):
+    """Torch keeps the moments of bf16 parameters in bf16; here they go on in float32."""
+    p, q = params((4, 5), 7, dtype=BF)
+    file = torch_file([p, q])
+    opt = optim.AdamW([p, q], masters=masters)
+    opt.load_state_dict(file)
+    for i, x in enumerate((p, q)):
+        for name in ("exp_avg", "exp_avg_sq"):
+            assert file["state"][i][name].dtype == BF and opt.state[x][name].dtype == F
+            assert torch.equal(opt.state[x][name], file["state"][i][name].float())
+    opt.step()
+    assert calls[-1][2]["step"] == 4
+    eight = optim.AdamW([p, q], bits=8)
+    eight.step()
+    again = optim.AdamW([p, q], bits=8)
+    again.load_state_dict(eight.state_dict())
+    assert {k: x.dtype for k, x in again.state[p].items() if k != "step"} == optim._states(8)
