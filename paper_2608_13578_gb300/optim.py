@@ -242,13 +242,13 @@ class AdamW(torch.optim.Optimizer):
 
     bits: 32, or 8 for states in 8 bits; masters: float32 values of bf16 parameters are kept
     and updated.  capturable: the count of steps is kept on the device, so that a captured
-    ``step`` goes on counting at each replay (the group then counts as one); with an lr that is
-    a float32 on the device, the rate can change between replays too.  ``step`` takes a
-    grad_scale (one float32 on the device, as from clipping by the norm).  Files of
-    torch.optim.AdamW load where bits is 32; masters (then begun from the parameters) and
-    capturable=True stay as they are.
-    Groups and files that ask for a step of another kind (maximize, amsgrad, differentiable, a
-    weight decay that is not decoupled) or lack the group's states raise ValueError."""
+    ``step`` goes on counting at each replay (the group then counts as one, but for parameters
+    that were behind the others in a file); with an lr that is a float32 on the device, the rate
+    can change between replays too.  ``step`` takes a grad_scale (one float32 on the device, as
+    from clipping by the norm).  Files of torch.optim.AdamW load where bits is 32; masters (then
+    begun from the parameters) and capturable=True stay as they are.  Groups and files that ask
+    for a step of another kind (maximize, amsgrad, differentiable, a weight decay that is not
+    decoupled) or lack the group's states raise ValueError."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 1e-2, *, bits: int = 32, masters: bool = False,
@@ -283,14 +283,13 @@ class AdamW(torch.optim.Optimizer):
             else:
                 s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
                 s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
-            # one count for the group where it is on the device
             s["step"] = self._count(group, p.device) if group["capturable"] else 0
         if "master" not in s and _has_master(group, p):   # (a file may have states without)
             s["master"] = p.detach().to(_F32)
 
-    def _count(self, group, device):
+    def _count(self, group, device):   # on the device: one there for the group
         for p in group["params"]:
-            if "step" in self.state.get(p, {}):
+            if p.device == device and "step" in self.state.get(p, {}):
                 return self.state[p]["step"]
         return torch.zeros((), dtype=torch.int64, device=device)
 
@@ -321,18 +320,19 @@ class AdamW(torch.optim.Optimizer):
             for p in group["params"]:
                 if p.grad is not None:
                     self._init(p, group)
-                    kinds.setdefault((p.dtype, p.device), []).append(p)
+                    count = id(self.state[p]["step"]) if group["capturable"] else None
+                    kinds.setdefault((p.dtype, p.device, count), []).append(p)
             how = dict(lr=group["lr"], betas=group["betas"], eps=group["eps"],
                        weight_decay=group["weight_decay"], grad_scale=grad_scale)
-            counted = False
+            counted = set()
             for kind, params in kinds.items():
                 plan = self._plan((i, kind), group, params)
                 grads = [p.grad for p in params]
                 if group["capturable"]:
                     count = self.state[params[0]]["step"]
-                    if not counted:
+                    if id(count) not in counted:
                         count += 1
-                        counted = True
+                        counted.add(id(count))
                     plan.step(grads, step=count, **how)
                     continue
                 for p in params:
@@ -359,13 +359,13 @@ class AdamW(torch.optim.Optimizer):
         # the states in their own types (the base class gives them the parameters'): all floats are
         # float32, moments that torch kept in bf16 too
         for group, saved in zip(self.param_groups, state_dict["param_groups"]):
-            count = {}   # one count for the group where it is on the device
+            count = {}   # on the device: one there for all parameters of the same count
             for p, k in zip(group["params"], saved["params"]):
                 for name, x in state_dict["state"].get(k, {}).items():
                     if name == "step":
                         x = int(x)
                         if group["capturable"]:
-                            x = count.setdefault(p.device, torch.tensor(x, device=p.device))
+                            x = count.setdefault((p.device, x), torch.tensor(x, device=p.device))
                     elif isinstance(x, torch.Tensor):
                         x = x.detach().to(p.device, _F32 if x.is_floating_point() else x.dtype, copy=True)
                     self.state[p][name] = x

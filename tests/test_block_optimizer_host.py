@@ -220,3 +220,72 @@ def test_moments_of_another_width(calls, masters):
     again = optim.AdamW([p, q], bits=8)
     again.load_state_dict(eight.state_dict())
     assert {k: x.dtype for k, x in again.state[p].items() if k != "step"} == optim._states(8)
+
+
+# --------------------------------------------------------- counts on the device
+def two_devices():
+    """Parameters on two devices (the second without memory, which is enough for a count)."""
+    p, q = params(3, 4)
+    r = torch.nn.Parameter(torch.zeros(5, device="meta"))
+    r.grad = torch.zeros(5, device="meta")
+    return [p, r, q]
+
+
+def raised(count, before):
+    return count._version - before
+
+
+def test_a_count_for_each_device(calls):
+    """A capturable group over two devices has a count on each, and every step raises both,
+    from the start and after loading."""
+    ps = two_devices()
+    opt = optim.AdamW(ps, capturable=True)
+    opt.step()
+    for which in range(2):
+        counts = [opt.state[p]["step"] for p in ps]
+        assert [c.device.type for c in counts] == ["cpu", "meta", "cpu"]
+        assert counts[0] is counts[2]
+        for c in calls:
+            assert c[2]["step"].device == c[0][0].device
+        before = [c._version for c in counts]
+        opt.step()
+        assert [raised(c, b) for c, b in zip(counts, before)] == [1, 1, 1]
+        assert int(counts[0]) == 2 + 3 * which
+        if which == 0:
+            opt.step()
+            file = {"state": {i: {k: (x.new_zeros(x.shape, device="cpu") if k != "step" else 3)
+                                  for k, x in opt.state[p].items()} for i, p in enumerate(ps)},
+                    "param_groups": opt.state_dict()["param_groups"]}
+            opt = optim.AdamW(ps, capturable=True)
+            opt.load_state_dict(file)
+            opt.step()
+            calls.clear()
+
+
+def test_counts_of_a_file_that_differ(calls):
+    """Parameters that are behind in a file stay behind on the device."""
+    p, q, r = params(3, 4, 5)
+    late, q.grad = q.grad, None
+    old = torch.optim.AdamW([p, q, r])
+    old.step()
+    old.step()
+    q.grad = late
+    old.step()
+    opt = optim.AdamW([p, q, r], capturable=True)
+    opt.load_state_dict(old.state_dict())
+    assert [int(opt.state[x]["step"]) for x in (p, q, r)] == [3, 1, 3]
+    opt.step()
+    opt.step()
+    assert [int(opt.state[x]["step"]) for x in (p, q, r)] == [5, 3, 5]
+    assert opt.state[p]["step"] is opt.state[r]["step"]
+    assert sorted((len(c[0]), int(c[2]["step"])) for c in calls[-2:]) == [(1, 3), (2, 5)]
+
+
+def test_one_count_for_types(calls):
+    """Types of one group share the count, which a step raises once."""
+    ps = params(3, 4) + params(5, dtype=BF)
+    opt = optim.AdamW(ps, capturable=True)
+    for n in (1, 2):
+        opt.step()
+        assert len({id(opt.state[p]["step"]) for p in ps}) == 1 and int(opt.state[ps[0]]["step"]) == n
+    assert len(calls) == 4
