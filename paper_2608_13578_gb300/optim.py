@@ -217,6 +217,16 @@ def _states(bits):
     return {"exp_avg": _F32, "exp_avg_sq": _F32}
 
 
+def _capturing(p):
+    """Whether what runs on p's device now goes into a graph."""
+    if not p.is_cuda:
+        return False
+    if p.get_device() != _current_device():
+        with torch.cuda.device(p.device):
+            return torch.cuda.is_current_stream_capturing()
+    return torch.cuda.is_current_stream_capturing()
+
+
 def _has_master(group, p):
     return group["masters"] and p.dtype != _F32
 
@@ -243,7 +253,8 @@ class AdamW(torch.optim.Optimizer):
     bits: 32, or 8 for states in 8 bits; masters: float32 values of bf16 parameters are kept
     and updated.  capturable: the count of steps is kept on the device, so that a captured
     ``step`` goes on counting at each replay (the group then counts as one, but for parameters
-    that were behind the others in a file); with an lr that is a float32 on the device, the rate
+    that were behind the others in a file; a parameter's first step, which begins its states, is
+    to be outside of the capture, and without capturable a capture is refused); with an lr that is a float32 on the device, the rate
     can change between replays too.  ``step`` takes a grad_scale (one float32 on the device, as
     from clipping by the norm).  Files of torch.optim.AdamW load where bits is 32; masters (then
     begun from the parameters) and capturable=True stay as they are.  Groups and files that ask
@@ -272,6 +283,10 @@ class AdamW(torch.optim.Optimizer):
 
     def _init(self, p, group):
         s = self.state[p]
+        missing = "master" not in s and _has_master(group, p)   # (a file may have states without)
+        if (missing or not s) and _capturing(p):
+            raise RuntimeError("a parameter's first step begins its states, and would at each replay: "
+                               "take it before the capture")
         if not s:
             flat = torch.preserve_format if p.is_contiguous() else torch.contiguous_format
             if group["bits"] == 8:
@@ -284,7 +299,7 @@ class AdamW(torch.optim.Optimizer):
                 s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
                 s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
             s["step"] = self._count(group, p.device) if group["capturable"] else 0
-        if "master" not in s and _has_master(group, p):   # (a file may have states without)
+        if missing:
             s["master"] = p.detach().to(_F32)
 
     def _count(self, group, device):   # on the device: one there for the group
@@ -319,6 +334,9 @@ class AdamW(torch.optim.Optimizer):
             kinds = {}
             for p in group["params"]:
                 if p.grad is not None:
+                    if not kinds and not group["capturable"] and _capturing(p):
+                        raise RuntimeError("a captured step would repeat its count: capturable=True keeps "
+                                           "the count on the device")
                     self._init(p, group)
                     count = id(self.state[p]["step"]) if group["capturable"] else None
                     kinds.setdefault((p.dtype, p.device, count), []).append(p)

@@ -289,3 +289,35 @@ def test_one_count_for_types(calls):
         opt.step()
         assert len({id(opt.state[p]["step"]) for p in ps}) == 1 and int(opt.state[ps[0]]["step"]) == n
     assert len(calls) == 4
+
+
+# ------------------------------------------------------------- what a capture holds
+def test_steps_that_a_capture_would_freeze(calls, monkeypatch):
+    """Under capture a count on the host, and states or masters that begin there (and would
+    begin anew at each replay), are refused; a capturable step after a first one is not."""
+    capturing = [False]
+    monkeypatch.setattr(optim, "_capturing", lambda p: capturing[0])
+    p, q = params(3, 4, dtype=BF)
+    opt = optim.AdamW([p])
+    opt.step()
+    capturing[0] = True
+    with pytest.raises(RuntimeError, match="capturable"):
+        opt.step()
+    assert opt.state[p]["step"] == 1
+    opt = optim.AdamW([p, q], capturable=True, masters=True)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        opt.step()
+    late, q.grad = q.grad, None
+    capturing[0] = False
+    opt.step()
+    capturing[0] = True
+    opt.step()
+    assert int(opt.state[p]["step"]) == 2
+    q.grad = late
+    with pytest.raises(RuntimeError, match="before the capture"):
+        opt.step()
+    assert int(opt.state[p]["step"]) == 2 and not opt.state.get(q)
+    del opt.state[p]["master"]
+    q.grad = None
+    with pytest.raises(RuntimeError, match="before the capture"):
+        opt.step()
