@@ -253,13 +253,15 @@ class AdamW(torch.optim.Optimizer):
     bits: 32, or 8 for states in 8 bits; masters: float32 values of bf16 parameters are kept
     and updated.  capturable: the count of steps is kept on the device, so that a captured
     ``step`` goes on counting at each replay (the group then counts as one, but for parameters
-    that were behind the others in a file; a parameter's first step, which begins its states, is
-    to be outside of the capture, and without capturable a capture is refused); with an lr that is a float32 on the device, the rate
-    can change between replays too.  ``step`` takes a grad_scale (one float32 on the device, as
-    from clipping by the norm).  Files of torch.optim.AdamW load where bits is 32; masters (then
-    begun from the parameters) and capturable=True stay as they are.  Groups and files that ask
-    for a step of another kind (maximize, amsgrad, differentiable, a weight decay that is not
-    decoupled) or lack the group's states raise ValueError."""
+    that were behind the others in a file); with an lr that is a float32 on the device, the rate
+    can change between replays too.  A parameter's first step, which begins its states, is to be
+    outside of the capture; captures that hold one, or are not capturable, raise RuntimeError.
+    ``step`` takes a grad_scale (one float32 on the device, as from clipping by the norm).
+
+    Files of torch.optim.AdamW load where bits is 32; masters (then begun from the parameters) and
+    capturable=True stay as they are.  Groups and files that ask for a step of another kind
+    (maximize, amsgrad, differentiable, a weight decay that is not decoupled) or lack the group's
+    states raise ValueError."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 1e-2, *, bits: int = 32, masters: bool = False,
@@ -348,19 +350,25 @@ class AdamW(torch.optim.Optimizer):
                 grads = [p.grad for p in params]
                 if group["capturable"]:
                     count = self.state[params[0]]["step"]
-                    if id(count) not in counted:
+                    first = id(count) not in counted
+                    if first:
                         count += 1
-                        counted.add(id(count))
-                    plan.step(grads, step=count, **how)
+                    try:
+                        plan.step(grads, step=count, **how)
+                    except Exception:   # a refused step does not count
+                        if first:
+                            count -= 1
+                        raise
+                    counted.add(id(count))
                     continue
-                for p in params:
-                    self.state[p]["step"] += 1
-                steps = [self.state[p]["step"] for p in params]
-                if steps.count(steps[0]) == len(steps):
-                    plan.step(grads, step=steps[0], **how)
-                else:   # parameters that had no gradient in some steps are behind
-                    for n in sorted(set(steps)):
-                        plan.step([g if k == n else None for g, k in zip(grads, steps)], step=n, **how)
+                steps = [self.state[p]["step"] + 1 for p in params]
+                each = sorted(set(steps))
+                for n in each:   # parameters that had no gradient in some steps are behind
+                    plan.step(grads if len(each) == 1 else
+                              [g if k == n else None for g, k in zip(grads, steps)], step=n, **how)
+                    for p, k in zip(params, steps):
+                        if k == n:
+                            self.state[p]["step"] = n
         return loss
 
     @torch.no_grad()

@@ -321,3 +321,38 @@ def test_steps_that_a_capture_would_freeze(calls, monkeypatch):
     q.grad = None
     with pytest.raises(RuntimeError, match="before the capture"):
         opt.step()
+
+
+# ----------------------------------------------------------------- refused steps
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_refused_step_does_not_count(calls, monkeypatch, capturable):
+    p, q, r = params(3, 4) + params(5, dtype=BF)
+    late, q.grad = q.grad, None
+    opt = optim.AdamW([p, q, r], capturable=capturable)
+    opt.step()
+    q.grad = late
+    opt.step()          # q is a step behind where the count is on the host
+
+    def counts():
+        return [int(opt.state[x]["step"]) for x in (p, q, r)]
+    before = counts()
+    assert before == ([2, 2, 2] if capturable else [2, 1, 2])
+    plan = type(next(iter(opt._plans.values()))[1])
+
+    def refuse(self, grads, **how):
+        raise ValueError("refused")
+    with monkeypatch.context() as m:
+        m.setattr(plan, "step", refuse)
+        with pytest.raises(ValueError, match="refused"):
+            opt.step()
+    assert counts() == before
+    opt.step()
+    assert counts() == [n + 1 for n in before]
+    # what was stepped before the refusal counts: p and q, but not r, where counts are apart
+    with monkeypatch.context() as m:
+        step = plan.step
+        m.setattr(plan, "step", lambda self, grads, **how: (
+            refuse if self.params[0].dtype == BF else step)(self, grads, **how))
+        with pytest.raises(ValueError, match="refused"):
+            opt.step()
+    assert counts() == ([4, 4, 4] if capturable else [4, 3, 3])
