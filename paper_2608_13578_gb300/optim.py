@@ -164,7 +164,7 @@ class AdamWPlan:
                                 betas[1], eps, weight_decay, grad_scale, step_ptr, lr_ptr)
         C.check(C.LIB.bcmt_adamw_step(ctypes.byref(p), self._address, _raw_stream(dev.index)))
         # written through their addresses, which autograd cannot see
-        increment_version(self._all)
+        increment_version([t for x in self._lists for t, g in zip(x, at) if g] if holes else self._all)
 
 
 def _one(t, name, dtype, dev):

@@ -311,3 +311,24 @@ def test_reorder_arguments(host):
     for tensors, out in (([t], [t]), ([t, t.clone()], [t.clone(), t]), ([t, t], [o[:2], o[1:3]])):
         assert code(b.C, b.beam_reorder, tensors, p, out) == b.C.BCMT_ERR_ARG
     assert b.beam_reorder([], p) == []
+
+
+def test_versions_of_what_is_written(host, monkeypatch):
+    """A step moves the version counters of the tensors that it writes, not of those whose
+    gradient is None."""
+    optim = host[2]
+    monkeypatch.setattr(optim.C.LIB, "bcmt_adamw_step", lambda *a: 0)
+    f, i8, u8 = torch.zeros, torch.int8, torch.uint8
+    sets = [dict(params=[f(300), f(4), f(5)], m=[f(300), f(4), f(5)], v=[f(300), f(4), f(5)]),
+            dict(params=[f(n).bfloat16() for n in (300, 4)], m=[f(300, dtype=i8), f(4, dtype=i8)],
+                 v=[f(300, dtype=u8), f(4, dtype=u8)], m_scales=[f(2), f(1)], v_scales=[f(2), f(1)],
+                 masters=[f(300), f(4)])]
+    for lists in sets:
+        plan = optim.AdamWPlan(**lists)
+        grads = [torch.ones_like(p) for p in lists["params"]]
+        for missing in (None, 1, 0):
+            given = [None if i == missing else g for i, g in enumerate(grads)]
+            before = {k: [t._version for t in ts] for k, ts in lists.items()}
+            plan.step(given, lr=1e-3, step=1)
+            for k, ts in lists.items():
+                assert [t._version - b for t, b in zip(ts, before[k])] == [int(g is not None) for g in given], k
