@@ -302,8 +302,9 @@ def make_optimizer(model: GPT, lr: float = 3e-4, bits: int = 0, masters: bool = 
 
 def _clip_scale(params, clip: float):
     """clip / the gradients' norm where that is below 1, else 1: one float32 on the device."""
-    each = torch._foreach_norm([p.grad for p in params if p.grad is not None])
-    norm = torch.linalg.vector_norm(torch.stack([n.float() for n in each]))
+    # (float32 norms: those of bf16 gradients would be rounded to bf16, 8 bits)
+    each = torch._foreach_norm([p.grad for p in params if p.grad is not None], 2, torch.float32)
+    norm = torch.linalg.vector_norm(torch.stack(each))
     return (clip / (norm + 1e-6)).clamp(max=1.0)
 
 

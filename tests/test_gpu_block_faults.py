@@ -1,10 +1,10 @@
-"""Calls that a captured graph would repeat wrongly."""
+"""The optimizer under capture and the norm that clips its gradients."""
 
 import pytest
 import torch
 
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+BF, F = torch.bfloat16, torch.float32
 
 
 # ---------------------------------------------------------------- the optimizer
@@ -31,3 +31,16 @@ def test_captures_that_would_not_count_on(cuda_ok, how, say):
     if how:
         with torch.cuda.graph(torch.cuda.CUDAGraph()):
             opt.step()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_the_norm_that_clips(cuda_ok, dtype):
+    """As on the CPU: a sum of 4121 squares in fp32 is off by at most 4121 * 2^-24, its root by half of
+    that; the few other operations are within the rest of 2^-12."""
+    from paper_2608_13578_gb300 import gpt
+    p, q = (torch.nn.Parameter(torch.zeros(n, dtype=d, device="cuda")) for n, d in ((4121, dtype), (50, F)))
+    p.grad, q.grad = torch.full_like(p, 0.01), torch.full_like(q, 1e-3)
+    norm = float(p.grad.double().square().sum() + q.grad.double().square().sum()) ** 0.5
+    scale = gpt._clip_scale([p, q], 0.5)
+    assert scale.dtype == F and scale.is_cuda
+    assert abs(float(scale) * (norm + 1e-6) / 0.5 - 1.0) <= 2.0 ** -12
