@@ -22,6 +22,7 @@ from .lm_ops import (_address, _buffer, _check, _current_device, _dense, _device
                      _on_its_device, _raw_stream)
 
 KINDS = ("layer", "rms")
+_ALL = (True,) * 7   # gradients
 
 
 @functools.lru_cache(maxsize=4096)
@@ -112,17 +113,18 @@ def residual_norm_forward(branch, x, weight, bias=None, *, post_weight=None, pos
 
 def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=None,
                            post_bias=None, gate=None, residual_scale: float = 1.0,
-                           kind: str = "layer", eps: float = 1e-5):
+                           kind: str = "layer", eps: float = 1e-5, wanted=_ALL):
     """(dbranch, dx, dweight, dbias, dpost_weight, dpost_bias, dgate) from the forward's
     arguments, its h and the gradients dh (None: zero) and dn of its results; None for what
     was not given.  dbranch and dx are one tensor where they are equal (no post norm, no gate,
-    residual_scale 1)."""
+    residual_scale 1).  wanted: which of the seven to compute; the others are None, but for
+    dbranch, which comes anyway."""
     # (dh may be None: the device is that of branch)
     if isinstance(branch, torch.Tensor) and branch.is_cuda and branch.get_device() != _current_device():
         with torch.cuda.device(branch.device):
             return residual_norm_backward(
                 dh, dn, branch, h, weight, bias, post_weight=post_weight, post_bias=post_bias,
-                gate=gate, residual_scale=residual_scale, kind=kind, eps=eps)
+                gate=gate, residual_scale=residual_scale, kind=kind, eps=eps, wanted=wanted)
     dev, shape, dt, wt, gates = _arguments(branch, weight, bias, post_weight, post_bias, gate, kind)
     dtype = branch.dtype
     _same(dn, "dn", shape, dtype, dev)
@@ -139,20 +141,21 @@ def residual_norm_backward(dh, dn, branch, h, weight, bias=None, *, post_weight=
     one = post_weight is None and gate is None and alpha == 1.0
     gate = _dense(gate)
     like = torch.empty_like
+    _, want_x, want_w, want_b, want_pw, want_pb, want_gate = wanted
     dbranch = like(branch)
-    dx = None if one else like(branch)
-    dw = like(weight)
-    db = None if bias is None else like(weight)
-    dpw = None if post_weight is None else like(weight)
-    dpb = None if post_bias is None else like(weight)
-    dgate = None if gate is None else like(gate)
+    dx = None if one or not want_x else like(branch)
+    dw = like(weight) if want_w else None
+    db = None if bias is None or not want_b else like(weight)
+    dpw = None if post_weight is None or not want_pw else like(weight)
+    dpb = None if post_bias is None or not want_pb else like(weight)
+    dgate = None if gate is None or not want_gate else like(gate)
     ws = _buffer(max(256, nbytes), dev)
     C.check(C.LIB.bcmt_residual_norm_backward(
         p, _address(dh), dn.data_ptr(), branch.data_ptr(), h.data_ptr(), weight.data_ptr(),
         _address(post_weight), _address(post_bias), _address(gate), dbranch.data_ptr(),
-        _address(dx), dw.data_ptr(), _address(db), _address(dpw), _address(dpb), _address(dgate),
+        _address(dx), _address(dw), _address(db), _address(dpw), _address(dpb), _address(dgate),
         ws.data_ptr(), _raw_stream(dev.index)))
-    return dbranch, dbranch if one else dx, dw, db, dpw, dpb, dgate
+    return dbranch, dbranch if one and want_x else dx, dw, db, dpw, dpb, dgate
 
 
 class ResidualNorm(torch.autograd.Function):
@@ -179,7 +182,8 @@ class ResidualNorm(torch.autograd.Function):
             dn = torch.zeros_like(h)
         return residual_norm_backward(
             dh, dn, branch, h, weight, bias, post_weight=post_weight, post_bias=post_bias,
-            gate=gate, residual_scale=alpha, kind=kind, eps=eps) + (None,) * 3
+            gate=gate, residual_scale=alpha, kind=kind, eps=eps,
+            wanted=ctx.needs_input_grad[:7]) + (None,) * 3
 
 
 def residual_norm(branch, x, weight, bias=None, *, post_weight=None, post_bias=None, gate=None,

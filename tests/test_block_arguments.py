@@ -332,3 +332,36 @@ def test_versions_of_what_is_written(host, monkeypatch):
             plan.step(given, lr=1e-3, step=1)
             for k, ts in lists.items():
                 assert [t._version - b for t, b in zip(ts, before[k])] == [int(g is not None) for g in given], k
+
+
+@pytest.mark.parametrize("frozen", [(), ("x",), ("branch", "x"), ("weight", "bias", "post_weight", "post_bias"),
+                                    ("gate",), ("branch", "weight", "post_bias", "gate"),
+                                    ("x", "weight", "bias", "post_weight", "post_bias", "gate")], ids=str)
+@pytest.mark.parametrize("plain", [False, True])
+def test_gradients_that_nobody_wants(host, monkeypatch, frozen, plain):
+    """A backward pass asks the library for the gradients of what requires them, and for dbranch,
+    which it always gives."""
+    norms = host[1]
+    seen = []
+    monkeypatch.setattr(norms.C.LIB, "bcmt_residual_norm_forward", lambda *a: 0)
+    monkeypatch.setattr(norms.C.LIB, "bcmt_residual_norm_backward", lambda *a: seen.append(a) or 0)
+    monkeypatch.setattr(norms, "_plan", lambda *a: (None, 0))
+    names = ["branch", "x", "weight", "bias", "post_weight", "post_bias", "gate"]
+    given = names[:4] if plain else names       # plain: dbranch and dx are one tensor
+    t = {k: torch.ones(*((2, 3, 8) if k in ("branch", "x") else (8,))) for k in given}
+    for k in set(given) - set(frozen):
+        t[k].requires_grad_()
+    h, n = norms.residual_norm(t["branch"], t["x"], t["weight"], t["bias"],
+                               **{k: t[k] for k in given[4:]})
+    (h.sum() + n.sum()).backward()
+    (a,) = seen
+    outputs = dict(zip(["branch", "x", "weight", "bias", "post_weight", "post_bias", "gate"], a[9:16]))
+    for k in names:
+        wanted = k in given and k not in frozen
+        assert k not in given or (t[k].grad is not None) == wanted, k
+        if k == "branch":
+            assert outputs[k]
+        elif k == "x" and plain:
+            assert outputs[k] is None
+        else:
+            assert bool(outputs[k]) == wanted, k

@@ -1,4 +1,5 @@
-"""The optimizer under capture and the norm that clips its gradients."""
+"""The optimizer under capture, the norm that clips its gradients, and norms whose gradients are not all
+wanted."""
 
 import pytest
 import torch
@@ -44,3 +45,50 @@ def test_the_norm_that_clips(cuda_ok, dtype):
     scale = gpt._clip_scale([p, q], 0.5)
     assert scale.dtype == F and scale.is_cuda
     assert abs(float(scale) * (norm + 1e-6) / 0.5 - 1.0) <= 2.0 ** -12
+
+
+# -------------------------------------------------------------------- norms
+NAMES = ["branch", "x", "weight", "bias", "post_weight", "post_bias", "gate"]
+
+
+def arguments(shape, dtype, post, gate, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    D = shape[-1]
+    sizes = dict(branch=shape, x=shape, weight=(D,), bias=(D,), post_weight=(D,) if post else None,
+                 post_bias=(D,) if post else None, gate=gate)
+    return {k: None if s is None else torch.randn(s, generator=g).to(dtype).cuda() for k, s in sizes.items()}
+
+
+def both(norms, t, wanted=None):
+    """Gradients of every argument (None where there is none) of sums over h and n."""
+    t = {k: None if v is None else v.clone().requires_grad_(wanted is None or wanted[i])
+         for i, (k, v) in enumerate(t.items())}
+    h, n = norms.residual_norm(t["branch"], t["x"], t["weight"], t["bias"], post_weight=t["post_weight"],
+                               post_bias=t["post_bias"], gate=t["gate"], residual_scale=0.7)
+    at = torch.linspace(-1, 1, h.numel(), device="cuda", dtype=h.dtype).view(h.shape)
+    ((h * at).sum() + (n * at.flip(0)).sum()).backward()
+    return [None if v is None else v.grad for v in t.values()]
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("D", [40, 264, 1001, 4096])
+def test_gradients_that_are_wanted_are_the_same(cuda_ok, D, post, dtype):
+    """Each gradient alone, and all but each one, bit for bit as all together; gates of all rows,
+    of groups (with several segments, and several groups a worker), of every row, and none."""
+    from paper_2608_13578_gb300 import bcmt as C, norms
+    for rows, gates in ((2, 0), (700, 1), (700, 2), (700, 350), (330, 330)):
+        shape = (gates, rows // gates, D) if gates else (rows, D)
+        t = arguments(shape, dtype, post, (gates, 1, D) if gates else None)
+        every = both(norms, t)
+        for i in range(7):
+            for only in (True, False):
+                wanted = [(k == i) == only for k in range(7)]
+                if not any(w and v is not None for w, v in zip(wanted, t.values())):
+                    continue
+                for k, (a, b) in enumerate(zip(both(norms, t, wanted), every)):
+                    if wanted[k] and b is not None:
+                        assert torch.equal(a, b), (NAMES[k], wanted, gates)
+                    else:
+                        assert a is None
+    C.bcmt_device_status()
