@@ -405,8 +405,12 @@ bcmt_status bcmt_adamw_values(const void* m_codes, const float* m_scale, const v
  * candidates, equal ones by the lower k V + v, become the beams: their scores,
  * parents (k), tokens (v) and whether they have ended (the parent had, or v is
  * eos).  Logits of -inf are tokens ruled out and scores of -inf beams that are not
- * there: their candidates, -inf too, come last, in the order of k V + v.  What
- * decides is held in 64 bits.  A beam with a logit or score that is NaN or +inf
+ * there: their candidates, -inf too, come last, in the order of k V + v.
+ * Candidates of one beam go by their logits.  Those of different beams are compared
+ * in 64 bits, with log-sums of which only the largest terms (K of every 4096 at least)
+ * are added with more than 32 bits; the others are fp32 exponentials and sums, so that a
+ * log-sum is off by at most (3 ln V + 25) 2^-24, and candidates of different beams that
+ * are nearer than twice that may change places.  A beam with a logit or score that is NaN or +inf
  * counts as not there and is reported as BCMT_ERR_ARG by the next
  * bcmt_device_status (BCMT_FLAG_CHECK: by the call); the logits of beams that have
  * ended, or have a score of -inf, are not read.

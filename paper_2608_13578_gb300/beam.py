@@ -31,7 +31,8 @@ def _plan(N, K, V, dt, eos, ld):
 def beam_select(logits, scores, finished=None, eos: Optional[int] = None):
     """(scores, parents, tokens, finished) of the K best continuations of each search, the
     best first: candidates ``scores[n, k] + log_softmax(logits[n, k])[v]``, equal ones in the
-    order of k V + v.
+    order of k V + v.  Candidates of different beams that are nearer than (6 ln V + 50) 2^-24
+    may change places: most of each row's sum of exponentials is taken in fp32.
 
     logits [N, K, V] (bf16 or fp32, 1 <= K <= 32; rows of one stride, as in a slice of the last
     tokens, are read in place; -inf: ruled out), scores [N, K] fp32 (-inf: no beam there, as

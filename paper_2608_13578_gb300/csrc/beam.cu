@@ -7,9 +7,13 @@
 //
 // Selection takes two launches.  A CTA of the first reads one chunk of one row into
 // registers and leaves its largest K entries, its maximum and its sum of exponentials;
-// the second merges the chunks of a search.  What decides between beams is held in 64
-// bits: a sum's few large terms (those selected) are added as exponentials of more than 32
-// bits, the others in fp32, and scores are rounded to fp32 at the end.
+// the second merges the chunks of a search.  Scores are compared in 64 bits and rounded to
+// fp32 at the end.  Of a row's sum only the few large terms (those selected) are added as
+// exponentials of more than 32 bits; the others are fp32: one at a distance d below the
+// maximum is off by 3 d 2^-24 of itself by its argument (the difference, the factor log2 e and
+// their product are rounded once each), 2^-22 by ex2.approx and 20 * 2^-24 by additions.  A
+// row's terms are at ln V at most in their weighted mean, so the logarithm is off by at most
+// (3 ln V + 25) 2^-24; 64-bit exponentials for all would take the chip's slow units.
 #include <math.h>
 
 #include <algorithm>

@@ -1,5 +1,7 @@
-"""The optimizer under capture, the norm that clips its gradients, and norms whose gradients are not all
-wanted."""
+"""The optimizer under capture, the norm that clips its gradients, norms whose gradients are not all
+wanted, and beam search's sums over a large background."""
+
+import math
 
 import pytest
 import torch
@@ -92,3 +94,49 @@ def test_gradients_that_are_wanted_are_the_same(cuda_ok, D, post, dtype):
                     else:
                         assert a is None
     C.bcmt_device_status()
+
+
+# -------------------------------------------------------------- beam search
+V = 32000
+
+
+def rows_of(background, dtype=F):
+    """Logits [1, beams, V]: a best token of 0, eight tokens in every 4096 above the background,
+    which the lists take, and the background itself, which they do not."""
+    x = torch.tensor(background)[:, None].expand(-1, V).clone()
+    x[:, ::512] += 1.0
+    x[:, 77] = 0.0
+    return x[None].to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("d", [0.71875, 3.3, 6.71875, 9.828125, 11.3, 15.0])
+def test_sums_over_a_large_background(cuda_ok, d, dtype):
+    """The log-sum is off by the background's share of it times (3 d + 25) 2^-24 (its argument's three
+    roundings, 2^-22 of ex2.approx, 20 additions), the score by a rounding of its own."""
+    from paper_2608_13578_gb300 import beam
+    x = rows_of([-d, -d - 0.5], dtype)
+    got = beam.beam_select(x, torch.zeros(1, 2, device="cuda"))
+    lp = x.double().log_softmax(-1)[0]
+    for score, parent, token in zip(*[t[0].tolist() for t in got[:3]]):
+        z = x[0, parent].double()
+        share = float((z == z.min()).sum() * z.min().exp() / z.exp().sum())
+        want = float(lp[parent, token])
+        bound = share * (3 * float(z.max() - z.min()) + 25) * 2.0 ** -24 + abs(want) * 2.0 ** -24
+        assert abs(score - want) <= bound, (score, want, bound)
+
+
+@pytest.mark.parametrize("d", [6.71875, 9.828125])
+def test_beams_that_differ_by_their_backgrounds(cuda_ok, d):
+    """Best tokens of equal logits, sums whose backgrounds differ by 2^-14: the difference of the
+    scores is more than twice the log-sums' bound, and decides."""
+    from paper_2608_13578_gb300 import beam
+    bound = 2 * (3 * math.log(V) + 25) * 2.0 ** -24
+    for low in (0, 1):
+        x = rows_of([-d - (k == low) * 2.0 ** -14 for k in (0, 1)])
+        lp = x.double().log_softmax(-1)[0, :, 77]
+        assert float(lp[low] - lp[1 - low]) > bound
+        got = beam.beam_select(x, torch.zeros(1, 2, device="cuda"))
+        assert got[1].tolist() == [[low, 1 - low]] and got[2].tolist() == [[77, 77]]
+        got = beam.beam_select(x.repeat(1, 2, 1)[:, 1:3].contiguous(), torch.zeros(1, 2, device="cuda"))
+        assert got[1].tolist() == [[1 - low, low]]
