@@ -1,10 +1,13 @@
 """The optimizer under capture, the norm that clips its gradients, norms whose gradients are not all
-wanted, and beam search's sums over a large background."""
+wanted or whose result takes the place of an input, and beam search's sums over a large background."""
 
 import math
 
 import pytest
 import torch
+
+from tests import block_reference as R
+from tests import test_gpu_norms as T
 
 pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
@@ -94,6 +97,46 @@ def test_gradients_that_are_wanted_are_the_same(cuda_ok, D, post, dtype):
                     else:
                         assert a is None
     C.bcmt_device_status()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("over", ["x", "branch"])
+@pytest.mark.parametrize("rows,D,gates", [(14600, 257, 0), (7308, 1001, 7), (3656, 2047, 3656), (1832, 4099, 1),
+                                          (700, 768, 7)])
+def test_result_over_an_input_of_many_rows(cuda_ok, rows, D, gates, over, dtype):
+    """h over the residual or the branch where rows come in 16-byte pieces that neighbours share, and
+    are requested ahead."""
+    from paper_2608_13578_gb300 import bcmt as C, norms
+    shape = (gates, rows // gates, D) if gates else (rows, D)
+    t = arguments(shape, dtype, True, (gates, 1, D) if gates else None)
+    h, n = norms.residual_norm_forward(t["branch"], t["x"], t["weight"], t["bias"], post_weight=t["post_weight"],
+                                       post_bias=t["post_bias"], gate=t["gate"], residual_scale=0.5)
+    dt = C.BCMT_BF16 if dtype == BF else C.BCMT_F32
+    p = C.bcmt_norm_params(rows, D, dt, dt, 0, gates, 0, 0.5, 1e-5)
+    for _ in range(3):
+        u, m = {k: None if v is None else v.clone() for k, v in t.items()}, torch.empty_like(n)
+        C.bcmt_residual_norm_forward(p, u["branch"], u["x"], u["weight"], u["bias"], u["post_weight"],
+                                     u["post_bias"], u["gate"], u[over], m, torch.cuda.current_stream().cuda_stream)
+        assert torch.equal(u[over], h) and torch.equal(m, n)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("kind,post,gated", [("layer", True, 1), ("rms", True, 8), ("layer", False, 0),
+                                             ("rms", False, None)])
+@pytest.mark.parametrize("rows,D", [(14600, 257), (14600, 511), (11000, 700), (7304, 1001), (4904, 1500),
+                                    (3656, 2047), (1832, 4099), (1224, 6399)])
+def test_forward_of_workers_side_by_side(cuda_ok, dtype, kind, post, gated, rows, D):
+    """Enough rows of odd widths for the ring with as many workers a CTA as fit (four rows for each
+    of 152 CTAs); gated: gates (None: one for every row, 0: without)."""
+    from paper_2608_13578_gb300 import norms
+    gates = rows if gated is None else gated
+    shape = (gates, rows // gates, D) if gates else (rows, D)
+    t, _, _ = T.make(shape, dtype, F, kind, post, (gates, 1, D) if gates else None)
+    h, n = T.forward(norms, t, 0.9, kind)
+    kw = dict(post_weight=t["post_weight"], post_bias=t["post_bias"], gate=t["gate"], kind=kind, alpha=0.9)
+    (rh, rn), (bh, bn) = R.norm_forward(t["branch"], t["x"], t["weight"], t["bias"], **kw)
+    T.close(h, rh, bh, T.ROUNDINGS, "h")
+    T.close(n, rn, bn, T.ROUNDINGS, "n")
 
 
 # -------------------------------------------------------------- beam search
