@@ -139,6 +139,29 @@ def test_forward_of_workers_side_by_side(cuda_ok, dtype, kind, post, gated, rows
     T.close(n, rn, bn, T.ROUNDINGS, "n")
 
 
+def full(D, post):
+    """Rows that fill the backward's CTAs with as many workers as registers allow, and some more."""
+    R = 32 // (8 if D <= 64 else 16 if D <= 128 else 32)
+    one = D <= 512 or (post and D <= 768)      # a warp a row
+    warps = 20 if D <= 256 else 12 if one and D > 512 else 16
+    wide = 1 if one else (D + 511) // 512      # (J = 2 at the widths below)
+    return (warps // (wide * (2 if post else 1))) * 152 * R + 8
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("kind,post,gated", [("layer", True, 1), ("rms", True, 8), ("layer", True, None),
+                                             ("layer", False, 0), ("rms", False, 8)])
+@pytest.mark.parametrize("D", [64, 100, 200, 256, 511, 512, 768, 1001, 1024, 2048])
+def test_backward_of_workers_side_by_side(cuda_ok, D, kind, post, gated, dtype):
+    """As many workers a CTA as fit, with and without a post norm."""
+    from paper_2608_13578_gb300 import norms
+    rows = full(D, post)
+    gates = rows if gated is None else gated
+    shape = (gates, rows // gates, D) if gates else (rows, D)
+    t, dh, dn = T.make(shape, dtype, F, kind, post, (gates, 1, D) if gates else None)
+    T.check(norms, t, dh, dn, 0.9, kind)
+
+
 # -------------------------------------------------------------- beam search
 V = 32000
 
