@@ -146,8 +146,9 @@ __device__ __forceinline__ float warp_merge(float a, float b) {
 // K-th lowest place among the threads' first ones, which are in K threads.  Up to kCoarseK
 // beams the maxima of every eight threads give a threshold that is found in one sort, and
 // lets few more elements through (K = 8: 9 of 4096); where they are too many, the other
-// follows.  Seven barriers a chunk and issue slots (53%) decide: 64 x 8 x 32000 bf16 30 us (5 at
-// the copy's rate; 32 with the fine threshold), 40 x 5 x 50257 fp32 16 us.
+// follows.  What every chunk pays whatever passes its threshold (a sort, a ranking, four
+// barriers) and issue slots (53%) decide: 64 x 8 x 32000 bf16 30 us (5 at the copy's rate; 32 with
+// the fine threshold), 40 x 5 x 50257 fp32 16 us.  Element by element 16 take 36 bytes of spills.
 constexpr int kCoarseK = 16;
 template <class T, int E, bool VEC>
 __global__ void __launch_bounds__(kThreads, E == 16 ? 4 : 5) beam_chunk_kernel(const BeamArgs a, int nchunk) {

@@ -25,7 +25,8 @@ namespace bcmt {
 // Forward: a row belongs to TPR threads, each with J times eight of its columns; the row
 // stays in registers between its loads and its stores.  Up to 1024 columns a row is one
 // warp's, so that its sums need no barrier.  Bytes and the launch decide: 8192 x 512 bf16
-// 7.2 us (5.1 at the copy's rate), 8192 x 4096 59 us (40), 16384 x 768 fp32 36 us (30).  Few
+// 7.2 us (5.1 at the copy's rate), 16384 x 768 fp32 36 us (30); in wide rows a CTA's loads wait for
+// its sums, 8192 x 4096 59 us (40).  Few
 // rows that are no multiples of 16 bytes, or short ones, go element by element (65000 x 201 bf16:
 // 46 us, 16).
 template <class T, int TPR, int J, bool VEC>
@@ -420,7 +421,14 @@ NormPlan norm_plan(long long rows, int D, int es, long long groups, bool post, i
   if (rows < 1) return p;
   p.mode = groups == 0 ? kGateNone : groups == rows ? kGateRows : groups == 1 ? kGateOne : kGateGroups;
   // threads of a row: 8, 16 or one warp of 8 J columns a lane, or the warps that cost least
-  // by a count of instructions (190 a group of eight columns, 180 for the sums)
+  // by a count of instructions (190 a group of eight columns, 180 for the sums; spills and the
+  // type are not in it).  Measured, 403 MB of layer-normed rows with a post norm and 16 gates, us
+  // with J = 2 / 3 / 4 (from 3 on, rows of several warps spill):
+  //   D      768      1024     1280         1536         2048         2560         2816         4096
+  //   bf16   245/143  191/249  267/208/427  229/179/367  200/227/293  287/215/297  271/200/275  224/253/293
+  //   fp32   207/215  211/248  214/231/342  208/223/318  211/233/293  222/271/356  227/263/344  231/273/328
+  // The rule takes the faster side in bf16 but for 2560, where it takes two; in fp32 two are
+  // faster at each, and it takes three at 768, 1280, 1536 and 2816.
   p.tpr = D <= 64 ? 8 : D <= 128 ? 16 : 32;
   p.J = 1;
   const int most = 16 / (post ? 2 : 1);

@@ -33,7 +33,7 @@ namespace bcmt {
 // thread), and issue slots (990 instructions for both roles of a row of 768).  Measured, both
 // kernels of a call: 16384 x 768 bf16 40 us (22.7 at the copy's rate), 16384 x 4096 165 us (121), 4095 x 1001
 // fp32 with a gate per row 31 us (20), 65536 x 64 18 us (7.6), 8192 x 8192 without a post norm
-// 142 us (121).  One role with 8 columns a lane took 57, 211, 106 and 88 us for the first four.
+// 140 us (121), 8192 x 512 14 us (6.3), 16384 x 768 32 us (19).  One role with 8 columns a lane took 57, 211, 106 and 88 us for the first four.
 enum { kRolePre, kRolePost, kRoleAll };
 
 template <class T, int TPR, int J, bool VEC, bool ROWS, int ROLE>
