@@ -283,12 +283,20 @@ class AdamW(torch.optim.Optimizer):
             _options({**self.defaults, **param_group})
         super().add_param_group(param_group)
 
-    def _init(self, p, group):
+    def _init(self, p, group, moved):
+        """What p's state lacks: everything at its first step, a master that a file had none of, and
+        the count where the group has it now (moved: those of this step, by device and value)."""
         s = self.state[p]
-        missing = "master" not in s and _has_master(group, p)   # (a file may have states without)
-        if (missing or not s) and _capturing(p):
+        capturable = bool(group["capturable"])
+        missing = "master" not in s and _has_master(group, p)
+        move = bool(s) and isinstance(s["step"], torch.Tensor) is not capturable
+        if (missing or move or not s) and _capturing(p):
             raise RuntimeError("a parameter's first step begins its states, and would at each replay: "
                                "take it before the capture")
+        if move:
+            n = int(s["step"])
+            s["step"] = n if not capturable else \
+                moved.setdefault((p.device, n), torch.tensor(n, device=p.device))
         if not s:
             flat = torch.preserve_format if p.is_contiguous() else torch.contiguous_format
             if group["bits"] == 8:
@@ -300,18 +308,18 @@ class AdamW(torch.optim.Optimizer):
             else:
                 s["exp_avg"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
                 s["exp_avg_sq"] = torch.zeros_like(p, dtype=_F32, memory_format=flat)
-            s["step"] = self._count(group, p.device) if group["capturable"] else 0
+            s["step"] = self._count(group, p.device) if capturable else 0
         if missing:
             s["master"] = p.detach().to(_F32)
 
     def _count(self, group, device):   # on the device: one there for the group
         for p in group["params"]:
-            if p.device == device and "step" in self.state.get(p, {}):
-                return self.state[p]["step"]
+            count = self.state[p].get("step") if p in self.state and p.device == device else None
+            if isinstance(count, torch.Tensor):
+                return count
         return torch.zeros((), dtype=torch.int64, device=device)
 
-    def _plan(self, key, group, params):
-        states = [self.state[p] for p in params]
+    def _plan(self, key, group, params, states):
         names = list(_states(group["bits"]))
         names += ["master"] if _has_master(group, params[0]) else []
         ids = [id(p) for p in params] + [id(s[k]) for s in states for k in names]
@@ -333,23 +341,32 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for i, group in enumerate(self.param_groups):
-            kinds = {}
+            kinds, moved = {}, {}
+            capturable, masters = bool(group["capturable"]), group["masters"]
             for p in group["params"]:
-                if p.grad is not None:
-                    if not kinds and not group["capturable"] and _capturing(p):
-                        raise RuntimeError("a captured step would repeat its count: capturable=True keeps "
-                                           "the count on the device")
-                    self._init(p, group)
-                    count = id(self.state[p]["step"]) if group["capturable"] else None
-                    kinds.setdefault((p.dtype, p.device, count), []).append(p)
+                if p.grad is None:
+                    continue
+                if not kinds and not capturable and _capturing(p):
+                    raise RuntimeError("a captured step would repeat its count: capturable=True keeps "
+                                       "the count on the device")
+                s = self.state[p]
+                if (not s or isinstance(s["step"], torch.Tensor) is not capturable
+                        or (masters and "master" not in s)):
+                    self._init(p, group, moved)
+                kind = (p.dtype, p.device, id(s["step"]) if capturable else None)
+                if kind not in kinds:
+                    kinds[kind] = [], []
+                params, states = kinds[kind]
+                params.append(p)
+                states.append(s)
             how = dict(lr=group["lr"], betas=group["betas"], eps=group["eps"],
                        weight_decay=group["weight_decay"], grad_scale=grad_scale)
             counted = set()
-            for kind, params in kinds.items():
-                plan = self._plan((i, kind), group, params)
+            for kind, (params, states) in kinds.items():
+                plan = self._plan((i, kind), group, params, states)
                 grads = [p.grad for p in params]
-                if group["capturable"]:
-                    count = self.state[params[0]]["step"]
+                if capturable:
+                    count = states[0]["step"]
                     first = id(count) not in counted
                     if first:
                         count += 1
@@ -361,14 +378,14 @@ class AdamW(torch.optim.Optimizer):
                         raise
                     counted.add(id(count))
                     continue
-                steps = [self.state[p]["step"] + 1 for p in params]
+                steps = [s["step"] + 1 for s in states]
                 each = sorted(set(steps))
                 for n in each:   # parameters that had no gradient in some steps are behind
                     plan.step(grads if len(each) == 1 else
                               [g if k == n else None for g, k in zip(grads, steps)], step=n, **how)
-                    for p, k in zip(params, steps):
+                    for s, k in zip(states, steps):
                         if k == n:
-                            self.state[p]["step"] = n
+                            s["step"] = n
         return loss
 
     @torch.no_grad()

@@ -356,3 +356,29 @@ def test_a_refused_step_does_not_count(calls, monkeypatch, capturable):
         with pytest.raises(ValueError, match="refused"):
             opt.step()
     assert counts() == ([4, 4, 4] if capturable else [4, 3, 3])
+
+
+def test_a_group_that_becomes_capturable(calls, monkeypatch):
+    """capturable set in a group that has been stepped: the counts move to the device, or back, and
+    go on; not within a capture."""
+    p, q, r = params(3, 4) + params(5, dtype=BF)
+    late, q.grad = q.grad, None
+    opt = optim.AdamW([p, q, r])
+    opt.step()
+    q.grad = late
+    opt.step()
+    opt.param_groups[0]["capturable"] = True
+    with monkeypatch.context() as m:
+        m.setattr(optim, "_capturing", lambda p: True)
+        with pytest.raises(RuntimeError, match="before the capture"):
+            opt.step()
+    for n in (3, 4):
+        opt.step()
+        assert [int(opt.state[x]["step"]) for x in (p, q, r)] == [n, n - 1, n]
+        assert opt.state[p]["step"] is opt.state[r]["step"] is not opt.state[q]["step"]
+        assert all(isinstance(c[2]["step"], torch.Tensor) for c in calls[-3:])
+    opt.param_groups[0]["capturable"] = False
+    for n in (5, 6):
+        opt.step()
+        assert [opt.state[x]["step"] for x in (p, q, r)] == [n, n - 1, n]
+        assert sorted(c[2]["step"] for c in calls[-3:]) == [n - 1, n, n]

@@ -39,6 +39,42 @@ def test_captures_that_would_not_count_on(cuda_ok, how, say):
             opt.step()
 
 
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_file_of_bf16_goes_on_with_masters(cuda_ok, capturable):
+    """States of torch's AdamW over bf16 weights, loaded with masters: the steps that follow are those of
+    float32 weights that begin where the bf16 ones are (tolerance as in test_gpu_optim)."""
+    from paper_2608_13578_gb300 import optim
+    g = torch.Generator().manual_seed(0)
+    shapes, how = [(40, 7), (300,), (1000,)], dict(lr=1e-3, weight_decay=0.05)
+    a = [torch.nn.Parameter((torch.randn(s, generator=g) * 0.1).to(BF).cuda()) for s in shapes]
+
+    def gradients(*lists):
+        for ps in zip(*lists):
+            d = torch.randn(ps[0].shape, generator=g).to(BF).cuda()
+            for p in ps:
+                p.grad = d.to(p.dtype)
+    old = torch.optim.AdamW(a, **how)
+    for _ in range(3):
+        gradients(a)
+        old.step()
+    b = [torch.nn.Parameter(p.detach().clone()) for p in a]
+    c = [torch.nn.Parameter(p.detach().float()) for p in a]
+    ob, oc = optim.AdamW(b, masters=True, capturable=capturable, **how), torch.optim.AdamW(c, **how)
+    file = old.state_dict()
+    ob.load_state_dict(file)
+    oc.load_state_dict(file)
+    for s in oc.state.values():
+        assert s["exp_avg"].dtype == F
+    for _ in range(3):
+        gradients(b, c)
+        ob.step()
+        oc.step()
+    for p, q in zip(b, c):
+        w = ob.state[p]["master"]
+        assert float((w - q.detach()).abs().max()) <= 3 * 16 * (1e-3 * 2.0 ** -20 + 2 * R.U * float(q.detach().abs().max()))
+        assert torch.equal(p.detach(), w.to(BF)) and int(ob.state[p]["step"]) == 6
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 def test_the_norm_that_clips(cuda_ok, dtype):
     """As on the CPU: a sum of 4121 squares in fp32 is off by at most 4121 * 2^-24, its root by half of
